@@ -580,6 +580,146 @@ int actkv_compact_noalloc(const actkv_pool_t* pool /* host */, const actkv_table
 #define ACTKV_STALL_ANSWER  0x7fffffff
 int actkv_debug_inject_stall(int32_t after_tile, int32_t wait_limit_us);
 
+/* ---------------------------------------------------------------------------------------
+ * Decoding on the cache between two compression steps: actkv_resize -> actkv_append ->
+ * actkv_attend (whose LSE is the lse_in of actkv_score / actkv_score_accumulate) -> actkv_logprob,
+ * and actkv_copy for the branches of a trace.
+ * (The paper leaves these to the serving system: Section 2.3 defines the attention, Section 2.5 the paged
+ * cache and its block table, Section 7.1 takes the LSE from the attention backend.)
+ */
+
+/* actkv_attend — attention of the newest tokens of every request over its cached entries
+ * (Section 2.3), read through the block table, split over the cache's length and joined.
+ *
+ * For layer l, request r, window row w < W_r and q-head qh of KV head h = qh / G, over the keys
+ * j < L_r that the row sees, s_j = sm_scale * <q[l, win_indptr[r]+w, qh, :], K[l, slot(r, j), h, :]>:
+ *   lse = log sum_j exp(s_j)                 -> lse_out (float32, natural log; NULL to skip)
+ *   out = sum_j exp(s_j - lse) V[l, slot(r, j), h, :]          (bf16, rounded once)
+ * causal != 0: the window is the last W_r cached tokens (append them first), row w sees
+ * j <= L_r - W_r + w; causal == 0: every row sees every key.  window_left = S > 0 (sliding-window
+ * layers): only the S keys up to the row's own position count, as in actkv_score_sliding.
+ * A row that sees no key (W_r > L_r, L_r = 0), or whose logits are all -inf, gets out = 0 and
+ * lse = -inf.  What a masked or unused slot holds (infinities and NaN too) does not reach any row.  A
+ * logit that is NaN or +inf makes its row NaN.
+ * Logits, maxima, sums and the output's accumulation are float32; the probabilities enter the
+ * product with V as two bf16 summands (16 bits of mantissa), so that the output is as good as a
+ * float32 computation rounded once.  The result does not depend on anything but the arguments and
+ * the number of SMs: no atomics, a fixed order of the sums.
+ * q, out     bf16 [NLs, sum_win, n_q_heads, head_dim], NLs = layer_end - layer_begin; may not overlap.
+ * win_indptr int32 [n_req+1]; W_r = 0: the request is skipped.  lse_out float32 [NLs, sum_win, n_q_heads].
+ * sum_win, max_win, max_tok: host copies (upper bounds are accepted) of win_indptr[n_req], max W_r, max L_r:
+ * a captured graph stays valid while the lengths grow up to max_tok.
+ * A request whose seq_len is negative, above max_tok or above what its table row holds, or whose window
+ * does not fit the host's bounds is reported as ACTKV_E_INVALID and its rows are left as they were; a page id
+ * out of range is reported and replaced by page 0 for the read.
+ * head_dim a multiple of 8, at most 256; any page size; strides multiples of 8 elements; base, q and out
+ * 16-byte aligned.
+ */
+size_t actkv_attend_workspace_bytes(const actkv_pool_t* pool /* host */, int32_t n_req, int32_t n_layers_sub,
+                                    int32_t n_q_heads, int32_t max_win, int32_t max_tok);
+int actkv_attend(const actkv_pool_t* pool /* host */, const actkv_tables_t* tables /* host */,
+                 int32_t layer_begin, int32_t layer_end,
+                 const void* q, const int32_t* win_indptr, int32_t n_q_heads,
+                 float sm_scale, int32_t causal, int32_t window_left, void* out, float* lse_out,
+                 int32_t sum_win, int32_t max_win, int32_t max_tok,
+                 void* ws, size_t ws_bytes, int32_t* status, actkv_stream_t stream);
+
+/* Rows of heads: element (layer l, row i, head h, dim d) at base + l*stride_layer + i*stride_row +
+ * h*stride_head + d, strides in elements; l is relative to layer_begin.  Heads of one fused QKV
+ * product are handed over as they lie. */
+typedef struct {
+  const void* base;             /* device, bf16 */
+  int64_t stride_layer, stride_row, stride_head;
+} actkv_rows_t;
+
+/* Rotary positions with up to 4 axes (text: 1; time, height, width: 3).  The first rotary_dim dims of a head
+ * turn in pairs i < rotary_dim/2: (i, i + rotary_dim/2), or (2i, 2i+1) when interleaved; the others pass
+ * unchanged.  Pair i belongs to the axis in whose section it falls (section[0] pairs for axis 0, and so on;
+ * they sum to rotary_dim/2) and turns by positions[axis][row] * inv_freq[i]. */
+typedef struct {
+  int32_t rotary_dim;           /* even, <= head_dim */
+  int32_t interleaved;
+  int32_t n_axes;               /* 1 .. 4 */
+  int32_t section[4];           /* pairs per axis */
+  const float* inv_freq;        /* device, float32 [rotary_dim/2] */
+} actkv_rope_t;
+
+/* actkv_append — the new tokens' keys and values into their slots, queries and keys turned to their
+ * positions on the way (Section 2.5: the block table places logical token j; positions are an input
+ * because after a compression a token's position is no longer its index in the cache).
+ *
+ * For request r and w < W_r the row i = win_indptr[r] + w is logical token j = L_r - W_r + w (seq_len
+ * already counts the new tokens: actkv_resize first):
+ *   K[l, slot(r, j), h, :] = rotate(k[l, i, h, :]),  V[l, slot(r, j), h, :] = v[l, i, h, :],
+ *   q_out[l, i, qh, :] = rotate(q[l, i, qh, :]).
+ * The angle is formed and reduced to half a turn in float64, sine and cosine in float32; products in float32,
+ * rounded once to bf16.
+ * q may be NULL (then q_out is not written); q_out bf16 [NLs, sum_win, n_q_heads, head_dim], which may be
+ * the memory of q when q lies that way, and overlaps nothing else.  rope NULL: nothing turns, positions
+ * is not read.  positions int32 [n_axes, sum_win].
+ * A row whose token falls outside its request (W_r > L_r) or table, or whose page id is out of range, is reported and
+ * its K and V dropped.  k, v and the pool may not overlap.
+ */
+int actkv_append(const actkv_pool_t* pool /* host */, const actkv_tables_t* tables /* host */,
+                 int32_t layer_begin, int32_t layer_end,
+                 const actkv_rows_t* q /* host */, const actkv_rows_t* k /* host */, const actkv_rows_t* v /* host */,
+                 const int32_t* win_indptr, int32_t n_q_heads,
+                 const actkv_rope_t* rope /* host */, const int32_t* positions, void* q_out,
+                 int32_t sum_win, int32_t* status, actkv_stream_t stream);
+
+/* actkv_resize — requests grow, are cut back or freed: pages from and to the free list (Section 2.5;
+ * Section 7.2, last paragraph, for the freed blocks).
+ *
+ * For every request with new_len[r] >= 0 (negative: left as it is), Y_r and X_r pages before and after:
+ * X_r > Y_r: page_table[r][Y_r + i] = free_list[free_count - 1 - (off_r + i)], off_r = what requests
+ * before r pop; X_r < Y_r: pages X_r .. Y_r - 1 are pushed after all pops, r and page ascending, their
+ * table entries become -1.  seq_len[r] = new_len[r].  The stack discipline is that of actkv_compact: pages
+ * freed by a call do not serve that call.
+ * All or nothing: a free list too short (ACTKV_E_NOFREE), a length beyond the table row, a free count or
+ * a page id out of range (ACTKV_E_INVALID, ACTKV_E_BADPAGE) is reported and nothing is modified; the same
+ * when status is already set.
+ * Only page_size and n_pages of the pool are used.  One launch of one cluster; no workspace.
+ */
+int actkv_resize(const actkv_pool_t* pool /* host */, const actkv_tables_t* tables /* host */,
+                 const int32_t* new_len, int32_t* status, actkv_stream_t stream);
+
+/* actkv_copy — branches of a trace: K and V rows of the first length[i] tokens of request src[i] into
+ * the slots of request dst[i], i < n_copy, layers [layer_begin, layer_end).  The slots must exist: fork = actkv_resize
+ * (dst from 0 to length) + actkv_copy.  Every branch has pages of its own, as the compaction calls
+ * require.  Tables are not touched.  Pairs that share a source read it once.
+ * src, dst, length int32 [n_copy] (device); max_len: host upper bound on length.
+ * A pair whose src, dst or length is out of range (length > seq_len of either, > max_len), with src == dst, or with
+ * a bad page id is reported and dropped (a bad page: only that page).  A request that occurs twice as dst, or both
+ * as src and dst, is reported as ACTKV_E_INVALID; what its rows hold afterwards is unspecified.
+ */
+int actkv_copy(const actkv_pool_t* pool /* host */, const actkv_tables_t* tables /* host */,
+               int32_t layer_begin, int32_t layer_end,
+               const int32_t* src, const int32_t* dst, const int32_t* length, int32_t n_copy, int32_t max_len,
+               int32_t* status, actkv_stream_t stream);
+
+/* actkv_logprob — log probabilities of given tokens, entropy and the most probable alternatives of every
+ * logits row, in one pass over the row (log P as in Section 6.1, whose monitor reads the same logits).
+ *
+ * lse_i = log sum_t exp(z_it);  logprob[i, g] = z[i, given[i, g]] - lse_i;
+ * entropy_i = -sum_t P_i(t) log P_i(t);  top_index[i, 0..top_k) = the top_k largest logits, descending, among
+ * equal ones the lower token first, top_logprob their log probabilities.
+ * logits  [n_rows, vocab] with row_stride elements between rows, ACTKV_F32 or ACTKV_BF16.
+ * given   int32 [n_rows, n_given]; negative: no token, logprob 0; >= vocab: reported as ACTKV_E_BADINDEX,
+ *         logprob NaN.  NULL with n_given = 0.
+ * logprob, entropy, lse, top_logprob: float32, entropy / lse may be NULL; top_index int32.  0 <= top_k <= 64;
+ *         places past the vocabulary: index -1, log probability -inf.
+ * Masked tokens (logit -inf) have probability 0.  A row with nothing but -inf: lse = -inf, log probabilities
+ * -inf, entropy 0.  A NaN, or a logit of +inf, makes lse, entropy and every log probability NaN; the index order then
+ * takes logits by their bit patterns (NaN with sign 0 above +inf).
+ */
+#define ACTKV_F32   0
+#define ACTKV_BF16  1
+#define ACTKV_LOGPROB_MAX_TOP 64
+int actkv_logprob(const void* logits, int32_t dtype, int32_t n_rows, int32_t vocab, int64_t row_stride,
+                  const int32_t* given, int32_t n_given, int32_t top_k,
+                  float* logprob, float* entropy, float* lse, float* top_logprob, int32_t* top_index,
+                  int32_t* status, actkv_stream_t stream);
+
 /* Library version string (host pointer to static storage). */
 const char* actkv_version(void);
 

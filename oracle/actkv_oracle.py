@@ -510,3 +510,106 @@ def budget(logits, tok_indptr, hist, hist_len, budget_in, p: BudgetParams, seq_l
         slopes[r] = fit_slope(Rr)
         out[r] = budget_update(int(budget_in[r]), slopes[r], p, None if seq_len is None else int(seq_len[r]))
     return hist, hist_len.astype(np.int32), out, slopes, T
+
+
+# --------------------------------------------------------------------------------------------
+# Decoding between two compression steps: attention of the newest tokens (Section 2.3), new tokens into the paged
+# cache (Section 2.5), pages claimed and given back (Section 7.2, last paragraph), branches, log probabilities
+
+
+def attend_unit(q: np.ndarray, k: np.ndarray, v: np.ndarray, sm_scale: float, causal: bool, window_left: int = 0):
+    """Attention of one (layer, request, KV head): q [W, G, D], k, v [L, D] float64 -> out [W, G, D], lse [W, G].
+
+    Row w stands at position p = L - W + w (causal) or L - 1 and sees the keys j <= p, with a sliding window only
+    j > p - window_left.  A row that sees nothing: out 0, lse -inf.
+    """
+    W, G, D = q.shape
+    L = k.shape[0]
+    out = np.zeros((W, G, D))
+    lse = np.full((W, G), -np.inf)
+    for w in range(W):
+        p = L - W + w if causal else L - 1
+        lo = max(0, p - window_left + 1) if window_left > 0 else 0
+        if p < lo:
+            continue
+        s = sm_scale * (q[w] @ k[lo:p + 1].T)
+        m = s.max(axis=1, keepdims=True)
+        e = np.exp(s - m)
+        lse[w] = m[:, 0] + np.log(e.sum(axis=1))
+        out[w] = (e @ v[lo:p + 1]) / e.sum(axis=1, keepdims=True)
+    return out, lse
+
+
+def attend(pool_bits, page_table, seq_len, q_bits, win_indptr, n_q_heads: int, sm_scale: float, causal: bool,
+           window_left: int = 0, layers=None):
+    """All units: out float64 [NLs, sum_win, n_q_heads, D], lse [NLs, sum_win, n_q_heads]."""
+    n_layers, _, _, P, H, D = pool_bits.shape
+    layers = list(range(n_layers)) if layers is None else layers
+    G = n_q_heads // H
+    out = np.zeros(q_bits.shape)
+    lse = np.full(q_bits.shape[:3], -np.inf)
+    for a, layer in enumerate(layers):
+        for r in range(len(seq_len)):
+            w0, w1 = int(win_indptr[r]), int(win_indptr[r + 1])
+            slots = slot_map(page_table[r], int(seq_len[r]), P)
+            for h in range(H):
+                k, v = (bf16_bits_to_f64(gather_rows(pool_bits, layer, c, h, slots)).reshape(-1, D) for c in (0, 1))
+                q = bf16_bits_to_f64(q_bits[a, w0:w1, h * G:(h + 1) * G])
+                out[a, w0:w1, h * G:(h + 1) * G], lse[a, w0:w1, h * G:(h + 1) * G] = attend_unit(q, k, v, sm_scale, causal, window_left)
+    return out, lse
+
+
+def rotate(x: np.ndarray, positions: np.ndarray, inv_freq: np.ndarray, sections, interleaved: bool) -> np.ndarray:
+    """x float64 [..., rows, heads, D] turned: pair i of row t by positions[axis(i), t] * inv_freq[i]."""
+    y = np.array(x, dtype=np.float64)
+    half = len(inv_freq)
+    axis = np.repeat(np.arange(len(sections)), sections)
+    for i in range(half):
+        a, b = (2 * i, 2 * i + 1) if interleaved else (i, i + half)
+        t = positions[axis[i]].astype(np.float64) * float(inv_freq[i])
+        c, s = np.cos(t)[:, None], np.sin(t)[:, None]
+        y[..., a] = x[..., a] * c - x[..., b] * s
+        y[..., b] = x[..., b] * c + x[..., a] * s
+    return y
+
+
+def resize(tables: Tables, new_len, page_size: int) -> Tables:
+    """Tables after requests grew, were cut back or freed; raises ValueError when the free list is too short."""
+    pt, sl = tables.page_table.copy(), tables.seq_len.copy()
+    free, fc = tables.free_list.copy(), int(tables.free_count)
+    pages = lambda n: -(-int(n) // page_size)
+    take = sum(max(0, pages(n) - pages(L)) for n, L in zip(new_len, sl) if n >= 0)
+    if take > fc:
+        raise ValueError("free list too short")
+    for r, n in enumerate(new_len):
+        if n >= 0:
+            for i in range(pages(sl[r]), pages(n)):
+                fc -= 1
+                pt[r, i] = free[fc]
+    for r, n in enumerate(new_len):
+        if n >= 0:
+            for i in range(pages(n), pages(sl[r])):
+                free[fc] = pt[r, i]
+                fc += 1
+                pt[r, i] = -1
+            sl[r] = n
+    return Tables(pt, sl, free, fc)
+
+
+def log_probabilities(logits: np.ndarray):
+    """Row-wise (lse, log P, entropy) of float64 logits [rows, vocab]; a row of -inf: -inf, -inf, 0."""
+    z = np.asarray(logits, dtype=np.float64)
+    m = z.max(axis=1)
+    with np.errstate(invalid="ignore", divide="ignore"):
+        safe = np.where(np.isneginf(m), 0.0, m)
+        e = np.exp(z - safe[:, None])
+        lse = safe + np.log(e.sum(axis=1))
+        logp = np.where(np.isneginf(m)[:, None], -np.inf, z - lse[:, None])
+        p = np.exp(logp)
+        ent = -np.where(p > 0, p * logp, 0.0).sum(axis=1)
+    return lse, logp, ent
+
+
+def top_tokens(logits: np.ndarray, k: int) -> np.ndarray:
+    """The k largest logits of every row, descending, equal ones by token: int [rows, min(k, vocab)]."""
+    return np.argsort(-np.asarray(logits, dtype=np.float64), axis=1, kind="stable")[:, :k]

@@ -6,6 +6,7 @@ on a non-zero return code.  There is no fallback: a missing or unloadable librar
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from typing import Optional
@@ -30,6 +31,7 @@ EXPORTS = ["actkv_budget_workspace_bytes", "actkv_budget", "actkv_score_workspac
            "actkv_compact_inplace", "actkv_score_path", "actkv_debug_inject_stall", "actkv_score_sliding", "actkv_keepscore_select",
            "actkv_compact_deferred_workspace_bytes", "actkv_compact_begin", "actkv_compact_end", "actkv_score_overlap", "actkv_compact_stats",
            "actkv_compact_inplace_deferred_workspace_bytes", "actkv_compact_inplace_begin", "actkv_compact_inplace_end",
+           "actkv_attend_workspace_bytes", "actkv_attend", "actkv_append", "actkv_resize", "actkv_copy", "actkv_logprob",
            "actkv_version"]
 
 
@@ -64,6 +66,17 @@ class BudgetParams(C.Structure):
 class TieReport(C.Structure):
     _fields_ = [("threshold", C.c_float), ("n_equal_kept", C.c_int32), ("n_equal_total", C.c_int32),
                 ("n_keep", C.c_int32)]
+
+
+class RowsDesc(C.Structure):
+    """actkv_rows_t: rows of heads with strides."""
+    _fields_ = [("base", C.c_void_p), ("stride_layer", C.c_int64), ("stride_row", C.c_int64), ("stride_head", C.c_int64)]
+
+
+class RopeDesc(C.Structure):
+    """actkv_rope_t: which dims turn, by which axis, how fast."""
+    _fields_ = [("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("n_axes", C.c_int32), ("section", C.c_int32 * 4),
+                ("inv_freq", C.c_void_p)]
 
 
 class HostStep(C.Structure):
@@ -175,6 +188,20 @@ def load():
                                         i32, vp, vp, vp, i32, i32, i32, i32, vp, sz, vp, vp]
     lib.actkv_score_path.restype = i32
     lib.actkv_score_path.argtypes = [C.POINTER(PoolDesc), i32, i32, f32, vp, i32]
+    lib.actkv_attend_workspace_bytes.restype = sz
+    lib.actkv_attend_workspace_bytes.argtypes = [C.POINTER(PoolDesc), i32, i32, i32, i32, i32]
+    lib.actkv_attend.restype = i32
+    lib.actkv_attend.argtypes = [C.POINTER(PoolDesc), C.POINTER(TablesDesc), i32, i32, vp, vp, i32, f32, i32, i32, vp, vp,
+                                 i32, i32, i32, vp, sz, vp, vp]
+    lib.actkv_append.restype = i32
+    lib.actkv_append.argtypes = [C.POINTER(PoolDesc), C.POINTER(TablesDesc), i32, i32, C.POINTER(RowsDesc),
+                                 C.POINTER(RowsDesc), C.POINTER(RowsDesc), vp, i32, C.POINTER(RopeDesc), vp, vp, i32, vp, vp]
+    lib.actkv_resize.restype = i32
+    lib.actkv_resize.argtypes = [C.POINTER(PoolDesc), C.POINTER(TablesDesc), vp, vp, vp]
+    lib.actkv_copy.restype = i32
+    lib.actkv_copy.argtypes = [C.POINTER(PoolDesc), C.POINTER(TablesDesc), i32, i32, vp, vp, vp, i32, i32, vp, vp]
+    lib.actkv_logprob.restype = i32
+    lib.actkv_logprob.argtypes = [vp, i32, i32, i32, i64, vp, i32, i32, vp, vp, vp, vp, vp, vp, vp]
     lib.actkv_debug_inject_stall.restype = i32
     lib.actkv_debug_inject_stall.argtypes = [i32, i32]
     _lib = lib
@@ -494,3 +521,145 @@ def actkv_compact_noalloc(pool: PoolDesc, tables: TablesDesc, layer_begin, layer
                                       _ptr(budget, torch.int32, "budget"), max_keep,
                                       _ptr(status, torch.int32, "status"), _stream(stream))
     _check("actkv_compact_noalloc", rc)
+
+
+# ---------------------------------------------------------------------------------------------
+# decoding between two compression steps
+#
+# These calls may be made while another device than the tensors' is current; all tensors of a call are on one device.
+
+
+def _on(dev: torch.device):
+    """Context in which `dev` is the current device (none is entered when it already is)."""
+    return contextlib.nullcontext() if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
+
+
+def _same_device(dev, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != dev:
+            raise TypeError(f"{name}: on {t.device}, expected {dev}")
+
+
+def _sized(t, n: int, name: str):
+    if t is not None and t.numel() < n:
+        raise ValueError(f"{name}: {t.numel()} elements, expected at least {n}")
+
+
+def actkv_attend_workspace_bytes(pool: PoolDesc, n_req, n_layers_sub, n_q_heads, max_win, max_tok) -> int:
+    return load().actkv_attend_workspace_bytes(C.byref(pool), n_req, n_layers_sub, n_q_heads, max_win, max_tok)
+
+
+def actkv_attend(pool: PoolDesc, tables: TablesDesc, layer_begin, layer_end, q, win_indptr, n_q_heads, sm_scale, causal,
+                 window_left, out, lse_out, sum_win, max_win, max_tok, ws, status, stream=None):
+    dev = q.device
+    _same_device(dev, win_indptr=win_indptr, out=out, lse_out=lse_out, ws=ws, status=status)
+    rows = (layer_end - layer_begin) * sum_win * n_q_heads
+    _sized(q, rows * pool.head_dim, "q")
+    _sized(out, rows * pool.head_dim, "out")
+    _sized(lse_out, rows, "lse_out")
+    _sized(win_indptr, tables.n_req + 1, "win_indptr")
+    with _on(dev):
+        rc = load().actkv_attend(pool, tables, layer_begin, layer_end, _ptr(q, torch.bfloat16, "q"),
+                                 _ptr(win_indptr, torch.int32, "win_indptr"), n_q_heads, float(sm_scale), 1 if causal else 0,
+                                 window_left, _ptr(out, torch.bfloat16, "out"), _ptr(lse_out, torch.float32, "lse_out"), sum_win,
+                                 max_win, max_tok, _ptr(ws, None, "ws"), ws.numel() * ws.element_size(),
+                                 _ptr(status, torch.int32, "status"), _stream(stream))
+    _check("actkv_attend", rc)
+
+
+def rows_desc(t: torch.Tensor, name: str = "rows") -> RowsDesc:
+    """Descriptor of a bf16 tensor [layers, rows, heads, head_dim] (any strides with a contiguous head dimension)."""
+    if not t.is_cuda:
+        raise TypeError(f"{name}: expected a CUDA tensor")
+    if t.dtype != torch.bfloat16 or t.dim() != 4 or (t.stride(3) != 1 and t.shape[3] != 1):
+        raise TypeError(f"{name}: expected bf16 [layers, rows, heads, D] with contiguous D")
+    st = t.stride()
+    return RowsDesc(t.data_ptr(), st[0], st[1], st[2])
+
+
+def rope_desc(inv_freq: Optional[torch.Tensor], sections, interleaved: bool = False) -> RopeDesc:
+    """sections: rotary pairs per axis (1 to 4 axes); inv_freq float32 [sum(sections)] on the device."""
+    n = len(sections)
+    if not 1 <= n <= 4:
+        raise ValueError(f"rope: {n} axes, expected 1 to 4")
+    if inv_freq is not None and inv_freq.numel() != sum(sections):
+        raise ValueError(f"rope: {inv_freq.numel()} frequencies for {sum(sections)} pairs")
+    return RopeDesc(2 * sum(sections), 1 if interleaved else 0, n, (C.c_int32 * 4)(*sections),
+                    _ptr(inv_freq, torch.float32, "inv_freq"))
+
+
+def actkv_append(pool: PoolDesc, tables: TablesDesc, layer_begin, layer_end, q, k, v, win_indptr, n_q_heads,
+                 rope: Optional[RopeDesc], positions, q_out, status, stream=None):
+    """q, k, v [layers, rows, heads, head_dim] (strided; q may be None), positions int32 [axes, rows]."""
+    dev, sum_win, nls = k.device, k.shape[1], layer_end - layer_begin
+    _same_device(dev, q=q, v=v, win_indptr=win_indptr, positions=positions, q_out=q_out, status=status)
+    D, hk = pool.head_dim, pool.n_kv_heads
+    if k.shape != (nls, sum_win, hk, D) or v.shape != k.shape or (q is not None and q.shape != (nls, sum_win, n_q_heads, D)):
+        raise ValueError("actkv_append: q, k and v are [layers, rows, heads, head_dim] of this call and pool")
+    if q is not None:
+        if q_out is None:
+            raise ValueError("q_out: expected with q")
+        _sized(q_out, nls * sum_win * n_q_heads * D, "q_out")
+    if rope is not None and rope.rotary_dim:
+        if positions is None:
+            raise ValueError("positions: expected with rope")
+        _sized(positions, rope.n_axes * sum_win, "positions")
+    _sized(win_indptr, tables.n_req + 1, "win_indptr")
+    with _on(dev):
+        rc = load().actkv_append(pool, tables, layer_begin, layer_end, None if q is None else rows_desc(q, "q"),
+                                 rows_desc(k, "k"), rows_desc(v, "v"), _ptr(win_indptr, torch.int32, "win_indptr"), n_q_heads,
+                                 rope, _ptr(positions, torch.int32, "positions"), _ptr(q_out, torch.bfloat16, "q_out"), sum_win,
+                                 _ptr(status, torch.int32, "status"), _stream(stream))
+    _check("actkv_append", rc)
+
+
+def actkv_resize(pool: PoolDesc, tables: TablesDesc, new_len, status, stream=None):
+    _same_device(new_len.device, status=status)
+    _sized(new_len, tables.n_req, "new_len")
+    with _on(new_len.device):
+        rc = load().actkv_resize(pool, tables, _ptr(new_len, torch.int32, "new_len"), _ptr(status, torch.int32, "status"),
+                                 _stream(stream))
+    _check("actkv_resize", rc)
+
+
+def actkv_copy(pool: PoolDesc, tables: TablesDesc, layer_begin, layer_end, src, dst, length, max_len, status, stream=None):
+    dev, n = src.device, src.numel()
+    _same_device(dev, dst=dst, length=length, status=status)
+    _sized(dst, n, "dst")
+    _sized(length, n, "length")
+    with _on(dev):
+        rc = load().actkv_copy(pool, tables, layer_begin, layer_end, _ptr(src, torch.int32, "src"), _ptr(dst, torch.int32, "dst"),
+                               _ptr(length, torch.int32, "length"), n, max_len, _ptr(status, torch.int32, "status"),
+                               _stream(stream))
+    _check("actkv_copy", rc)
+
+
+_LOGIT_TYPES = {torch.float32: 0, torch.bfloat16: 1}
+
+
+def actkv_logprob(logits, given, logprob, entropy, lse, top_logprob, top_index, status, stream=None):
+    """logits [rows, vocab] float32 or bf16, rows any distance apart; given int32 [rows, n] or None; top_logprob /
+    top_index [rows, k] or None."""
+    if not logits.is_cuda:
+        raise TypeError("logits: expected a CUDA tensor")
+    if logits.dtype not in _LOGIT_TYPES or logits.dim() != 2 or (logits.stride(1) != 1 and logits.shape[1] != 1):
+        raise TypeError("logits: expected float32 or bf16 [rows, vocab] with contiguous rows")
+    n, vocab = logits.shape
+    dev = logits.device
+    _same_device(dev, given=given, logprob=logprob, entropy=entropy, lse=lse, top_logprob=top_logprob, top_index=top_index,
+                 status=status)
+    n_given = 0 if given is None or n == 0 else given.numel() // n
+    top_k = 0 if top_index is None or n == 0 else top_index.numel() // n
+    if n_given and (given.numel() != n * n_given or logprob is None or logprob.numel() != given.numel()):
+        raise ValueError("given, logprob: expected [rows, n]")
+    if top_k and (top_index.numel() != n * top_k or top_logprob is None or top_logprob.numel() != top_index.numel()):
+        raise ValueError("top_logprob, top_index: expected [rows, k]")
+    _sized(entropy, n, "entropy")
+    _sized(lse, n, "lse")
+    with _on(dev):
+        rc = load().actkv_logprob(logits.data_ptr(), _LOGIT_TYPES[logits.dtype], n, vocab, logits.stride(0) if n > 1 else vocab,
+                                  _ptr(given, torch.int32, "given"), n_given, top_k, _ptr(logprob, torch.float32, "logprob"),
+                                  _ptr(entropy, torch.float32, "entropy"), _ptr(lse, torch.float32, "lse"),
+                                  _ptr(top_logprob, torch.float32, "top_logprob"), _ptr(top_index, torch.int32, "top_index"),
+                                  _ptr(status, torch.int32, "status"), _stream(stream))
+    _check("actkv_logprob", rc)

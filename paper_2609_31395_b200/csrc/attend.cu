@@ -1,0 +1,682 @@
+// actkv_attend: attention of the newest tokens over the paged cache (Section 2.3), with the LSE that Section 7.1 takes from
+// the attention backend.
+//
+// One pass over K and V.  Keys come in tiles of 16; a warp forms the logits of a tile, D[key, row] = K Q^T, keeps a running
+// reference m and a running sum l of exp2(t - m) per row (t in log2 units), and accumulates O^T[dim, row] += V^T P^T.  With
+// the keys on the long side of the matrix instruction (m16n8k16) 8 rows fill it, the usual number of query heads per KV head;
+// with the rows on that side half of every product would be padding.
+//   The reference moves only when a logit exceeds it by more than 8 (a factor of 256 in a probability: nothing in float32),
+// so that most tiles need no maximum over the lanes and no rescaling.
+//   P enters the second product as two bf16 summands, p truncated to bf16 and the rest: with one, the rounding of P is as
+// large as that of the output (together 1.4 times the error of a float32 computation).  The tensor pipe has the room.
+//
+// What bounds it: reading K and V, 4 D bytes a key and KV head.
+//
+// Work.  All (layer, head, request, block of rows) units in one line, each as long as its key tiles; every CTA takes an equal
+// piece of the line, from the lengths on the device, so that ragged requests are balanced and a captured graph follows
+// growing caches.  A unit that lies in several pieces leaves (m, l, O) partials, joined by attend_join_kernel in piece order.
+// Within a CTA the groups of RG warps take the tiles of a piece in turn; the warps of a group share a ring of tiles
+// in shared memory and have 8 NT rows each.
+#include <algorithm>
+
+#include "common.cuh"
+
+namespace actkv {
+namespace at {
+
+constexpr int NW = 4, NTH = NW * 32;
+constexpr int KT = 16;                    // keys per tile
+constexpr int MIN_TILES = 8;              // fewest tiles of a CTA's piece
+constexpr int MAX_CTAS = 2 * 148;         // two CTAs per SM: one streams while the other starts or ends a unit
+constexpr float NO_REF = -3.0e38f;        // the reference before the first logit (finite: no infinity meets another)
+constexpr float REF_SLACK = 8.f;
+constexpr int MAX_GROUP = 32;             // query heads per KV head, as the score kernels
+
+struct Args {
+  PoolView pool;
+  TablesView tab;
+  const __nv_bfloat16* q;
+  const int32_t* win_indptr;
+  __nv_bfloat16* out;
+  float* lse;
+  int2* desc;                    // [units] first and last piece of a unit
+  float2* part_ml;               // [2 * MAX_CTAS][rows of a block] (m, l)
+  float* part;                   // [2 * MAX_CTAS][rows of a block][DP]
+  int32_t* status;
+  int32_t layer_begin, nls, n_q_heads, group;
+  int32_t sum_win, max_win, max_tok;
+  int32_t rb_max;                // blocks of rows per request, at most
+  int32_t page_shift;
+  float scale_log2;
+  int32_t causal, win_left;
+};
+
+struct Req {
+  int L, W, win0;                // W = 0: nothing to do
+  int lo_tile, tiles;            // key tiles that some row sees (one at least, so that every row is written)
+};
+__device__ __forceinline__ Req load_req(const Args& a, int r, bool tell) {
+  const int w0 = a.win_indptr[r], w1 = a.win_indptr[r + 1], L = a.tab.seq_len[r];
+  Req q{L, w1 - w0, w0, 0, 0};
+  const bool ok = L >= 0 && L <= a.max_tok && (int64_t)L <= (int64_t)a.tab.max_pages * a.pool.page_size && w0 >= 0 &&
+                  w1 >= w0 && w1 <= a.sum_win && q.W <= a.max_win;
+  if (!ok) {
+    if (tell) report(a.status, ACTKV_E_INVALID, r, L);
+    q.W = 0;
+  }
+  if (q.W > 0) {
+    const int first = a.causal ? L - q.W : L - 1;                          // the position of the first row
+    q.lo_tile = a.win_left > 0 ? max(0, first - a.win_left + 1) / KT : 0;
+    q.tiles = max(1, (L + KT - 1) / KT - q.lo_tile);
+  }
+  return q;
+}
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t bytes) {     // the rest of 16 is zeroed
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t v) {
+  uint32_t d;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
+  return d;
+}
+
+// What a launch variant is made of.  NT: row tiles of 8 per warp; RG: warps that share a ring (and have different rows).
+template <int DP, int NT, int RG>
+struct Cfg {
+  static constexpr int NG = NW / RG;
+  static constexpr int RB = 8 * NT * RG;                                   // rows of a block
+  static constexpr int TILE = KT * DP * 2 * 2;                             // bytes: K and V
+  static constexpr int CTAS = DP > 128 ? 1 : 2;                            // per SM
+  static constexpr int STAGES = (DP > 128 ? 192 : 96) * 1024 / (NG * TILE) > 16 ? 16 : (DP > 128 ? 192 : 96) * 1024 / (NG * TILE);
+  static constexpr int RING = NG * STAGES * TILE;
+  static constexpr int RED = NW * 8 * (DP + 4) * 4;
+  static_assert(RED <= RING, "the join of the warps reuses the ring");
+};
+
+template <int DP, int NT, int RG>
+__global__ void __launch_bounds__(NTH, (Cfg<DP, NT, RG>::CTAS)) attend_kernel(const Args a) {
+  using C = Cfg<DP, NT, RG>;
+  pdl_begin();
+  extern __shared__ __align__(128) uint8_t at_smem[];
+  __shared__ int64_t s_warp[NW];
+  __shared__ int64_t s_off;
+  __shared__ int s_r;
+  __shared__ float2 s_ml[NW][8 * NT];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int grp = warp / RG, part = warp % RG;
+  const int R = a.tab.n_req, G = a.group, D = a.pool.head_dim, P = a.pool.page_size;
+
+  // ---- this CTA's piece of the line: thread t sums requests [t * per_t, (t + 1) * per_t) ----
+  const int per_t = (R + NTH - 1) / NTH;
+  int64_t mine = 0;
+  for (int r = tid * per_t; r < min(R, (tid + 1) * per_t); ++r) {
+    const Req q = load_req(a, r, blockIdx.x == 0);
+    mine += (int64_t)q.tiles * ((q.W * G + C::RB - 1) / C::RB);
+  }
+  int64_t incl = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int64_t t = __shfl_up_sync(0xffffffffu, incl, d);
+    if (lane >= d) incl += t;
+  }
+  if (lane == 31) s_warp[warp] = incl;
+  __syncthreads();
+  int64_t T = 0;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    if (w == warp) incl += T;
+    T += s_warp[w];
+  }
+  const int64_t total = T * a.nls * a.pool.n_kv_heads;
+  const int64_t per = max((int64_t)MIN_TILES, (total + gridDim.x - 1) / gridDim.x);
+  int64_t x = (int64_t)blockIdx.x * per;
+  const int64_t x1 = min(total, x + per);
+  if (x >= x1) return;
+  int lh = (int)(x / T);
+  {
+    const int64_t rem = x - lh * T;
+    if (rem >= incl - mine && rem < incl) {                                // this thread's requests hold the start
+      int64_t off = rem - (incl - mine);
+      int r = tid * per_t;
+      for (;; ++r) {
+        const Req q = load_req(a, r, false);
+        const int64_t n = (int64_t)q.tiles * ((q.W * G + C::RB - 1) / C::RB);
+        if (off < n) break;
+        off -= n;
+      }
+      s_r = r;
+      s_off = off;
+    }
+  }
+  __syncthreads();
+  int r = s_r;
+  int64_t off = s_off;
+
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(at_smem) + grp * C::STAGES * C::TILE;
+  const int g = lane >> 2, t2 = (lane & 3) * 2;
+  const int nch = D / 8;                                                   // 16-byte chunks of a row
+  if (D < DP) {                                                            // dims past head_dim: zeros, never written again
+    const int spare = DP / 8 - nch;
+    for (int i = tid; i < C::RING / (DP * 2) * spare; i += NTH) {
+      const int row = i / spare, c = nch + i % spare;
+      *reinterpret_cast<uint4*>(at_smem + row * DP * 2 + ((c ^ (row & 7)) << 4)) = make_uint4(0, 0, 0, 0);
+    }
+    __syncthreads();
+  }
+  auto group_sync = [&]() {
+    if (RG == 1) __syncwarp();
+    else asm volatile("bar.sync %0, %1;" ::"r"(1 + grp), "n"(RG * 32) : "memory");
+  };
+
+  while (x < x1) {
+    const Req q = load_req(a, r, false);
+    const int rbs = (q.W * G + C::RB - 1) / C::RB;
+    if (q.W == 0) {
+      if (++r == R) { r = 0; ++lh; }
+      off = 0;
+      continue;
+    }
+    const int rb = (int)(off / q.tiles), t_in = (int)(off - (int64_t)rb * q.tiles);
+    const int n_tiles = (int)min((int64_t)(q.tiles - t_in), x1 - x);
+    const int layer = lh / a.pool.n_kv_heads, h = lh - layer * a.pool.n_kv_heads;
+    const int L = q.L, rows = q.W * G;
+
+    // ---- rows of this warp ----
+    const int row0 = rb * C::RB + part * 8 * NT;
+    const bool active = row0 < rows;
+    const int64_t qrow = (int64_t)layer * a.sum_win + q.win0;
+    uint32_t qf[DP / 16][NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int rho = row0 + n * 8 + g;
+      const int w = rho / G;
+      const __nv_bfloat16* src = a.q + ((qrow + w) * a.n_q_heads + h * G + (rho - w * G)) * D + t2;
+#pragma unroll
+      for (int ks = 0; ks < DP / 16; ++ks)
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+          qf[ks][n][c] = (rho < rows && 2 * ks + c < nch) ? *reinterpret_cast<const uint32_t*>(src + ks * 16 + c * 8) : 0u;
+    }
+    // keys that all rows of this warp see
+    const int pos0 = a.causal ? L - q.W : L - 1;                           // position of window row 0
+    const int step = a.causal ? 1 : 0;
+    const int w_lo = row0 / G, w_hi = min(row0 + 8 * NT, rows) - 1;
+    const int all_hi = pos0 + step * w_lo;
+    const int all_lo = a.win_left > 0 ? pos0 + step * (w_hi / G) - a.win_left + 1 : 0;
+
+    float acc[DP / 16][NT][4], m[NT][2], l[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int mt = 0; mt < DP / 16; ++mt)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) acc[mt][n][c] = 0.f;
+      m[n][0] = m[n][1] = NO_REF;
+      l[n][0] = l[n][1] = 0.f;
+    }
+
+    // ---- the stream of this group's tiles ----
+    const __nv_bfloat16* kbase = a.pool.base + (int64_t)(a.layer_begin + layer) * a.pool.stride_layer + (int64_t)h * a.pool.stride_head;
+    const int first = q.lo_tile + t_in + grp, end = q.lo_tile + t_in + n_tiles;
+    auto page_of = [&](int tile) -> int {                                  // page of key tile * 16 + lane % 16, -1 behind the end
+      const int key = tile * KT + (lane & 15);
+      if (tile >= end || key >= L) return -1;
+      const int lp = a.page_shift >= 0 ? key >> a.page_shift : key / P;
+      return checked_page(a.tab, a.pool.n_pages, r, lp, a.status);
+    };
+    auto issue = [&](int tile, int stage, int page) {
+      if (tile < end) {
+        const int key = tile * KT + (lane & 15);
+        const int slot = a.page_shift >= 0 ? key & (P - 1) : key % P;
+        const int64_t koff = page >= 0 ? (int64_t)page * a.pool.stride_page + (int64_t)slot * a.pool.stride_slot : -1;
+        constexpr int CH = DP / 8, RPI = 32 / CH;                          // chunks of a row, rows per step of the warp
+        constexpr int MINE = KT / RG;                                      // rows of the tile that this warp loads
+        const int c = lane % CH;
+#pragma unroll
+        for (int i = 0; i < MINE / RPI; ++i) {
+          const int row = part * MINE + i * RPI + lane / CH;
+          const int64_t o = __shfl_sync(0xffffffffu, koff, row);
+          const uint32_t dst = ring + stage * C::TILE + row * DP * 2 + ((c ^ (row & 7)) << 4);
+          const __nv_bfloat16* src = kbase + (o < 0 ? 0 : o + c * 8);
+          if (c < nch) {
+            cp_async16(dst, src, o < 0 ? 0 : 16);
+            cp_async16(dst + C::TILE / 2, o < 0 ? src : src + a.pool.stride_kv, o < 0 ? 0 : 16);
+          }
+        }
+      }
+      cp_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < C::STAGES - 1; ++i) issue(first + i * C::NG, i, page_of(first + i * C::NG));
+    int page_next = page_of(first + (C::STAGES - 1) * C::NG);
+    int stage = 0, stage_w = C::STAGES - 1;
+#pragma unroll 1
+    for (int tile = first; tile < end; tile += C::NG) {
+      cp_wait<C::STAGES - 2>();
+      group_sync();                                                        // the tile is here; the previous one has been read
+      issue(tile + (C::STAGES - 1) * C::NG, stage_w, page_next);
+      page_next = page_of(tile + C::STAGES * C::NG);
+      const uint32_t ks_addr = ring + stage * C::TILE;
+      stage = stage + 1 == C::STAGES ? 0 : stage + 1;
+      stage_w = stage_w + 1 == C::STAGES ? 0 : stage_w + 1;
+      if (!active) continue;
+
+      // logits of 16 keys
+      float s[NT][4];
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) s[n][c] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < DP / 16; ++ks) {
+        uint32_t kf[4];
+        const int row = lane & 15, c = 2 * ks + (lane >> 4);
+        ldsm4(kf, ks_addr + row * DP * 2 + ((c ^ (row & 7)) << 4));
+#pragma unroll
+        for (int n = 0; n < NT; ++n) mma16816(s[n], kf, qf[ks][n][0], qf[ks][n][1]);
+      }
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) s[n][c] *= a.scale_log2;
+      const int key0 = tile * KT;
+      const bool masked = key0 + KT - 1 > all_hi || key0 < all_lo;
+      if (masked) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const int key = key0 + g + (c >> 1) * 8;
+            const int pos = pos0 + step * ((row0 + n * 8 + t2 + (c & 1)) / G);
+            if (key > pos || (a.win_left > 0 && key <= pos - a.win_left)) s[n][c] = -INFINITY;
+          }
+      }
+      // the references, when some logit has left them behind
+      bool beyond = false;
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) beyond |= s[n][c] > m[n][c & 1] + REF_SLACK;
+      if (__any_sync(0xffffffffu, beyond)) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            float v = fmaxf(fmaxf(s[n][c], s[n][c + 2]), m[n][c]);
+            v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 4));
+            v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
+            v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
+            const float f = exp2f(m[n][c] - v);
+            m[n][c] = v;
+            l[n][c] *= f;
+#pragma unroll
+            for (int mt = 0; mt < DP / 16; ++mt) {
+              acc[mt][n][c] *= f;
+              acc[mt][n][c + 2] *= f;
+            }
+          }
+      }
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          s[n][c] = exp2f(s[n][c] - m[n][c & 1]);
+          l[n][c & 1] += s[n][c];
+        }
+      // V of a tile that not every row sees whole: an infinity or NaN there must not meet a probability of 0 in a product
+      const uint32_t vs_addr = ks_addr + C::TILE / 2;
+      if (masked) {
+        bool odd = false;
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i) {
+          uint4 v;
+          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(vs_addr + (i * 32 + lane) * 16) : "memory");
+          for (uint32_t u : {v.x, v.y, v.z, v.w}) odd |= (u & 0x7f80u) == 0x7f80u || (u & 0x7f800000u) == 0x7f800000u;
+        }
+        if (__any_sync(0xffffffffu, odd)) {
+#pragma unroll 1
+          for (int kk = 0; kk < KT; ++kk) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              const float p0 = __shfl_sync(0xffffffffu, kk < 8 ? s[n][0] : s[n][2], (kk & 7) * 4 + (lane & 3));
+              const float p1 = __shfl_sync(0xffffffffu, kk < 8 ? s[n][1] : s[n][3], (kk & 7) * 4 + (lane & 3));
+#pragma unroll
+              for (int mt = 0; mt < DP / 16; ++mt)
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf) {
+                  uint16_t raw;
+                  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(raw) : "r"(vs_addr + kk * DP * 2 + (((2 * mt + hf) ^ (kk & 7)) << 4) + g * 2) : "memory");
+                  const float v = __uint_as_float((uint32_t)raw << 16);
+                  if (p0 != 0.f) acc[mt][n][2 * hf] = fmaf(p0, v, acc[mt][n][2 * hf]);
+                  if (p1 != 0.f) acc[mt][n][2 * hf + 1] = fmaf(p1, v, acc[mt][n][2 * hf + 1]);
+                }
+            }
+          }
+          continue;
+        }
+      }
+      uint32_t ph[NT][2], pl[NT][2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const uint32_t u0 = __float_as_uint(s[n][2 * c]), u1 = __float_as_uint(s[n][2 * c + 1]);
+          const float r0 = s[n][2 * c] - __uint_as_float(u0 & 0xffff0000u), r1 = s[n][2 * c + 1] - __uint_as_float(u1 & 0xffff0000u);
+          uint32_t lo;
+          asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(lo) : "f"(r1), "f"(r0));
+          ph[n][c] = transpose8(__byte_perm(u0, u1, 0x7632));
+          pl[n][c] = transpose8(lo);
+        }
+#pragma unroll
+      for (int mt = 0; mt < DP / 16; ++mt) {
+        uint32_t vf[4];
+        const int row = (lane & 7) + ((lane >> 4) << 3), c = 2 * mt + ((lane >> 3) & 1);
+        ldsm4t(vf, vs_addr + row * DP * 2 + ((c ^ (row & 7)) << 4));
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          mma16816(acc[mt][n], vf, ph[n][0], ph[n][1]);
+          mma16816(acc[mt][n], vf, pl[n][0], pl[n][1]);
+        }
+      }
+    }
+    cp_wait<0>();
+
+    // ---- the groups' shares of the piece together ----
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        l[n][c] += __shfl_xor_sync(0xffffffffu, l[n][c], 4);
+        l[n][c] += __shfl_xor_sync(0xffffffffu, l[n][c], 8);
+        l[n][c] += __shfl_xor_sync(0xffffffffu, l[n][c], 16);
+        if (lane < 4) s_ml[warp][n * 8 + t2 + c] = make_float2(m[n][c], l[n][c]);
+      }
+    __syncthreads();                                                       // ... and nobody reads the rings any more
+    const int64_t u0 = x - t_in;                                           // the unit's place on the line
+    const int b0 = (int)(u0 / per), b1 = (int)((u0 + q.tiles - 1) / per);
+    const bool whole = b0 == b1;
+    const int64_t unit = ((int64_t)lh * R + r) * a.rb_max + rb;
+    const int64_t slot = 2 * (int64_t)blockIdx.x + ((int)blockIdx.x == b0 ? 1 : 0);
+    if (t_in == 0 && tid == 0) a.desc[unit] = make_int2(b0, b1);
+    float* red = reinterpret_cast<float*>(at_smem);
+    constexpr int RS = DP + 4;
+#pragma unroll 1
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int nn = 0; nn < NT; ++nn) {
+        if (nn != n) continue;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int row = t2 + c;
+          float M = NO_REF;
+#pragma unroll
+          for (int k = 0; k < C::NG; ++k) M = fmaxf(M, s_ml[k * RG + part][nn * 8 + row].x);
+          const float f = exp2f(m[nn][c] - M);
+          float* dst = red + (warp * 8 + row) * RS + g;
+#pragma unroll
+          for (int mt = 0; mt < DP / 16; ++mt) {
+            dst[mt * 16] = acc[mt][nn][c] * f;
+            dst[mt * 16 + 8] = acc[mt][nn][c + 2] * f;
+          }
+        }
+      }
+      __syncthreads();
+      for (int i = tid; i < RG * 8 * (DP / 4); i += NTH) {
+        const int d = (i % (DP / 4)) * 4, row = i / (DP / 4) % 8, pt = i / (DP / 4 * 8);
+        const int in_block = (pt * NT + n) * 8 + row, rho = rb * C::RB + in_block;
+        if (rho >= rows) continue;
+        float M = NO_REF, sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < C::NG; ++k) M = fmaxf(M, s_ml[k * RG + pt][n * 8 + row].x);
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < C::NG; ++k) {
+          const float2 ml = s_ml[k * RG + pt][n * 8 + row];
+          sum = fmaf(ml.y, exp2f(ml.x - M), sum);
+          const float4 v = *reinterpret_cast<const float4*>(red + ((k * RG + pt) * 8 + row) * RS + d);
+          o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w;
+        }
+        if (whole) {
+          const int w = rho / G;
+          const int64_t at = (qrow + w) * a.n_q_heads + h * G + (rho - w * G);
+          if (d < D) {
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            __nv_bfloat162 v[2] = {__floats2bfloat162_rn(o.x * inv, o.y * inv), __floats2bfloat162_rn(o.z * inv, o.w * inv)};
+            *reinterpret_cast<uint2*>(a.out + at * D + d) = *reinterpret_cast<uint2*>(v);
+          }
+          if (d == 0 && a.lse != nullptr) a.lse[at] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
+        } else {
+          *reinterpret_cast<float4*>(a.part + (slot * C::RB + in_block) * DP + d) = o;
+          if (d == 0) a.part_ml[slot * C::RB + in_block] = make_float2(M, sum);
+        }
+      }
+      __syncthreads();
+    }
+    x += n_tiles;
+    off += n_tiles;
+    if (off == (int64_t)q.tiles * rbs) {
+      off = 0;
+      if (++r == R) { r = 0; ++lh; }
+    }
+    // (dims past head_dim: the join has written over their zeros)
+    if (D < DP && x < x1) {
+      const int spare = DP / 8 - nch;
+      for (int i = tid; i < C::RED / (DP * 2) * spare + spare; i += NTH) {
+        const int row = i / spare, c = nch + i % spare;
+        *reinterpret_cast<uint4*>(at_smem + row * DP * 2 + ((c ^ (row & 7)) << 4)) = make_uint4(0, 0, 0, 0);
+      }
+      __syncthreads();
+    }
+  }
+}
+
+// The partials of one row of a unit that lies in several pieces, in piece order.  One CTA per (row, unit).
+constexpr int JN = 256;
+template <int DP>
+__global__ void __launch_bounds__(JN) attend_join_kernel(const Args a, int32_t RB) {
+  pdl_begin();
+  __shared__ float s_w[2 * MAX_CTAS + 2];
+  __shared__ float s_red[JN / 32][DP];
+  __shared__ float s_r[JN / 32], s_s[JN / 32];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int64_t unit = blockIdx.x;
+  const int rb = (int)(unit % a.rb_max);
+  const int64_t lr = unit / a.rb_max;
+  const int r = (int)(lr % a.tab.n_req), lh = (int)(lr / a.tab.n_req);
+  const int rho = rb * RB + blockIdx.y, G = a.group, D = a.pool.head_dim;
+  const int2 b = a.desc[unit];                                             // (read beside the request's: not valid where W = 0)
+  const Req q = load_req(a, r, false);
+  if (rho >= q.W * G || b.x == b.y) return;
+  const int n = b.y - b.x + 1, row = blockIdx.y;
+  auto slot = [&](int i) { return 2 * (int64_t)(b.x + i) + (i == 0 ? 1 : 0); };
+  float M = NO_REF;
+  for (int i = tid; i < n; i += JN) M = fmaxf(M, a.part_ml[slot(i) * RB + row].x);
+#pragma unroll
+  for (int o = 16; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+  if (lane == 0) s_r[warp] = M;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < JN / 32; ++w) M = fmaxf(M, s_r[w]);
+  float sum = 0.f;
+  for (int i = tid; i < n; i += JN) {
+    const float2 ml = a.part_ml[slot(i) * RB + row];
+    const float f = exp2f(ml.x - M);
+    s_w[i] = f;
+    sum = fmaf(ml.y, f, sum);
+  }
+#pragma unroll
+  for (int o = 16; o >= 1; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (lane == 0) s_s[warp] = sum;
+  __syncthreads();
+  sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < JN / 32; ++w) sum += s_s[w];
+  float o[DP / 32];
+#pragma unroll
+  for (int k = 0; k < DP / 32; ++k) o[k] = 0.f;
+#pragma unroll 4
+  for (int i = warp; i < n; i += JN / 32) {
+    const float* src = a.part + (slot(i) * RB + row) * DP;
+    const float f = s_w[i];
+#pragma unroll
+    for (int k = 0; k < DP / 32; ++k) o[k] = fmaf(src[k * 32 + lane], f, o[k]);
+  }
+#pragma unroll
+  for (int k = 0; k < DP / 32; ++k) s_red[warp][k * 32 + lane] = o[k];
+  __syncthreads();
+  const int layer = lh / a.pool.n_kv_heads, h = lh - layer * a.pool.n_kv_heads, w = rho / G;
+  const int64_t at = ((int64_t)layer * a.sum_win + q.win0 + w) * a.n_q_heads + h * G + (rho - w * G);
+  if (tid < D) {
+    float v = 0.f;
+#pragma unroll
+    for (int k = 0; k < JN / 32; ++k) v += s_red[k][tid];
+    a.out[at * D + tid] = __float2bfloat16_rn(sum == 0.f ? 0.f : v / sum);
+  }
+  if (tid == 0 && a.lse != nullptr) a.lse[at] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
+}
+
+// rows of a block for this many rows per request at most: the smallest variant that holds them
+inline int block_rows(int D, int64_t rows) {
+  if (D > 128) return rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+  return rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+}
+inline int padded_dim(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
+
+struct WsLayout {
+  size_t desc_off, ml_off, part_off, total;
+  int RB, DP;
+  int64_t rb_max, units;
+};
+inline WsLayout ws_layout(int Hkv, int D, int64_t n_req, int64_t nls, int G, int64_t max_win) {
+  WsLayout l;
+  l.RB = block_rows(D, max_win * G);
+  l.DP = padded_dim(D);
+  l.rb_max = std::max<int64_t>(1, (max_win * G + l.RB - 1) / l.RB);
+  l.units = nls * Hkv * n_req * l.rb_max;
+  l.desc_off = 0;
+  l.ml_off = align_up((size_t)l.units * sizeof(int2), 256);
+  l.part_off = l.ml_off + align_up((size_t)2 * MAX_CTAS * l.RB * sizeof(float2), 256);
+  l.total = l.part_off + (size_t)2 * MAX_CTAS * l.RB * l.DP * 4;
+  return l;
+}
+
+template <int DP, int NT, int RG>
+int launch(const Args& a, int64_t tiles_bound, int64_t units, cudaStream_t s) {
+  using C = Cfg<DP, NT, RG>;
+  if (ensure_dyn_smem(attend_kernel<DP, NT, RG>, C::RING) != cudaSuccess) return ACTKV_E_CUDA;
+  const int64_t grid = std::max<int64_t>(1, std::min<int64_t>(MAX_CTAS / 2 * C::CTAS, (tiles_bound + MIN_TILES - 1) / MIN_TILES));
+  launch_pdl(attend_kernel<DP, NT, RG>, (unsigned)grid, NTH, C::RING, s, a);
+  ACTKV_CHECK_LAUNCH();
+  if (grid > 1) {
+    launch_pdl(attend_join_kernel<DP>, dim3((unsigned)units, C::RB), JN, 0, s, a, (int32_t)C::RB);
+    ACTKV_CHECK_LAUNCH();
+  }
+  return ACTKV_OK;
+}
+
+}  // namespace at
+}  // namespace actkv
+
+extern "C" {
+
+size_t actkv_attend_workspace_bytes(const actkv_pool_t* pool, int32_t n_req, int32_t n_layers_sub, int32_t n_q_heads,
+                                    int32_t max_win, int32_t max_tok) {
+  if (!pool || pool->n_kv_heads <= 0 || pool->head_dim <= 0 || n_req < 0 || n_layers_sub < 0 || n_q_heads <= 0 ||
+      max_win < 0 || max_tok < 0)
+    return 0;
+  return actkv::at::ws_layout(pool->n_kv_heads, pool->head_dim, n_req, n_layers_sub, n_q_heads / pool->n_kv_heads, max_win).total;
+}
+
+int actkv_attend(const actkv_pool_t* pool, const actkv_tables_t* tables, int32_t layer_begin, int32_t layer_end, const void* q,
+                 const int32_t* win_indptr, int32_t n_q_heads, float sm_scale, int32_t causal, int32_t window_left, void* out,
+                 float* lse_out, int32_t sum_win, int32_t max_win, int32_t max_tok, void* ws, size_t ws_bytes, int32_t* status,
+                 actkv_stream_t stream) {
+  using namespace actkv;
+  using namespace actkv::at;
+  if (!pool || !tables || !pool->base) return ACTKV_E_INVALID;
+  if (layer_begin < 0 || layer_end > pool->n_layers || layer_begin > layer_end) return ACTKV_E_INVALID;
+  const int D = pool->head_dim, Hkv = pool->n_kv_heads, R = tables->n_req;
+  if (D <= 0 || D % 8 != 0 || D > 256 || Hkv <= 0 || pool->page_size <= 0 || pool->n_pages <= 0) return ACTKV_E_INVALID;
+  if (n_q_heads <= 0 || n_q_heads % Hkv != 0) return ACTKV_E_INVALID;
+  const int G = n_q_heads / Hkv;
+  if (G > MAX_GROUP || R < 0 || sum_win < 0 || max_win < 0 || max_tok < 0 || window_left < 0) return ACTKV_E_INVALID;
+  if (((uintptr_t)pool->base & 15) || pool->stride_layer % 8 || pool->stride_kv % 8 || pool->stride_page % 8 ||
+      pool->stride_slot % 8 || pool->stride_head % 8 || ((uintptr_t)q & 15) || ((uintptr_t)out & 15))
+    return ACTKV_E_INVALID;
+  const int nls = layer_end - layer_begin;
+  if (R == 0 || nls == 0 || sum_win == 0) return ACTKV_OK;
+  if (!q || !win_indptr || !out || max_win == 0 || !tables->seq_len) return ACTKV_E_INVALID;
+  if (!tables->page_table || tables->max_pages < 0) return ACTKV_E_INVALID;
+  if (q == out || (int64_t)max_win * G > (1 << 24)) return ACTKV_E_INVALID;
+  const WsLayout lay = ws_layout(Hkv, D, R, nls, G, max_win);
+  if (!ws || ws_bytes < lay.total) return ACTKV_E_WORKSPACE;
+  if (lay.units > 0x7fffffff) return ACTKV_E_TOOBIG;
+  Args a;
+  a.pool = make_view(pool);
+  a.tab = make_view(tables);
+  a.q = (const __nv_bfloat16*)q;
+  a.win_indptr = win_indptr;
+  a.out = (__nv_bfloat16*)out;
+  a.lse = lse_out;
+  a.desc = (int2*)((char*)ws + lay.desc_off);
+  a.part_ml = (float2*)((char*)ws + lay.ml_off);
+  a.part = (float*)((char*)ws + lay.part_off);
+  a.status = status;
+  a.layer_begin = layer_begin;
+  a.nls = nls;
+  a.n_q_heads = n_q_heads;
+  a.group = G;
+  a.sum_win = sum_win;
+  a.max_win = max_win;
+  a.max_tok = max_tok;
+  a.rb_max = (int32_t)lay.rb_max;
+  a.page_shift = (pool->page_size & (pool->page_size - 1)) == 0 ? __builtin_ctz((unsigned)pool->page_size) : -1;
+  a.scale_log2 = sm_scale * kLog2e;
+  a.causal = causal;
+  a.win_left = window_left;
+  const int64_t bound = lay.units * std::max<int64_t>(1, ((int64_t)max_tok + KT - 1) / KT);
+  cudaStream_t s = (cudaStream_t)stream;
+  if (lay.DP == 256) {
+    switch (lay.RB) {
+      case 8: return launch<256, 1, 1>(a, bound, lay.units, s);
+      case 16: return launch<256, 2, 1>(a, bound, lay.units, s);
+      case 32: return launch<256, 2, 2>(a, bound, lay.units, s);
+      default: return launch<256, 2, 4>(a, bound, lay.units, s);
+    }
+  }
+  if (lay.DP == 128) {
+    switch (lay.RB) {
+      case 8: return launch<128, 1, 1>(a, bound, lay.units, s);
+      case 16: return launch<128, 2, 1>(a, bound, lay.units, s);
+      case 32: return launch<128, 4, 1>(a, bound, lay.units, s);
+      case 64: return launch<128, 4, 2>(a, bound, lay.units, s);
+      default: return launch<128, 4, 4>(a, bound, lay.units, s);
+    }
+  }
+  switch (lay.RB) {
+    case 8: return launch<64, 1, 1>(a, bound, lay.units, s);
+    case 16: return launch<64, 2, 1>(a, bound, lay.units, s);
+    case 32: return launch<64, 4, 1>(a, bound, lay.units, s);
+    case 64: return launch<64, 4, 2>(a, bound, lay.units, s);
+    default: return launch<64, 4, 4>(a, bound, lay.units, s);
+  }
+}
+
+}  // extern "C"

@@ -1,0 +1,389 @@
+// actkv_logprob: log probabilities of given tokens, entropy and the top alternatives of every logits row, in one sweep.
+//
+// Per thread, with m the largest logit it has met: S = sum exp(x - m), T = sum exp(x - m) (x - m); when m moves by d,
+// S' = S e^-d and T' = (T - d S) e^-d.  Joined over the row: lse = m + ln S, log P(t) = (x_t - m) - ln S, entropy = ln S - T / S.
+//
+// Top alternatives: a logit is a candidate when it reaches a bound of which the row is known to hold top_k logits.  The first
+// bound comes from the first LP_STEP logits: the top_k-th largest of the maxima of 128 chunks of them.  Candidates are kept in
+// shared memory as 64-bit keys (order-preserving image of the logit, then the token, lower ones first), so that ties need no
+// further rule; whenever more than LP_TIGHT have gathered they are cut to the top_k largest, the smallest of which is the new bound.
+// In random order a row of 152K yields about 300 candidates and one cut; in ascending order every step ends in a cut, and the
+// result is the same.
+//
+// What bounds it: reading the logits once.  Few rows: a cluster of CTAs per row, joined through distributed shared memory.
+#include <cooperative_groups.h>
+
+#include "common.cuh"
+
+namespace actkv {
+namespace lp {
+
+constexpr int NT = 512, NWARP = NT / 32;
+constexpr int LP_STEP = 8192;             // logits of a CTA between two looks at the candidates
+constexpr int LP_TIGHT = 256;
+constexpr int LP_CAP = LP_STEP + LP_TIGHT;
+constexpr int RANK_MAX = 1024;            // candidates ranked against each other; more are cut by digits first
+constexpr float NO_REF = -3.402823466e38f;
+constexpr float FAR = -1e4f;              // exp of it is 0
+
+struct Args {
+  const void* logits;
+  int64_t row_stride;
+  const int32_t* given;
+  float *logprob, *entropy, *lse, *top_logprob;
+  int32_t* top_index;
+  int32_t* status;
+  int32_t vocab, n_given, top_k;
+};
+
+__device__ __forceinline__ uint32_t okey(float x) {
+  uint32_t b = __float_as_uint(x);
+  if (b == 0x80000000u) b = 0u;                                            // -0 and +0 are equal
+  return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
+}
+__device__ __forceinline__ float okey_inv(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k); }
+__device__ __forceinline__ uint64_t key_of(float x, uint32_t token) { return ((uint64_t)okey(x) << 32) | (0xffffffffu - token); }
+
+template <typename T> struct Vec;
+template <> struct Vec<float> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ void open(const uint4& v, float* x) {
+    x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
+  }
+};
+template <> struct Vec<__nv_bfloat16> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ void open(const uint4& v, float* x) {
+    const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(u[i] << 16);
+      x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+    }
+  }
+};
+__device__ __forceinline__ float to_f(float x) { return x; }
+__device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
+
+struct Smem {
+  uint64_t cand[LP_CAP];
+  uint64_t best[ACTKV_LOGPROB_MAX_TOP];   // the CTA's own top_k, descending
+  float4 red[NWARP];                      // (m, S, T) of the warps
+  float chunk[128];
+  uint32_t hist[256];
+  float4 mst;                             // (m, S, T) of the CTA
+  int n_best;
+  uint32_t n_cand, thr;
+  uint32_t pick[2];
+};
+
+// The k largest of cand[0 .. n) in descending order into cand[0 .. min(n, k)).  All threads call it, between barriers.
+__device__ __noinline__ void cut(Smem* sm, int n, int k) {
+  const int tid = threadIdx.x;
+  if (n > RANK_MAX) {
+    // the k-th largest key, digit by digit; then only what is not smaller stays (k keys: they are all different)
+    uint64_t prefix = 0;
+    uint32_t left = (uint32_t)k;
+    for (int shift = 56; shift >= 0; shift -= 8) {
+      for (int i = tid; i < 256; i += NT) sm->hist[i] = 0;
+      __syncthreads();
+      for (int i = tid; i < n; i += NT) {
+        const uint64_t key = sm->cand[i];
+        if (shift == 56 || (key >> (shift + 8)) == prefix) atomicAdd(&sm->hist[(uint32_t)(key >> shift) & 255u], 1u);
+      }
+      __syncthreads();
+      if (tid == 0) {
+        uint32_t above = 0;
+        int d = 255;
+        for (; d > 0; --d) {
+          if (above + sm->hist[d] >= left) break;
+          above += sm->hist[d];
+        }
+        sm->pick[0] = (uint32_t)d;
+        sm->pick[1] = left - above;
+      }
+      __syncthreads();
+      prefix = (prefix << 8) | sm->pick[0];
+      left = sm->pick[1];
+      __syncthreads();
+    }
+    uint64_t mine[(LP_CAP + NT - 1) / NT];
+#pragma unroll
+    for (int j = 0; j < (LP_CAP + NT - 1) / NT; ++j) {
+      const int i = tid + j * NT;
+      mine[j] = i < n ? sm->cand[i] : 0;
+      if (!(i < n && mine[j] >= prefix)) mine[j] = 0;                      // (no key is 0: a token is below 2^31)
+    }
+    if (tid == 0) sm->pick[0] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < (LP_CAP + NT - 1) / NT; ++j)
+      if (mine[j] != 0) sm->cand[atomicAdd(&sm->pick[0], 1u)] = mine[j];
+    __syncthreads();
+    n = (int)sm->pick[0];
+    __syncthreads();
+  }
+  uint64_t a[RANK_MAX / NT];
+  int rank[RANK_MAX / NT];
+#pragma unroll
+  for (int j = 0; j < RANK_MAX / NT; ++j) {
+    const int i = tid + j * NT;
+    rank[j] = 0x7fffffff;
+    a[j] = 0;
+    if (i < n) {
+      a[j] = sm->cand[i];
+      int r = 0;
+      for (int o = 0; o < n; ++o) r += sm->cand[o] > a[j] ? 1 : 0;
+      rank[j] = r;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < RANK_MAX / NT; ++j)
+    if (rank[j] < k) sm->cand[rank[j]] = a[j];
+  __syncthreads();
+}
+
+__device__ __forceinline__ float4 join(float4 a, float4 b) {               // (m, S, T)
+  const float m = fmaxf(a.x, b.x);
+  // (distances of up to 2^128 are cut where the exponential is 0 long since: no infinity meets that 0)
+  const float da = fmaxf(a.x - m, FAR), db = fmaxf(b.x - m, FAR);
+  const float fa = exp2f(da * kLog2e), fb = exp2f(db * kLog2e);
+  return make_float4(m, a.y * fa + b.y * fb, (a.z + da * a.y) * fa + (b.z + db * b.y) * fb, 0.f);
+}
+
+template <typename T, int C>
+__global__ void __launch_bounds__(NT, 2) logprob_kernel(const Args a) {
+  const void* logits = a.logits;
+  pdl_begin(logits);
+  extern __shared__ __align__(16) uint8_t lp_smem[];
+  Smem* sm = reinterpret_cast<Smem*>(lp_smem);
+  constexpr int VE = Vec<T>::N, U = LP_STEP / NT / VE;                     // vectors of a thread per step
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int row = blockIdx.x / C, part = blockIdx.x % C;
+  const int vocab = a.vocab, k = a.top_k;
+  const T* z = reinterpret_cast<const T*>(logits) + (int64_t)row * a.row_stride;
+  const int mis = (int)(((uintptr_t)z & 15) / sizeof(T));                  // logits of the first vector that belong to others
+  const uint4* zv = reinterpret_cast<const uint4*>(z - mis);
+  const int nv = (int)(((int64_t)mis + vocab + VE - 1) / VE);
+  const int v0 = (int)((int64_t)nv * part / C), v1 = (int)((int64_t)nv * (part + 1) / C);
+
+  if (tid == 0) sm->n_cand = 0;
+  int32_t tok = -1;
+  float ztok = 0.f;
+  if (part == 0 && tid < a.n_given) {                                      // (early: beside the row's own loads)
+    tok = a.given[(int64_t)row * a.n_given + tid];
+    if (tok >= 0 && tok < vocab) ztok = to_f(z[tok]);
+  }
+
+  auto load = [&](int v, float* x) {
+    if (v < v1 && v * (int64_t)VE >= mis && (v + 1) * (int64_t)VE <= (int64_t)mis + vocab) {
+      Vec<T>::open(__ldg(zv + v), x);
+    } else {
+#pragma unroll
+      for (int e = 0; e < VE; ++e) {
+        const int64_t t = (int64_t)v * VE + e - mis;
+        x[e] = v < v1 && t >= 0 && t < vocab ? to_f(z[t]) : -INFINITY;
+      }
+    }
+  };
+
+  float m = NO_REF, S = 0.f, Tt = 0.f;
+  uint32_t thr = 0;                                                        // keys from here on are candidates
+  float thr_f = -INFINITY;
+  bool first = true;
+  for (int vb = v0; vb < v1; vb += NT * U) {
+    float x[U * VE];
+#pragma unroll
+    for (int u = 0; u < U; ++u) load(vb + u * NT + tid, x + u * VE);
+    float mx = x[0];
+#pragma unroll
+    for (int e = 1; e < U * VE; ++e) mx = fmaxf(mx, x[e]);
+    if (first && k > 0) {
+      // a first bound: k of the 128 chunks have a logit that reaches the k-th largest of their maxima
+      float cm = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+      cm = fmaxf(cm, __shfl_xor_sync(0xffffffffu, cm, 2));
+      if ((tid & 3) == 0) sm->chunk[tid >> 2] = cm > -INFINITY ? cm : -INFINITY;     // (NaN alone: no bound)
+      __syncthreads();
+      if (tid < 128) {
+        const float v = sm->chunk[tid];
+        int rank = 0;
+        for (int o = 0; o < 128; ++o) {
+          const float w = sm->chunk[o];
+          rank += w > v || (w == v && o < tid) ? 1 : 0;
+        }
+        if (rank == k - 1) sm->thr = v == -INFINITY ? 0u : okey(v);
+      }
+      __syncthreads();
+      thr = sm->thr;
+      thr_f = thr == 0 ? -INFINITY : okey_inv(thr);
+    }
+    first = false;
+    if (mx > m) {
+      const float d = fmaxf(m - mx, FAR), f = exp2f(d * kLog2e);
+      Tt = (Tt + d * S) * f;
+      S *= f;
+      m = mx;
+    }
+    float bs = 0.f;
+#pragma unroll
+    for (int e = 0; e < U * VE; ++e) {
+      const float y = x[e] - m;
+      const float p = exp2f(y * kLog2e);
+      bs += p;
+      Tt = fmaf(p, fmaxf(y, FAR), Tt);
+    }
+    S += bs;
+    int over = 0;
+    if (k > 0) {
+      if (mx >= thr_f || bs != bs) {
+#pragma unroll
+        for (int e = 0; e < U * VE; ++e) {
+          const int64_t t = ((int64_t)vb + (e / VE) * NT + tid) * VE + e % VE - mis;
+          if (t >= 0 && t < vocab && vb + (e / VE) * NT + tid < v1 && okey(x[e]) >= thr) {
+            const uint32_t at = atomicAdd(&sm->n_cand, 1u);
+            sm->cand[at] = key_of(x[e], (uint32_t)t);                      // (at most LP_TIGHT before the step: it fits)
+            over |= at >= LP_TIGHT;
+          }
+        }
+      }
+      if (__syncthreads_or(over)) {
+        cut(sm, (int)sm->n_cand, k);
+        if (tid == 0) sm->n_cand = (uint32_t)k;                            // (more than LP_TIGHT >= k there were)
+        // what comes later is larger as a token: an equal logit no longer counts
+        thr = (uint32_t)(sm->cand[k - 1] >> 32);
+        thr = thr == 0xffffffffu ? thr : thr + 1;
+        thr_f = okey_inv(thr);
+        if (thr_f != thr_f) thr_f = INFINITY;                              // (the bound is a NaN: only NaN go on, by bs)
+        __syncthreads();
+      }
+    }
+  }
+
+  // ---- the CTA's (m, S, T) and top k ----
+  float4 mst = make_float4(m, S, Tt, 0.f);
+#pragma unroll
+  for (int o = 16; o >= 1; o >>= 1) {
+    const float4 b = make_float4(__shfl_xor_sync(0xffffffffu, mst.x, o), __shfl_xor_sync(0xffffffffu, mst.y, o),
+                                 __shfl_xor_sync(0xffffffffu, mst.z, o), 0.f);
+    mst = (lane & o) ? join(b, mst) : join(mst, b);
+  }
+  if (lane == 0) sm->red[warp] = mst;
+  __syncthreads();
+  const int n_mine = (int)min((uint32_t)LP_CAP, sm->n_cand);
+  if (k > 0) cut(sm, n_mine, k);
+  mst = sm->red[0];
+#pragma unroll
+  for (int w = 1; w < NWARP; ++w) mst = join(mst, sm->red[w]);
+  int n_top = min(n_mine, k);
+  if constexpr (C > 1) {
+    namespace cg = cooperative_groups;
+    cg::cluster_group cl = cg::this_cluster();
+    if (tid < n_top) sm->best[tid] = sm->cand[tid];
+    if (tid == 0) {
+      sm->mst = mst;
+      sm->n_best = n_top;
+    }
+    cl.sync();
+    if (part == 0) {
+      int n = 0;
+      float4 all = mst;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const Smem* other = cl.map_shared_rank(sm, c);
+        const int nb = other->n_best;
+        if (c > 0) all = join(all, other->mst);
+        if (tid < nb) sm->cand[n + tid] = other->best[tid];
+        n += nb;
+      }
+      mst = all;
+      __syncthreads();
+      if (k > 0) cut(sm, n, k);
+      n_top = min(n, k);
+    }
+    cl.sync();                                                             // (the others' shared memory has been read)
+    if (part != 0) return;
+  }
+
+  // ---- results ----
+  const float ls = logf(mst.y);
+  const bool none = mst.y == 0.f;
+  auto lp_of = [&](float v) { return none ? -INFINITY : (v - mst.x) - ls; };
+  if (tid == 0) {
+    if (a.lse != nullptr) a.lse[row] = none ? -INFINITY : mst.x + ls;
+    if (a.entropy != nullptr) a.entropy[row] = none ? 0.f : ls - mst.z / mst.y;
+  }
+  for (int j = tid; j < k; j += NT) {
+    const uint64_t key = j < n_top ? sm->cand[j] : 0;
+    a.top_index[(int64_t)row * k + j] = j < n_top ? (int32_t)(0xffffffffu - (uint32_t)key) : -1;
+    a.top_logprob[(int64_t)row * k + j] = j < n_top ? lp_of(okey_inv((uint32_t)(key >> 32))) : -INFINITY;
+  }
+  for (int j = tid; j < a.n_given; j += NT) {
+    if (j != tid) {
+      tok = a.given[(int64_t)row * a.n_given + j];
+      if (tok >= 0 && tok < vocab) ztok = to_f(z[tok]);
+    }
+    float v = 0.f;
+    if (tok >= vocab) {
+      report(a.status, ACTKV_E_BADINDEX, row, tok);
+      v = __uint_as_float(0x7fc00000u);
+    } else if (tok >= 0) {
+      v = lp_of(ztok);
+    }
+    a.logprob[(int64_t)row * a.n_given + j] = v;
+  }
+}
+
+template <typename T, int C>
+int launch(const Args& a, int n_rows, cudaStream_t s) {
+  if (ensure_dyn_smem(logprob_kernel<T, C>, sizeof(Smem)) != cudaSuccess) return ACTKV_E_CUDA;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)n_rows * C);
+  cfg.blockDim = dim3(NT);
+  cfg.dynamicSmemBytes = sizeof(Smem);
+  cfg.stream = s;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = C;
+  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = C > 1 ? 2 : 1;
+  (void)cudaLaunchKernelEx(&cfg, logprob_kernel<T, C>, a);
+  ACTKV_CHECK_LAUNCH();
+  return ACTKV_OK;
+}
+
+template <typename T>
+int dispatch(const Args& a, int n_rows, cudaStream_t s) {
+  // CTAs per row: enough for two per SM, none with fewer than a step's logits
+  int c = 1;
+  while (c < 8 && (int64_t)n_rows * c < 148 && a.vocab / (2 * c) >= LP_STEP / 2) c *= 2;
+  switch (c) {
+    case 1: return launch<T, 1>(a, n_rows, s);
+    case 2: return launch<T, 2>(a, n_rows, s);
+    case 4: return launch<T, 4>(a, n_rows, s);
+    default: return launch<T, 8>(a, n_rows, s);
+  }
+}
+
+}  // namespace lp
+}  // namespace actkv
+
+extern "C" int actkv_logprob(const void* logits, int32_t dtype, int32_t n_rows, int32_t vocab, int64_t row_stride,
+                             const int32_t* given, int32_t n_given, int32_t top_k, float* logprob, float* entropy, float* lse,
+                             float* top_logprob, int32_t* top_index, int32_t* status, actkv_stream_t stream) {
+  using namespace actkv;
+  using namespace actkv::lp;
+  if (dtype != ACTKV_F32 && dtype != ACTKV_BF16) return ACTKV_E_INVALID;
+  if (n_rows < 0 || vocab <= 0 || row_stride < vocab || n_given < 0 || top_k < 0 || top_k > ACTKV_LOGPROB_MAX_TOP) return ACTKV_E_INVALID;
+  if (n_rows == 0) return ACTKV_OK;
+  if (!logits || ((uintptr_t)logits & (dtype == ACTKV_F32 ? 3 : 1))) return ACTKV_E_INVALID;
+  if (n_given > 0 && (!given || !logprob)) return ACTKV_E_INVALID;
+  if (top_k > 0 && (!top_logprob || !top_index)) return ACTKV_E_INVALID;
+  if (n_rows > 0x7fffffff / 8) return ACTKV_E_TOOBIG;
+  Args a{logits, row_stride, given, logprob, entropy, lse, top_logprob, top_index, status, vocab, n_given, top_k};
+  cudaStream_t s = (cudaStream_t)stream;
+  return dtype == ACTKV_F32 ? dispatch<float>(a, n_rows, s) : dispatch<__nv_bfloat16>(a, n_rows, s);
+}

@@ -330,6 +330,74 @@ class Compressor:
             raise B.ActKVError(f"device status {st}", st[0])
 
 
+class Rope:
+    """Rotary positions: `sections` rotary pairs per axis, `inv_freq` float32 [sum(sections)] on the device."""
+
+    def __init__(self, inv_freq: torch.Tensor, sections, interleaved: bool = False):
+        self.inv_freq = inv_freq                 # (the descriptor holds its address)
+        self.desc = B.rope_desc(inv_freq, list(sections), interleaved)
+
+
+class Decoder:
+    """Decoding on the paged cache between two compression steps: resize -> append -> attend, and copies for branches.
+
+    Holds the descriptors of the pool and its tables and the workspace of `attend`; max_rows, max_win and max_tok bound a call's
+    rows, a request's rows and a request's length.  Calls on two streams at once need a Decoder each (the workspace)."""
+
+    def __init__(self, pool: torch.Tensor, page_table, seq_len, free_list, free_count, n_q_heads: int, max_rows: int = 1,
+                 max_win: int = 1, max_tok: int = 1, layers_per_call: int = 1):
+        B.load()
+        self.dev, self.pool = pool.device, pool
+        self.page_table, self.seq_len, self.free_list, self.free_count = page_table, seq_len, free_list, free_count
+        self.pd = B.pool_desc(pool)
+        self.td = B.tables_desc(page_table, seq_len, free_list, free_count)
+        self.n_q_heads, self.max_rows, self.max_win, self.max_tok = n_q_heads, max_rows, max_win, max_tok
+        self.lpc = layers_per_call
+        self.status = torch.zeros(4, dtype=torch.int32, device=self.dev)
+        self.ws = _ws(B.actkv_attend_workspace_bytes(self.pd, self.td.n_req, layers_per_call, n_q_heads, max_win, max_tok), self.dev)
+
+    def _layers(self, l0, l1, n):
+        l1 = l0 + n if l1 is None else l1
+        assert l1 - l0 == n and n <= self.lpc
+        return l1
+
+    def resize(self, new_len, stream=None):
+        """Lengths of all requests from now on (negative: as it is): pages from and to the free list."""
+        B.actkv_resize(self.pd, self.td, new_len, self.status, stream)
+
+    def append(self, k, v, win_indptr, q=None, q_out=None, rope: Optional[Rope] = None, positions=None, l0=0, l1=None, stream=None):
+        """The newest tokens' k and v [layers, rows, KV heads, D] into their slots; q turned into q_out."""
+        l1 = self._layers(l0, l1, k.shape[0])
+        B.actkv_append(self.pd, self.td, l0, l1, q, k, v, win_indptr, self.n_q_heads, None if rope is None else rope.desc,
+                       positions, q_out, self.status, stream)
+
+    def attend(self, q, win_indptr, sm_scale, causal, out, lse=None, window_left=0, l0=0, l1=None, stream=None):
+        """Attention of q [layers, rows, q-heads, D] over the cache; lse is what `Compressor` takes as lse_in."""
+        l1 = self._layers(l0, l1, q.shape[0])
+        assert q.shape[1] <= self.max_rows
+        B.actkv_attend(self.pd, self.td, l0, l1, q, win_indptr, self.n_q_heads, sm_scale, causal, window_left, out, lse,
+                       q.shape[1], self.max_win, self.max_tok, self.ws, self.status, stream)
+
+    def copy(self, src, dst, length, max_len, l0=0, l1=None, stream=None):
+        """The first length[i] tokens of request src[i] into the pages of request dst[i]."""
+        B.actkv_copy(self.pd, self.td, l0, self.pd.n_layers if l1 is None else l1, src, dst, length, max_len, self.status, stream)
+
+    def check_status(self):
+        st = self.status.cpu().tolist()
+        if st[0] != 0:
+            raise B.ActKVError(f"device status {st}", st[0])
+
+
+class LogprobBuffers:
+    """Result buffers of actkv_logprob for up to `rows` logits rows."""
+
+    def __init__(self, rows: int, n_given: int, top_k: int, device):
+        f = lambda *shape: torch.empty(shape, dtype=torch.float32, device=device)
+        self.logprob, self.entropy, self.lse, self.top_logprob = f(rows, n_given), f(rows), f(rows), f(rows, top_k)
+        self.top_index = torch.empty((rows, top_k), dtype=torch.int32, device=device)
+        self.status = torch.zeros(4, dtype=torch.int32, device=device)
+
+
 class LrfuState:
     """Device buffers of the attention-aware LRFU policy (Section 5.1) for one pool: the persistent
     keep-scores KS [layers * KV heads, sum_tok] in the score layout, the survivors' keep-scores
