@@ -6,7 +6,6 @@ on a non-zero return code.  There is no fallback: a missing or unloadable librar
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 import os
 from typing import Optional
@@ -526,23 +525,43 @@ def actkv_compact_noalloc(pool: PoolDesc, tables: TablesDesc, layer_begin, layer
 # ---------------------------------------------------------------------------------------------
 # decoding between two compression steps
 #
-# These calls may be made while another device than the tensors' is current; all tensors of a call are on one device.
+# These calls may be made while another device than the tensors' is current; all tensors of a call are on one device.  They
+# are made once per layer and token, so the checks take a few tenths of a microsecond per tensor.
 
 
-def _on(dev: torch.device):
-    """Context in which `dev` is the current device (none is entered when it already is)."""
-    return contextlib.nullcontext() if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
-
-
-def _same_device(dev, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.device != dev:
-            raise TypeError(f"{name}: on {t.device}, expected {dev}")
-
-
-def _sized(t, n: int, name: str):
-    if t is not None and t.numel() < n:
+def _arg(t, dtype, index, n, name):
+    """Address of a contiguous tensor of this type on device `index` with at least n elements (None: null)."""
+    if t is None:
+        return None
+    if t.get_device() != index:
+        raise TypeError(f"{name}: on {t.device}, expected cuda:{index}")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if not t.is_contiguous():
+        raise TypeError(f"{name}: expected a contiguous tensor")
+    if t.numel() < n:
         raise ValueError(f"{name}: {t.numel()} elements, expected at least {n}")
+    return t.data_ptr()
+
+
+def _cuda_index(t, name):
+    index = t.get_device()
+    if index < 0:
+        raise TypeError(f"{name}: expected a CUDA tensor")
+    return index
+
+
+def _call(name, index, stream, *args):
+    """Calls the entry point on `stream`, or on the current stream of device `index`, with that device current."""
+    raw = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+    fn = getattr(_lib or load(), name)
+    if torch._C._cuda_getDevice() == index:
+        rc = fn(*args, raw)
+    else:
+        with torch.cuda.device(index):
+            rc = fn(*args, raw)
+    if rc != 0:
+        raise ActKVError(name, rc)
 
 
 def actkv_attend_workspace_bytes(pool: PoolDesc, n_req, n_layers_sub, n_q_heads, max_win, max_tok) -> int:
@@ -551,29 +570,21 @@ def actkv_attend_workspace_bytes(pool: PoolDesc, n_req, n_layers_sub, n_q_heads,
 
 def actkv_attend(pool: PoolDesc, tables: TablesDesc, layer_begin, layer_end, q, win_indptr, n_q_heads, sm_scale, causal,
                  window_left, out, lse_out, sum_win, max_win, max_tok, ws, status, stream=None):
-    dev = q.device
-    _same_device(dev, win_indptr=win_indptr, out=out, lse_out=lse_out, ws=ws, status=status)
+    i = _cuda_index(q, "q")
     rows = (layer_end - layer_begin) * sum_win * n_q_heads
-    _sized(q, rows * pool.head_dim, "q")
-    _sized(out, rows * pool.head_dim, "out")
-    _sized(lse_out, rows, "lse_out")
-    _sized(win_indptr, tables.n_req + 1, "win_indptr")
-    with _on(dev):
-        rc = load().actkv_attend(pool, tables, layer_begin, layer_end, _ptr(q, torch.bfloat16, "q"),
-                                 _ptr(win_indptr, torch.int32, "win_indptr"), n_q_heads, float(sm_scale), 1 if causal else 0,
-                                 window_left, _ptr(out, torch.bfloat16, "out"), _ptr(lse_out, torch.float32, "lse_out"), sum_win,
-                                 max_win, max_tok, _ptr(ws, None, "ws"), ws.numel() * ws.element_size(),
-                                 _ptr(status, torch.int32, "status"), _stream(stream))
-    _check("actkv_attend", rc)
+    n = rows * pool.head_dim
+    _call("actkv_attend", i, stream, pool, tables, layer_begin, layer_end, _arg(q, torch.bfloat16, i, n, "q"),
+          _arg(win_indptr, torch.int32, i, tables.n_req + 1, "win_indptr"), n_q_heads, sm_scale, 1 if causal else 0, window_left,
+          _arg(out, torch.bfloat16, i, n, "out"), _arg(lse_out, torch.float32, i, rows, "lse_out"), sum_win, max_win, max_tok,
+          _arg(ws, torch.uint8, i, 0, "ws"), ws.numel(), _arg(status, torch.int32, i, 4, "status"))
 
 
 def rows_desc(t: torch.Tensor, name: str = "rows") -> RowsDesc:
     """Descriptor of a bf16 tensor [layers, rows, heads, head_dim] (any strides with a contiguous head dimension)."""
-    if not t.is_cuda:
-        raise TypeError(f"{name}: expected a CUDA tensor")
-    if t.dtype != torch.bfloat16 or t.dim() != 4 or (t.stride(3) != 1 and t.shape[3] != 1):
-        raise TypeError(f"{name}: expected bf16 [layers, rows, heads, D] with contiguous D")
+    _cuda_index(t, name)
     st = t.stride()
+    if t.dtype is not torch.bfloat16 or len(st) != 4 or (st[3] != 1 and t.shape[3] != 1):
+        raise TypeError(f"{name}: expected bf16 [layers, rows, heads, D] with contiguous D")
     return RowsDesc(t.data_ptr(), st[0], st[1], st[2])
 
 
@@ -591,47 +602,38 @@ def rope_desc(inv_freq: Optional[torch.Tensor], sections, interleaved: bool = Fa
 def actkv_append(pool: PoolDesc, tables: TablesDesc, layer_begin, layer_end, q, k, v, win_indptr, n_q_heads,
                  rope: Optional[RopeDesc], positions, q_out, status, stream=None):
     """q, k, v [layers, rows, heads, head_dim] (strided; q may be None), positions int32 [axes, rows]."""
-    dev, sum_win, nls = k.device, k.shape[1], layer_end - layer_begin
-    _same_device(dev, q=q, v=v, win_indptr=win_indptr, positions=positions, q_out=q_out, status=status)
-    D, hk = pool.head_dim, pool.n_kv_heads
-    if k.shape != (nls, sum_win, hk, D) or v.shape != k.shape or (q is not None and q.shape != (nls, sum_win, n_q_heads, D)):
+    i, nls, D = _cuda_index(k, "k"), layer_end - layer_begin, pool.head_dim
+    shape = k.shape
+    sum_win = shape[1]
+    if shape != (nls, sum_win, pool.n_kv_heads, D) or v.shape != shape or (q is not None and q.shape != (nls, sum_win, n_q_heads, D)):
         raise ValueError("actkv_append: q, k and v are [layers, rows, heads, head_dim] of this call and pool")
-    if q is not None:
-        if q_out is None:
-            raise ValueError("q_out: expected with q")
-        _sized(q_out, nls * sum_win * n_q_heads * D, "q_out")
+    if v.get_device() != i or (q is not None and q.get_device() != i):
+        raise TypeError(f"q, k, v: expected on cuda:{i}")
+    if q is not None and q_out is None:
+        raise ValueError("q_out: expected with q")
+    n_pos = 0
     if rope is not None and rope.rotary_dim:
         if positions is None:
             raise ValueError("positions: expected with rope")
-        _sized(positions, rope.n_axes * sum_win, "positions")
-    _sized(win_indptr, tables.n_req + 1, "win_indptr")
-    with _on(dev):
-        rc = load().actkv_append(pool, tables, layer_begin, layer_end, None if q is None else rows_desc(q, "q"),
-                                 rows_desc(k, "k"), rows_desc(v, "v"), _ptr(win_indptr, torch.int32, "win_indptr"), n_q_heads,
-                                 rope, _ptr(positions, torch.int32, "positions"), _ptr(q_out, torch.bfloat16, "q_out"), sum_win,
-                                 _ptr(status, torch.int32, "status"), _stream(stream))
-    _check("actkv_append", rc)
+        n_pos = rope.n_axes * sum_win
+    _call("actkv_append", i, stream, pool, tables, layer_begin, layer_end, None if q is None else rows_desc(q, "q"),
+          rows_desc(k, "k"), rows_desc(v, "v"), _arg(win_indptr, torch.int32, i, tables.n_req + 1, "win_indptr"), n_q_heads, rope,
+          _arg(positions, torch.int32, i, n_pos, "positions"),
+          _arg(q_out, torch.bfloat16, i, 0 if q is None else nls * sum_win * n_q_heads * D, "q_out"), sum_win,
+          _arg(status, torch.int32, i, 4, "status"))
 
 
 def actkv_resize(pool: PoolDesc, tables: TablesDesc, new_len, status, stream=None):
-    _same_device(new_len.device, status=status)
-    _sized(new_len, tables.n_req, "new_len")
-    with _on(new_len.device):
-        rc = load().actkv_resize(pool, tables, _ptr(new_len, torch.int32, "new_len"), _ptr(status, torch.int32, "status"),
-                                 _stream(stream))
-    _check("actkv_resize", rc)
+    i = _cuda_index(new_len, "new_len")
+    _call("actkv_resize", i, stream, pool, tables, _arg(new_len, torch.int32, i, tables.n_req, "new_len"),
+          _arg(status, torch.int32, i, 4, "status"))
 
 
 def actkv_copy(pool: PoolDesc, tables: TablesDesc, layer_begin, layer_end, src, dst, length, max_len, status, stream=None):
-    dev, n = src.device, src.numel()
-    _same_device(dev, dst=dst, length=length, status=status)
-    _sized(dst, n, "dst")
-    _sized(length, n, "length")
-    with _on(dev):
-        rc = load().actkv_copy(pool, tables, layer_begin, layer_end, _ptr(src, torch.int32, "src"), _ptr(dst, torch.int32, "dst"),
-                               _ptr(length, torch.int32, "length"), n, max_len, _ptr(status, torch.int32, "status"),
-                               _stream(stream))
-    _check("actkv_copy", rc)
+    i, n = _cuda_index(src, "src"), src.numel()
+    _call("actkv_copy", i, stream, pool, tables, layer_begin, layer_end, _arg(src, torch.int32, i, n, "src"),
+          _arg(dst, torch.int32, i, n, "dst"), _arg(length, torch.int32, i, n, "length"), n, max_len,
+          _arg(status, torch.int32, i, 4, "status"))
 
 
 _LOGIT_TYPES = {torch.float32: 0, torch.bfloat16: 1}
@@ -640,26 +642,20 @@ _LOGIT_TYPES = {torch.float32: 0, torch.bfloat16: 1}
 def actkv_logprob(logits, given, logprob, entropy, lse, top_logprob, top_index, status, stream=None):
     """logits [rows, vocab] float32 or bf16, rows any distance apart; given int32 [rows, n] or None; top_logprob /
     top_index [rows, k] or None."""
-    if not logits.is_cuda:
-        raise TypeError("logits: expected a CUDA tensor")
-    if logits.dtype not in _LOGIT_TYPES or logits.dim() != 2 or (logits.stride(1) != 1 and logits.shape[1] != 1):
+    i = _cuda_index(logits, "logits")
+    kind = _LOGIT_TYPES.get(logits.dtype)
+    st = logits.stride()
+    if kind is None or len(st) != 2 or (st[1] != 1 and logits.shape[1] != 1):
         raise TypeError("logits: expected float32 or bf16 [rows, vocab] with contiguous rows")
     n, vocab = logits.shape
-    dev = logits.device
-    _same_device(dev, given=given, logprob=logprob, entropy=entropy, lse=lse, top_logprob=top_logprob, top_index=top_index,
-                 status=status)
     n_given = 0 if given is None or n == 0 else given.numel() // n
     top_k = 0 if top_index is None or n == 0 else top_index.numel() // n
     if n_given and (given.numel() != n * n_given or logprob is None or logprob.numel() != given.numel()):
         raise ValueError("given, logprob: expected [rows, n]")
     if top_k and (top_index.numel() != n * top_k or top_logprob is None or top_logprob.numel() != top_index.numel()):
         raise ValueError("top_logprob, top_index: expected [rows, k]")
-    _sized(entropy, n, "entropy")
-    _sized(lse, n, "lse")
-    with _on(dev):
-        rc = load().actkv_logprob(logits.data_ptr(), _LOGIT_TYPES[logits.dtype], n, vocab, logits.stride(0) if n > 1 else vocab,
-                                  _ptr(given, torch.int32, "given"), n_given, top_k, _ptr(logprob, torch.float32, "logprob"),
-                                  _ptr(entropy, torch.float32, "entropy"), _ptr(lse, torch.float32, "lse"),
-                                  _ptr(top_logprob, torch.float32, "top_logprob"), _ptr(top_index, torch.int32, "top_index"),
-                                  _ptr(status, torch.int32, "status"), _stream(stream))
-    _check("actkv_logprob", rc)
+    _call("actkv_logprob", i, stream, logits.data_ptr(), kind, n, vocab, st[0] if n > 1 else vocab,
+          _arg(given, torch.int32, i, 0, "given"), n_given, top_k, _arg(logprob, torch.float32, i, 0, "logprob"),
+          _arg(entropy, torch.float32, i, n, "entropy"), _arg(lse, torch.float32, i, n, "lse"),
+          _arg(top_logprob, torch.float32, i, 0, "top_logprob"), _arg(top_index, torch.int32, i, 0, "top_index"),
+          _arg(status, torch.int32, i, 4, "status"))

@@ -47,12 +47,14 @@ __device__ __forceinline__ uint64_t key_of(float x, uint32_t token) { return ((u
 template <typename T> struct Vec;
 template <> struct Vec<float> {
   static constexpr int N = 4;
+  static __device__ __forceinline__ uint4 none() { return make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u); }   // -inf
   static __device__ __forceinline__ void open(const uint4& v, float* x) {
     x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
   }
 };
 template <> struct Vec<__nv_bfloat16> {
   static constexpr int N = 8;
+  static __device__ __forceinline__ uint4 none() { return make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }
   static __device__ __forceinline__ void open(const uint4& v, float* x) {
     const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -123,6 +125,20 @@ __device__ __noinline__ void cut(Smem* sm, int n, int k) {
     n = (int)sm->pick[0];
     __syncthreads();
   }
+  // ranks by counting: with few candidates, 8 lanes share one
+  if (n <= NT / 8) {
+    const int i = tid >> 3;
+    const uint64_t a = i < n ? sm->cand[i] : 0;
+    int r = 0;
+    for (int o = tid & 7; o < n; o += 8) r += sm->cand[o] > a ? 1 : 0;
+    r += __shfl_xor_sync(0xffffffffu, r, 1);
+    r += __shfl_xor_sync(0xffffffffu, r, 2);
+    r += __shfl_xor_sync(0xffffffffu, r, 4);
+    __syncthreads();
+    if (i < n && (tid & 7) == 0 && r < k) sm->cand[r] = a;
+    __syncthreads();
+    return;
+  }
   uint64_t a[RANK_MAX / NT];
   int rank[RANK_MAX / NT];
 #pragma unroll
@@ -133,6 +149,7 @@ __device__ __noinline__ void cut(Smem* sm, int n, int k) {
     if (i < n) {
       a[j] = sm->cand[i];
       int r = 0;
+#pragma unroll 4
       for (int o = 0; o < n; ++o) r += sm->cand[o] > a[j] ? 1 : 0;
       rank[j] = r;
     }
@@ -176,14 +193,25 @@ __global__ void __launch_bounds__(NT, 2) logprob_kernel(const Args a) {
     if (tok >= 0 && tok < vocab) ztok = to_f(z[tok]);
   }
 
-  auto load = [&](int v, float* x) {
-    if (v < v1 && v * (int64_t)VE >= mis && (v + 1) * (int64_t)VE <= (int64_t)mis + vocab) {
-      Vec<T>::open(__ldg(zv + v), x);
-    } else {
+  // vectors of which all logits are the row's own; the others (at most one at each end) are read one by one
+  const int in0 = mis > 0 ? 1 : 0, in1 = (int)(((int64_t)mis + vocab) / VE);
+  uint4 next[U];
+  auto load = [&](int vb) {
 #pragma unroll
-      for (int e = 0; e < VE; ++e) {
-        const int64_t t = (int64_t)v * VE + e - mis;
-        x[e] = v < v1 && t >= 0 && t < vocab ? to_f(z[t]) : -INFINITY;
+    for (int u = 0; u < U; ++u) {
+      const int v = vb + u * NT + tid;
+      next[u] = Vec<T>::none();
+      if (v < v1) {
+        if (v >= in0 && v < in1) {
+          next[u] = __ldg(zv + v);
+        } else {
+          T* one = reinterpret_cast<T*>(&next[u]);
+#pragma unroll
+          for (int e = 0; e < VE; ++e) {
+            const int64_t t = (int64_t)v * VE + e - mis;
+            if (t >= 0 && t < vocab) one[e] = z[t];
+          }
+        }
       }
     }
   };
@@ -192,10 +220,12 @@ __global__ void __launch_bounds__(NT, 2) logprob_kernel(const Args a) {
   uint32_t thr = 0;                                                        // keys from here on are candidates
   float thr_f = -INFINITY;
   bool first = true;
+  load(v0);
   for (int vb = v0; vb < v1; vb += NT * U) {
     float x[U * VE];
 #pragma unroll
-    for (int u = 0; u < U; ++u) load(vb + u * NT + tid, x + u * VE);
+    for (int u = 0; u < U; ++u) Vec<T>::open(next[u], x + u * VE);
+    if (vb + NT * U < v1) load(vb + NT * U);                               // (in flight while this step is worked on)
     float mx = x[0];
 #pragma unroll
     for (int e = 1; e < U * VE; ++e) mx = fmaxf(mx, x[e]);
@@ -205,15 +235,17 @@ __global__ void __launch_bounds__(NT, 2) logprob_kernel(const Args a) {
       cm = fmaxf(cm, __shfl_xor_sync(0xffffffffu, cm, 2));
       if ((tid & 3) == 0) sm->chunk[tid >> 2] = cm > -INFINITY ? cm : -INFINITY;     // (NaN alone: no bound)
       __syncthreads();
-      if (tid < 128) {
-        const float v = sm->chunk[tid];
-        int rank = 0;
-        for (int o = 0; o < 128; ++o) {
-          const float w = sm->chunk[o];
-          rank += w > v || (w == v && o < tid) ? 1 : 0;
-        }
-        if (rank == k - 1) sm->thr = v == -INFINITY ? 0u : okey(v);
+      const int c = tid >> 2;
+      const float v = sm->chunk[c];
+      int rank = 0;
+#pragma unroll 8
+      for (int o = tid & 3; o < 128; o += 4) {
+        const float w = sm->chunk[o];
+        rank += w > v || (w == v && o < c) ? 1 : 0;
       }
+      rank += __shfl_xor_sync(0xffffffffu, rank, 1);
+      rank += __shfl_xor_sync(0xffffffffu, rank, 2);
+      if (rank == k - 1 && (tid & 3) == 0) sm->thr = v == -INFINITY ? 0u : okey(v);
       __syncthreads();
       thr = sm->thr;
       thr_f = thr == 0 ? -INFINITY : okey_inv(thr);

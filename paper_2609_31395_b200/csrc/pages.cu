@@ -1,147 +1,209 @@
 // actkv_resize and actkv_copy: pages of a request claimed, given back, and copied into those of another (Section 2.5, Section
 // 7.2 last paragraph).
 //
-// resize_kernel  one CTA.  Whether the call can be carried out (enough free pages, all ids in range) is known before
-//                anything is written; pops are read before pushes overwrite their places on the stack.
-//                Bound by latency: four round trips to memory.
+// resize_kernel  one CTA, or a cluster of them.  Whether the call can be carried out (enough free pages, all ids in range) is
+//                known before anything is written; pops are read before pushes overwrite their places on the stack.
+//                Bound by latency: two round trips to memory and a scan over the requests.
 // copy_kernel    one CTA per (page of a source, source, layer and K or V): the rows are read once and written to every
 //                branch of that source.  Bound by reading and writing every byte once.
+#include <cooperative_groups.h>
+
 #include "common.cuh"
 
 namespace actkv {
 namespace pg {
 
-constexpr int RZ_NT = 1024;
+namespace cg = cooperative_groups;
 
-// Requests base .. base + RZ_NT - 1, one per thread: pages before and after, what the ones before it pop and push.
-struct Share {
-  int L, N, Y, X;                // lengths, pages
-  int64_t pop, push;             // exclusive prefixes over this batch
-  int64_t pops, pushes;          // totals of this batch
-};
-__device__ __forceinline__ void scan2(int64_t& a, int64_t& b, int64_t& ta, int64_t& tb) {     // exclusive; totals
-  __shared__ int64_t s_a[RZ_NT / 32], s_b[RZ_NT / 32];
+constexpr int RZ_KEEP = 4;       // ids that a thread holds between the check and the writes
+
+// Exclusive prefixes of two counts below 2^31 (packed in one word) over the CTA, and their totals.
+template <int NT>
+__device__ __forceinline__ uint64_t scan_pair(uint64_t v, uint64_t& total, uint64_t* s_warp) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int64_t ia = a, ib = b;
+  uint64_t incl = v;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
-    const int64_t x = __shfl_up_sync(0xffffffffu, ia, d), y = __shfl_up_sync(0xffffffffu, ib, d);
-    if (lane >= d) { ia += x; ib += y; }
+    const uint64_t t = __shfl_up_sync(0xffffffffu, incl, d);
+    if (lane >= d) incl += t;
   }
   __syncthreads();
-  if (lane == 31) { s_a[warp] = ia; s_b[warp] = ib; }
+  if (lane == 31) s_warp[warp] = incl;
   __syncthreads();
-  ia -= a;
-  ib -= b;
-  ta = tb = 0;
-  for (int w = 0; w < RZ_NT / 32; ++w) {
-    if (w == warp) { ia += ta; ib += tb; }
-    ta += s_a[w];
-    tb += s_b[w];
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < NT / 32; ++w) {
+    if (w == warp) incl += total;
+    total += s_warp[w];
   }
-  a = ia;
-  b = ib;
-}
-__device__ __forceinline__ Share share_of(const TablesView& tab, int P, const int32_t* new_len, int base) {
-  const int r = base + threadIdx.x;
-  Share s{0, -1, 0, 0, 0, 0, 0, 0};
-  if (r < tab.n_req) {
-    s.L = tab.seq_len[r];
-    s.N = new_len[r];
-    s.Y = s.L <= 0 ? 0 : (s.L - 1) / P + 1;
-    s.X = s.N < 0 ? s.Y : s.N == 0 ? 0 : (s.N - 1) / P + 1;
-    s.pop = max(0, s.X - s.Y);
-    s.push = max(0, s.Y - s.X);
-  }
-  scan2(s.pop, s.push, s.pops, s.pushes);
-  return s;
+  return incl - v;
 }
 
-__global__ void __launch_bounds__(RZ_NT) resize_kernel(TablesView tab, int32_t P, int32_t n_pages, const int32_t* __restrict__ new_len,
-                                                       int32_t* status) {
+// The entries that move, pops first, then pushes, are one list over all requests; CTA c of the CS of the cluster takes entries
+// (c * NT + thread) + n * CS * NT of it.  Requests are taken NT at a time (a batch; more than one only beyond NT requests).
+// Writes begin when every CTA has found its entries in order (first cluster barrier).  Ids are read before it and kept in
+// registers; those of a longer list are read again: pops before the second barrier, behind which pushes overwrite their places.
+template <int NT, int CS>
+__global__ void __launch_bounds__(NT) resize_kernel(TablesView tab, int32_t P, int32_t n_pages, const int32_t* __restrict__ new_len,
+                                                    int32_t* status) {
   pdl_begin(new_len);
-  __shared__ int64_t s_off[2][RZ_NT + 1];
-  __shared__ int32_t s_y[RZ_NT], s_x[RZ_NT];
+  __shared__ uint32_t s_pop[NT], s_push[NT];     // exclusive prefixes within the batch
+  __shared__ int32_t s_y[NT], s_x[NT];
+  __shared__ uint64_t s_warp[NT / 32];
+  __shared__ int s_bad;
   const int R = tab.n_req, tid = threadIdx.x;
+  int rank = 0;
+  if constexpr (CS > 1) rank = (int)cg::this_cluster().block_rank();
   const int32_t fc = *tab.free_count;
-  if (__syncthreads_or(status_set(status))) return;
+  const int failed = status_set(status) ? 1 : 0;
+  int32_t L = 0, N = -1, Y = 0, X = 0;
+  uint64_t before = 0, total = 0;
+  auto batch = [&](int base) {                   // one request per thread: pages before and after, what the ones before it move
+    const int r = base + tid;
+    L = 0, N = -1;
+    if (r < R) {
+      L = tab.seq_len[r];
+      N = new_len[r];
+    }
+    Y = L <= 0 ? 0 : (L - 1) / P + 1;
+    X = N < 0 ? Y : N == 0 ? 0 : (N - 1) / P + 1;
+    const uint64_t mine = (uint64_t)(uint32_t)max(0, X - Y) | ((uint64_t)(uint32_t)max(0, Y - X) << 32);
+    const bool far = L < 0 || Y > tab.max_pages || X > tab.max_pages;
+    before = scan_pair<NT>(far ? 0 : mine, total, s_warp);
+    s_pop[tid] = (uint32_t)before;
+    s_push[tid] = (uint32_t)(before >> 32);
+    s_y[tid] = Y;
+    s_x[tid] = X;
+    return far;
+  };
   // ---- what the call takes, and whether it can ----
   int64_t pops = 0, pushes = 0;
-  bool bad = fc < 0 || fc > n_pages;
-  if (bad && tid == 0) report(status, ACTKV_E_INVALID, -1, fc);
-  for (int base = 0; base < R; base += RZ_NT) {
-    const Share s = share_of(tab, P, new_len, base);
-    if (base + tid < R && (s.L < 0 || s.Y > tab.max_pages || s.X > tab.max_pages)) {
-      bad = true;
-      report(status, ACTKV_E_INVALID, base + tid, s.N);
-    }
-    pops += s.pops;
-    pushes += s.pushes;
+  bool bad = false;
+  auto fail = [&](bool is, int32_t code, int32_t where, int64_t what) {
+    if (is && !bad && !failed && rank == 0) report(status, code, where, (int32_t)min(what, (int64_t)0x7fffffff));
+    bad |= is;
+  };
+  const int n_batches = (R + NT - 1) / NT;
+  for (int b = n_batches - 1; b >= 0; --b) {     // (the first batch stays in place)
+    const bool far = batch(b * NT);
+    fail(far, ACTKV_E_INVALID, b * NT + tid, N);
+    pops += (uint32_t)total;
+    pushes += (int64_t)(total >> 32);
   }
-  if (pops > fc && !bad) {
-    bad = true;
-    if (tid == 0) report(status, ACTKV_E_NOFREE, (int32_t)min(pops, (int64_t)0x7fffffff), fc);
-  }
-  if (fc - pops + pushes > n_pages && !bad) {
-    bad = true;
-    if (tid == 0) report(status, ACTKV_E_INVALID, -2, (int32_t)min(fc - pops + pushes, (int64_t)0x7fffffff));
-  }
-  if (__syncthreads_or(bad)) return;
-  // entry e of the batch's pops (which = 0) or pushes (1): the request (last one whose prefix is <= e) and its place
-  auto find = [&](int which, int64_t e, int n) {
-    int lo = 0, hi = n - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (s_off[which][mid] <= e) lo = mid;
-      else hi = mid - 1;
-    }
+  bad = __syncthreads_or(bad || failed) != 0;
+  const bool solo = tid == 0;
+  if (fc < 0 || fc > n_pages) { if (solo) fail(true, ACTKV_E_INVALID, -1, fc); bad = true; }
+  if (pops > fc) { if (solo) fail(true, ACTKV_E_NOFREE, (int32_t)min(pops, (int64_t)0x7fffffff), fc); bad = true; }
+  if (fc - pops + pushes > n_pages) { if (solo) fail(true, ACTKV_E_INVALID, -2, fc - pops + pushes); bad = true; }
+  // entry e of the batch's pops or pushes: the request (the last one whose prefix is <= e)
+  auto find = [&](const uint32_t* pre, uint32_t e, int n) {
+    int lo = 0;
+    for (int step = NT / 2; step > 0; step >>= 1)
+      if (lo + step < n && pre[lo + step] <= e) lo += step;
     return lo;
   };
-  // phase 0: every id that moves is a page id; 1: pops; 2: pushes and lengths
-  for (int phase = 0; phase < 3; ++phase) {
+  int32_t id[RZ_KEEP];
+  int32_t* to[RZ_KEEP];                          // pops: the table entry; pushes: the entry they leave
+  // which: 0 look all entries over and keep the first, 1 write the pops that were not kept, 2 the pushes
+  auto sweep = [&](int which) {
     int64_t pop0 = 0, push0 = 0;
-    for (int base = 0; base < R; base += RZ_NT) {
-      const Share s = share_of(tab, P, new_len, base);
-      s_off[0][tid] = s.pop;
-      s_off[1][tid] = s.push;
-      s_y[tid] = s.Y;
-      s_x[tid] = s.X;
+    for (int b = 0; b < n_batches; ++b) {
+      if (n_batches > 1) batch(b * NT);
       __syncthreads();
-      const int n = min(RZ_NT, R - base);
-      if (phase < 2)
-        for (int64_t e = tid; e < s.pops; e += RZ_NT) {
-          const int32_t id = tab.free_list[fc - 1 - (pop0 + e)];
-          if (phase == 0) {
-            if ((uint32_t)id >= (uint32_t)n_pages) { bad = true; report(status, ACTKV_E_BADPAGE, -1, id); }
-          } else {
-            const int k = find(0, e, n);
-            tab.page_table[(int64_t)(base + k) * tab.max_pages + s_y[k] + (e - s_off[0][k])] = id;
+      const int n = min(NT, R - b * NT);
+      const uint32_t np = (uint32_t)total, nq = (uint32_t)(total >> 32);
+      const uint32_t e0 = rank * NT + tid;
+      int kept = 0;
+      for (uint64_t e = e0; e < (uint64_t)np + nq; e += CS * NT, ++kept) {
+        const bool pop = e < np;
+        if (which > 0 && (pop != (which == 1) || (n_batches == 1 && kept < RZ_KEEP))) continue;
+        const uint32_t i = (uint32_t)(pop ? e : e - np);
+        const int k = find(pop ? s_pop : s_push, i, n);
+        int32_t* entry = tab.page_table + (int64_t)(b * NT + k) * tab.max_pages + (pop ? s_y[k] + (int32_t)(i - s_pop[k]) : s_x[k] + (int32_t)(i - s_push[k]));
+        const int32_t page = pop ? tab.free_list[fc - 1 - (pop0 + i)] : *entry;
+        if (which == 0) {
+          if ((uint32_t)page >= (uint32_t)n_pages) {
+            if (!bad) report(status, ACTKV_E_BADPAGE, pop ? -1 : b * NT + k, page);
+            bad = true;
           }
+#pragma unroll
+          for (int j = 0; j < RZ_KEEP; ++j)
+            if (kept == j) { id[j] = page; to[j] = entry; }
+        } else if (pop) {
+          *entry = page;
+        } else {
+          tab.free_list[fc - pops + push0 + i] = page;
+          *entry = -1;
         }
-      if (phase != 1)
-        for (int64_t e = tid; e < s.pushes; e += RZ_NT) {
-          const int k = find(1, e, n);
-          int32_t* entry = tab.page_table + (int64_t)(base + k) * tab.max_pages + s_x[k] + (e - s_off[1][k]);
-          const int32_t id = *entry;
-          if (phase == 0) {
-            if ((uint32_t)id >= (uint32_t)n_pages) { bad = true; report(status, ACTKV_E_BADPAGE, base + k, id); }
-          } else {
-            tab.free_list[fc - pops + push0 + e] = id;
-            *entry = -1;
-          }
-        }
-      if (phase == 2 && base + tid < R && s.N >= 0) tab.seq_len[base + tid] = s.N;
-      pop0 += s.pops;
-      push0 += s.pushes;
-      __syncthreads();
+      }
+      pop0 += np;
+      push0 += nq;
+      if (n_batches > 1) __syncthreads();
     }
-    if (__syncthreads_or(bad)) return;
+  };
+  if (!bad) sweep(0);
+  int any = __syncthreads_or(bad);
+  if constexpr (CS > 1) {
+    cg::cluster_group cl = cg::this_cluster();
+    if (tid == 0) s_bad = any;
+    cl.sync();
+    any = 0;
+    for (int c = 0; c < CS; ++c) any |= *cl.map_shared_rank(&s_bad, c);
   }
-  if (tid == 0) *tab.free_count = (int32_t)(fc - pops + pushes);
+  if (!any) {
+    const uint32_t np = (uint32_t)total;
+    const bool more = n_batches > 1 || pops + pushes > (int64_t)RZ_KEEP * CS * NT;      // (uniform over the cluster)
+    if (more) {
+      sweep(1);
+      __syncthreads();
+      if constexpr (CS > 1) cg::this_cluster().sync();
+    }
+    if (n_batches == 1) {
+#pragma unroll
+      for (int j = 0; j < RZ_KEEP; ++j) {
+        const int64_t e = (int64_t)rank * NT + tid + (int64_t)j * CS * NT;
+        if (e < np) {
+          *to[j] = id[j];
+        } else if (e < pops + pushes) {
+          tab.free_list[fc - pops + (e - np)] = id[j];
+          *to[j] = -1;
+        }
+      }
+    }
+    if (more) sweep(2);
+    if constexpr (CS > 1) {
+      if (n_batches > 1) cg::this_cluster().sync();                       // (one batch: everybody has its lengths in registers)
+    }
+    if (rank == 0)
+      for (int r = tid; r < R; r += NT) {
+        const int32_t n = n_batches == 1 ? N : new_len[r];
+        if (n >= 0) tab.seq_len[r] = n;
+      }
+    if (rank == 0 && tid == 0) *tab.free_count = (int32_t)(fc - pops + pushes);
+  }
+  if constexpr (CS > 1) cg::this_cluster().sync();                        // (flags are read from one another's shared memory)
+}
+
+template <int NT, int CS>
+int launch_resize(const actkv_pool_t* pool, const actkv_tables_t* tables, const int32_t* new_len, int32_t* status, cudaStream_t s) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(CS);
+  cfg.blockDim = dim3(NT);
+  cfg.stream = s;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = CS;
+  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = CS > 1 ? 2 : 1;
+  (void)cudaLaunchKernelEx(&cfg, resize_kernel<NT, CS>, make_view(tables), pool->page_size, pool->n_pages, new_len, status);
+  ACTKV_CHECK_LAUNCH();
+  return ACTKV_OK;
 }
 
 constexpr int CP_NT = 128;
-constexpr int CP_MAXB = 64;      // branches a CTA serves per sweep over the pairs
 
 struct CopyArgs {
   PoolView pool;
@@ -151,53 +213,60 @@ struct CopyArgs {
   int32_t* status;
 };
 
-__device__ __forceinline__ bool pair_ok(const CopyArgs& a, int i, bool tell) {
-  const int s = a.src[i], d = a.dst[i], n = a.length[i], R = a.tab.n_req;
-  bool ok = (uint32_t)s < (uint32_t)R && (uint32_t)d < (uint32_t)R && s != d && n >= 0 && n <= a.max_len;
-  if (ok) ok = n <= a.tab.seq_len[s] && n <= a.tab.seq_len[d] && (n == 0 || (n - 1) / a.pool.page_size < a.tab.max_pages);
-  if (!ok && tell) report(a.status, ACTKV_E_INVALID, i, n);
-  return ok;
-}
-
-// grid: (logical page, pair, layer * 2 + kv).  The first pair of a source works for all pairs of that source.
+// grid: (logical page, pair, layer * 2 + kv).  The first sound pair of a source works for all pairs of that source; CP_NT pairs
+// are looked at together, one per thread, in two round trips to memory.
 template <bool VEC>
 __global__ void __launch_bounds__(CP_NT) copy_kernel(const CopyArgs a) {
   pdl_begin();
-  __shared__ int64_t s_dst[CP_MAXB];
-  __shared__ int s_slots[CP_MAXB];
+  __shared__ int64_t s_dst[CP_NT];
+  __shared__ int s_slots[CP_NT];
   __shared__ int s_n;
   const int tid = threadIdx.x, lp = blockIdx.x, i = blockIdx.y, layer = blockIdx.z >> 1, kv = blockIdx.z & 1;
-  const int P = a.pool.page_size, H = a.pool.n_kv_heads, D = a.pool.head_dim;
-  if (blockIdx.x == 0 && blockIdx.z == 0) {      // one CTA of every pair looks it over
-    if (tid == 0) pair_ok(a, i, true);
+  const int P = a.pool.page_size, H = a.pool.n_kv_heads, D = a.pool.head_dim, R = a.tab.n_req;
+  const bool first = blockIdx.x == 0 && blockIdx.z == 0;                   // one CTA of every pair reports what is wrong with it
+  const int src = a.src[i];
+  if ((uint32_t)src >= (uint32_t)R) {
+    if (first && tid == 0) report(a.status, ACTKV_E_INVALID, i, src);
+    return;
+  }
+  if (first) {
     const int d = a.dst[i];
     for (int j = tid; j < a.n_copy; j += CP_NT)
       if (j != i && (a.dst[j] == d || a.src[j] == d)) report(a.status, ACTKV_E_INVALID, i, d);
   }
-  const int src = a.src[i];
-  int before = 0;
-  for (int j = tid; j < i; j += CP_NT) before |= a.src[j] == src && pair_ok(a, j, false) ? 1 : 0;
-  if (__syncthreads_or(before) || !pair_ok(a, i, false)) return;
-  const int src_page = page_or_neg(a.tab, a.pool.n_pages, src, lp < a.tab.max_pages ? lp : 0, nullptr);
+  const int32_t* src_row = a.tab.page_table + (int64_t)src * a.tab.max_pages;
+  const int col = lp < a.tab.max_pages ? lp : a.tab.max_pages - 1;         // (max_len may be beyond the table; no sound pair is)
+  const int src_page = a.tab.max_pages > 0 ? src_row[col] : -1, src_len = a.tab.seq_len[src];
   __nv_bfloat16* base = const_cast<__nv_bfloat16*>(a.pool.base) + (int64_t)(a.layer_begin + layer) * a.pool.stride_layer +
                         (kv ? a.pool.stride_kv : 0);
-  for (int j0 = i; j0 < a.n_copy; j0 += CP_MAXB) {
-    // ---- the branches among pairs j0 .. j0 + CP_MAXB - 1 that have tokens on this page ----
+  for (int j0 = 0; j0 < a.n_copy; j0 += CP_NT) {
+    // ---- the branches among pairs j0 .. j0 + CP_NT - 1 that have tokens on this page ----
     if (tid == 0) s_n = 0;
     __syncthreads();
-    if (tid < CP_MAXB && j0 + tid < a.n_copy && a.src[j0 + tid] == src && pair_ok(a, j0 + tid, false)) {
-      const int slots = min(P, a.length[j0 + tid] - lp * P);
-      if (slots > 0) {
-        if (src_page < 0) page_or_neg(a.tab, a.pool.n_pages, src, lp, a.status);
-        const int page = page_or_neg(a.tab, a.pool.n_pages, a.dst[j0 + tid], lp, a.status);
-        if (page >= 0 && src_page >= 0) {
-          const int at = atomicAdd(&s_n, 1);
-          s_dst[at] = (int64_t)page * a.pool.stride_page;
-          s_slots[at] = slots;
+    const int j = j0 + tid;
+    bool sound = false;
+    if (j < a.n_copy && (j == i || a.src[j] == src)) {
+      const int d = a.dst[j], n = a.length[j];
+      if ((uint32_t)d < (uint32_t)R && d != src && n >= 0 && n <= a.max_len) {
+        const int dst_len = a.tab.seq_len[d], page = a.tab.max_pages > 0 ? a.tab.page_table[(int64_t)d * a.tab.max_pages + col] : -1;
+        sound = n <= src_len && n <= dst_len && (n == 0 || (n - 1) / P < a.tab.max_pages);
+        const int slots = min(P, n - lp * P);
+        if (sound && j >= i && slots > 0) {
+          const bool src_ok = (uint32_t)src_page < (uint32_t)a.pool.n_pages, dst_ok = (uint32_t)page < (uint32_t)a.pool.n_pages;
+          if (src_ok && dst_ok) {
+            const int at = atomicAdd(&s_n, 1);
+            s_dst[at] = (int64_t)page * a.pool.stride_page;
+            s_slots[at] = slots;
+          } else {
+            report(a.status, ACTKV_E_BADPAGE, src_ok ? d : src, src_ok ? page : src_page);
+          }
         }
       }
+      if (j == i && !sound && first) report(a.status, ACTKV_E_INVALID, i, n);
     }
-    __syncthreads();
+    // (an unsound pair copies nothing itself; when it comes first, the next sound one works for the rest)
+    if (__syncthreads_or((sound && j < i) || (j == i && !sound))) return;
+    if (j0 + CP_NT <= i) continue;
     const int n = s_n;
     int most = 0;
     for (int b = 0; b < n; ++b) most = max(most, s_slots[b]);
@@ -246,9 +315,10 @@ int actkv_resize(const actkv_pool_t* pool, const actkv_tables_t* tables, const i
     return ACTKV_E_INVALID;
   if (tables->n_req == 0) return ACTKV_OK;
   if (!new_len || !tables->page_table || !tables->seq_len || !tables->free_list || !tables->free_count) return ACTKV_E_INVALID;
-  launch_pdl(pg::resize_kernel, 1, pg::RZ_NT, 0, (cudaStream_t)stream, make_view(tables), pool->page_size, pool->n_pages, new_len, status);
-  ACTKV_CHECK_LAUNCH();
-  return ACTKV_OK;
+  if ((int64_t)tables->n_req * tables->max_pages > 0x7fffffff) return ACTKV_E_TOOBIG;
+  cudaStream_t s = (cudaStream_t)stream;
+  if (tables->n_req <= 32) return pg::launch_resize<256, 1>(pool, tables, new_len, status, s);
+  return pg::launch_resize<512, 8>(pool, tables, new_len, status, s);
 }
 
 int actkv_copy(const actkv_pool_t* pool, const actkv_tables_t* tables, int32_t layer_begin, int32_t layer_end, const int32_t* src,
