@@ -3,12 +3,14 @@
 // Per thread, with m the largest logit it has met: S = sum exp(x - m), T = sum exp(x - m) (x - m); when m moves by d,
 // S' = S e^-d and T' = (T - d S) e^-d.  Joined over the row: lse = m + ln S, log P(t) = (x_t - m) - ln S, entropy = ln S - T / S.
 //
-// Top alternatives: a logit is a candidate when it reaches a bound of which the row is known to hold top_k logits.  The first
-// bound comes from the first LP_STEP logits: the top_k-th largest of the maxima of 128 chunks of them.  Candidates are kept in
-// shared memory as 64-bit keys (order-preserving image of the logit, then the token, lower ones first), so that ties need no
-// further rule; whenever more than LP_TIGHT have gathered they are cut to the top_k largest, the smallest of which is the new bound.
-// In random order a row of 152K yields about 300 candidates and one cut; in ascending order every step ends in a cut, and the
-// result is the same.
+// Top alternatives.  While it streams, a thread notes the maximum of every 16 logits (a slot).  Behind the sweep the CTA has 128
+// groups of threads; the top_k-th largest of the groups' maxima is a bound that top_k logits reach, so only they and the few
+// others that reach it (64: about 25 more, in random order) can be among the top_k.  The slots that reach
+// the bound are read again, a thread per logit, and the candidates are ranked by counting, as 64-bit keys (order-preserving image of
+// the logit, then the token, lower ones first), so that ties need no further rule.  No barrier and no shared counter while
+// the row is read: with candidates gathered on the way, under a bound from the row's beginning, 1500 rows of 152K took 278 us
+// at top_k 8, of which 126 went to that.  Rows with more candidates than the list holds (long ties, a row in an order
+// that puts its largest logits into few threads) are read a second time, step by step, with the list cut to top_k whenever it fills.
 //
 // What bounds it: reading the logits once.  Few rows: a cluster of CTAs per row, joined through distributed shared memory.
 #include <cooperative_groups.h>
@@ -19,10 +21,11 @@ namespace actkv {
 namespace lp {
 
 constexpr int NT = 512, NWARP = NT / 32;
-constexpr int LP_STEP = 8192;             // logits of a CTA between two looks at the candidates
-constexpr int LP_TIGHT = 256;
-constexpr int LP_CAP = LP_STEP + LP_TIGHT;
-constexpr int RANK_MAX = 1024;            // candidates ranked against each other; more are cut by digits first
+constexpr int PER = 16;                   // logits of a thread per step
+constexpr int SLOTS = 24;                 // maxima that a thread notes, at most (longer rows: of several steps each)
+constexpr int LIST = 1024;                // candidates ranked against each other
+constexpr int TIGHT = 256;                // second reading: candidates that stay between two steps, at most
+constexpr int CAP = 4096 + TIGHT;         // ... and with a step's (one vector per thread)
 constexpr float NO_REF = -3.402823466e38f;
 constexpr float FAR = -1e4f;              // exp of it is 0
 
@@ -68,21 +71,39 @@ __device__ __forceinline__ float to_f(float x) { return x; }
 __device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
 
 struct Smem {
-  uint64_t cand[LP_CAP];
-  uint64_t best[ACTKV_LOGPROB_MAX_TOP];   // the CTA's own top_k, descending
+  union {
+    float slot[SLOTS][NT];
+    uint64_t cand[CAP];
+  };
+  uint64_t list[LIST];                    // candidates; then the CTA's top k, descending
   float4 red[NWARP];                      // (m, S, T) of the warps
-  float chunk[128];
+  float group[128];
   uint32_t hist[256];
   float4 mst;                             // (m, S, T) of the CTA
   int n_best;
-  uint32_t n_cand, thr;
+  uint32_t item[LIST];                    // slots that are read again
+  uint32_t n_cand, n_item, thr;
   uint32_t pick[2];
 };
 
+template <int W>
+__device__ __forceinline__ void rank_few(uint64_t* cand, int n, int k) {
+  const int tid = threadIdx.x, i = tid / W;
+  const uint64_t a = i < n ? cand[i] : 0;
+  int r = 0;
+#pragma unroll 4
+  for (int o = tid % W; o < n; o += W) r += cand[o] > a ? 1 : 0;
+#pragma unroll
+  for (int d = 1; d < W; d <<= 1) r += __shfl_xor_sync(0xffffffffu, r, d);
+  __syncthreads();
+  if (i < n && tid % W == 0 && r < k) cand[r] = a;
+  __syncthreads();
+}
+
 // The k largest of cand[0 .. n) in descending order into cand[0 .. min(n, k)).  All threads call it, between barriers.
-__device__ __noinline__ void cut(Smem* sm, int n, int k) {
+__device__ __noinline__ void cut(Smem* sm, uint64_t* cand, int n, int k) {
   const int tid = threadIdx.x;
-  if (n > RANK_MAX) {
+  if (n > LIST) {
     // the k-th largest key, digit by digit; then only what is not smaller stays (k keys: they are all different)
     uint64_t prefix = 0;
     uint32_t left = (uint32_t)k;
@@ -90,7 +111,7 @@ __device__ __noinline__ void cut(Smem* sm, int n, int k) {
       for (int i = tid; i < 256; i += NT) sm->hist[i] = 0;
       __syncthreads();
       for (int i = tid; i < n; i += NT) {
-        const uint64_t key = sm->cand[i];
+        const uint64_t key = cand[i];
         if (shift == 56 || (key >> (shift + 8)) == prefix) atomicAdd(&sm->hist[(uint32_t)(key >> shift) & 255u], 1u);
       }
       __syncthreads();
@@ -109,55 +130,45 @@ __device__ __noinline__ void cut(Smem* sm, int n, int k) {
       left = sm->pick[1];
       __syncthreads();
     }
-    uint64_t mine[(LP_CAP + NT - 1) / NT];
+    uint64_t mine[(CAP + NT - 1) / NT];
 #pragma unroll
-    for (int j = 0; j < (LP_CAP + NT - 1) / NT; ++j) {
+    for (int j = 0; j < (CAP + NT - 1) / NT; ++j) {
       const int i = tid + j * NT;
-      mine[j] = i < n ? sm->cand[i] : 0;
+      mine[j] = i < n ? cand[i] : 0;
       if (!(i < n && mine[j] >= prefix)) mine[j] = 0;                      // (no key is 0: a token is below 2^31)
     }
     if (tid == 0) sm->pick[0] = 0;
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < (LP_CAP + NT - 1) / NT; ++j)
-      if (mine[j] != 0) sm->cand[atomicAdd(&sm->pick[0], 1u)] = mine[j];
+    for (int j = 0; j < (CAP + NT - 1) / NT; ++j)
+      if (mine[j] != 0) cand[atomicAdd(&sm->pick[0], 1u)] = mine[j];
     __syncthreads();
     n = (int)sm->pick[0];
     __syncthreads();
   }
-  // ranks by counting: with few candidates, 8 lanes share one
-  if (n <= NT / 8) {
-    const int i = tid >> 3;
-    const uint64_t a = i < n ? sm->cand[i] : 0;
-    int r = 0;
-    for (int o = tid & 7; o < n; o += 8) r += sm->cand[o] > a ? 1 : 0;
-    r += __shfl_xor_sync(0xffffffffu, r, 1);
-    r += __shfl_xor_sync(0xffffffffu, r, 2);
-    r += __shfl_xor_sync(0xffffffffu, r, 4);
-    __syncthreads();
-    if (i < n && (tid & 7) == 0 && r < k) sm->cand[r] = a;
-    __syncthreads();
-    return;
-  }
-  uint64_t a[RANK_MAX / NT];
-  int rank[RANK_MAX / NT];
+  // ranks by counting; with few candidates several lanes share one
+  if (n <= NT / 8) return rank_few<8>(cand, n, k);
+  if (n <= NT / 4) return rank_few<4>(cand, n, k);
+  if (n <= NT / 2) return rank_few<2>(cand, n, k);
+  uint64_t a[LIST / NT];
+  int rank[LIST / NT];
 #pragma unroll
-  for (int j = 0; j < RANK_MAX / NT; ++j) {
+  for (int j = 0; j < LIST / NT; ++j) {
     const int i = tid + j * NT;
     rank[j] = 0x7fffffff;
     a[j] = 0;
     if (i < n) {
-      a[j] = sm->cand[i];
+      a[j] = cand[i];
       int r = 0;
 #pragma unroll 4
-      for (int o = 0; o < n; ++o) r += sm->cand[o] > a[j] ? 1 : 0;
+      for (int o = 0; o < n; ++o) r += cand[o] > a[j] ? 1 : 0;
       rank[j] = r;
     }
   }
   __syncthreads();
 #pragma unroll
-  for (int j = 0; j < RANK_MAX / NT; ++j)
-    if (rank[j] < k) sm->cand[rank[j]] = a[j];
+  for (int j = 0; j < LIST / NT; ++j)
+    if (rank[j] < k) cand[rank[j]] = a[j];
   __syncthreads();
 }
 
@@ -169,13 +180,51 @@ __device__ __forceinline__ float4 join(float4 a, float4 b) {               // (m
   return make_float4(m, a.y * fa + b.y * fb, (a.z + da * a.y) * fa + (b.z + db * b.y) * fb, 0.f);
 }
 
+// Second reading of a row's part, for the top k of rows whose candidates do not fit the list: a vector per thread and step, the list
+// cut to the k largest whenever more than TIGHT are in it.  Logits below the image `thr` are none of them.
+template <typename T>
+__device__ __noinline__ int top_again(Smem* sm, const T* z, const uint4* zv, int mis, int vocab, int v0, int v1, int k, uint32_t thr) {
+  constexpr int VE = Vec<T>::N;
+  const int tid = threadIdx.x;
+  static_assert(NT * VE + TIGHT <= CAP, "a step fits");
+  __syncthreads();
+  if (tid == 0) sm->n_cand = 0;
+  __syncthreads();
+  for (int vb = v0; vb < v1; vb += NT) {
+    const int v = vb + tid;
+    int over = 0;
+    for (int e = 0; e < VE; ++e) {
+      const int64_t t = (int64_t)v * VE + e - mis;
+      if (v >= v1 || t < 0 || t >= vocab) continue;
+      const float x = to_f(z[t]);
+      if (okey(x) < thr) continue;
+      const uint32_t at = atomicAdd(&sm->n_cand, 1u);
+      sm->cand[at] = key_of(x, (uint32_t)t);                               // (at most TIGHT before the step: it fits)
+      over |= at >= TIGHT;
+    }
+    if (__syncthreads_or(over)) {
+      cut(sm, sm->cand, (int)sm->n_cand, k);
+      if (tid == 0) sm->n_cand = (uint32_t)k;                              // (more than TIGHT >= k there were)
+      // what comes later is larger as a token: an equal logit no longer counts
+      thr = (uint32_t)(sm->cand[k - 1] >> 32);
+      thr = thr == 0xffffffffu ? thr : thr + 1;
+      __syncthreads();
+    }
+  }
+  const int n = (int)sm->n_cand;
+  cut(sm, sm->cand, n, k);
+  for (int i = tid; i < min(n, k); i += NT) sm->list[i] = sm->cand[i];
+  __syncthreads();
+  return min(n, k);
+}
+
 template <typename T, int C>
 __global__ void __launch_bounds__(NT, 2) logprob_kernel(const Args a) {
   const void* logits = a.logits;
   pdl_begin(logits);
   extern __shared__ __align__(16) uint8_t lp_smem[];
   Smem* sm = reinterpret_cast<Smem*>(lp_smem);
-  constexpr int VE = Vec<T>::N, U = LP_STEP / NT / VE;                     // vectors of a thread per step
+  constexpr int VE = Vec<T>::N, U = PER / VE;                              // vectors of a thread per step
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int row = blockIdx.x / C, part = blockIdx.x % C;
   const int vocab = a.vocab, k = a.top_k;
@@ -184,8 +233,27 @@ __global__ void __launch_bounds__(NT, 2) logprob_kernel(const Args a) {
   const uint4* zv = reinterpret_cast<const uint4*>(z - mis);
   const int nv = (int)(((int64_t)mis + vocab + VE - 1) / VE);
   const int v0 = (int)((int64_t)nv * part / C), v1 = (int)((int64_t)nv * (part + 1) / C);
-
-  if (tid == 0) sm->n_cand = 0;
+  // vectors of which all logits are the row's own; the others (at most one at each end) are read one by one
+  const int in0 = mis > 0 ? 1 : 0, in1 = (int)(((int64_t)mis + vocab) / VE);
+  auto read = [&](int v) {
+    uint4 r = Vec<T>::none();
+    if (v < v1) {
+      if (v >= in0 && v < in1) {
+        r = __ldg(zv + v);
+      } else {
+        T* one = reinterpret_cast<T*>(&r);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) {
+          const int64_t t = (int64_t)v * VE + e - mis;
+          if (t >= 0 && t < vocab) one[e] = z[t];
+        }
+      }
+    }
+    return r;
+  };
+  uint4 next[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) next[u] = read(v0 + u * NT + tid);
   int32_t tok = -1;
   float ztok = 0.f;
   if (part == 0 && tid < a.n_given) {                                      // (early: beside the row's own loads)
@@ -193,64 +261,28 @@ __global__ void __launch_bounds__(NT, 2) logprob_kernel(const Args a) {
     if (tok >= 0 && tok < vocab) ztok = to_f(z[tok]);
   }
 
-  // vectors of which all logits are the row's own; the others (at most one at each end) are read one by one
-  const int in0 = mis > 0 ? 1 : 0, in1 = (int)(((int64_t)mis + vocab) / VE);
-  uint4 next[U];
-  auto load = [&](int vb) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int v = vb + u * NT + tid;
-      next[u] = Vec<T>::none();
-      if (v < v1) {
-        if (v >= in0 && v < in1) {
-          next[u] = __ldg(zv + v);
-        } else {
-          T* one = reinterpret_cast<T*>(&next[u]);
-#pragma unroll
-          for (int e = 0; e < VE; ++e) {
-            const int64_t t = (int64_t)v * VE + e - mis;
-            if (t >= 0 && t < vocab) one[e] = z[t];
-          }
-        }
-      }
-    }
-  };
-
+  const int steps = (v1 - v0 + NT * U - 1) / (NT * U), per_slot = (steps + SLOTS - 1) / SLOTS;
   float m = NO_REF, S = 0.f, Tt = 0.f;
-  uint32_t thr = 0;                                                        // keys from here on are candidates
-  float thr_f = -INFINITY;
-  bool first = true;
-  load(v0);
+  float tm = -INFINITY, slot_max = -INFINITY;                              // of the thread's logits, of the slot's
+  int slot = 0, in_slot = 0;
   for (int vb = v0; vb < v1; vb += NT * U) {
-    float x[U * VE];
+    float x[PER];
 #pragma unroll
     for (int u = 0; u < U; ++u) Vec<T>::open(next[u], x + u * VE);
-    if (vb + NT * U < v1) load(vb + NT * U);                               // (in flight while this step is worked on)
+    if (vb + NT * U < v1) {                                                // (in flight while this step is worked on)
+#pragma unroll
+      for (int u = 0; u < U; ++u) next[u] = read(vb + NT * U + u * NT + tid);
+    }
     float mx = x[0];
 #pragma unroll
-    for (int e = 1; e < U * VE; ++e) mx = fmaxf(mx, x[e]);
-    if (first && k > 0) {
-      // a first bound: k of the 128 chunks have a logit that reaches the k-th largest of their maxima
-      float cm = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-      cm = fmaxf(cm, __shfl_xor_sync(0xffffffffu, cm, 2));
-      if ((tid & 3) == 0) sm->chunk[tid >> 2] = cm > -INFINITY ? cm : -INFINITY;     // (NaN alone: no bound)
-      __syncthreads();
-      const int c = tid >> 2;
-      const float v = sm->chunk[c];
-      int rank = 0;
-#pragma unroll 8
-      for (int o = tid & 3; o < 128; o += 4) {
-        const float w = sm->chunk[o];
-        rank += w > v || (w == v && o < c) ? 1 : 0;
-      }
-      rank += __shfl_xor_sync(0xffffffffu, rank, 1);
-      rank += __shfl_xor_sync(0xffffffffu, rank, 2);
-      if (rank == k - 1 && (tid & 3) == 0) sm->thr = v == -INFINITY ? 0u : okey(v);
-      __syncthreads();
-      thr = sm->thr;
-      thr_f = thr == 0 ? -INFINITY : okey_inv(thr);
+    for (int e = 1; e < PER; ++e) mx = fmaxf(mx, x[e]);
+    slot_max = fmaxf(slot_max, mx);
+    if (++in_slot == per_slot) {
+      sm->slot[slot++][tid] = slot_max;
+      tm = fmaxf(tm, slot_max);
+      slot_max = -INFINITY;
+      in_slot = 0;
     }
-    first = false;
     if (mx > m) {
       const float d = fmaxf(m - mx, FAR), f = exp2f(d * kLog2e);
       Tt = (Tt + d * S) * f;
@@ -259,40 +291,20 @@ __global__ void __launch_bounds__(NT, 2) logprob_kernel(const Args a) {
     }
     float bs = 0.f;
 #pragma unroll
-    for (int e = 0; e < U * VE; ++e) {
+    for (int e = 0; e < PER; ++e) {
       const float y = x[e] - m;
       const float p = exp2f(y * kLog2e);
       bs += p;
       Tt = fmaf(p, fmaxf(y, FAR), Tt);
     }
     S += bs;
-    int over = 0;
-    if (k > 0) {
-      if (mx >= thr_f || bs != bs) {
-#pragma unroll
-        for (int e = 0; e < U * VE; ++e) {
-          const int64_t t = ((int64_t)vb + (e / VE) * NT + tid) * VE + e % VE - mis;
-          if (t >= 0 && t < vocab && vb + (e / VE) * NT + tid < v1 && okey(x[e]) >= thr) {
-            const uint32_t at = atomicAdd(&sm->n_cand, 1u);
-            sm->cand[at] = key_of(x[e], (uint32_t)t);                      // (at most LP_TIGHT before the step: it fits)
-            over |= at >= LP_TIGHT;
-          }
-        }
-      }
-      if (__syncthreads_or(over)) {
-        cut(sm, (int)sm->n_cand, k);
-        if (tid == 0) sm->n_cand = (uint32_t)k;                            // (more than LP_TIGHT >= k there were)
-        // what comes later is larger as a token: an equal logit no longer counts
-        thr = (uint32_t)(sm->cand[k - 1] >> 32);
-        thr = thr == 0xffffffffu ? thr : thr + 1;
-        thr_f = okey_inv(thr);
-        if (thr_f != thr_f) thr_f = INFINITY;                              // (the bound is a NaN: only NaN go on, by bs)
-        __syncthreads();
-      }
-    }
+  }
+  if (in_slot > 0) {
+    sm->slot[slot++][tid] = slot_max;
+    tm = fmaxf(tm, slot_max);
   }
 
-  // ---- the CTA's (m, S, T) and top k ----
+  // ---- (m, S, T) of the warps; maxima of the groups ----
   float4 mst = make_float4(m, S, Tt, 0.f);
 #pragma unroll
   for (int o = 16; o >= 1; o >>= 1) {
@@ -301,36 +313,125 @@ __global__ void __launch_bounds__(NT, 2) logprob_kernel(const Args a) {
     mst = (lane & o) ? join(b, mst) : join(mst, b);
   }
   if (lane == 0) sm->red[warp] = mst;
+  float gm = fmaxf(tm, __shfl_xor_sync(0xffffffffu, tm, 1));
+  gm = fmaxf(gm, __shfl_xor_sync(0xffffffffu, gm, 2));
+  if ((tid & 3) == 0) sm->group[tid >> 2] = gm;
+  if (tid == 0) sm->n_cand = sm->n_item = 0;
   __syncthreads();
-  const int n_mine = (int)min((uint32_t)LP_CAP, sm->n_cand);
-  if (k > 0) cut(sm, n_mine, k);
   mst = sm->red[0];
 #pragma unroll
   for (int w = 1; w < NWARP; ++w) mst = join(mst, sm->red[w]);
-  int n_top = min(n_mine, k);
+
+  int n_top = 0;
+  if (k > 0) {
+    // the bound: the k-th largest of the groups' maxima (four threads count a group's rank)
+    {
+      const int c = tid >> 2;
+      const float v = sm->group[c];
+      int rank = 0;
+#pragma unroll 8
+      for (int o = tid & 3; o < 128; o += 4) {
+        const float w = sm->group[o];
+        rank += w > v || (w == v && o < c) ? 1 : 0;
+      }
+      rank += __shfl_xor_sync(0xffffffffu, rank, 1);
+      rank += __shfl_xor_sync(0xffffffffu, rank, 2);
+      if (rank == k - 1 && (tid & 3) == 0) sm->thr = v == -INFINITY ? 0u : okey(v);
+    }
+    __syncthreads();
+    const uint32_t thr = sm->thr;
+    const float bound = thr == 0 ? -INFINITY : okey_inv(thr);
+    // slots that reach it, then their logits, spread over all threads: one round trip to memory
+    if (tm >= bound)
+      for (int sl = 0; sl < slot; ++sl)
+        if (sm->slot[sl][tid] >= bound) {
+          const uint32_t at = atomicAdd(&sm->n_item, 1u);
+          if (at < LIST) sm->item[at] = (uint32_t)(sl * NT + tid);
+        }
+    __syncthreads();
+    const uint32_t items = sm->n_item;
+    if (items <= LIST) {
+      const int per_item = per_slot * PER;
+      for (int i = tid; i < (int)items * per_item; i += NT) {
+        const int it = i / per_item, in = i - it * per_item, st = in / PER, e = in % PER;
+        const int sl = (int)(sm->item[it] / NT), who = (int)(sm->item[it] % NT), step = sl * per_slot + st;
+        const int v = v0 + (step * U + e / VE) * NT + who;
+        const int64_t t = (int64_t)v * VE + e % VE - mis;
+        if (step >= steps || v >= v1 || t < 0 || t >= vocab) continue;
+        const float x = to_f(z[t]);
+        if (okey(x) >= thr) {
+          const uint32_t at = atomicAdd(&sm->n_cand, 1u);
+          if (at < LIST) sm->list[at] = key_of(x, (uint32_t)t);
+        }
+      }
+    }
+    __syncthreads();
+    const uint32_t n = sm->n_cand;
+    if (items <= LIST && n <= LIST) {
+      cut(sm, sm->list, (int)n, k);
+      n_top = min((int)n, k);
+    } else {
+      n_top = top_again<T>(sm, z, zv, mis, vocab, v0, v1, k, thr);
+    }
+  }
   if constexpr (C > 1) {
     namespace cg = cooperative_groups;
     cg::cluster_group cl = cg::this_cluster();
-    if (tid < n_top) sm->best[tid] = sm->cand[tid];
     if (tid == 0) {
       sm->mst = mst;
       sm->n_best = n_top;
     }
     cl.sync();
     if (part == 0) {
-      int n = 0;
-      float4 all = mst;
+      // the others' parts: every thread one key, all reads in flight at once
+      int n = n_top;
+      int from[C];
+#pragma unroll
+      for (int c = 1; c < C; ++c) {
+        from[c] = n;
+        n += cl.map_shared_rank(sm, c)->n_best;
+      }
+#pragma unroll
+      for (int c = 1; c < C; ++c) {
+        const Smem* other = cl.map_shared_rank(sm, c);
+        mst = join(mst, other->mst);
+      }
+      from[0] = 0;
+      auto list_of = [&](int i) {
+        int c = 0;
+#pragma unroll
+        for (int d = 1; d < C; ++d) c = i >= from[d] ? d : c;
+        return c;
+      };
+      auto start_of = [&](int c) {
+        int at = 0;
+#pragma unroll
+        for (int d = 1; d < C; ++d) at = c >= d ? from[d] : at;
+        return at;
+      };
+      for (int i = n_top + tid; i < n; i += NT) {
+        const int c = list_of(i);
+        sm->list[i] = cl.map_shared_rank(sm, c)->list[i - start_of(c)];
+      }
+      __syncthreads();
+      // every part is sorted: a key's rank is its place in its own part and, by bisection, those of the others
+      static_assert(C * ACTKV_LOGPROB_MAX_TOP <= NT, "one key per thread");
+      const uint64_t mine = tid < n ? sm->list[tid] : 0;
+      int rank = 0;
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        const Smem* other = cl.map_shared_rank(sm, c);
-        const int nb = other->n_best;
-        if (c > 0) all = join(all, other->mst);
-        if (tid < nb) sm->cand[n + tid] = other->best[tid];
-        n += nb;
+        int lo = from[c], hi = c + 1 < C ? from[c + 1] : n;
+        const int begin = lo;
+        while (lo < hi) {
+          const int mid = (lo + hi) >> 1;
+          if (sm->list[mid] > mine) lo = mid + 1;
+          else hi = mid;
+        }
+        rank += lo - begin;
       }
-      mst = all;
       __syncthreads();
-      if (k > 0) cut(sm, n, k);
+      if (tid < n && rank < k) sm->list[rank] = mine;
+      __syncthreads();
       n_top = min(n, k);
     }
     cl.sync();                                                             // (the others' shared memory has been read)
@@ -346,7 +447,7 @@ __global__ void __launch_bounds__(NT, 2) logprob_kernel(const Args a) {
     if (a.entropy != nullptr) a.entropy[row] = none ? 0.f : ls - mst.z / mst.y;
   }
   for (int j = tid; j < k; j += NT) {
-    const uint64_t key = j < n_top ? sm->cand[j] : 0;
+    const uint64_t key = j < n_top ? sm->list[j] : 0;
     a.top_index[(int64_t)row * k + j] = j < n_top ? (int32_t)(0xffffffffu - (uint32_t)key) : -1;
     a.top_logprob[(int64_t)row * k + j] = j < n_top ? lp_of(okey_inv((uint32_t)(key >> 32))) : -INFINITY;
   }
@@ -391,7 +492,7 @@ template <typename T>
 int dispatch(const Args& a, int n_rows, cudaStream_t s) {
   // CTAs per row: enough for two per SM, none with fewer than a step's logits
   int c = 1;
-  while (c < 8 && (int64_t)n_rows * c < 148 && a.vocab / (2 * c) >= LP_STEP / 2) c *= 2;
+  while (c < 8 && (int64_t)n_rows * c < 148 && a.vocab / (2 * c) >= NT * PER / 2) c *= 2;
   switch (c) {
     case 1: return launch<T, 1>(a, n_rows, s);
     case 2: return launch<T, 2>(a, n_rows, s);
