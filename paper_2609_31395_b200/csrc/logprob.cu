@@ -20,12 +20,11 @@
 namespace actkv {
 namespace lp {
 
-constexpr int NT = 512, NWARP = NT / 32;
+constexpr int GROUPS = 128;               // groups of threads whose maxima give the bound
 constexpr int PER = 16;                   // logits of a thread per step
 constexpr int SLOTS = 24;                 // maxima that a thread notes, at most (longer rows: of several steps each)
 constexpr int LIST = 1024;                // candidates ranked against each other
 constexpr int TIGHT = 256;                // second reading: candidates that stay between two steps, at most
-constexpr int CAP = 4096 + TIGHT;         // ... and with a step's (one vector per thread)
 constexpr float NO_REF = -3.402823466e38f;
 constexpr float FAR = -1e4f;              // exp of it is 0
 
@@ -70,14 +69,16 @@ template <> struct Vec<__nv_bfloat16> {
 __device__ __forceinline__ float to_f(float x) { return x; }
 __device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
 
+template <int NT>
 struct Smem {
+  static constexpr int CAP = NT * 8 + TIGHT;   // second reading: candidates with those of a step (one vector per thread)
   union {
     float slot[SLOTS][NT];
     uint64_t cand[CAP];
   };
   uint64_t list[LIST];                    // candidates; then the CTA's top k, descending
-  float4 red[NWARP];                      // (m, S, T) of the warps
-  float group[128];
+  float4 red[NT / 32];                     // (m, S, T) of the warps
+  float group[GROUPS];
   uint32_t hist[256];
   float4 mst;                             // (m, S, T) of the CTA
   int n_best;
@@ -86,7 +87,7 @@ struct Smem {
   uint32_t pick[2];
 };
 
-template <int W>
+template <int NT, int W>
 __device__ __forceinline__ void rank_few(uint64_t* cand, int n, int k) {
   const int tid = threadIdx.x, i = tid / W;
   const uint64_t a = i < n ? cand[i] : 0;
@@ -101,7 +102,9 @@ __device__ __forceinline__ void rank_few(uint64_t* cand, int n, int k) {
 }
 
 // The k largest of cand[0 .. n) in descending order into cand[0 .. min(n, k)).  All threads call it, between barriers.
-__device__ __noinline__ void cut(Smem* sm, uint64_t* cand, int n, int k) {
+template <int NT>
+__device__ __noinline__ void cut(Smem<NT>* sm, uint64_t* cand, int n, int k) {
+  constexpr int CAP = Smem<NT>::CAP;
   const int tid = threadIdx.x;
   if (n > LIST) {
     // the k-th largest key, digit by digit; then only what is not smaller stays (k keys: they are all different)
@@ -147,9 +150,9 @@ __device__ __noinline__ void cut(Smem* sm, uint64_t* cand, int n, int k) {
     __syncthreads();
   }
   // ranks by counting; with few candidates several lanes share one
-  if (n <= NT / 8) return rank_few<8>(cand, n, k);
-  if (n <= NT / 4) return rank_few<4>(cand, n, k);
-  if (n <= NT / 2) return rank_few<2>(cand, n, k);
+  if (n <= NT / 8) return rank_few<NT, 8>(cand, n, k);
+  if (n <= NT / 4) return rank_few<NT, 4>(cand, n, k);
+  if (n <= NT / 2) return rank_few<NT, 2>(cand, n, k);
   uint64_t a[LIST / NT];
   int rank[LIST / NT];
 #pragma unroll
@@ -182,11 +185,11 @@ __device__ __forceinline__ float4 join(float4 a, float4 b) {               // (m
 
 // Second reading of a row's part, for the top k of rows whose candidates do not fit the list: a vector per thread and step, the list
 // cut to the k largest whenever more than TIGHT are in it.  Logits below the image `thr` are none of them.
-template <typename T>
-__device__ __noinline__ int top_again(Smem* sm, const T* z, const uint4* zv, int mis, int vocab, int v0, int v1, int k, uint32_t thr) {
+template <int NT, typename T>
+__device__ __noinline__ int top_again(Smem<NT>* sm, const T* z, const uint4* zv, int mis, int vocab, int v0, int v1, int k, uint32_t thr) {
   constexpr int VE = Vec<T>::N;
   const int tid = threadIdx.x;
-  static_assert(NT * VE + TIGHT <= CAP, "a step fits");
+  static_assert(NT * VE + TIGHT <= Smem<NT>::CAP, "a step fits");
   __syncthreads();
   if (tid == 0) sm->n_cand = 0;
   __syncthreads();
@@ -203,7 +206,7 @@ __device__ __noinline__ int top_again(Smem* sm, const T* z, const uint4* zv, int
       over |= at >= TIGHT;
     }
     if (__syncthreads_or(over)) {
-      cut(sm, sm->cand, (int)sm->n_cand, k);
+      cut<NT>(sm, sm->cand, (int)sm->n_cand, k);
       if (tid == 0) sm->n_cand = (uint32_t)k;                              // (more than TIGHT >= k there were)
       // what comes later is larger as a token: an equal logit no longer counts
       thr = (uint32_t)(sm->cand[k - 1] >> 32);
@@ -212,18 +215,18 @@ __device__ __noinline__ int top_again(Smem* sm, const T* z, const uint4* zv, int
     }
   }
   const int n = (int)sm->n_cand;
-  cut(sm, sm->cand, n, k);
+  cut<NT>(sm, sm->cand, n, k);
   for (int i = tid; i < min(n, k); i += NT) sm->list[i] = sm->cand[i];
   __syncthreads();
   return min(n, k);
 }
 
-template <typename T, int C>
-__global__ void __launch_bounds__(NT, 2) logprob_kernel(const Args a) {
+template <typename T, int NT, int C>
+__global__ void __launch_bounds__(NT, 1024 / NT) logprob_kernel(const Args a) {
   const void* logits = a.logits;
   pdl_begin(logits);
   extern __shared__ __align__(16) uint8_t lp_smem[];
-  Smem* sm = reinterpret_cast<Smem*>(lp_smem);
+  Smem<NT>* sm = reinterpret_cast<Smem<NT>*>(lp_smem);
   constexpr int VE = Vec<T>::N, U = PER / VE;                              // vectors of a thread per step
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int row = blockIdx.x / C, part = blockIdx.x % C;
@@ -313,30 +316,32 @@ __global__ void __launch_bounds__(NT, 2) logprob_kernel(const Args a) {
     mst = (lane & o) ? join(b, mst) : join(mst, b);
   }
   if (lane == 0) sm->red[warp] = mst;
-  float gm = fmaxf(tm, __shfl_xor_sync(0xffffffffu, tm, 1));
-  gm = fmaxf(gm, __shfl_xor_sync(0xffffffffu, gm, 2));
-  if ((tid & 3) == 0) sm->group[tid >> 2] = gm;
+  constexpr int TG = NT / GROUPS;                                          // threads of a group
+  float gm = tm;
+#pragma unroll
+  for (int d = 1; d < TG; d <<= 1) gm = fmaxf(gm, __shfl_xor_sync(0xffffffffu, gm, d));
+  if (tid % TG == 0) sm->group[tid / TG] = gm;
   if (tid == 0) sm->n_cand = sm->n_item = 0;
   __syncthreads();
   mst = sm->red[0];
 #pragma unroll
-  for (int w = 1; w < NWARP; ++w) mst = join(mst, sm->red[w]);
+  for (int w = 1; w < NT / 32; ++w) mst = join(mst, sm->red[w]);
 
   int n_top = 0;
   if (k > 0) {
-    // the bound: the k-th largest of the groups' maxima (four threads count a group's rank)
+    // the bound: the k-th largest of the groups' maxima (the threads of a group count its rank)
     {
-      const int c = tid >> 2;
+      const int c = tid / TG;
       const float v = sm->group[c];
       int rank = 0;
 #pragma unroll 8
-      for (int o = tid & 3; o < 128; o += 4) {
+      for (int o = tid % TG; o < GROUPS; o += TG) {
         const float w = sm->group[o];
         rank += w > v || (w == v && o < c) ? 1 : 0;
       }
-      rank += __shfl_xor_sync(0xffffffffu, rank, 1);
-      rank += __shfl_xor_sync(0xffffffffu, rank, 2);
-      if (rank == k - 1 && (tid & 3) == 0) sm->thr = v == -INFINITY ? 0u : okey(v);
+#pragma unroll
+      for (int d = 1; d < TG; d <<= 1) rank += __shfl_xor_sync(0xffffffffu, rank, d);
+      if (rank == k - 1 && tid % TG == 0) sm->thr = v == -INFINITY ? 0u : okey(v);
     }
     __syncthreads();
     const uint32_t thr = sm->thr;
@@ -368,10 +373,10 @@ __global__ void __launch_bounds__(NT, 2) logprob_kernel(const Args a) {
     __syncthreads();
     const uint32_t n = sm->n_cand;
     if (items <= LIST && n <= LIST) {
-      cut(sm, sm->list, (int)n, k);
+      cut<NT>(sm, sm->list, (int)n, k);
       n_top = min((int)n, k);
     } else {
-      n_top = top_again<T>(sm, z, zv, mis, vocab, v0, v1, k, thr);
+      n_top = top_again<NT, T>(sm, z, zv, mis, vocab, v0, v1, k, thr);
     }
   }
   if constexpr (C > 1) {
@@ -393,7 +398,7 @@ __global__ void __launch_bounds__(NT, 2) logprob_kernel(const Args a) {
       }
 #pragma unroll
       for (int c = 1; c < C; ++c) {
-        const Smem* other = cl.map_shared_rank(sm, c);
+        const Smem<NT>* other = cl.map_shared_rank(sm, c);
         mst = join(mst, other->mst);
       }
       from[0] = 0;
@@ -467,13 +472,13 @@ __global__ void __launch_bounds__(NT, 2) logprob_kernel(const Args a) {
   }
 }
 
-template <typename T, int C>
+template <typename T, int NT, int C>
 int launch(const Args& a, int n_rows, cudaStream_t s) {
-  if (ensure_dyn_smem(logprob_kernel<T, C>, sizeof(Smem)) != cudaSuccess) return ACTKV_E_CUDA;
+  if (ensure_dyn_smem(logprob_kernel<T, NT, C>, sizeof(Smem<NT>)) != cudaSuccess) return ACTKV_E_CUDA;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)n_rows * C);
   cfg.blockDim = dim3(NT);
-  cfg.dynamicSmemBytes = sizeof(Smem);
+  cfg.dynamicSmemBytes = sizeof(Smem<NT>);
   cfg.stream = s;
   cudaLaunchAttribute at[2];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -483,22 +488,22 @@ int launch(const Args& a, int n_rows, cudaStream_t s) {
   at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = C > 1 ? 2 : 1;
-  (void)cudaLaunchKernelEx(&cfg, logprob_kernel<T, C>, a);
+  (void)cudaLaunchKernelEx(&cfg, logprob_kernel<T, NT, C>, a);
   ACTKV_CHECK_LAUNCH();
   return ACTKV_OK;
 }
 
 template <typename T>
 int dispatch(const Args& a, int n_rows, cudaStream_t s) {
-  // CTAs per row: enough for two per SM, none with fewer than a step's logits
+  // CTAs per row: up to 4 while every CTA has an SM to itself and at least 4096 logits.  (Rows of 152K, 20 alternatives, us at 1 / 2 / 4 / 8
+  // CTAs: 16 rows 18.7 / 14.0 / 10.9 / 14.8, 64 rows 18.8 / 14.2 / 16.4 / 29.8, 100 rows 19.0 / 21.8 / 24.4 / 45.3.)
   int c = 1;
-  while (c < 8 && (int64_t)n_rows * c < 148 && a.vocab / (2 * c) >= NT * PER / 2) c *= 2;
-  switch (c) {
-    case 1: return launch<T, 1>(a, n_rows, s);
-    case 2: return launch<T, 2>(a, n_rows, s);
-    case 4: return launch<T, 4>(a, n_rows, s);
-    default: return launch<T, 8>(a, n_rows, s);
-  }
+  while (c < 4 && (int64_t)n_rows * 2 * c <= 148 && a.vocab / (2 * c) >= 4096) c *= 2;
+  if (c == 4) return launch<T, 512, 4>(a, n_rows, s);
+  if (c == 2) return launch<T, 512, 2>(a, n_rows, s);
+  // Many rows: four CTAs of 256 threads per SM hide the selection of one behind the reading of the others (1500 rows: 165 us, with two of
+  // 512 175); fewer rows than they need to fill the SMs are read faster by 512 threads (296 rows: 43.5 and 35.3).
+  return n_rows >= 512 ? launch<T, 256, 1>(a, n_rows, s) : launch<T, 512, 1>(a, n_rows, s);
 }
 
 }  // namespace lp
