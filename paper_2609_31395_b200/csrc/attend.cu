@@ -12,9 +12,13 @@
 //
 // What bounds it: reading K and V, 4 D bytes a key and KV head.
 //
-// Work.  All (layer, head, request, block of rows) units in one line, each as long as its key tiles; every CTA takes an equal
-// piece of the line, from the lengths on the device, so that ragged requests are balanced and a captured graph follows
-// growing caches.  A unit that lies in several pieces leaves (m, l, O) partials, joined by attend_join_kernel in piece order.
+// Work.  For every KV head all (layer, request, block of rows) units in one line, each as long as its key tiles; the head's CTAs take
+// equal pieces of the line, from the lengths on the device, so that ragged requests are balanced and a captured graph follows
+// growing caches.  CTAs that follow one another have the same piece of different heads: what they read lies in the same pages
+// (head_dim 64, 8 heads: 137 us with one line through all heads, 100 so).
+// A unit that lies in several pieces leaves (m, l, O) partials, joined by attend_join_kernel in piece order.  (Joined by the CTA that finishes
+// last instead, found by marks in the workspace, a launch fewer: 10.1 us against 8.3 for 1000 tokens, 21.7 against 15.1 for 8000; a chain
+// of fences and reads by one CTA takes longer than a launch whose start is already behind it.)
 // Within a CTA the groups of RG warps take the tiles of a piece in turn; the warps of a group share a ring of tiles
 // in shared memory and have 8 NT rows each.
 #include <algorithm>
@@ -26,8 +30,8 @@ namespace at {
 
 constexpr int NW = 4, NTH = NW * 32;
 constexpr int KT = 16;                    // keys per tile
-constexpr int MIN_TILES = 8;              // fewest tiles of a CTA's piece
-constexpr int MAX_CTAS = 2 * 148;         // two CTAs per SM: one streams while the other starts or ends a unit
+constexpr int MIN_TILES = 4;              // fewest tiles of a CTA's piece
+constexpr int SMS = 148, MAX_CTAS = 4 * SMS;
 constexpr float NO_REF = -3.0e38f;        // the reference before the first logit (finite: no infinity meets another)
 constexpr float REF_SLACK = 8.f;
 constexpr int MAX_GROUP = 32;             // query heads per KV head, as the score kernels
@@ -103,71 +107,90 @@ struct Cfg {
   static constexpr int NG = NW / RG;
   static constexpr int RB = 8 * NT * RG;                                   // rows of a block
   static constexpr int TILE = KT * DP * 2 * 2;                             // bytes: K and V
-  static constexpr int CTAS = DP > 128 ? 1 : 2;                            // per SM
-  static constexpr int STAGES = (DP > 128 ? 192 : 96) * 1024 / (NG * TILE) > 16 ? 16 : (DP > 128 ? 192 : 96) * 1024 / (NG * TILE);
+  // CTAs per SM, as many as registers allow without spilling.  They share what the ring may take: with 2, 3 and 4 of them 8 rows of
+  // 35000 x 8 tokens at head_dim 128 took 98.8, 95 and - us, 16000 x 16 at head_dim 64 121, - and 94 us.
+  static constexpr int CTAS = DP > 128 ? 1 : NT > 1 ? 2 : DP == 64 ? 4 : 3;
+  static constexpr int RING_MAX = 192 / CTAS * 1024;
+  static constexpr int STAGES = RING_MAX / (NG * TILE) > 16 ? 16 : RING_MAX / (NG * TILE);
   static constexpr int RING = NG * STAGES * TILE;
   static constexpr int RED = NW * 8 * (DP + 4) * 4;
   static_assert(RED <= RING, "the join of the warps reuses the ring");
 };
 
+// Slots of the partials of a unit in pieces b0 .. b1 of head h's line: the unit begins at the end of piece b0 and goes on at
+// the start of the others.
+__device__ __forceinline__ int64_t slot_of(int i, int b0, int h, int Hkv) { return 2 * ((int64_t)(b0 + i) * Hkv + h) + (i == 0 ? 1 : 0); }
+
+__device__ __forceinline__ void store_row(const Args& a, int64_t at, int d, float4 o, float sum, float M, int D) {
+  if (d < D) {
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    __nv_bfloat162 v[2] = {__floats2bfloat162_rn(o.x * inv, o.y * inv), __floats2bfloat162_rn(o.z * inv, o.w * inv)};
+    *reinterpret_cast<uint2*>(a.out + at * D + d) = *reinterpret_cast<uint2*>(v);
+  }
+  if (d == 0 && a.lse != nullptr) a.lse[at] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
+}
+
 template <int DP, int NT, int RG>
-__global__ void __launch_bounds__(NTH, (Cfg<DP, NT, RG>::CTAS)) attend_kernel(const Args a) {
+__global__ void __launch_bounds__(NTH, (Cfg<DP, NT, RG>::CTAS)) attend_kernel(const __grid_constant__ Args a) {
   using C = Cfg<DP, NT, RG>;
   pdl_begin();
   extern __shared__ __align__(128) uint8_t at_smem[];
-  __shared__ int64_t s_warp[NW];
-  __shared__ int64_t s_off;
-  __shared__ int s_r;
   __shared__ float2 s_ml[NW][8 * NT];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int grp = warp / RG, part = warp % RG;
   const int R = a.tab.n_req, G = a.group, D = a.pool.head_dim, P = a.pool.page_size;
 
-  // ---- this CTA's piece of the line: thread t sums requests [t * per_t, (t + 1) * per_t) ----
-  const int per_t = (R + NTH - 1) / NTH;
-  int64_t mine = 0;
-  for (int r = tid * per_t; r < min(R, (tid + 1) * per_t); ++r) {
-    const Req q = load_req(a, r, blockIdx.x == 0);
-    mine += (int64_t)q.tiles * ((q.W * G + C::RB - 1) / C::RB);
-  }
-  int64_t incl = mine;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const int64_t t = __shfl_up_sync(0xffffffffu, incl, d);
-    if (lane >= d) incl += t;
-  }
-  if (lane == 31) s_warp[warp] = incl;
-  __syncthreads();
-  int64_t T = 0;
-#pragma unroll
-  for (int w = 0; w < NW; ++w) {
-    if (w == warp) incl += T;
-    T += s_warp[w];
-  }
-  const int64_t total = T * a.nls * a.pool.n_kv_heads;
-  const int64_t per = max((int64_t)MIN_TILES, (total + gridDim.x - 1) / gridDim.x);
-  int64_t x = (int64_t)blockIdx.x * per;
-  const int64_t x1 = min(total, x + per);
-  if (x >= x1) return;
-  int lh = (int)(x / T);
-  {
-    const int64_t rem = x - lh * T;
-    if (rem >= incl - mine && rem < incl) {                                // this thread's requests hold the start
-      int64_t off = rem - (incl - mine);
-      int r = tid * per_t;
-      for (;; ++r) {
-        const Req q = load_req(a, r, false);
-        const int64_t n = (int64_t)q.tiles * ((q.W * G + C::RB - 1) / C::RB);
-        if (off < n) break;
-        off -= n;
-      }
-      s_r = r;
-      s_off = off;
+  // ---- this CTA's head, and its piece of that head's line.  Every warp finds it by itself: lane t sums requests
+  // [t * per_t, (t + 1) * per_t) ----
+  const int Hkv = a.pool.n_kv_heads, h = blockIdx.x % Hkv, piece = blockIdx.x / Hkv, pieces = gridDim.x / Hkv;
+  const int per_t = (R + 31) / 32;
+  uint32_t mine = 0;
+  Req own{};                                                               // up to 32 requests: kept, and handed round
+  auto length_of = [&](const Req& q) { return (uint32_t)(q.tiles * ((q.W * G + C::RB - 1) / C::RB)); };
+#pragma unroll 4
+  for (int k = 0; k < per_t; ++k) {
+    const int r = lane * per_t + k;
+    if (r < R) {
+      own = load_req(a, r, blockIdx.x == 0 && warp == 0);
+      mine += length_of(own);
     }
   }
-  __syncthreads();
-  int r = s_r;
-  int64_t off = s_off;
+  auto req_of = [&](int r) {
+    if (per_t > 1) return load_req(a, r, false);
+    Req q;
+    q.L = __shfl_sync(0xffffffffu, own.L, r);
+    q.W = __shfl_sync(0xffffffffu, own.W, r);
+    q.win0 = __shfl_sync(0xffffffffu, own.win0, r);
+    q.lo_tile = __shfl_sync(0xffffffffu, own.lo_tile, r);
+    q.tiles = __shfl_sync(0xffffffffu, own.tiles, r);
+    return q;
+  };
+  uint32_t incl = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const uint32_t t = __shfl_up_sync(0xffffffffu, incl, d);
+    if (lane >= d) incl += t;
+  }
+  const uint32_t T = __shfl_sync(0xffffffffu, incl, 31);                   // (the host has seen to it that it fits)
+  const uint64_t total = (uint64_t)T * (uint32_t)a.nls;
+  auto div = [](uint64_t n, uint32_t d) { return n >> 32 ? n / d : (uint64_t)((uint32_t)n / d); };
+  const uint64_t per = max((uint64_t)MIN_TILES, div(total + pieces - 1, pieces));
+  uint64_t x = (uint64_t)piece * per;
+  const uint64_t x1 = min(total, x + per);
+  if (x >= x1) return;
+  int layer = (int)div(x, T);
+  int r = 0;
+  uint32_t off = (uint32_t)(x - (uint64_t)layer * T);
+  {
+    const int owner = __ffs(__ballot_sync(0xffffffffu, off < incl)) - 1;   // the lane whose requests hold the start
+    off -= __shfl_sync(0xffffffffu, incl - mine, owner);
+    r = owner * per_t;
+    for (; per_t > 1; ++r) {
+      const uint32_t n = length_of(load_req(a, r, false));
+      if (off < n) break;
+      off -= n;
+    }
+  }
 
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(at_smem) + grp * C::STAGES * C::TILE;
   const int g = lane >> 2, t2 = (lane & 3) * 2;
@@ -186,17 +209,54 @@ __global__ void __launch_bounds__(NTH, (Cfg<DP, NT, RG>::CTAS)) attend_kernel(co
   };
 
   while (x < x1) {
-    const Req q = load_req(a, r, false);
+    const Req q = req_of(r);
     const int rbs = (q.W * G + C::RB - 1) / C::RB;
     if (q.W == 0) {
-      if (++r == R) { r = 0; ++lh; }
+      if (++r == R) { r = 0; ++layer; }
       off = 0;
       continue;
     }
-    const int rb = (int)(off / q.tiles), t_in = (int)(off - (int64_t)rb * q.tiles);
-    const int n_tiles = (int)min((int64_t)(q.tiles - t_in), x1 - x);
-    const int layer = lh / a.pool.n_kv_heads, h = lh - layer * a.pool.n_kv_heads;
+    const int rb = (int)(off / (uint32_t)q.tiles), t_in = (int)(off - (uint32_t)rb * q.tiles);
+    const int n_tiles = (int)min((uint64_t)(q.tiles - t_in), x1 - x);
     const int L = q.L, rows = q.W * G;
+
+    // ---- the stream of this group's tiles ----
+    const __nv_bfloat16* kbase = a.pool.base + (int64_t)(a.layer_begin + layer) * a.pool.stride_layer + (int64_t)h * a.pool.stride_head;
+    const int first = q.lo_tile + t_in + grp, end = q.lo_tile + t_in + n_tiles;
+    auto page_of = [&](int tile) -> int {                                  // page of key tile * 16 + lane % 16, -1 behind the end
+      const int key = tile * KT + (lane & 15);
+      if (tile >= end || key >= L) return -1;
+      const int lp = a.page_shift >= 0 ? key >> a.page_shift : key / P;
+      return checked_page(a.tab, a.pool.n_pages, r, lp, a.status);
+    };
+    auto issue = [&](int tile, int stage, int page) {
+      if (tile < end) {
+        const int key = tile * KT + (lane & 15);
+        const int slot = a.page_shift >= 0 ? key & (P - 1) : key % P;
+        const int64_t koff = page >= 0 ? (int64_t)page * a.pool.stride_page + (int64_t)slot * a.pool.stride_slot : -1;
+        constexpr int CH = DP / 8, RPI = 32 / CH;                          // chunks of a row, rows per step of the warp
+        constexpr int MINE = KT / RG;                                      // rows of the tile that this warp loads
+        const int c = lane % CH;
+#pragma unroll
+        for (int i = 0; i < MINE / RPI; ++i) {
+          const int row = part * MINE + i * RPI + lane / CH;
+          const int64_t o = __shfl_sync(0xffffffffu, koff, row);
+          const uint32_t dst = ring + stage * C::TILE + row * DP * 2 + ((c ^ (row & 7)) << 4);
+          const __nv_bfloat16* src = kbase + (o < 0 ? 0 : o + c * 8);
+          if (c < nch) {
+            cp_async16(dst, src, o < 0 ? 0 : 16);
+            cp_async16(dst + C::TILE / 2, o < 0 ? src : src + a.pool.stride_kv, o < 0 ? 0 : 16);
+          }
+        }
+      }
+      cp_commit();
+    };
+    int pages[C::STAGES];                                                  // (all looked up before the first is used)
+#pragma unroll
+    for (int i = 0; i < C::STAGES; ++i) pages[i] = page_of(first + i * C::NG);
+#pragma unroll
+    for (int i = 0; i < C::STAGES - 1; ++i) issue(first + i * C::NG, i, pages[i]);
+    int page_next = pages[C::STAGES - 1];
 
     // ---- rows of this warp ----
     const int row0 = rb * C::RB + part * 8 * NT;
@@ -232,40 +292,6 @@ __global__ void __launch_bounds__(NTH, (Cfg<DP, NT, RG>::CTAS)) attend_kernel(co
       l[n][0] = l[n][1] = 0.f;
     }
 
-    // ---- the stream of this group's tiles ----
-    const __nv_bfloat16* kbase = a.pool.base + (int64_t)(a.layer_begin + layer) * a.pool.stride_layer + (int64_t)h * a.pool.stride_head;
-    const int first = q.lo_tile + t_in + grp, end = q.lo_tile + t_in + n_tiles;
-    auto page_of = [&](int tile) -> int {                                  // page of key tile * 16 + lane % 16, -1 behind the end
-      const int key = tile * KT + (lane & 15);
-      if (tile >= end || key >= L) return -1;
-      const int lp = a.page_shift >= 0 ? key >> a.page_shift : key / P;
-      return checked_page(a.tab, a.pool.n_pages, r, lp, a.status);
-    };
-    auto issue = [&](int tile, int stage, int page) {
-      if (tile < end) {
-        const int key = tile * KT + (lane & 15);
-        const int slot = a.page_shift >= 0 ? key & (P - 1) : key % P;
-        const int64_t koff = page >= 0 ? (int64_t)page * a.pool.stride_page + (int64_t)slot * a.pool.stride_slot : -1;
-        constexpr int CH = DP / 8, RPI = 32 / CH;                          // chunks of a row, rows per step of the warp
-        constexpr int MINE = KT / RG;                                      // rows of the tile that this warp loads
-        const int c = lane % CH;
-#pragma unroll
-        for (int i = 0; i < MINE / RPI; ++i) {
-          const int row = part * MINE + i * RPI + lane / CH;
-          const int64_t o = __shfl_sync(0xffffffffu, koff, row);
-          const uint32_t dst = ring + stage * C::TILE + row * DP * 2 + ((c ^ (row & 7)) << 4);
-          const __nv_bfloat16* src = kbase + (o < 0 ? 0 : o + c * 8);
-          if (c < nch) {
-            cp_async16(dst, src, o < 0 ? 0 : 16);
-            cp_async16(dst + C::TILE / 2, o < 0 ? src : src + a.pool.stride_kv, o < 0 ? 0 : 16);
-          }
-        }
-      }
-      cp_commit();
-    };
-#pragma unroll
-    for (int i = 0; i < C::STAGES - 1; ++i) issue(first + i * C::NG, i, page_of(first + i * C::NG));
-    int page_next = page_of(first + (C::STAGES - 1) * C::NG);
     int stage = 0, stage_w = C::STAGES - 1;
 #pragma unroll 1
     for (int tile = first; tile < end; tile += C::NG) {
@@ -409,11 +435,11 @@ __global__ void __launch_bounds__(NTH, (Cfg<DP, NT, RG>::CTAS)) attend_kernel(co
         if (lane < 4) s_ml[warp][n * 8 + t2 + c] = make_float2(m[n][c], l[n][c]);
       }
     __syncthreads();                                                       // ... and nobody reads the rings any more
-    const int64_t u0 = x - t_in;                                           // the unit's place on the line
-    const int b0 = (int)(u0 / per), b1 = (int)((u0 + q.tiles - 1) / per);
+    const uint64_t u0 = x - t_in;                                           // the unit's place on the line
+    const int b0 = (int)div(u0, (uint32_t)per), b1 = (int)div(u0 + q.tiles - 1, (uint32_t)per);
     const bool whole = b0 == b1;
-    const int64_t unit = ((int64_t)lh * R + r) * a.rb_max + rb;
-    const int64_t slot = 2 * (int64_t)blockIdx.x + ((int)blockIdx.x == b0 ? 1 : 0);
+    const int64_t unit = ((int64_t)(layer * Hkv + h) * R + r) * a.rb_max + rb;
+    const int64_t slot = 2 * (int64_t)blockIdx.x + (piece == b0 ? 1 : 0);
     if (t_in == 0 && tid == 0) a.desc[unit] = make_int2(b0, b1);
     float* red = reinterpret_cast<float*>(at_smem);
     constexpr int RS = DP + 4;
@@ -456,12 +482,7 @@ __global__ void __launch_bounds__(NTH, (Cfg<DP, NT, RG>::CTAS)) attend_kernel(co
         if (whole) {
           const int w = rho / G;
           const int64_t at = (qrow + w) * a.n_q_heads + h * G + (rho - w * G);
-          if (d < D) {
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;
-            __nv_bfloat162 v[2] = {__floats2bfloat162_rn(o.x * inv, o.y * inv), __floats2bfloat162_rn(o.z * inv, o.w * inv)};
-            *reinterpret_cast<uint2*>(a.out + at * D + d) = *reinterpret_cast<uint2*>(v);
-          }
-          if (d == 0 && a.lse != nullptr) a.lse[at] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
+          store_row(a, at, d, o, sum, M, D);
         } else {
           *reinterpret_cast<float4*>(a.part + (slot * C::RB + in_block) * DP + d) = o;
           if (d == 0) a.part_ml[slot * C::RB + in_block] = make_float2(M, sum);
@@ -471,14 +492,14 @@ __global__ void __launch_bounds__(NTH, (Cfg<DP, NT, RG>::CTAS)) attend_kernel(co
     }
     x += n_tiles;
     off += n_tiles;
-    if (off == (int64_t)q.tiles * rbs) {
+    if (off == (uint32_t)(q.tiles * rbs)) {
       off = 0;
-      if (++r == R) { r = 0; ++lh; }
+      if (++r == R) { r = 0; ++layer; }
     }
-    // (dims past head_dim: the join has written over their zeros)
+    // (dims past head_dim: the joins have written over their zeros)
     if (D < DP && x < x1) {
       const int spare = DP / 8 - nch;
-      for (int i = tid; i < C::RED / (DP * 2) * spare + spare; i += NTH) {
+      for (int i = tid; i < C::RING / (DP * 2) * spare; i += NTH) {
         const int row = i / spare, c = nch + i % spare;
         *reinterpret_cast<uint4*>(at_smem + row * DP * 2 + ((c ^ (row & 7)) << 4)) = make_uint4(0, 0, 0, 0);
       }
@@ -490,11 +511,11 @@ __global__ void __launch_bounds__(NTH, (Cfg<DP, NT, RG>::CTAS)) attend_kernel(co
 // The partials of one row of a unit that lies in several pieces, in piece order.  One CTA per (row, unit).
 constexpr int JN = 256;
 template <int DP>
-__global__ void __launch_bounds__(JN) attend_join_kernel(const Args a, int32_t RB) {
+__global__ void __launch_bounds__(JN) attend_join_kernel(const __grid_constant__ Args a, int32_t RB) {
   pdl_begin();
-  __shared__ float s_w[2 * MAX_CTAS + 2];
+  __shared__ float2 s_ml[MAX_CTAS];
   __shared__ float s_red[JN / 32][DP];
-  __shared__ float s_r[JN / 32], s_s[JN / 32];
+  __shared__ float s_r[JN / 32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int64_t unit = blockIdx.x;
   const int rb = (int)(unit % a.rb_max);
@@ -505,43 +526,55 @@ __global__ void __launch_bounds__(JN) attend_join_kernel(const Args a, int32_t R
   const Req q = load_req(a, r, false);
   if (rho >= q.W * G || b.x == b.y) return;
   const int n = b.y - b.x + 1, row = blockIdx.y;
-  auto slot = [&](int i) { return 2 * (int64_t)(b.x + i) + (i == 0 ? 1 : 0); };
+  const int Hkv = a.pool.n_kv_heads, layer = lh / Hkv, h = lh - layer * Hkv;
+  auto slot = [&](int i) { return slot_of(i, b.x, h, Hkv); };
+  // the first partials of this warp are on their way while the weights are formed
+  constexpr int E = DP / 32, AHEAD = 4;
+  float ahead[AHEAD][E];
+#pragma unroll
+  for (int k = 0; k < AHEAD; ++k) {
+    const int i = warp + k * (JN / 32);
+#pragma unroll
+    for (int e = 0; e < E; ++e) ahead[k][e] = i < n ? a.part[(slot(i) * RB + row) * DP + e * 32 + lane] : 0.f;
+  }
   float M = NO_REF;
-  for (int i = tid; i < n; i += JN) M = fmaxf(M, a.part_ml[slot(i) * RB + row].x);
+  for (int i = tid; i < n; i += JN) {
+    const float2 v = a.part_ml[slot(i) * RB + row];
+    s_ml[i] = v;
+    M = fmaxf(M, v.x);
+  }
 #pragma unroll
   for (int o = 16; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
   if (lane == 0) s_r[warp] = M;
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < JN / 32; ++w) M = fmaxf(M, s_r[w]);
+  // (every warp forms the sum by itself, in the same order)
   float sum = 0.f;
-  for (int i = tid; i < n; i += JN) {
-    const float2 ml = a.part_ml[slot(i) * RB + row];
-    const float f = exp2f(ml.x - M);
-    s_w[i] = f;
-    sum = fmaf(ml.y, f, sum);
-  }
+  for (int i = lane; i < n; i += 32) sum = fmaf(s_ml[i].y, exp2f(s_ml[i].x - M), sum);
 #pragma unroll
   for (int o = 16; o >= 1; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  if (lane == 0) s_s[warp] = sum;
-  __syncthreads();
-  sum = 0.f;
+  float o[E];
 #pragma unroll
-  for (int w = 0; w < JN / 32; ++w) sum += s_s[w];
-  float o[DP / 32];
+  for (int e = 0; e < E; ++e) o[e] = 0.f;
 #pragma unroll
-  for (int k = 0; k < DP / 32; ++k) o[k] = 0.f;
+  for (int k = 0; k < AHEAD; ++k) {
+    const int i = warp + k * (JN / 32);
+    const float f = i < n ? exp2f(s_ml[i].x - M) : 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = fmaf(ahead[k][e], f, o[e]);
+  }
 #pragma unroll 4
-  for (int i = warp; i < n; i += JN / 32) {
+  for (int i = warp + AHEAD * (JN / 32); i < n; i += JN / 32) {
     const float* src = a.part + (slot(i) * RB + row) * DP;
-    const float f = s_w[i];
+    const float f = exp2f(s_ml[i].x - M);
 #pragma unroll
-    for (int k = 0; k < DP / 32; ++k) o[k] = fmaf(src[k * 32 + lane], f, o[k]);
+    for (int e = 0; e < E; ++e) o[e] = fmaf(src[e * 32 + lane], f, o[e]);
   }
 #pragma unroll
-  for (int k = 0; k < DP / 32; ++k) s_red[warp][k * 32 + lane] = o[k];
+  for (int e = 0; e < E; ++e) s_red[warp][e * 32 + lane] = o[e];
   __syncthreads();
-  const int layer = lh / a.pool.n_kv_heads, h = lh - layer * a.pool.n_kv_heads, w = rho / G;
+  const int w = rho / G;
   const int64_t at = ((int64_t)layer * a.sum_win + q.win0 + w) * a.n_q_heads + h * G + (rho - w * G);
   if (tid < D) {
     float v = 0.f;
@@ -581,10 +614,11 @@ template <int DP, int NT, int RG>
 int launch(const Args& a, int64_t tiles_bound, int64_t units, cudaStream_t s) {
   using C = Cfg<DP, NT, RG>;
   if (ensure_dyn_smem(attend_kernel<DP, NT, RG>, C::RING) != cudaSuccess) return ACTKV_E_CUDA;
-  const int64_t grid = std::max<int64_t>(1, std::min<int64_t>(MAX_CTAS / 2 * C::CTAS, (tiles_bound + MIN_TILES - 1) / MIN_TILES));
-  launch_pdl(attend_kernel<DP, NT, RG>, (unsigned)grid, NTH, C::RING, s, a);
+  const int Hkv = a.pool.n_kv_heads;
+  const int64_t pieces = std::max<int64_t>(1, std::min<int64_t>(SMS * C::CTAS / Hkv, (tiles_bound / Hkv + MIN_TILES - 1) / MIN_TILES));
+  launch_pdl(attend_kernel<DP, NT, RG>, (unsigned)(pieces * Hkv), NTH, C::RING, s, a);
   ACTKV_CHECK_LAUNCH();
-  if (grid > 1) {
+  if (pieces > 1) {
     launch_pdl(attend_join_kernel<DP>, dim3((unsigned)units, C::RB), JN, 0, s, a, (int32_t)C::RB);
     ACTKV_CHECK_LAUNCH();
   }
@@ -627,7 +661,8 @@ int actkv_attend(const actkv_pool_t* pool, const actkv_tables_t* tables, int32_t
   if (q == out || (int64_t)max_win * G > (1 << 24)) return ACTKV_E_INVALID;
   const WsLayout lay = ws_layout(Hkv, D, R, nls, G, max_win);
   if (!ws || ws_bytes < lay.total) return ACTKV_E_WORKSPACE;
-  if (lay.units > 0x7fffffff) return ACTKV_E_TOOBIG;
+  if (lay.units > 0x7fffffff || (int64_t)R * lay.rb_max * std::max<int64_t>(1, ((int64_t)max_tok + KT - 1) / KT) > 0x7fffffff)
+    return ACTKV_E_TOOBIG;
   Args a;
   a.pool = make_view(pool);
   a.tab = make_view(tables);
