@@ -23,7 +23,7 @@
 // in shared memory and have 8 NT rows each.
 #include <algorithm>
 
-#include "common.cuh"
+#include "attend_tc.cuh"
 
 namespace actkv {
 namespace at {
@@ -31,50 +31,6 @@ namespace at {
 constexpr int NW = 4, NTH = NW * 32;
 constexpr int KT = 16;                    // keys per tile
 constexpr int MIN_TILES = 4;              // fewest tiles of a CTA's piece
-constexpr int SMS = 148, MAX_CTAS = 4 * SMS;
-constexpr float NO_REF = -3.0e38f;        // the reference before the first logit (finite: no infinity meets another)
-constexpr float REF_SLACK = 8.f;
-constexpr int MAX_GROUP = 32;             // query heads per KV head, as the score kernels
-
-struct Args {
-  PoolView pool;
-  TablesView tab;
-  const __nv_bfloat16* q;
-  const int32_t* win_indptr;
-  __nv_bfloat16* out;
-  float* lse;
-  int2* desc;                    // [units] first and last piece of a unit
-  float2* part_ml;               // [2 * MAX_CTAS][rows of a block] (m, l)
-  float* part;                   // [2 * MAX_CTAS][rows of a block][DP]
-  int32_t* status;
-  int32_t layer_begin, nls, n_q_heads, group;
-  int32_t sum_win, max_win, max_tok;
-  int32_t rb_max;                // blocks of rows per request, at most
-  int32_t page_shift;
-  float scale_log2;
-  int32_t causal, win_left;
-};
-
-struct Req {
-  int L, W, win0;                // W = 0: nothing to do
-  int lo_tile, tiles;            // key tiles that some row sees (one at least, so that every row is written)
-};
-__device__ __forceinline__ Req load_req(const Args& a, int r, bool tell) {
-  const int w0 = a.win_indptr[r], w1 = a.win_indptr[r + 1], L = a.tab.seq_len[r];
-  Req q{L, w1 - w0, w0, 0, 0};
-  const bool ok = L >= 0 && L <= a.max_tok && (int64_t)L <= (int64_t)a.tab.max_pages * a.pool.page_size && w0 >= 0 &&
-                  w1 >= w0 && w1 <= a.sum_win && q.W <= a.max_win;
-  if (!ok) {
-    if (tell) report(a.status, ACTKV_E_INVALID, r, L);
-    q.W = 0;
-  }
-  if (q.W > 0) {
-    const int first = a.causal ? L - q.W : L - 1;                          // the position of the first row
-    q.lo_tile = a.win_left > 0 ? max(0, first - a.win_left + 1) / KT : 0;
-    q.tiles = max(1, (L + KT - 1) / KT - q.lo_tile);
-  }
-  return q;
-}
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t bytes) {     // the rest of 16 is zeroed
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
@@ -117,19 +73,6 @@ struct Cfg {
   static_assert(RED <= RING, "the join of the warps reuses the ring");
 };
 
-// Slots of the partials of a unit in pieces b0 .. b1 of head h's line: the unit begins at the end of piece b0 and goes on at
-// the start of the others.
-__device__ __forceinline__ int64_t slot_of(int i, int b0, int h, int Hkv) { return 2 * ((int64_t)(b0 + i) * Hkv + h) + (i == 0 ? 1 : 0); }
-
-__device__ __forceinline__ void store_row(const Args& a, int64_t at, int d, float4 o, float sum, float M, int D) {
-  if (d < D) {
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    __nv_bfloat162 v[2] = {__floats2bfloat162_rn(o.x * inv, o.y * inv), __floats2bfloat162_rn(o.z * inv, o.w * inv)};
-    *reinterpret_cast<uint2*>(a.out + at * D + d) = *reinterpret_cast<uint2*>(v);
-  }
-  if (d == 0 && a.lse != nullptr) a.lse[at] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
-}
-
 template <int DP, int NT, int RG>
 __global__ void __launch_bounds__(NTH, (Cfg<DP, NT, RG>::CTAS)) attend_kernel(const __grid_constant__ Args a) {
   using C = Cfg<DP, NT, RG>;
@@ -138,59 +81,11 @@ __global__ void __launch_bounds__(NTH, (Cfg<DP, NT, RG>::CTAS)) attend_kernel(co
   __shared__ float2 s_ml[NW][8 * NT];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int grp = warp / RG, part = warp % RG;
-  const int R = a.tab.n_req, G = a.group, D = a.pool.head_dim, P = a.pool.page_size;
+  const int G = a.group, D = a.pool.head_dim, P = a.pool.page_size;
 
-  // ---- this CTA's head, and its piece of that head's line.  Every warp finds it by itself: lane t sums requests
-  // [t * per_t, (t + 1) * per_t) ----
-  const int Hkv = a.pool.n_kv_heads, h = blockIdx.x % Hkv, piece = blockIdx.x / Hkv, pieces = gridDim.x / Hkv;
-  const int per_t = (R + 31) / 32;
-  uint32_t mine = 0;
-  Req own{};                                                               // up to 32 requests: kept, and handed round
-  auto length_of = [&](const Req& q) { return (uint32_t)(q.tiles * ((q.W * G + C::RB - 1) / C::RB)); };
-#pragma unroll 4
-  for (int k = 0; k < per_t; ++k) {
-    const int r = lane * per_t + k;
-    if (r < R) {
-      own = load_req(a, r, blockIdx.x == 0 && warp == 0);
-      mine += length_of(own);
-    }
-  }
-  auto req_of = [&](int r) {
-    if (per_t > 1) return load_req(a, r, false);
-    Req q;
-    q.L = __shfl_sync(0xffffffffu, own.L, r);
-    q.W = __shfl_sync(0xffffffffu, own.W, r);
-    q.win0 = __shfl_sync(0xffffffffu, own.win0, r);
-    q.lo_tile = __shfl_sync(0xffffffffu, own.lo_tile, r);
-    q.tiles = __shfl_sync(0xffffffffu, own.tiles, r);
-    return q;
-  };
-  uint32_t incl = mine;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const uint32_t t = __shfl_up_sync(0xffffffffu, incl, d);
-    if (lane >= d) incl += t;
-  }
-  const uint32_t T = __shfl_sync(0xffffffffu, incl, 31);                   // (the host has seen to it that it fits)
-  const uint64_t total = (uint64_t)T * (uint32_t)a.nls;
-  auto div = [](uint64_t n, uint32_t d) { return n >> 32 ? n / d : (uint64_t)((uint32_t)n / d); };
-  const uint64_t per = max((uint64_t)MIN_TILES, div(total + pieces - 1, pieces));
-  uint64_t x = (uint64_t)piece * per;
-  const uint64_t x1 = min(total, x + per);
-  if (x >= x1) return;
-  int layer = (int)div(x, T);
-  int r = 0;
-  uint32_t off = (uint32_t)(x - (uint64_t)layer * T);
-  {
-    const int owner = __ffs(__ballot_sync(0xffffffffu, off < incl)) - 1;   // the lane whose requests hold the start
-    off -= __shfl_sync(0xffffffffu, incl - mine, owner);
-    r = owner * per_t;
-    for (; per_t > 1; ++r) {
-      const uint32_t n = length_of(load_req(a, r, false));
-      if (off < n) break;
-      off -= n;
-    }
-  }
+  Line<KT, C::RB, MIN_TILES> line(a, blockIdx.x == 0 && warp == 0);
+  if (line.x >= line.x1) return;
+  const int h = line.h;
 
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(at_smem) + grp * C::STAGES * C::TILE;
   const int g = lane >> 2, t2 = (lane & 3) * 2;
@@ -208,16 +103,10 @@ __global__ void __launch_bounds__(NTH, (Cfg<DP, NT, RG>::CTAS)) attend_kernel(co
     else asm volatile("bar.sync %0, %1;" ::"r"(1 + grp), "n"(RG * 32) : "memory");
   };
 
-  while (x < x1) {
-    const Req q = req_of(r);
-    const int rbs = (q.W * G + C::RB - 1) / C::RB;
-    if (q.W == 0) {
-      if (++r == R) { r = 0; ++layer; }
-      off = 0;
-      continue;
-    }
-    const int rb = (int)(off / (uint32_t)q.tiles), t_in = (int)(off - (uint32_t)rb * q.tiles);
-    const int n_tiles = (int)min((uint64_t)(q.tiles - t_in), x1 - x);
+  Seg sg;
+  while (line.next(sg)) {
+    const Req& q = sg.q;
+    const int r = sg.r, rb = sg.rb, t_in = sg.t_in, n_tiles = sg.n_tiles, layer = sg.layer;
     const int L = q.L, rows = q.W * G;
 
     // ---- the stream of this group's tiles ----
@@ -435,12 +324,9 @@ __global__ void __launch_bounds__(NTH, (Cfg<DP, NT, RG>::CTAS)) attend_kernel(co
         if (lane < 4) s_ml[warp][n * 8 + t2 + c] = make_float2(m[n][c], l[n][c]);
       }
     __syncthreads();                                                       // ... and nobody reads the rings any more
-    const uint64_t u0 = x - t_in;                                           // the unit's place on the line
-    const int b0 = (int)div(u0, (uint32_t)per), b1 = (int)div(u0 + q.tiles - 1, (uint32_t)per);
-    const bool whole = b0 == b1;
-    const int64_t unit = ((int64_t)(layer * Hkv + h) * R + r) * a.rb_max + rb;
-    const int64_t slot = 2 * (int64_t)blockIdx.x + (piece == b0 ? 1 : 0);
-    if (t_in == 0 && tid == 0) a.desc[unit] = make_int2(b0, b1);
+    const bool whole = sg.b0 == sg.b1;
+    const int64_t slot = line.slot(sg);
+    if (t_in == 0 && tid == 0) a.desc[line.unit(sg)] = make_int2(sg.b0, sg.b1);
     float* red = reinterpret_cast<float*>(at_smem);
     constexpr int RS = DP + 4;
 #pragma unroll 1
@@ -490,14 +376,8 @@ __global__ void __launch_bounds__(NTH, (Cfg<DP, NT, RG>::CTAS)) attend_kernel(co
       }
       __syncthreads();
     }
-    x += n_tiles;
-    off += n_tiles;
-    if (off == (uint32_t)(q.tiles * rbs)) {
-      off = 0;
-      if (++r == R) { r = 0; ++layer; }
-    }
-    // (dims past head_dim: the joins have written over their zeros)
-    if (D < DP && x < x1) {
+    // (dims past head_dim: the join has written over their zeros)
+    if (D < DP) {
       const int spare = DP / 8 - nch;
       for (int i = tid; i < C::RING / (DP * 2) * spare; i += NTH) {
         const int row = i / spare, c = nch + i % spare;
@@ -523,7 +403,7 @@ __global__ void __launch_bounds__(JN) attend_join_kernel(const __grid_constant__
   const int r = (int)(lr % a.tab.n_req), lh = (int)(lr / a.tab.n_req);
   const int rho = rb * RB + blockIdx.y, G = a.group, D = a.pool.head_dim;
   const int2 b = a.desc[unit];                                             // (read beside the request's: not valid where W = 0)
-  const Req q = load_req(a, r, false);
+  const Req q = load_req<KT>(a, r, false);
   if (rho >= q.W * G || b.x == b.y) return;
   const int n = b.y - b.x + 1, row = blockIdx.y;
   const int Hkv = a.pool.n_kv_heads, layer = lh / Hkv, h = lh - layer * Hkv;
@@ -585,8 +465,14 @@ __global__ void __launch_bounds__(JN) attend_join_kernel(const __grid_constant__
   if (tid == 0 && a.lse != nullptr) a.lse[at] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
 }
 
+// The tensor-core kernel takes what has more rows than one instruction of the warp-level one holds.
+// Its loads are boxes of a page's rows: pages of 16 to 128 tokens.
+inline bool use_tc(int D, int P, int64_t rows) {
+  return (D == 64 || D == 128) && (P == 16 || P == 32 || P == 64 || P == 128) && rows > 8;
+}
 // rows of a block for this many rows per request at most: the smallest variant that holds them
-inline int block_rows(int D, int64_t rows) {
+inline int block_rows(int D, int P, int64_t rows) {
+  if (use_tc(D, P, rows)) return rows <= 32 ? 32 : 64;
   if (D > 128) return rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
   return rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
 }
@@ -597,9 +483,9 @@ struct WsLayout {
   int RB, DP;
   int64_t rb_max, units;
 };
-inline WsLayout ws_layout(int Hkv, int D, int64_t n_req, int64_t nls, int G, int64_t max_win) {
+inline WsLayout ws_layout(int Hkv, int D, int P, int64_t n_req, int64_t nls, int G, int64_t max_win) {
   WsLayout l;
-  l.RB = block_rows(D, max_win * G);
+  l.RB = block_rows(D, P, max_win * G);
   l.DP = padded_dim(D);
   l.rb_max = std::max<int64_t>(1, (max_win * G + l.RB - 1) / l.RB);
   l.units = nls * Hkv * n_req * l.rb_max;
@@ -610,19 +496,32 @@ inline WsLayout ws_layout(int Hkv, int D, int64_t n_req, int64_t nls, int G, int
   return l;
 }
 
+template <int DP>
+int launch_join(const Args& a, int64_t pieces, int64_t units, int RB, cudaStream_t s) {
+  if (pieces == 1) return ACTKV_OK;
+  launch_pdl(attend_join_kernel<DP>, dim3((unsigned)units, RB), JN, 0, s, a, (int32_t)RB);
+  ACTKV_CHECK_LAUNCH();
+  return ACTKV_OK;
+}
+// CTAs of a head's line when the SMs take `per_sm` each
+inline int64_t pieces_of(int64_t tiles_bound, int Hkv, int per_sm, int min_tiles) {
+  return std::max<int64_t>(1, std::min<int64_t>(SMS * per_sm / Hkv, (tiles_bound / Hkv + min_tiles - 1) / min_tiles));
+}
 template <int DP, int NT, int RG>
 int launch(const Args& a, int64_t tiles_bound, int64_t units, cudaStream_t s) {
   using C = Cfg<DP, NT, RG>;
   if (ensure_dyn_smem(attend_kernel<DP, NT, RG>, C::RING) != cudaSuccess) return ACTKV_E_CUDA;
-  const int Hkv = a.pool.n_kv_heads;
-  const int64_t pieces = std::max<int64_t>(1, std::min<int64_t>(SMS * C::CTAS / Hkv, (tiles_bound / Hkv + MIN_TILES - 1) / MIN_TILES));
-  launch_pdl(attend_kernel<DP, NT, RG>, (unsigned)(pieces * Hkv), NTH, C::RING, s, a);
+  const int64_t pieces = pieces_of(tiles_bound, a.pool.n_kv_heads, C::CTAS, MIN_TILES);
+  launch_pdl(attend_kernel<DP, NT, RG>, (unsigned)(pieces * a.pool.n_kv_heads), NTH, C::RING, s, a);
   ACTKV_CHECK_LAUNCH();
-  if (pieces > 1) {
-    launch_pdl(attend_join_kernel<DP>, dim3((unsigned)units, C::RB), JN, 0, s, a, (int32_t)C::RB);
-    ACTKV_CHECK_LAUNCH();
-  }
-  return ACTKV_OK;
+  return launch_join<DP>(a, pieces, units, C::RB, s);
+}
+template <int D>
+int launch_wide(const Args& a, const actkv_pool_t* pool, int64_t max_tok, int64_t units, int RB, cudaStream_t s) {
+  const int64_t bound = units * std::max<int64_t>(1, (max_tok + tcx::TKEYS - 1) / tcx::TKEYS);
+  const int64_t pieces = pieces_of(bound, a.pool.n_kv_heads, 1, tcx::MIN_TILES_TC);
+  const int rc = RB == 32 ? tcx::launch_tc<D, 32>(a, pool, pieces, s) : tcx::launch_tc<D, 64>(a, pool, pieces, s);
+  return rc != ACTKV_OK ? rc : launch_join<D>(a, pieces, units, RB, s);
 }
 
 }  // namespace at
@@ -635,7 +534,7 @@ size_t actkv_attend_workspace_bytes(const actkv_pool_t* pool, int32_t n_req, int
   if (!pool || pool->n_kv_heads <= 0 || pool->head_dim <= 0 || n_req < 0 || n_layers_sub < 0 || n_q_heads <= 0 ||
       max_win < 0 || max_tok < 0)
     return 0;
-  return actkv::at::ws_layout(pool->n_kv_heads, pool->head_dim, n_req, n_layers_sub, n_q_heads / pool->n_kv_heads, max_win).total;
+  return actkv::at::ws_layout(pool->n_kv_heads, pool->head_dim, pool->page_size, n_req, n_layers_sub, n_q_heads / pool->n_kv_heads, max_win).total;
 }
 
 int actkv_attend(const actkv_pool_t* pool, const actkv_tables_t* tables, int32_t layer_begin, int32_t layer_end, const void* q,
@@ -659,7 +558,7 @@ int actkv_attend(const actkv_pool_t* pool, const actkv_tables_t* tables, int32_t
   if (!q || !win_indptr || !out || max_win == 0 || !tables->seq_len) return ACTKV_E_INVALID;
   if (!tables->page_table || tables->max_pages < 0) return ACTKV_E_INVALID;
   if (q == out || (int64_t)max_win * G > (1 << 24)) return ACTKV_E_INVALID;
-  const WsLayout lay = ws_layout(Hkv, D, R, nls, G, max_win);
+  const WsLayout lay = ws_layout(Hkv, D, pool->page_size, R, nls, G, max_win);
   if (!ws || ws_bytes < lay.total) return ACTKV_E_WORKSPACE;
   if (lay.units > 0x7fffffff || (int64_t)R * lay.rb_max * std::max<int64_t>(1, ((int64_t)max_tok + KT - 1) / KT) > 0x7fffffff)
     return ACTKV_E_TOOBIG;
@@ -688,6 +587,8 @@ int actkv_attend(const actkv_pool_t* pool, const actkv_tables_t* tables, int32_t
   a.win_left = window_left;
   const int64_t bound = lay.units * std::max<int64_t>(1, ((int64_t)max_tok + KT - 1) / KT);
   cudaStream_t s = (cudaStream_t)stream;
+  if (use_tc(D, pool->page_size, (int64_t)max_win * G))
+    return D == 64 ? launch_wide<64>(a, pool, max_tok, lay.units, lay.RB, s) : launch_wide<128>(a, pool, max_tok, lay.units, lay.RB, s);
   if (lay.DP == 256) {
     switch (lay.RB) {
       case 8: return launch<256, 1, 1>(a, bound, lay.units, s);

@@ -1,0 +1,500 @@
+// actkv_attend on the tensor cores of the fifth generation (tcgen05): 9 and more rows per request and KV head (drafted tokens, chunks,
+// large groups), head_dim 64 or 128.
+//
+// Why a second kernel.  Of every key the warp-level kernel loads fragments for each 8 rows and carries every instruction of the softmax
+// in the warps that feed the matrix pipe: 32 rows took 1.8 times, 64 rows 3.0 times what 8 rows take (16 requests of 16000 tokens, 4 heads of
+// 128 dims: 89 us with 8 rows; 32: 153, 64: 248).  Here a tile of 128 keys is one operand:
+//   S[key, row] = K Q^T       M = 128 keys, N = NR rows, both operands K-major in shared memory, S in tensor memory;
+//   P = exp2(S - reference)   one warpgroup, a thread per key; bf16 summands (p truncated, and the rest) of all rows into shared memory;
+//   O^T[dim, row] += V^T P    M = head_dim, N = 2 NR: the two summands side by side, so that V is read once; both operands lie with the
+//                             long side contiguous (V as the pool has it: [key][dim], P as its thread writes it: [key][row]).
+// Sums of P are kept per thread and row in registers and joined at the end of a stretch.  The references live in shared memory and move
+// (then O is rescaled) only when a logit exceeds one by more than 8: in the first tile, hardly ever after.
+//
+// Roles of a CTA (one per SM): warps 0-3 softmax and epilogue, warp 4 issues the MMAs, warps 8-11 load.  K and V tiles are entries of one
+// ring, in the order of use: K0, K1, V0, K2, V1, ...  S and P have two buffers each, so that S of the next tile is formed while the
+// warpgroup is at this one.  All waits are bounded; one that gives up raises a flag that ends every role (ACTKV_E_TIMEOUT).
+//
+// What bounds it: reading K and V (up to 64 rows and 128 dims).  Shared memory comes next: a tile's operands are read by the MMAs
+// once each (64 rows, 128 dims: 1150 cycles of 2850 that the tile's bytes take to arrive).
+#pragma once
+
+#include "attend_line.cuh"
+#include "pool_map.cuh"
+#include "ring.cuh"
+
+namespace actkv {
+namespace at {
+namespace tcx {
+
+using namespace actkv::tc;
+
+constexpr int TKEYS = 128;
+// (warps 5-7 only fill up the second warpgroup, as registers are handed round by warpgroups)
+constexpr int SOFT = 128, MMA_WARP = 4, LOAD0 = 256, THREADS = LOAD0 + 128;
+constexpr int SOFT_REGS = 232, REST_REGS = 128;                // 168 each at launch: 128 * 232 + 256 * 128 <= 384 * 168
+constexpr int MIN_TILES_TC = 1;
+
+template <int D, int NR>
+struct Tc {
+  static constexpr int UNIT = TKEYS * D * 2;                   // bytes of a K or V tile: halves of 64 dims, rows of 128 bytes
+  static constexpr int PBUF = TKEYS * 2 * NR * 2;              // bytes of a P buffer: [key] rows of 128 bytes; 64 rows: summands apart
+  static constexpr int QBYTES = NR * D * 2;
+  static constexpr int STAGES = 128 * 1024 / UNIT;             // 4 or 8
+  static constexpr int TM_COLS = 4 * NR;                       // S twice, O twice as wide
+  static constexpr int P_OFF = STAGES * UNIT, Q_OFF = P_OFF + 2 * PBUF, CTL_OFF = Q_OFF + QBYTES;
+};
+
+template <int D, int NR>
+struct Ctl {
+  uint64_t full[8], empty[8];              // ring
+  uint64_t s_full[2], s_empty[2], p_full[2], p_empty[2];
+  uint64_t q_full, o_full, o_empty, drained;
+  uint32_t tmem;
+  int abort;
+  int stop[2];
+  unsigned last[8];                        // parity of the last load into each entry
+  int poisoned;
+  alignas(16) float ref[NR];               // (read as vectors)
+  float fac[NR], inv[NR];
+  int pos[NR];
+  int64_t at[NR];                          // output row
+  float wmax[4][NR];
+  uint32_t poison[2][NR][D / 32];          // (row, dim) that met +infinity / -infinity in a tile not every row sees whole (NaN: both)
+};
+template <int D, int NR>
+constexpr size_t smem_bytes() { return Tc<D, NR>::CTL_OFF + sizeof(Ctl<D, NR>) + 1024; }       // (the ring begins on 1024 bytes)
+
+__device__ __forceinline__ void soft_sync() { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ bool soft_any(bool v) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %1, 0;\n\t"
+      "barrier.cta.red.or.pred q, 1, 128, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(r) : "r"(v ? 1u : 0u) : "memory");
+  return r != 0;
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const float* v) {
+  const uint32_t* r = reinterpret_cast<const uint32_t*>(v);
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+      ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// Operand with the long side (M or N) contiguous, 128-byte swizzle: rows of 64 bf16, one per k; eight rows of k are 1024 bytes,
+// the next 64 of the long side `lead` bytes away.
+__device__ __forceinline__ uint64_t smem_desc_mn(uint32_t addr, uint32_t lead) {
+  return (uint64_t)((addr & 0x3FFFF) >> 4) | ((uint64_t)(lead >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) |
+         ((uint64_t)2 << 61);
+}
+// Place in the order K0, K1, V0, K2, V1, ..., K(n-1), V(n-2), V(n-1) of a stretch of n tiles.
+__device__ __forceinline__ int place_k(int i) { return i == 0 ? 0 : 2 * i - 1; }
+__device__ __forceinline__ int place_v(int i, int n) { return i < n - 1 ? 2 * i + 2 : 2 * n - 1; }
+
+template <int D, int NR>
+__global__ void __launch_bounds__(THREADS, 1) attend_tc_kernel(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap kmap,
+                                                               const __grid_constant__ CUtensorMap vmap, const int k5,
+                                                               const long long limit) {
+  using T = Tc<D, NR>;
+  using CT = Ctl<D, NR>;
+  pdl_begin();
+  extern __shared__ uint8_t tcx_raw[];
+  uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(tcx_raw) + 1023) & ~(uintptr_t)1023);
+  CT* ctl = reinterpret_cast<CT*>(base + T::CTL_OFF);
+  const uint32_t sbase = smem_u32(base);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int G = a.group;
+  volatile int* abort_flag = &ctl->abort;
+
+  if (tid == 0) {
+    for (int i = 0; i < T::STAGES; ++i) {
+      mbar_init(smem_u32(&ctl->full[i]), 1);
+      mbar_init(smem_u32(&ctl->empty[i]), 1);
+      ctl->last[i] = RING_UNUSED;
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&ctl->s_full[i]), 1);
+      mbar_init(smem_u32(&ctl->s_empty[i]), SOFT);
+      mbar_init(smem_u32(&ctl->p_full[i]), SOFT);
+      mbar_init(smem_u32(&ctl->p_empty[i]), 1);
+      ctl->stop[i] = 0;
+    }
+    mbar_init(smem_u32(&ctl->q_full), SOFT);
+    mbar_init(smem_u32(&ctl->o_full), 1);
+    mbar_init(smem_u32(&ctl->o_empty), SOFT);
+    mbar_init(smem_u32(&ctl->drained), 1);
+    ctl->abort = 0;
+    ctl->poisoned = 0;
+    fence_barrier_init();
+  }
+  for (int i = tid; i < 2 * NR * (D / 32); i += THREADS) (&ctl->poison[0][0][0])[i] = 0;
+  if (warp == MMA_WARP) {
+    tmem_alloc(smem_u32(&ctl->tmem), T::TM_COLS);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = ctl->tmem, tm_o = tmem + 2 * NR;
+  Line<TKEYS, NR, MIN_TILES_TC> line(a, blockIdx.x == 0 && warp == 0);
+  Seg sg;
+
+  if (warp < 4) {
+    reg_inc<SOFT_REGS>();
+    // ================================ softmax: thread = key of the tile ================================
+    uint32_t t = 0, seg = 0, ring0 = 0;                        // tiles, stretches, ring entries so far
+    bool dead = false;
+    const uint32_t lane_off = (uint32_t)(warp * 32) << 16;
+    while (line.next(sg)) {
+      const Req& q = sg.q;
+      const int L = q.L, rows = q.W * G, row0 = sg.rb * NR, n_rows = min(NR, rows - row0);
+      const int pos0 = a.causal ? L - q.W : L - 1, step = a.causal ? 1 : 0;
+      const int all_hi = pos0 + step * (row0 / G);
+      const int all_lo = a.win_left > 0 ? pos0 + step * ((row0 + n_rows - 1) / G) - a.win_left + 1 : 0;
+      const int64_t qrow = (int64_t)sg.layer * a.sum_win + q.win0;
+      // Q of the stretch (every S of the one before is complete: the last one has been waited for)
+#pragma unroll
+      for (int i = tid; i < NR * (D / 8); i += SOFT) {
+        const int row = i / (D / 8), c = i % (D / 8), rho = row0 + row, w = rho / G;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (row < n_rows)
+          v = *reinterpret_cast<const uint4*>(a.q + ((qrow + w) * a.n_q_heads + line.h * G + (rho - w * G)) * D + c * 8);
+        *reinterpret_cast<uint4*>(base + T::Q_OFF + (c >> 3) * (NR * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = v;
+      }
+      if (tid < NR) {
+        ctl->ref[tid] = NO_REF;
+        const int rho = row0 + min(tid, n_rows - 1), w = rho / G;
+        ctl->pos[tid] = pos0 + step * w;
+        ctl->at[tid] = (qrow + w) * a.n_q_heads + line.h * G + (rho - w * G);
+      }
+      fence_proxy_async();
+      mbar_arrive(smem_u32(&ctl->q_full));
+      soft_sync();
+      float l[NR];
+#pragma unroll
+      for (int n = 0; n < NR; ++n) l[n] = 0.f;
+
+      for (int i = 0; i < sg.n_tiles; ++i, ++t) {
+        const int b = t & 1;
+        const uint32_t use = t >> 1;
+        if (!mbar_wait_warp(smem_u32(&ctl->s_full[b]), use & 1, abort_flag, limit)) dead = true;
+        tc_fence_after();
+        const uint32_t ts = tmem + b * NR + lane_off;
+        const int key = (q.lo_tile + sg.t_in + i) * TKEYS + tid;
+        const bool masked = key - tid + TKEYS - 1 > all_hi || key - tid < all_lo;
+        float x[NR];
+        auto load = [&]() {
+#pragma unroll
+          for (int c = 0; c < NR; c += 32) tmem_ld32(ts + c, x + c);
+          tmem_ld_wait();
+#pragma unroll
+          for (int n = 0; n < NR; ++n) x[n] *= a.scale_log2;
+          if (masked) {
+#pragma unroll
+            for (int n = 0; n < NR; ++n) {
+              const int pos = ctl->pos[n];
+              if (key > pos || (a.win_left > 0 && key <= pos - a.win_left)) x[n] = -INFINITY;
+            }
+          }
+        };
+        load();
+        float over = -INFINITY;
+#pragma unroll
+        for (int n = 0; n < NR; n += 4) {
+          const float4 r = *reinterpret_cast<const float4*>(&ctl->ref[n]);
+          x[n] -= r.x;
+          x[n + 1] -= r.y;
+          x[n + 2] -= r.z;
+          x[n + 3] -= r.w;
+          over = fmaxf(over, fmaxf(fmaxf(x[n], x[n + 1]), fmaxf(x[n + 2], x[n + 3])));
+        }
+        if (dead) ctl->stop[b] = 1;
+        const bool move = soft_any(over > REF_SLACK);
+        if (*reinterpret_cast<volatile int*>(&ctl->stop[b])) goto out;     // (the same answer for all four warps)
+        if (move) {
+          // new references: the columns' maxima over the tile
+          load();
+#pragma unroll
+          for (int n = 0; n < NR; ++n) {
+            float v = x[n];
+#pragma unroll
+            for (int d = 16; d >= 1; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
+            if (lane == 0) ctl->wmax[warp][n] = v;
+          }
+          soft_sync();
+          if (tid < NR) {
+            const float old = ctl->ref[tid];
+            const float top = fmaxf(fmaxf(fmaxf(ctl->wmax[0][tid], ctl->wmax[1][tid]), fmaxf(ctl->wmax[2][tid], ctl->wmax[3][tid])), old);
+            ctl->ref[tid] = top;
+            ctl->fac[tid] = exp2f(old - top);
+          }
+          soft_sync();
+#pragma unroll
+          for (int n = 0; n < NR; ++n) l[n] *= ctl->fac[n];
+          if (i > 0) {
+            // O so far, when the product before this tile's is complete (this tile's waits for P)
+            const uint32_t before = t - 1;
+            if (!mbar_wait_warp(smem_u32(&ctl->p_empty[before & 1]), (before >> 1) & 1, abort_flag, limit)) dead = true;
+            tc_fence_after();
+#pragma unroll 1
+            for (int c = 0; c < 2 * NR; c += 32) {
+              float o[32];
+              tmem_ld32(tm_o + lane_off + c, o);
+              tmem_ld_wait();
+#pragma unroll
+              for (int n = 0; n < 32; ++n) o[n] *= ctl->fac[(c + n) % NR];
+              tmem_st32(tm_o + lane_off + c, o);
+            }
+            tmem_st_wait();
+          }
+#pragma unroll
+          for (int n = 0; n < NR; ++n) x[n] -= ctl->ref[n];
+        }
+        tc_fence_before();
+        mbar_arrive(smem_u32(&ctl->s_empty[b]));
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+          x[n] = exp2f(x[n]);
+          l[n] += x[n];
+        }
+        if (masked) {
+          // V of a key that some row must not see, or of a slot behind the end: infinities and NaN leave the product; what they make of the
+          // rows that do see the key is noted
+          const uint32_t e = ring0 + place_v(i, sg.n_tiles), sl = e % T::STAGES;
+          // (unguarded by the others: a wait of this thread alone; the entry stays until this tile's product)
+          if (!mbar_wait(smem_u32(&ctl->full[sl]), (e / T::STAGES) & 1, abort_flag, limit)) dead = true;
+          for (int c = 0; c < D / 8; ++c) {
+            uint8_t* at = base + sl * T::UNIT + (c >> 3) * 16384 + tid * 128 + (((c & 7) ^ (tid & 7)) << 4);
+            const uint4 v = *reinterpret_cast<const uint4*>(at);
+            bool odd = false;
+            for (uint32_t u : {v.x, v.y, v.z, v.w}) odd |= (u & 0x7f80u) == 0x7f80u || (u & 0x7f800000u) == 0x7f800000u;
+            if (!odd) continue;
+            for (int k = 0; k < 8; ++k) {
+              uint16_t* el = reinterpret_cast<uint16_t*>(at) + k;
+              const uint32_t bits = *el;
+              if ((bits & 0x7f80u) != 0x7f80u) continue;
+              *el = 0;
+              const bool nan = (bits & 0x7fu) != 0, neg = (bits & 0x8000u) != 0;
+              const int d = c * 8 + k;
+#pragma unroll
+              for (int n = 0; n < NR; ++n) {
+                if (!(x[n] > 0.f)) continue;
+                if (nan || !neg) atomicOr(&ctl->poison[0][n][d >> 5], 1u << (d & 31));
+                if (nan || neg) atomicOr(&ctl->poison[1][n][d >> 5], 1u << (d & 31));
+                ctl->poisoned = 1;
+              }
+            }
+          }
+        }
+        if (!mbar_wait_warp(smem_u32(&ctl->p_empty[b]), (use & 1) ^ 1, abort_flag, limit)) dead = true;
+        uint8_t* pr = base + T::P_OFF + b * T::PBUF + tid * 128;
+#pragma unroll
+        for (int c = 0; c < NR / 8; ++c) {
+          uint32_t hi[4], lo[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float p0 = x[c * 8 + 2 * k], p1 = x[c * 8 + 2 * k + 1];
+            const uint32_t u0 = __float_as_uint(p0), u1 = __float_as_uint(p1);
+            const float r0 = p0 - __uint_as_float(u0 & 0xffff0000u), r1 = p1 - __uint_as_float(u1 & 0xffff0000u);
+            hi[k] = __byte_perm(u0, u1, 0x7632);
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(lo[k]) : "f"(r1), "f"(r0));
+          }
+          // rows of 128 bytes: 64 rows: one summand each, 16 KB apart; 32 rows: both
+          uint8_t* ph = pr + ((c ^ (tid & 7)) << 4);
+          uint8_t* pl = NR == 64 ? ph + 16384 : pr + (((c + 4) ^ (tid & 7)) << 4);
+          *reinterpret_cast<uint4*>(ph) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+          *reinterpret_cast<uint4*>(pl) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        }
+        fence_proxy_async();
+        mbar_arrive(smem_u32(&ctl->p_full[b]));
+      }
+      ring0 += 2 * (uint32_t)sg.n_tiles;
+
+      // ---- the stretch's rows ----
+#pragma unroll
+      for (int n = 0; n < NR; ++n) {
+        float v = l[n];
+#pragma unroll
+        for (int d = 16; d >= 1; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+        if (lane == 0) ctl->wmax[warp][n] = v;
+      }
+      if (!mbar_wait_warp(smem_u32(&ctl->o_full), seg & 1, abort_flag, limit)) dead = true;
+      tc_fence_after();
+      soft_sync();
+      const bool whole = sg.b0 == sg.b1;
+      const int64_t slot = line.slot(sg);
+      if (sg.t_in == 0 && tid == 0) a.desc[line.unit(sg)] = make_int2(sg.b0, sg.b1);
+      if (tid < NR) {
+        const float sum = ctl->wmax[0][tid] + ctl->wmax[1][tid] + ctl->wmax[2][tid] + ctl->wmax[3][tid], M = ctl->ref[tid];
+        ctl->inv[tid] = !whole ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
+        if (tid < n_rows) {
+          if (!whole) a.part_ml[slot * NR + tid] = make_float2(M, sum);
+          else if (a.lse != nullptr)
+            a.lse[ctl->at[tid]] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
+        }
+      }
+      soft_sync();
+      {
+        // M = 128: dim = lane of tensor memory; M = 64: 16 dims in the first 16 lanes of every warp
+        const int d = D == 128 ? tid : warp * 16 + lane;
+        const bool mine = D == 128 || lane < 16;
+        const bool poisoned = ctl->poisoned != 0;
+#pragma unroll 1
+        for (int c = 0; c < NR; c += 32) {
+          float o[32], o2[32];
+          tmem_ld32(tm_o + lane_off + c, o);
+          tmem_ld32(tm_o + lane_off + NR + c, o2);
+          tmem_ld_wait();
+          if (mine) {
+#pragma unroll
+            for (int n = 0; n < 32; ++n) {
+              const int row = c + n;
+              if (row >= n_rows) continue;
+              float v = (o[n] + o2[n]) * ctl->inv[row];
+              if (poisoned) {
+                const uint32_t up = ctl->poison[0][row][d >> 5] >> (d & 31) & 1u, down = ctl->poison[1][row][d >> 5] >> (d & 31) & 1u;
+                if (up) v += INFINITY;
+                if (down) v += -INFINITY;
+              }
+              if (whole) a.out[ctl->at[row] * D + d] = __float2bfloat16_rn(v);
+              else a.part[(slot * NR + row) * D + d] = v;
+            }
+          }
+        }
+        tc_fence_before();
+        mbar_arrive(smem_u32(&ctl->o_empty));
+        soft_sync();                                           // references and poison are rewritten
+        if (poisoned) {
+          for (int i = tid; i < 2 * NR * (D / 32); i += SOFT) (&ctl->poison[0][0][0])[i] = 0;
+          if (tid == 0) ctl->poisoned = 0;
+          soft_sync();
+        }
+      }
+      ++seg;
+    }
+  } else if (warp < LOAD0 / 32) {
+    reg_dec<REST_REGS>();
+    if (warp != MMA_WARP) goto out;
+    // ================================ MMA issuer ================================
+    constexpr uint32_t IDESC_S = idesc_bf16(128, NR), IDESC_O = idesc_bf16(D, 2 * NR) | (1u << 15) | (1u << 16);
+    const uint64_t qd = smem_desc_sw128(sbase + T::Q_OFF);
+    uint32_t t = 0, seg = 0, ring0 = 0;
+    bool ok = true;
+    while (ok && line.next(sg)) {
+      const int n = sg.n_tiles;
+      ok = mbar_wait_warp(smem_u32(&ctl->q_full), seg & 1, abort_flag, limit);
+      for (int i = 0; ok && i <= n; ++i) {
+        if (i < n) {                                           // S of tile i
+          const uint32_t tt = t + i, b = tt & 1, e = ring0 + place_k(i), sl = e % T::STAGES;
+          ok = mbar_wait_warp(smem_u32(&ctl->full[sl]), (e / T::STAGES) & 1, abort_flag, limit) &&
+               mbar_wait_warp(smem_u32(&ctl->s_empty[b]), ((tt >> 1) & 1) ^ 1, abort_flag, limit);
+          if (!ok) break;
+          tc_fence_after();
+          if (elect_one()) {
+            const uint64_t kd = smem_desc_sw128(sbase + sl * T::UNIT);
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k)
+              umma_bf16(tmem + b * NR, kd + (uint64_t)(((k >> 2) * 16384 + (k & 3) * 32) >> 4),
+                        qd + (uint64_t)(((k >> 2) * (NR * 128) + (k & 3) * 32) >> 4), IDESC_S, k > 0 ? 1u : 0u);
+            umma_commit(smem_u32(&ctl->s_full[b]));
+            umma_commit(smem_u32(&ctl->empty[sl]));
+          }
+          __syncwarp();
+        }
+        if (i > 0) {                                           // O of tile i - 1
+          const uint32_t tt = t + i - 1, b = tt & 1, e = ring0 + place_v(i - 1, n), sl = e % T::STAGES;
+          ok = mbar_wait_warp(smem_u32(&ctl->full[sl]), (e / T::STAGES) & 1, abort_flag, limit) &&
+               mbar_wait_warp(smem_u32(&ctl->p_full[b]), (tt >> 1) & 1, abort_flag, limit);
+          if (ok && i == 1) ok = mbar_wait_warp(smem_u32(&ctl->o_empty), (seg & 1) ^ 1, abort_flag, limit);
+          if (!ok) break;
+          tc_fence_after();
+          if (elect_one()) {
+            const uint64_t vd = smem_desc_mn(sbase + sl * T::UNIT, 16384), pd = smem_desc_mn(sbase + T::P_OFF + b * T::PBUF, 16384);
+#pragma unroll
+            for (int k = 0; k < TKEYS / 16; ++k)
+              umma_bf16(tm_o, vd + (uint64_t)((k * 2048) >> 4), pd + (uint64_t)((k * 2048) >> 4), IDESC_O, (i > 1 || k > 0) ? 1u : 0u);
+            umma_commit(smem_u32(&ctl->p_empty[b]));
+            umma_commit(smem_u32(&ctl->empty[sl]));
+            if (i == n) umma_commit(smem_u32(&ctl->o_full));
+          }
+          __syncwarp();
+        }
+      }
+      t += n;
+      ring0 += 2 * (uint32_t)n;
+      ++seg;
+    }
+    // everything issued has retired before tensor memory is freed
+    if (elect_one()) umma_commit(smem_u32(&ctl->drained));
+    __syncwarp();
+    mbar_wait_warp(smem_u32(&ctl->drained), 0, nullptr, DRAIN_LIMIT_CYCLES);
+  } else {
+    reg_dec<REST_REGS>();
+    // ================================ loaders: entry e of the ring is warp e % 4's ================================
+    const int w = warp - (LOAD0 >> 5), ps = a.pool.page_size, ppt = TKEYS / ps, lp_shift = 31 - __clz(ppt);
+    constexpr int NH = D / 64;
+    uint32_t ring0 = 0;
+    bool ok = true;
+    while (ok && line.next(sg)) {
+      const int L = sg.q.L, n = sg.n_tiles, n_lp = (L + ps - 1) / ps;
+      for (int at = (int)((w - ring0) & 3); at < 2 * n; at += 4) {
+        // the inverse of place_k and place_v
+        const bool is_v = at == 2 * n - 1 || (at > 0 && (at & 1) == 0);
+        const int i = at == 0 ? 0 : at == 2 * n - 1 ? n - 1 : is_v ? at / 2 - 1 : (at + 1) / 2;
+        const uint32_t e = ring0 + at, sl = e % T::STAGES, ph = (e / T::STAGES) & 1;
+        // lane j < ppt NH: page j % ppt, half j / ppt.  Pages past the end: the last one again (their keys are masked)
+        int pid = 0;
+        if (lane < ppt && n_lp > 0)
+          pid = checked_page(a.tab, a.pool.n_pages, sg.r, min((sg.q.lo_tile + sg.t_in + i) * ppt + lane, n_lp - 1), a.status);
+        int got = 1;
+        if (lane == 0) {
+          got = mbar_wait(smem_u32(&ctl->empty[sl]), ph ^ 1, abort_flag, limit) ? 1 : 0;
+          if (got) {
+            ctl->last[sl] = ph;
+            if (n_lp > 0) mbar_expect_tx(smem_u32(&ctl->full[sl]), T::UNIT);
+            else mbar_arrive(smem_u32(&ctl->full[sl]));        // an empty request: every key is masked
+          }
+        }
+        ok = __shfl_sync(0xffffffffu, got, 0) != 0;
+        if (!ok) break;
+        pid = __shfl_sync(0xffffffffu, pid, lane & (ppt - 1));
+        if (lane < ppt * NH && n_lp > 0) {
+          const int half = lane >> lp_shift;
+          const uint32_t dst = sbase + sl * T::UNIT + half * 16384 + (lane & (ppt - 1)) * ps * 128, bar = smem_u32(&ctl->full[sl]);
+          const CUtensorMap* map = is_v ? &vmap : &kmap;
+          if (k5) tma_load_5d(dst, map, bar, half * 64, 0, line.h, pid, a.layer_begin + sg.layer);
+          else tma_load_4d(dst, map, bar, half * 64, line.h, pid * ps, a.layer_begin + sg.layer);
+        }
+      }
+      ring0 += 2 * (uint32_t)n;
+    }
+  }
+out:
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (*abort_flag && tid == 0) {
+    report(a.status, ACTKV_E_TIMEOUT, (int)blockIdx.x, line.h);
+    // loads still in flight land in this CTA's shared memory: waited for, with a limit
+    for (int i = 0; i < T::STAGES; ++i) mbar_wait(smem_u32(&ctl->full[i]), ctl->last[i], nullptr, DRAIN_LIMIT_CYCLES / 64);
+  }
+  if (warp == MMA_WARP) tmem_dealloc(tmem, T::TM_COLS);
+}
+
+template <int D, int NR>
+int launch_tc(const Args& a, const actkv_pool_t* pool, int64_t pieces, cudaStream_t s) {
+  CUtensorMap kmap, vmap;
+  if (!make_kvmap(pool, 0, &kmap) || !make_kvmap(pool, 1, &vmap)) return ACTKV_E_CUDA;
+  if (ensure_dyn_smem(attend_tc_kernel<D, NR>, smem_bytes<D, NR>()) != cudaSuccess) return ACTKV_E_CUDA;
+  launch_pdl(attend_tc_kernel<D, NR>, (unsigned)(pieces * a.pool.n_kv_heads), THREADS, smem_bytes<D, NR>(), s, a, kmap, vmap,
+             pool_needs_5d(pool) ? 1 : 0, WAIT_LIMIT_CYCLES);
+  ACTKV_CHECK_LAUNCH();
+  return ACTKV_OK;
+}
+
+}  // namespace tcx
+}  // namespace at
+}  // namespace actkv

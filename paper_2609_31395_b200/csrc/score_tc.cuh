@@ -18,37 +18,18 @@
 // ACTKV_E_TIMEOUT in the status word, every role leaves its loop, outstanding MMAs are drained,
 // TMEM is freed and the CTA returns.
 //
-// This file: tensor-map creation and launch configuration (host side).
+// This file: launch configuration (host side); the pool's tensor maps: pool_map.cuh.
 #pragma once
 
 #include <algorithm>
 #include <atomic>
 
+#include "pool_map.cuh"
 #include "score_tc_lse.cuh"
 #include "score_tc_pool.cuh"
 
 namespace actkv {
 namespace tc {
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-// The driver entry point is looked up through the runtime, so the library does not link libcuda.
-inline EncodeTiledFn encode_fn() {
-  static EncodeTiledFn fn = []() -> EncodeTiledFn {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess ||
-        q != cudaDriverEntryPointSuccess)
-      return nullptr;
-    return (EncodeTiledFn)p;
-  }();
-  return fn;
-}
-
-// The four-dimensional K map needs the slots of consecutive pages to continue at the slot stride.
-inline bool pool_needs_5d(const actkv_pool_t* pool) { return pool->stride_page != (int64_t)pool->page_size * pool->stride_slot; }
 
 inline int pow2_at_least(int g) { int p = 1; while (p < g) p <<= 1; return p; }
 
@@ -104,36 +85,6 @@ inline int lse_split(int64_t units, int tiles, double len, double win, double ov
     if (t < best_t * (equal ? 0.99 : 0.995)) { best_t = t; best = n; }
   }
   return best;
-}
-
-inline bool make_kmap(const actkv_pool_t* pool, CUtensorMap* kmap) {
-  EncodeTiledFn enc = encode_fn();
-  if (!enc) return false;
-  // K half of the pool.  Slot-major pages whose slots continue across pages: [layer][slot (page*16 + s)]
-  // [head][dim], four dimensions (measured 13 % faster than five on the K stream).  Any other page layout
-  // (head-major pages): [layer][page][head][slot][dim] with the caller's strides.  A box is one page of
-  // one head, 64 dims: page_size rows of 128 B.
-  CUresult res;
-  if (!pool_needs_5d(pool)) {
-    cuuint64_t dims[4] = {(cuuint64_t)pool->head_dim, (cuuint64_t)pool->n_kv_heads, (cuuint64_t)pool->n_pages * pool->page_size,
-                          (cuuint64_t)pool->n_layers};
-    cuuint64_t strides[3] = {(cuuint64_t)pool->stride_head * 2, (cuuint64_t)pool->stride_slot * 2,
-                             (cuuint64_t)pool->stride_layer * 2};
-    cuuint32_t box[4] = {64, 1, (cuuint32_t)pool->page_size, 1};
-    cuuint32_t es[4] = {1, 1, 1, 1};
-    res = enc(kmap, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, pool->base, dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  } else {
-    cuuint64_t dims[5] = {(cuuint64_t)pool->head_dim, (cuuint64_t)pool->page_size, (cuuint64_t)pool->n_kv_heads,
-                          (cuuint64_t)pool->n_pages, (cuuint64_t)pool->n_layers};
-    cuuint64_t strides[4] = {(cuuint64_t)pool->stride_slot * 2, (cuuint64_t)pool->stride_head * 2,
-                             (cuuint64_t)pool->stride_page * 2, (cuuint64_t)pool->stride_layer * 2};
-    cuuint32_t box[5] = {64, (cuuint32_t)pool->page_size, 1, 1, 1};
-    cuuint32_t es[5] = {1, 1, 1, 1, 1};
-    res = enc(kmap, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, pool->base, dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  }
-  return res == CUDA_SUCCESS;
 }
 
 // q: [slab*sum_win + w][q head][head_dim]; a box is (64 dims, `heads` heads from the first of a group on, `tokens` window tokens)
