@@ -465,6 +465,59 @@ __global__ void __launch_bounds__(JN) attend_join_kernel(const __grid_constant__
   if (tid == 0 && a.lse != nullptr) a.lse[at] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
 }
 
+// The same with a warp per row, eight rows of a unit per CTA: for launches with more rows than CTAs of the kernel above fit on the SMs.
+template <int DP>
+__global__ void __launch_bounds__(JN) attend_join_rows_kernel(const __grid_constant__ Args a, int32_t RB) {
+  // (The next kernel may start when this one has ended, not before: CTAs of the next attention call that were placed beside
+  // waiting ones of this kernel found an SM each other's pieces did not: 64 requests of 8K-32K 474 us, so 366.)
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int lane = threadIdx.x & 31, row = blockIdx.y * (JN / 32) + (threadIdx.x >> 5);
+  const int64_t unit = blockIdx.x;
+  const int rb = (int)(unit % a.rb_max);
+  const int64_t lr = unit / a.rb_max;
+  const int r = (int)(lr % a.tab.n_req), lh = (int)(lr / a.tab.n_req);
+  const int rho = rb * RB + row, G = a.group, D = a.pool.head_dim;
+  const int2 b = a.desc[unit];
+  const Req q = load_req<KT>(a, r, false);
+  if (rho >= q.W * G || b.x == b.y) return;
+  const int n = b.y - b.x + 1, Hkv = a.pool.n_kv_heads, layer = lh / Hkv, h = lh - layer * Hkv;
+  auto slot = [&](int i) { return slot_of(i, b.x, h, Hkv); };
+  constexpr int E = DP / 32;
+  float M = NO_REF, sum = 0.f, o[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] = 0.f;
+  for (int i0 = 0; i0 < n; i0 += 32) {                                     // 32 pieces at a time, one per lane
+    const float2 ml = i0 + lane < n ? a.part_ml[slot(i0 + lane) * RB + row] : make_float2(NO_REF, 0.f);
+    float top = ml.x;
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+    top = fmaxf(top, M);
+    const float f = exp2f(M - top), w = exp2f(ml.x - top);
+    M = top;
+    float s = ml.y * w;
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+    sum = fmaf(sum, f, s);
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] *= f;
+    const int m = min(32, n - i0);
+#pragma unroll 8
+    for (int i = 0; i < m; ++i) {
+      const float wi = __shfl_sync(0xffffffffu, w, i);
+      const float* src = a.part + (slot(i0 + i) * RB + row) * DP + lane;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] = fmaf(src[e * 32], wi, o[e]);
+    }
+  }
+  const int w = rho / G;
+  const int64_t at = ((int64_t)layer * a.sum_win + q.win0 + w) * a.n_q_heads + h * G + (rho - w * G);
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    if (e * 32 + lane < D) a.out[at * D + e * 32 + lane] = __float2bfloat16_rn(o[e] * inv);
+  if (lane == 0 && a.lse != nullptr) a.lse[at] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
+}
+
 // The tensor-core kernel takes what has more rows than one instruction of the warp-level one holds.
 // Its loads are boxes of a page's rows: pages of 16 to 128 tokens.
 inline bool use_tc(int D, int P, int64_t rows) {
@@ -499,7 +552,9 @@ inline WsLayout ws_layout(int Hkv, int D, int P, int64_t n_req, int64_t nls, int
 template <int DP>
 int launch_join(const Args& a, int64_t pieces, int64_t units, int RB, cudaStream_t s) {
   if (pieces == 1) return ACTKV_OK;
-  launch_pdl(attend_join_kernel<DP>, dim3((unsigned)units, RB), JN, 0, s, a, (int32_t)RB);
+  // (64 rows, 128 units of two pieces: a CTA per row 120 us, a warp per row 6)
+  if (units * RB <= SMS * (2048 / JN)) launch_pdl(attend_join_kernel<DP>, dim3((unsigned)units, RB), JN, 0, s, a, (int32_t)RB);
+  else launch_pdl(attend_join_rows_kernel<DP>, dim3((unsigned)units, (RB + JN / 32 - 1) / (JN / 32)), JN, 0, s, a, (int32_t)RB);
   ACTKV_CHECK_LAUNCH();
   return ACTKV_OK;
 }

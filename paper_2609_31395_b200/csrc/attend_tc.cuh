@@ -5,15 +5,16 @@
 // in the warps that feed the matrix pipe: 32 rows took 1.8 times, 64 rows 3.0 times what 8 rows take (16 requests of 16000 tokens, 4 heads of
 // 128 dims: 89 us with 8 rows; 32: 153, 64: 248).  Here a tile of 128 keys is one operand:
 //   S[key, row] = K Q^T       M = 128 keys, N = NR rows, both operands K-major in shared memory, S in tensor memory;
-//   P = exp2(S - reference)   one warpgroup, a thread per key; bf16 summands (p truncated, and the rest) of all rows into shared memory;
+//   P = exp2(S - reference)   a thread per key; bf16 summands (p truncated, and the rest) of all rows into shared memory;
 //   O^T[dim, row] += V^T P    M = head_dim, N = 2 NR: the two summands side by side, so that V is read once; both operands lie with the
 //                             long side contiguous (V as the pool has it: [key][dim], P as its thread writes it: [key][row]).
-// Sums of P are kept per thread and row in registers and joined at the end of a stretch.  The references live in shared memory and move
-// (then O is rescaled) only when a logit exceeds one by more than 8: in the first tile, hardly ever after.
+// Two warpgroups take the tiles in turn, each with references, sums and an O of its own, joined at the end of a stretch (one warpgroup for all
+// tiles, 64 rows: 160 us at 128 dims, where its 3100 cycles a tile were the longest chain).  Sums of P are kept per thread and row in
+// registers.  The references live in shared memory and move (then O is rescaled) only when a logit exceeds one by more than 8: in
+// the first tile, hardly ever after.
 //
-// Roles of a CTA (one per SM): warps 0-3 softmax and epilogue, warp 4 issues the MMAs, warps 8-11 load.  K and V tiles are entries of one
-// ring, in the order of use: K0, K1, V0, K2, V1, ...  S and P have two buffers each, so that S of the next tile is formed while the
-// warpgroup is at this one.  All waits are bounded; one that gives up raises a flag that ends every role (ACTKV_E_TIMEOUT).
+// Roles of a CTA (one per SM): warps 0-7 softmax and epilogue, warp 8 issues the MMAs, warps 12-15 load.  K and V tiles are entries of one
+// ring, in the order of use: K0, K1, V0, K2, V1, ...  S and P have two buffers each, one for each warpgroup.  All waits are bounded; one that gives up raises a flag that ends every role (ACTKV_E_TIMEOUT).
 //
 // What bounds it: reading K and V (up to 64 rows and 128 dims).  Shared memory comes next: a tile's operands are read by the MMAs
 // once each (64 rows, 128 dims: 1150 cycles of 2850 that the tile's bytes take to arrive).
@@ -30,9 +31,9 @@ namespace tcx {
 using namespace actkv::tc;
 
 constexpr int TKEYS = 128;
-// (warps 5-7 only fill up the second warpgroup, as registers are handed round by warpgroups)
-constexpr int SOFT = 128, MMA_WARP = 4, LOAD0 = 256, THREADS = LOAD0 + 128;
-constexpr int SOFT_REGS = 232, REST_REGS = 128;                // 168 each at launch: 128 * 232 + 256 * 128 <= 384 * 168
+// (warps 9-11 only fill up the third warpgroup, as registers are handed round by warpgroups)
+constexpr int SOFT = 128, MMA_WARP = 8, LOAD_WARP = 12, THREADS = 512;
+constexpr int SOFT_REGS = 184, REST_REGS = 72;                 // 128 each at launch: 256 * 184 + 256 * 72 = 512 * 128
 constexpr int MIN_TILES_TC = 1;
 
 template <int D, int NR>
@@ -41,7 +42,7 @@ struct Tc {
   static constexpr int PBUF = TKEYS * 2 * NR * 2;              // bytes of a P buffer: [key] rows of 128 bytes; 64 rows: summands apart
   static constexpr int QBYTES = NR * D * 2;
   static constexpr int STAGES = 128 * 1024 / UNIT;             // 4 or 8
-  static constexpr int TM_COLS = 4 * NR;                       // S twice, O twice as wide
+  static constexpr int TM_COLS = 8 * NR;                       // S, two buffers; O, one per softmax warpgroup, twice as wide (6 NR in all)
   static constexpr int P_OFF = STAGES * UNIT, Q_OFF = P_OFF + 2 * PBUF, CTL_OFF = Q_OFF + QBYTES;
 };
 
@@ -52,29 +53,48 @@ struct Ctl {
   uint64_t q_full, o_full, o_empty, drained;
   uint32_t tmem;
   int abort;
-  int stop[2];
+  int stop[2][2];
   unsigned last[8];                        // parity of the last load into each entry
   int poisoned;
-  alignas(16) float ref[NR];               // (read as vectors)
-  float fac[NR], inv[NR];
+  alignas(16) float ref[2][NR];            // per softmax warpgroup (read as vectors)
+  float fac[2][NR];
+  float col[2][4][NR];                     // maxima or sums of the columns, per warp
   int pos[NR];
   int64_t at[NR];                          // output row
-  float wmax[4][NR];
   uint32_t poison[2][NR][D / 32];          // (row, dim) that met +infinity / -infinity in a tile not every row sees whole (NaN: both)
 };
 template <int D, int NR>
 constexpr size_t smem_bytes() { return Tc<D, NR>::CTL_OFF + sizeof(Ctl<D, NR>) + 1024; }       // (the ring begins on 1024 bytes)
 
-__device__ __forceinline__ void soft_sync() { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); }
-__device__ __forceinline__ bool soft_any(bool v) {
+// barriers 1 and 2: one softmax warpgroup; 3: both
+__device__ __forceinline__ void soft_sync(int wg) { asm volatile("barrier.cta.sync %0, 128;" ::"r"(1 + wg) : "memory"); }
+__device__ __forceinline__ void both_sync() { asm volatile("barrier.cta.sync 3, 256;" ::: "memory"); }
+__device__ __forceinline__ bool soft_any(int wg, bool v) {
   uint32_t r;
   asm volatile(
       "{\n\t.reg .pred p, q;\n\t"
       "setp.ne.b32 p, %1, 0;\n\t"
-      "barrier.cta.red.or.pred q, 1, 128, p;\n\t"
+      "barrier.cta.red.or.pred q, %2, 128, p;\n\t"
       "selp.u32 %0, 1, 0, q;\n\t}"
-      : "=r"(r) : "r"(v ? 1u : 0u) : "memory");
+      : "=r"(r) : "r"(v ? 1u : 0u), "r"(1 + wg) : "memory");
   return r != 0;
+}
+// Sums (or maxima) over the 32 lanes of N values each, by halves: a lane ends up with N / 32 columns, the first of which is returned.
+template <int N, bool MAX>
+__device__ __forceinline__ int across(float* v, int lane) {
+  int first = 0;
+#pragma unroll
+  for (int d = 16, n = N / 2; d >= 1; d >>= 1, n >>= 1) {
+    const bool up = lane & d;
+#pragma unroll
+    for (int k = 0; k < N / 2; ++k) {
+      if (k >= n) break;
+      const float mine = up ? v[n + k] : v[k], other = __shfl_xor_sync(0xffffffffu, up ? v[k] : v[n + k], d);
+      v[k] = MAX ? fmaxf(mine, other) : mine + other;
+    }
+    first += up ? n : 0;
+  }
+  return first;
 }
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const float* v) {
   const uint32_t* r = reinterpret_cast<const uint32_t*>(v);
@@ -120,11 +140,11 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tc_kernel(const __grid_cons
       mbar_init(smem_u32(&ctl->s_empty[i]), SOFT);
       mbar_init(smem_u32(&ctl->p_full[i]), SOFT);
       mbar_init(smem_u32(&ctl->p_empty[i]), 1);
-      ctl->stop[i] = 0;
+      ctl->stop[i][0] = ctl->stop[i][1] = 0;
     }
-    mbar_init(smem_u32(&ctl->q_full), SOFT);
+    mbar_init(smem_u32(&ctl->q_full), 2 * SOFT);
     mbar_init(smem_u32(&ctl->o_full), 1);
-    mbar_init(smem_u32(&ctl->o_empty), SOFT);
+    mbar_init(smem_u32(&ctl->o_empty), 2 * SOFT);
     mbar_init(smem_u32(&ctl->drained), 1);
     ctl->abort = 0;
     ctl->poisoned = 0;
@@ -142,12 +162,15 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tc_kernel(const __grid_cons
   Line<TKEYS, NR, MIN_TILES_TC> line(a, blockIdx.x == 0 && warp == 0);
   Seg sg;
 
-  if (warp < 4) {
+  if (warp < MMA_WARP) {
     reg_inc<SOFT_REGS>();
-    // ================================ softmax: thread = key of the tile ================================
-    uint32_t t = 0, seg = 0, ring0 = 0;                        // tiles, stretches, ring entries so far
+    // ================================ softmax: two warpgroups take the tiles in turn; thread = key of the tile ================================
+    const int wg = warp >> 2, kt = tid & 127;
+    uint32_t t0 = 0, seg = 0, ring0 = 0;                       // tiles, stretches, ring entries before this stretch
     bool dead = false;
-    const uint32_t lane_off = (uint32_t)(warp * 32) << 16;
+    const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16, to = tm_o + wg * 2 * NR + lane_off;
+    float* ref = ctl->ref[wg];
+    float* fac = ctl->fac[wg];
     while (line.next(sg)) {
       const Req& q = sg.q;
       const int L = q.L, rows = q.W * G, row0 = sg.rb * NR, n_rows = min(NR, rows - row0);
@@ -155,36 +178,40 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tc_kernel(const __grid_cons
       const int all_hi = pos0 + step * (row0 / G);
       const int all_lo = a.win_left > 0 ? pos0 + step * ((row0 + n_rows - 1) / G) - a.win_left + 1 : 0;
       const int64_t qrow = (int64_t)sg.layer * a.sum_win + q.win0;
-      // Q of the stretch (every S of the one before is complete: the last one has been waited for)
+      // Q of the stretch (every product of the one before is complete: o_full has been waited for)
 #pragma unroll
-      for (int i = tid; i < NR * (D / 8); i += SOFT) {
+      for (int i = tid; i < NR * (D / 8); i += 2 * SOFT) {
         const int row = i / (D / 8), c = i % (D / 8), rho = row0 + row, w = rho / G;
         uint4 v = make_uint4(0, 0, 0, 0);
         if (row < n_rows)
           v = *reinterpret_cast<const uint4*>(a.q + ((qrow + w) * a.n_q_heads + line.h * G + (rho - w * G)) * D + c * 8);
         *reinterpret_cast<uint4*>(base + T::Q_OFF + (c >> 3) * (NR * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = v;
       }
-      if (tid < NR) {
-        ctl->ref[tid] = NO_REF;
-        const int rho = row0 + min(tid, n_rows - 1), w = rho / G;
-        ctl->pos[tid] = pos0 + step * w;
-        ctl->at[tid] = (qrow + w) * a.n_q_heads + line.h * G + (rho - w * G);
+      if (kt < NR) {
+        ref[kt] = NO_REF;
+        if (wg == 0) {
+          const int rho = row0 + min(kt, n_rows - 1), w = rho / G;
+          ctl->pos[kt] = pos0 + step * w;
+          ctl->at[kt] = (qrow + w) * a.n_q_heads + line.h * G + (rho - w * G);
+        }
       }
       fence_proxy_async();
       mbar_arrive(smem_u32(&ctl->q_full));
-      soft_sync();
+      both_sync();
       float l[NR];
 #pragma unroll
       for (int n = 0; n < NR; ++n) l[n] = 0.f;
 
-      for (int i = 0; i < sg.n_tiles; ++i, ++t) {
-        const int b = t & 1;
+      const int i_first = (int)((wg - t0) & 1);
+      for (int i = i_first; i < sg.n_tiles; i += 2) {
+        const uint32_t t = t0 + i;
+        const int b = wg;                                      // (= t & 1)
         const uint32_t use = t >> 1;
         if (!mbar_wait_warp(smem_u32(&ctl->s_full[b]), use & 1, abort_flag, limit)) dead = true;
         tc_fence_after();
         const uint32_t ts = tmem + b * NR + lane_off;
-        const int key = (q.lo_tile + sg.t_in + i) * TKEYS + tid;
-        const bool masked = key - tid + TKEYS - 1 > all_hi || key - tid < all_lo;
+        const int key = (q.lo_tile + sg.t_in + i) * TKEYS + kt;
+        const bool masked = key - kt + TKEYS - 1 > all_hi || key - kt < all_lo;
         float x[NR];
         auto load = [&]() {
 #pragma unroll
@@ -204,54 +231,52 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tc_kernel(const __grid_cons
         float over = -INFINITY;
 #pragma unroll
         for (int n = 0; n < NR; n += 4) {
-          const float4 r = *reinterpret_cast<const float4*>(&ctl->ref[n]);
+          const float4 r = *reinterpret_cast<const float4*>(&ref[n]);
           x[n] -= r.x;
           x[n + 1] -= r.y;
           x[n + 2] -= r.z;
           x[n + 3] -= r.w;
           over = fmaxf(over, fmaxf(fmaxf(x[n], x[n + 1]), fmaxf(x[n + 2], x[n + 3])));
         }
-        if (dead) ctl->stop[b] = 1;
-        const bool move = soft_any(over > REF_SLACK);
-        if (*reinterpret_cast<volatile int*>(&ctl->stop[b])) goto out;     // (the same answer for all four warps)
+        if (dead) ctl->stop[wg][use & 1] = 1;
+        const bool move = soft_any(wg, over > REF_SLACK);
+        if (*reinterpret_cast<volatile int*>(&ctl->stop[wg][use & 1])) break;      // (the same answer for all four warps)
         if (move) {
           // new references: the columns' maxima over the tile
           load();
+          {
+            const int first = across<NR, true>(x, lane);
 #pragma unroll
-          for (int n = 0; n < NR; ++n) {
-            float v = x[n];
-#pragma unroll
-            for (int d = 16; d >= 1; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
-            if (lane == 0) ctl->wmax[warp][n] = v;
+            for (int n = 0; n < NR / 32; ++n) ctl->col[wg][warp & 3][first + n] = x[n];
           }
-          soft_sync();
-          if (tid < NR) {
-            const float old = ctl->ref[tid];
-            const float top = fmaxf(fmaxf(fmaxf(ctl->wmax[0][tid], ctl->wmax[1][tid]), fmaxf(ctl->wmax[2][tid], ctl->wmax[3][tid])), old);
-            ctl->ref[tid] = top;
-            ctl->fac[tid] = exp2f(old - top);
+          soft_sync(wg);
+          if (kt < NR) {
+            const float old = ref[kt];
+            const float top = fmaxf(fmaxf(fmaxf(ctl->col[wg][0][kt], ctl->col[wg][1][kt]), fmaxf(ctl->col[wg][2][kt], ctl->col[wg][3][kt])), old);
+            ref[kt] = top;
+            fac[kt] = exp2f(old - top);
           }
-          soft_sync();
+          soft_sync(wg);
 #pragma unroll
-          for (int n = 0; n < NR; ++n) l[n] *= ctl->fac[n];
-          if (i > 0) {
-            // O so far, when the product before this tile's is complete (this tile's waits for P)
-            const uint32_t before = t - 1;
-            if (!mbar_wait_warp(smem_u32(&ctl->p_empty[before & 1]), (before >> 1) & 1, abort_flag, limit)) dead = true;
+          for (int n = 0; n < NR; ++n) l[n] *= fac[n];
+          if (i >= 2) {
+            // O so far, when the product of this warpgroup's last tile is complete (this tile's waits for P)
+            if (!mbar_wait_warp(smem_u32(&ctl->p_empty[b]), (use & 1) ^ 1, abort_flag, limit)) dead = true;
             tc_fence_after();
 #pragma unroll 1
             for (int c = 0; c < 2 * NR; c += 32) {
               float o[32];
-              tmem_ld32(tm_o + lane_off + c, o);
+              tmem_ld32(to + c, o);
               tmem_ld_wait();
 #pragma unroll
-              for (int n = 0; n < 32; ++n) o[n] *= ctl->fac[(c + n) % NR];
-              tmem_st32(tm_o + lane_off + c, o);
+              for (int n = 0; n < 32; ++n) o[n] *= fac[(c + n) % NR];
+              tmem_st32(to + c, o);
             }
             tmem_st_wait();
           }
+          load();
 #pragma unroll
-          for (int n = 0; n < NR; ++n) x[n] -= ctl->ref[n];
+          for (int n = 0; n < NR; ++n) x[n] -= ref[n];
         }
         tc_fence_before();
         mbar_arrive(smem_u32(&ctl->s_empty[b]));
@@ -267,7 +292,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tc_kernel(const __grid_cons
           // (unguarded by the others: a wait of this thread alone; the entry stays until this tile's product)
           if (!mbar_wait(smem_u32(&ctl->full[sl]), (e / T::STAGES) & 1, abort_flag, limit)) dead = true;
           for (int c = 0; c < D / 8; ++c) {
-            uint8_t* at = base + sl * T::UNIT + (c >> 3) * 16384 + tid * 128 + (((c & 7) ^ (tid & 7)) << 4);
+            uint8_t* at = base + sl * T::UNIT + (c >> 3) * 16384 + kt * 128 + (((c & 7) ^ (kt & 7)) << 4);
             const uint4 v = *reinterpret_cast<const uint4*>(at);
             bool odd = false;
             for (uint32_t u : {v.x, v.y, v.z, v.w}) odd |= (u & 0x7f80u) == 0x7f80u || (u & 0x7f800000u) == 0x7f800000u;
@@ -290,7 +315,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tc_kernel(const __grid_cons
           }
         }
         if (!mbar_wait_warp(smem_u32(&ctl->p_empty[b]), (use & 1) ^ 1, abort_flag, limit)) dead = true;
-        uint8_t* pr = base + T::P_OFF + b * T::PBUF + tid * 128;
+        uint8_t* pr = base + T::P_OFF + b * T::PBUF + kt * 128;
 #pragma unroll
         for (int c = 0; c < NR / 8; ++c) {
           uint32_t hi[4], lo[4];
@@ -303,79 +328,102 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tc_kernel(const __grid_cons
             asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(lo[k]) : "f"(r1), "f"(r0));
           }
           // rows of 128 bytes: 64 rows: one summand each, 16 KB apart; 32 rows: both
-          uint8_t* ph = pr + ((c ^ (tid & 7)) << 4);
-          uint8_t* pl = NR == 64 ? ph + 16384 : pr + (((c + 4) ^ (tid & 7)) << 4);
+          uint8_t* ph = pr + ((c ^ (kt & 7)) << 4);
+          uint8_t* pl = NR == 64 ? ph + 16384 : pr + (((c + 4) ^ (kt & 7)) << 4);
           *reinterpret_cast<uint4*>(ph) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
           *reinterpret_cast<uint4*>(pl) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
         }
         fence_proxy_async();
         mbar_arrive(smem_u32(&ctl->p_full[b]));
       }
-      ring0 += 2 * (uint32_t)sg.n_tiles;
-
-      // ---- the stretch's rows ----
+      // ---- the stretch's rows: the two warpgroups' shares together, each puts out half of the rows ----
+      {
+        const int first = across<NR, false>(l, lane);
 #pragma unroll
-      for (int n = 0; n < NR; ++n) {
-        float v = l[n];
-#pragma unroll
-        for (int d = 16; d >= 1; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
-        if (lane == 0) ctl->wmax[warp][n] = v;
+        for (int n = 0; n < NR / 32; ++n) ctl->col[wg][warp & 3][first + n] = l[n];
       }
       if (!mbar_wait_warp(smem_u32(&ctl->o_full), seg & 1, abort_flag, limit)) dead = true;
       tc_fence_after();
-      soft_sync();
+      both_sync();
       const bool whole = sg.b0 == sg.b1;
       const int64_t slot = line.slot(sg);
+      const bool mine_too = i_first < sg.n_tiles;              // (a stretch of one tile: one warpgroup has none)
+      const bool theirs_too = (i_first ^ 1) < sg.n_tiles;
       if (sg.t_in == 0 && tid == 0) a.desc[line.unit(sg)] = make_int2(sg.b0, sg.b1);
-      if (tid < NR) {
-        const float sum = ctl->wmax[0][tid] + ctl->wmax[1][tid] + ctl->wmax[2][tid] + ctl->wmax[3][tid], M = ctl->ref[tid];
-        ctl->inv[tid] = !whole ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
-        if (tid < n_rows) {
-          if (!whole) a.part_ml[slot * NR + tid] = make_float2(M, sum);
-          else if (a.lse != nullptr)
-            a.lse[ctl->at[tid]] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
+      if (kt < NR) {
+        float M[2], sum[2];
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          M[g] = ctl->ref[g][kt];
+          sum[g] = ctl->col[g][0][kt] + ctl->col[g][1][kt] + ctl->col[g][2][kt] + ctl->col[g][3][kt];
+        }
+        const float top = fmaxf(M[0], M[1]), f0 = exp2f(M[0] - top), f1 = exp2f(M[1] - top), all = sum[0] * f0 + sum[1] * f1;
+        fac[kt] = (wg == 0 ? f0 : f1) * (!whole ? 1.f : all == 0.f ? 0.f : 1.f / all);
+        if (wg == 0 && kt < n_rows) {
+          if (!whole) a.part_ml[slot * NR + kt] = make_float2(top, all);
+          else if (a.lse != nullptr) a.lse[ctl->at[kt]] = all == 0.f ? -INFINITY : (top + log2f(all)) * kLn2;
         }
       }
-      soft_sync();
+      both_sync();
       {
         // M = 128: dim = lane of tensor memory; M = 64: 16 dims in the first 16 lanes of every warp
-        const int d = D == 128 ? tid : warp * 16 + lane;
+        const int d = D == 128 ? kt : (warp & 3) * 16 + lane;
         const bool mine = D == 128 || lane < 16;
         const bool poisoned = ctl->poisoned != 0;
-#pragma unroll 1
-        for (int c = 0; c < NR; c += 32) {
-          float o[32], o2[32];
-          tmem_ld32(tm_o + lane_off + c, o);
-          tmem_ld32(tm_o + lane_off + NR + c, o2);
+        float* swap = reinterpret_cast<float*>(base + T::P_OFF);               // [row][dim] (P is no longer needed)
+        static_assert(NR * D * 4 <= 2 * T::PBUF, "O of all rows fits where P was");
+        auto half = [&](int h, float* o) {                                     // this warpgroup's O of rows h * NR / 2 ..
+          float o2[NR / 2];
+          if constexpr (NR == 64) {
+            tmem_ld32(to + h * 32, o);
+            tmem_ld32(to + NR + h * 32, o2);
+          } else {
+            tmem_ld16(to + h * 16, o);
+            tmem_ld16(to + NR + h * 16, o2);
+          }
           tmem_ld_wait();
+#pragma unroll
+          for (int n = 0; n < NR / 2; ++n) o[n] = (o[n] + o2[n]) * fac[h * (NR / 2) + n];
+        };
+        float o[NR / 2];
+        if (mine_too) {
+          half(wg ^ 1, o);
           if (mine) {
 #pragma unroll
-            for (int n = 0; n < 32; ++n) {
-              const int row = c + n;
-              if (row >= n_rows) continue;
-              float v = (o[n] + o2[n]) * ctl->inv[row];
-              if (poisoned) {
-                const uint32_t up = ctl->poison[0][row][d >> 5] >> (d & 31) & 1u, down = ctl->poison[1][row][d >> 5] >> (d & 31) & 1u;
-                if (up) v += INFINITY;
-                if (down) v += -INFINITY;
-              }
-              if (whole) a.out[ctl->at[row] * D + d] = __float2bfloat16_rn(v);
-              else a.part[(slot * NR + row) * D + d] = v;
-            }
+            for (int n = 0; n < NR / 2; ++n) swap[((wg ^ 1) * (NR / 2) + n) * D + d] = o[n];
           }
+          half(wg, o);
         }
         tc_fence_before();
         mbar_arrive(smem_u32(&ctl->o_empty));
-        soft_sync();                                           // references and poison are rewritten
+        both_sync();
+        if (mine) {
+#pragma unroll
+          for (int n = 0; n < NR / 2; ++n) {
+            const int row = wg * (NR / 2) + n;
+            if (row >= n_rows) continue;
+            float v = (mine_too ? o[n] : 0.f) + (theirs_too ? swap[row * D + d] : 0.f);
+            if (poisoned) {
+              const uint32_t up = ctl->poison[0][row][d >> 5] >> (d & 31) & 1u, down = ctl->poison[1][row][d >> 5] >> (d & 31) & 1u;
+              if (up) v += INFINITY;
+              if (down) v += -INFINITY;
+            }
+            if (whole) a.out[ctl->at[row] * D + d] = __float2bfloat16_rn(v);
+            else a.part[(slot * NR + row) * D + d] = v;
+          }
+        }
+        both_sync();                                           // references, poison and P's place are rewritten
         if (poisoned) {
-          for (int i = tid; i < 2 * NR * (D / 32); i += SOFT) (&ctl->poison[0][0][0])[i] = 0;
+          for (int i = tid; i < 2 * NR * (D / 32); i += 2 * SOFT) (&ctl->poison[0][0][0])[i] = 0;
           if (tid == 0) ctl->poisoned = 0;
-          soft_sync();
+          both_sync();
         }
       }
+      t0 += (uint32_t)sg.n_tiles;
+      ring0 += 2 * (uint32_t)sg.n_tiles;
       ++seg;
     }
-  } else if (warp < LOAD0 / 32) {
+  } else if (warp < LOAD_WARP) {
     reg_dec<REST_REGS>();
     if (warp != MMA_WARP) goto out;
     // ================================ MMA issuer ================================
@@ -415,7 +463,8 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tc_kernel(const __grid_cons
             const uint64_t vd = smem_desc_mn(sbase + sl * T::UNIT, 16384), pd = smem_desc_mn(sbase + T::P_OFF + b * T::PBUF, 16384);
 #pragma unroll
             for (int k = 0; k < TKEYS / 16; ++k)
-              umma_bf16(tm_o, vd + (uint64_t)((k * 2048) >> 4), pd + (uint64_t)((k * 2048) >> 4), IDESC_O, (i > 1 || k > 0) ? 1u : 0u);
+              umma_bf16(tm_o + b * 2 * NR, vd + (uint64_t)((k * 2048) >> 4), pd + (uint64_t)((k * 2048) >> 4), IDESC_O,
+                        (i > 2 || k > 0) ? 1u : 0u);   // (the first two tiles begin a warpgroup's O each)
             umma_commit(smem_u32(&ctl->p_empty[b]));
             umma_commit(smem_u32(&ctl->empty[sl]));
             if (i == n) umma_commit(smem_u32(&ctl->o_full));
@@ -434,7 +483,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tc_kernel(const __grid_cons
   } else {
     reg_dec<REST_REGS>();
     // ================================ loaders: entry e of the ring is warp e % 4's ================================
-    const int w = warp - (LOAD0 >> 5), ps = a.pool.page_size, ppt = TKEYS / ps, lp_shift = 31 - __clz(ppt);
+    const int w = warp - LOAD_WARP, ps = a.pool.page_size, ppt = TKEYS / ps, lp_shift = 31 - __clz(ppt);
     constexpr int NH = D / 64;
     uint32_t ring0 = 0;
     bool ok = true;
