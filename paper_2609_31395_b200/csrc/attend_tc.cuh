@@ -13,8 +13,9 @@
 // registers.  The references live in shared memory and move (then O is rescaled) only when a logit exceeds one by more than 8: in
 // the first tile, hardly ever after.
 //
-// Roles of a CTA (one per SM): warps 0-7 softmax and epilogue, warp 8 issues the MMAs, warps 12-15 load.  K and V tiles are entries of one
-// ring, in the order of use: K0, K1, V0, K2, V1, ...  S and P have two buffers each, one for each warpgroup.  All waits are bounded; one that gives up raises a flag that ends every role (ACTKV_E_TIMEOUT).
+// Roles of a CTA (one per SM): warps 0-7 softmax and epilogue, warp 8 issues the products for S, warp 9
+// those for O, warps 12-15 load.  K and V have a ring each, S and P two buffers, one for each warpgroup; S runs ahead of the softmax by up
+// to two tiles.  All waits are bounded; one that gives up raises a flag that ends every role (ACTKV_E_TIMEOUT).
 //
 // What bounds it: reading K and V (up to 64 rows and 128 dims).  Shared memory comes next: a tile's operands are read by the MMAs
 // once each (64 rows, 128 dims: 1150 cycles of 2850 that the tile's bytes take to arrive).
@@ -31,8 +32,8 @@ namespace tcx {
 using namespace actkv::tc;
 
 constexpr int TKEYS = 128;
-// (warps 9-11 only fill up the third warpgroup, as registers are handed round by warpgroups)
-constexpr int SOFT = 128, MMA_WARP = 8, LOAD_WARP = 12, THREADS = 512;
+// (warps 10 and 11 only fill up the third warpgroup, as registers are handed round by warpgroups)
+constexpr int SOFT = 128, S_WARP = 8, O_WARP = 9, LOAD_WARP = 12, THREADS = 512;
 constexpr int SOFT_REGS = 184, REST_REGS = 72;                 // 128 each at launch: 256 * 184 + 256 * 72 = 512 * 128
 constexpr int MIN_TILES_TC = 1;
 
@@ -41,20 +42,20 @@ struct Tc {
   static constexpr int UNIT = TKEYS * D * 2;                   // bytes of a K or V tile: halves of 64 dims, rows of 128 bytes
   static constexpr int PBUF = TKEYS * 2 * NR * 2;              // bytes of a P buffer: [key] rows of 128 bytes; 64 rows: summands apart
   static constexpr int QBYTES = NR * D * 2;
-  static constexpr int STAGES = 128 * 1024 / UNIT;             // 4 or 8
+  static constexpr int STAGES = 64 * 1024 / UNIT;              // of the K ring, and of the V ring: 2 or 4
   static constexpr int TM_COLS = 8 * NR;                       // S, two buffers; O, one per softmax warpgroup, twice as wide (6 NR in all)
-  static constexpr int P_OFF = STAGES * UNIT, Q_OFF = P_OFF + 2 * PBUF, CTL_OFF = Q_OFF + QBYTES;
+  static constexpr int V_OFF = STAGES * UNIT, P_OFF = 2 * V_OFF, Q_OFF = P_OFF + 2 * PBUF, CTL_OFF = Q_OFF + QBYTES;
 };
 
 template <int D, int NR>
 struct Ctl {
-  uint64_t full[8], empty[8];              // ring
+  uint64_t full[2][4], empty[2][4];        // K ring, V ring
   uint64_t s_full[2], s_empty[2], p_full[2], p_empty[2];
   uint64_t q_full, o_full, o_empty, drained;
   uint32_t tmem;
   int abort;
   int stop[2][2];
-  unsigned last[8];                        // parity of the last load into each entry
+  unsigned last[2][4];                     // parity of the last load into each entry
   int poisoned;
   alignas(16) float ref[2][NR];            // per softmax warpgroup (read as vectors)
   float fac[2][NR];
@@ -110,10 +111,6 @@ __device__ __forceinline__ uint64_t smem_desc_mn(uint32_t addr, uint32_t lead) {
   return (uint64_t)((addr & 0x3FFFF) >> 4) | ((uint64_t)(lead >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) |
          ((uint64_t)2 << 61);
 }
-// Place in the order K0, K1, V0, K2, V1, ..., K(n-1), V(n-2), V(n-1) of a stretch of n tiles.
-__device__ __forceinline__ int place_k(int i) { return i == 0 ? 0 : 2 * i - 1; }
-__device__ __forceinline__ int place_v(int i, int n) { return i < n - 1 ? 2 * i + 2 : 2 * n - 1; }
-
 template <int D, int NR>
 __global__ void __launch_bounds__(THREADS, 1) attend_tc_kernel(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap kmap,
                                                                const __grid_constant__ CUtensorMap vmap, const int k5,
@@ -130,11 +127,12 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tc_kernel(const __grid_cons
   volatile int* abort_flag = &ctl->abort;
 
   if (tid == 0) {
-    for (int i = 0; i < T::STAGES; ++i) {
-      mbar_init(smem_u32(&ctl->full[i]), 1);
-      mbar_init(smem_u32(&ctl->empty[i]), 1);
-      ctl->last[i] = RING_UNUSED;
-    }
+    for (int kv = 0; kv < 2; ++kv)
+      for (int i = 0; i < T::STAGES; ++i) {
+        mbar_init(smem_u32(&ctl->full[kv][i]), 1);
+        mbar_init(smem_u32(&ctl->empty[kv][i]), 1);
+        ctl->last[kv][i] = RING_UNUSED;
+      }
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&ctl->s_full[i]), 1);
       mbar_init(smem_u32(&ctl->s_empty[i]), SOFT);
@@ -145,13 +143,13 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tc_kernel(const __grid_cons
     mbar_init(smem_u32(&ctl->q_full), 2 * SOFT);
     mbar_init(smem_u32(&ctl->o_full), 1);
     mbar_init(smem_u32(&ctl->o_empty), 2 * SOFT);
-    mbar_init(smem_u32(&ctl->drained), 1);
+    mbar_init(smem_u32(&ctl->drained), 2);
     ctl->abort = 0;
     ctl->poisoned = 0;
     fence_barrier_init();
   }
   for (int i = tid; i < 2 * NR * (D / 32); i += THREADS) (&ctl->poison[0][0][0])[i] = 0;
-  if (warp == MMA_WARP) {
+  if (warp == S_WARP) {
     tmem_alloc(smem_u32(&ctl->tmem), T::TM_COLS);
     tmem_relinquish();
   }
@@ -162,11 +160,11 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tc_kernel(const __grid_cons
   Line<TKEYS, NR, MIN_TILES_TC> line(a, blockIdx.x == 0 && warp == 0);
   Seg sg;
 
-  if (warp < MMA_WARP) {
+  if (warp < S_WARP) {
     reg_inc<SOFT_REGS>();
     // ================================ softmax: two warpgroups take the tiles in turn; thread = key of the tile ================================
     const int wg = warp >> 2, kt = tid & 127;
-    uint32_t t0 = 0, seg = 0, ring0 = 0;                       // tiles, stretches, ring entries before this stretch
+    uint32_t t0 = 0, seg = 0;                                  // tiles, stretches before this stretch
     bool dead = false;
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16, to = tm_o + wg * 2 * NR + lane_off;
     float* ref = ctl->ref[wg];
@@ -288,11 +286,11 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tc_kernel(const __grid_cons
         if (masked) {
           // V of a key that some row must not see, or of a slot behind the end: infinities and NaN leave the product; what they make of the
           // rows that do see the key is noted
-          const uint32_t e = ring0 + place_v(i, sg.n_tiles), sl = e % T::STAGES;
+          const uint32_t sl = t % T::STAGES;
           // (unguarded by the others: a wait of this thread alone; the entry stays until this tile's product)
-          if (!mbar_wait(smem_u32(&ctl->full[sl]), (e / T::STAGES) & 1, abort_flag, limit)) dead = true;
+          if (!mbar_wait(smem_u32(&ctl->full[1][sl]), (t / T::STAGES) & 1, abort_flag, limit)) dead = true;
           for (int c = 0; c < D / 8; ++c) {
-            uint8_t* at = base + sl * T::UNIT + (c >> 3) * 16384 + kt * 128 + (((c & 7) ^ (kt & 7)) << 4);
+            uint8_t* at = base + T::V_OFF + sl * T::UNIT + (c >> 3) * 16384 + kt * 128 + (((c & 7) ^ (kt & 7)) << 4);
             const uint4 v = *reinterpret_cast<const uint4*>(at);
             bool odd = false;
             for (uint32_t u : {v.x, v.y, v.z, v.w}) odd |= (u & 0x7f80u) == 0x7f80u || (u & 0x7f800000u) == 0x7f800000u;
@@ -420,25 +418,26 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tc_kernel(const __grid_cons
         }
       }
       t0 += (uint32_t)sg.n_tiles;
-      ring0 += 2 * (uint32_t)sg.n_tiles;
       ++seg;
     }
   } else if (warp < LOAD_WARP) {
     reg_dec<REST_REGS>();
-    if (warp != MMA_WARP) goto out;
-    // ================================ MMA issuer ================================
+    if (warp > O_WARP) goto out;
+    // ================================ MMA issuers: one for S, which runs ahead as its buffers allow, one for O ================================
     constexpr uint32_t IDESC_S = idesc_bf16(128, NR), IDESC_O = idesc_bf16(D, 2 * NR) | (1u << 15) | (1u << 16);
     const uint64_t qd = smem_desc_sw128(sbase + T::Q_OFF);
-    uint32_t t = 0, seg = 0, ring0 = 0;
+    const bool for_s = warp == S_WARP;
+    uint32_t t = 0, seg = 0;
     bool ok = true;
     while (ok && line.next(sg)) {
       const int n = sg.n_tiles;
-      ok = mbar_wait_warp(smem_u32(&ctl->q_full), seg & 1, abort_flag, limit);
-      for (int i = 0; ok && i <= n; ++i) {
-        if (i < n) {                                           // S of tile i
-          const uint32_t tt = t + i, b = tt & 1, e = ring0 + place_k(i), sl = e % T::STAGES;
-          ok = mbar_wait_warp(smem_u32(&ctl->full[sl]), (e / T::STAGES) & 1, abort_flag, limit) &&
-               mbar_wait_warp(smem_u32(&ctl->s_empty[b]), ((tt >> 1) & 1) ^ 1, abort_flag, limit);
+      if (for_s) ok = mbar_wait_warp(smem_u32(&ctl->q_full), seg & 1, abort_flag, limit);
+      else ok = mbar_wait_warp(smem_u32(&ctl->o_empty), (seg & 1) ^ 1, abort_flag, limit);
+      for (int i = 0; ok && i < n; ++i, ++t) {
+        const uint32_t b = t & 1, use = t >> 1, sl = t % T::STAGES, ph = (t / T::STAGES) & 1;
+        if (for_s) {
+          ok = mbar_wait_warp(smem_u32(&ctl->full[0][sl]), ph, abort_flag, limit) &&
+               mbar_wait_warp(smem_u32(&ctl->s_empty[b]), (use & 1) ^ 1, abort_flag, limit);
           if (!ok) break;
           tc_fence_after();
           if (elect_one()) {
@@ -448,63 +447,55 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tc_kernel(const __grid_cons
               umma_bf16(tmem + b * NR, kd + (uint64_t)(((k >> 2) * 16384 + (k & 3) * 32) >> 4),
                         qd + (uint64_t)(((k >> 2) * (NR * 128) + (k & 3) * 32) >> 4), IDESC_S, k > 0 ? 1u : 0u);
             umma_commit(smem_u32(&ctl->s_full[b]));
-            umma_commit(smem_u32(&ctl->empty[sl]));
+            umma_commit(smem_u32(&ctl->empty[0][sl]));
           }
-          __syncwarp();
-        }
-        if (i > 0) {                                           // O of tile i - 1
-          const uint32_t tt = t + i - 1, b = tt & 1, e = ring0 + place_v(i - 1, n), sl = e % T::STAGES;
-          ok = mbar_wait_warp(smem_u32(&ctl->full[sl]), (e / T::STAGES) & 1, abort_flag, limit) &&
-               mbar_wait_warp(smem_u32(&ctl->p_full[b]), (tt >> 1) & 1, abort_flag, limit);
-          if (ok && i == 1) ok = mbar_wait_warp(smem_u32(&ctl->o_empty), (seg & 1) ^ 1, abort_flag, limit);
+        } else {
+          ok = mbar_wait_warp(smem_u32(&ctl->full[1][sl]), ph, abort_flag, limit) &&
+               mbar_wait_warp(smem_u32(&ctl->p_full[b]), use & 1, abort_flag, limit);
           if (!ok) break;
           tc_fence_after();
           if (elect_one()) {
-            const uint64_t vd = smem_desc_mn(sbase + sl * T::UNIT, 16384), pd = smem_desc_mn(sbase + T::P_OFF + b * T::PBUF, 16384);
+            const uint64_t vd = smem_desc_mn(sbase + T::V_OFF + sl * T::UNIT, 16384), pd = smem_desc_mn(sbase + T::P_OFF + b * T::PBUF, 16384);
 #pragma unroll
             for (int k = 0; k < TKEYS / 16; ++k)
               umma_bf16(tm_o + b * 2 * NR, vd + (uint64_t)((k * 2048) >> 4), pd + (uint64_t)((k * 2048) >> 4), IDESC_O,
-                        (i > 2 || k > 0) ? 1u : 0u);   // (the first two tiles begin a warpgroup's O each)
+                        (i > 1 || k > 0) ? 1u : 0u);           // (the first two tiles begin a warpgroup's O each)
             umma_commit(smem_u32(&ctl->p_empty[b]));
-            umma_commit(smem_u32(&ctl->empty[sl]));
-            if (i == n) umma_commit(smem_u32(&ctl->o_full));
+            umma_commit(smem_u32(&ctl->empty[1][sl]));
+            if (i == n - 1) umma_commit(smem_u32(&ctl->o_full));
           }
-          __syncwarp();
         }
+        __syncwarp();
       }
-      t += n;
-      ring0 += 2 * (uint32_t)n;
       ++seg;
     }
     // everything issued has retired before tensor memory is freed
     if (elect_one()) umma_commit(smem_u32(&ctl->drained));
     __syncwarp();
-    mbar_wait_warp(smem_u32(&ctl->drained), 0, nullptr, DRAIN_LIMIT_CYCLES);
+    if (for_s) mbar_wait_warp(smem_u32(&ctl->drained), 0, nullptr, DRAIN_LIMIT_CYCLES);
   } else {
     reg_dec<REST_REGS>();
-    // ================================ loaders: entry e of the ring is warp e % 4's ================================
-    const int w = warp - LOAD_WARP, ps = a.pool.page_size, ppt = TKEYS / ps, lp_shift = 31 - __clz(ppt);
+    // ================================ loaders: two warps for K, two for V, on tiles in turn ================================
+    const int kv = (warp - LOAD_WARP) >> 1, ps = a.pool.page_size, ppt = TKEYS / ps, lp_shift = 31 - __clz(ppt);
     constexpr int NH = D / 64;
-    uint32_t ring0 = 0;
+    const CUtensorMap* map = kv ? &vmap : &kmap;
+    uint32_t t0 = 0;
     bool ok = true;
     while (ok && line.next(sg)) {
       const int L = sg.q.L, n = sg.n_tiles, n_lp = (L + ps - 1) / ps;
-      for (int at = (int)((w - ring0) & 3); at < 2 * n; at += 4) {
-        // the inverse of place_k and place_v
-        const bool is_v = at == 2 * n - 1 || (at > 0 && (at & 1) == 0);
-        const int i = at == 0 ? 0 : at == 2 * n - 1 ? n - 1 : is_v ? at / 2 - 1 : (at + 1) / 2;
-        const uint32_t e = ring0 + at, sl = e % T::STAGES, ph = (e / T::STAGES) & 1;
+      for (int i = (int)((warp - t0) & 1); i < n; i += 2) {
+        const uint32_t t = t0 + i, sl = t % T::STAGES, ph = (t / T::STAGES) & 1;
         // lane j < ppt NH: page j % ppt, half j / ppt.  Pages past the end: the last one again (their keys are masked)
         int pid = 0;
         if (lane < ppt && n_lp > 0)
           pid = checked_page(a.tab, a.pool.n_pages, sg.r, min((sg.q.lo_tile + sg.t_in + i) * ppt + lane, n_lp - 1), a.status);
         int got = 1;
         if (lane == 0) {
-          got = mbar_wait(smem_u32(&ctl->empty[sl]), ph ^ 1, abort_flag, limit) ? 1 : 0;
+          got = mbar_wait(smem_u32(&ctl->empty[kv][sl]), ph ^ 1, abort_flag, limit) ? 1 : 0;
           if (got) {
-            ctl->last[sl] = ph;
-            if (n_lp > 0) mbar_expect_tx(smem_u32(&ctl->full[sl]), T::UNIT);
-            else mbar_arrive(smem_u32(&ctl->full[sl]));        // an empty request: every key is masked
+            ctl->last[kv][sl] = ph;
+            if (n_lp > 0) mbar_expect_tx(smem_u32(&ctl->full[kv][sl]), T::UNIT);
+            else mbar_arrive(smem_u32(&ctl->full[kv][sl]));    // an empty request: every key is masked
           }
         }
         ok = __shfl_sync(0xffffffffu, got, 0) != 0;
@@ -512,13 +503,13 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tc_kernel(const __grid_cons
         pid = __shfl_sync(0xffffffffu, pid, lane & (ppt - 1));
         if (lane < ppt * NH && n_lp > 0) {
           const int half = lane >> lp_shift;
-          const uint32_t dst = sbase + sl * T::UNIT + half * 16384 + (lane & (ppt - 1)) * ps * 128, bar = smem_u32(&ctl->full[sl]);
-          const CUtensorMap* map = is_v ? &vmap : &kmap;
+          const uint32_t dst = sbase + kv * T::V_OFF + sl * T::UNIT + half * 16384 + (lane & (ppt - 1)) * ps * 128;
+          const uint32_t bar = smem_u32(&ctl->full[kv][sl]);
           if (k5) tma_load_5d(dst, map, bar, half * 64, 0, line.h, pid, a.layer_begin + sg.layer);
           else tma_load_4d(dst, map, bar, half * 64, line.h, pid * ps, a.layer_begin + sg.layer);
         }
       }
-      ring0 += 2 * (uint32_t)n;
+      t0 += (uint32_t)n;
     }
   }
 out:
@@ -528,9 +519,10 @@ out:
   if (*abort_flag && tid == 0) {
     report(a.status, ACTKV_E_TIMEOUT, (int)blockIdx.x, line.h);
     // loads still in flight land in this CTA's shared memory: waited for, with a limit
-    for (int i = 0; i < T::STAGES; ++i) mbar_wait(smem_u32(&ctl->full[i]), ctl->last[i], nullptr, DRAIN_LIMIT_CYCLES / 64);
+    for (int i = 0; i < 2 * T::STAGES; ++i)
+      mbar_wait(smem_u32(&ctl->full[i & 1][i >> 1]), ctl->last[i & 1][i >> 1], nullptr, DRAIN_LIMIT_CYCLES / 64);
   }
-  if (warp == MMA_WARP) tmem_dealloc(tmem, T::TM_COLS);
+  if (warp == S_WARP) tmem_dealloc(tmem, T::TM_COLS);
 }
 
 template <int D, int NR>
