@@ -566,7 +566,7 @@ int actkv_compact_noalloc(const actkv_pool_t* pool /* host */, const actkv_table
 
 /* ---------------------------------------------------------------------------------------
  * actkv_debug_inject_stall — fault-injection hook for the bounded waits of the tensor-core score
- * kernels (the paper has no counterpart).  Every wait inside those kernels (on a shared-memory
+ * kernels and of actkv_attend's (the paper has no counterpart).  Every wait inside those kernels (on a shared-memory
  * barrier) has a limit, after which the kernel writes ACTKV_E_TIMEOUT to status, all its roles
  * leave, outstanding tensor-core work is drained, tensor memory is freed and the kernel returns;
  * later stages of the step see the status and do nothing.  This hook makes that happen without a

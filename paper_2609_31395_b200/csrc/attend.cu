@@ -572,10 +572,13 @@ int launch(const Args& a, int64_t tiles_bound, int64_t units, cudaStream_t s) {
   return launch_join<DP>(a, pieces, units, C::RB, s);
 }
 template <int D>
-int launch_wide(const Args& a, const actkv_pool_t* pool, int64_t max_tok, int64_t units, int RB, cudaStream_t s) {
+int launch_wide(const Args& a, const actkv_pool_t* pool, int64_t max_tok, int64_t tiles_bound, int64_t units, int RB, cudaStream_t s) {
+  CUtensorMap kmap, vmap;
+  if (!tcx::make_maps(pool, &kmap, &vmap))
+    return RB == 32 ? launch<D, 4, 1>(a, tiles_bound, units, s) : launch<D, 4, 2>(a, tiles_bound, units, s);
   const int64_t bound = units * std::max<int64_t>(1, (max_tok + tcx::TKEYS - 1) / tcx::TKEYS);
   const int64_t pieces = pieces_of(bound, a.pool.n_kv_heads, 1, tcx::MIN_TILES_TC);
-  const int rc = RB == 32 ? tcx::launch_tc<D, 32>(a, pool, pieces, s) : tcx::launch_tc<D, 64>(a, pool, pieces, s);
+  const int rc = RB == 32 ? tcx::launch_tc<D, 32>(a, pool, kmap, vmap, pieces, s) : tcx::launch_tc<D, 64>(a, pool, kmap, vmap, pieces, s);
   return rc != ACTKV_OK ? rc : launch_join<D>(a, pieces, units, RB, s);
 }
 
@@ -643,7 +646,7 @@ int actkv_attend(const actkv_pool_t* pool, const actkv_tables_t* tables, int32_t
   const int64_t bound = lay.units * std::max<int64_t>(1, ((int64_t)max_tok + KT - 1) / KT);
   cudaStream_t s = (cudaStream_t)stream;
   if (use_tc(D, pool->page_size, (int64_t)max_win * G))
-    return D == 64 ? launch_wide<64>(a, pool, max_tok, lay.units, lay.RB, s) : launch_wide<128>(a, pool, max_tok, lay.units, lay.RB, s);
+    return D == 64 ? launch_wide<64>(a, pool, max_tok, bound, lay.units, lay.RB, s) : launch_wide<128>(a, pool, max_tok, bound, lay.units, lay.RB, s);
   if (lay.DP == 256) {
     switch (lay.RB) {
       case 8: return launch<256, 1, 1>(a, bound, lay.units, s);

@@ -24,6 +24,7 @@
 #include "attend_line.cuh"
 #include "pool_map.cuh"
 #include "ring.cuh"
+#include "stall_hook.cuh"
 
 namespace actkv {
 namespace at {
@@ -114,7 +115,7 @@ __device__ __forceinline__ uint64_t smem_desc_mn(uint32_t addr, uint32_t lead) {
 template <int D, int NR>
 __global__ void __launch_bounds__(THREADS, 1) attend_tc_kernel(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap kmap,
                                                                const __grid_constant__ CUtensorMap vmap, const int k5,
-                                                               const long long limit) {
+                                                               const long long limit, const int stall) {
   using T = Tc<D, NR>;
   using CT = Ctl<D, NR>;
   pdl_begin();
@@ -485,6 +486,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tc_kernel(const __grid_cons
       const int L = sg.q.L, n = sg.n_tiles, n_lp = (L + ps - 1) / ps;
       for (int i = (int)((warp - t0) & 1); i < n; i += 2) {
         const uint32_t t = t0 + i, sl = t % T::STAGES, ph = (t / T::STAGES) & 1;
+        if (stall >= 0 && i >= stall) { ok = false; break; }   // injected fault: this and all later tiles never arrive
         // lane j < ppt NH: page j % ppt, half j / ppt.  Pages past the end: the last one again (their keys are masked)
         int pid = 0;
         if (lane < ppt && n_lp > 0)
@@ -525,13 +527,15 @@ out:
   if (warp == S_WARP) tmem_dealloc(tmem, T::TM_COLS);
 }
 
+// False when the pool has no tensor map (the caller then takes the warp-level kernel).
+inline bool make_maps(const actkv_pool_t* pool, CUtensorMap* kmap, CUtensorMap* vmap) {
+  return make_kvmap(pool, 0, kmap) && make_kvmap(pool, 1, vmap);
+}
 template <int D, int NR>
-int launch_tc(const Args& a, const actkv_pool_t* pool, int64_t pieces, cudaStream_t s) {
-  CUtensorMap kmap, vmap;
-  if (!make_kvmap(pool, 0, &kmap) || !make_kvmap(pool, 1, &vmap)) return ACTKV_E_CUDA;
+int launch_tc(const Args& a, const actkv_pool_t* pool, const CUtensorMap& kmap, const CUtensorMap& vmap, int64_t pieces, cudaStream_t s) {
   if (ensure_dyn_smem(attend_tc_kernel<D, NR>, smem_bytes<D, NR>()) != cudaSuccess) return ACTKV_E_CUDA;
   launch_pdl(attend_tc_kernel<D, NR>, (unsigned)(pieces * a.pool.n_kv_heads), THREADS, smem_bytes<D, NR>(), s, a, kmap, vmap,
-             pool_needs_5d(pool) ? 1 : 0, WAIT_LIMIT_CYCLES);
+             pool_needs_5d(pool) ? 1 : 0, stall_hook().wait_cycles.load(), (int)stall_hook().stall_tile.load());
   ACTKV_CHECK_LAUNCH();
   return ACTKV_OK;
 }

@@ -8,7 +8,7 @@
 //                branch of that source.  Bound by reading and writing every byte once.
 #include <cooperative_groups.h>
 
-#include "common.cuh"
+#include "tc_ptx.cuh"
 
 namespace actkv {
 namespace pg {
@@ -213,93 +213,167 @@ struct CopyArgs {
   int32_t* status;
 };
 
-// grid: (logical page, pair, layer * 2 + kv).  The first sound pair of a source works for all pairs of that source; CP_NT pairs
-// are looked at together, one per thread, in two round trips to memory.
-template <bool VEC>
-__global__ void __launch_bounds__(CP_NT) copy_kernel(const CopyArgs a) {
-  pdl_begin();
-  __shared__ int64_t s_dst[CP_NT];
-  __shared__ int s_slots[CP_NT];
-  __shared__ int s_n;
-  const int tid = threadIdx.x, lp = blockIdx.x, i = blockIdx.y, layer = blockIdx.z >> 1, kv = blockIdx.z & 1;
-  const int P = a.pool.page_size, H = a.pool.n_kv_heads, D = a.pool.head_dim, R = a.tab.n_req;
-  const bool first = blockIdx.x == 0 && blockIdx.z == 0;                   // one CTA of every pair reports what is wrong with it
-  const int src = a.src[i];
-  if ((uint32_t)src >= (uint32_t)R) {
-    if (first && tid == 0) report(a.status, ACTKV_E_INVALID, i, src);
-    return;
+// What the CTAs of a copy find out first.  The first sound pair of a source works for all pairs of that source; NT pairs are looked at
+// together, one per thread, in two round trips to memory.
+template <int NT>
+struct CopySmem {
+  int64_t dst[NT];               // branches that have tokens on this page: element offset of their page,
+  int slots[NT];                 // tokens on it
+  int n;
+};
+struct CopySource {
+  int src, len, page, col;
+};
+// The source of pair i, for logical page lp; false: nothing to do.  `first`: one CTA of every pair, which reports what is wrong with it.
+template <int NT>
+__device__ __forceinline__ bool copy_source(const CopyArgs& a, int i, int lp, bool first, CopySource& s) {
+  const int tid = threadIdx.x;
+  s.src = a.src[i];
+  if ((uint32_t)s.src >= (uint32_t)a.tab.n_req) {
+    if (first && tid == 0) report(a.status, ACTKV_E_INVALID, i, s.src);
+    return false;
   }
   if (first) {
     const int d = a.dst[i];
-    for (int j = tid; j < a.n_copy; j += CP_NT)
+    for (int j = tid; j < a.n_copy; j += NT)
       if (j != i && (a.dst[j] == d || a.src[j] == d)) report(a.status, ACTKV_E_INVALID, i, d);
   }
-  const int32_t* src_row = a.tab.page_table + (int64_t)src * a.tab.max_pages;
-  const int col = lp < a.tab.max_pages ? lp : a.tab.max_pages - 1;         // (max_len may be beyond the table; no sound pair is)
-  const int src_page = a.tab.max_pages > 0 ? src_row[col] : -1, src_len = a.tab.seq_len[src];
-  __nv_bfloat16* base = const_cast<__nv_bfloat16*>(a.pool.base) + (int64_t)(a.layer_begin + layer) * a.pool.stride_layer +
-                        (kv ? a.pool.stride_kv : 0);
-  for (int j0 = 0; j0 < a.n_copy; j0 += CP_NT) {
-    // ---- the branches among pairs j0 .. j0 + CP_NT - 1 that have tokens on this page ----
-    if (tid == 0) s_n = 0;
-    __syncthreads();
-    const int j = j0 + tid;
-    bool sound = false;
-    if (j < a.n_copy && (j == i || a.src[j] == src)) {
-      const int d = a.dst[j], n = a.length[j];
-      if ((uint32_t)d < (uint32_t)R && d != src && n >= 0 && n <= a.max_len) {
-        const int dst_len = a.tab.seq_len[d], page = a.tab.max_pages > 0 ? a.tab.page_table[(int64_t)d * a.tab.max_pages + col] : -1;
-        sound = n <= src_len && n <= dst_len && (n == 0 || (n - 1) / P < a.tab.max_pages);
-        const int slots = min(P, n - lp * P);
-        if (sound && j >= i && slots > 0) {
-          const bool src_ok = (uint32_t)src_page < (uint32_t)a.pool.n_pages, dst_ok = (uint32_t)page < (uint32_t)a.pool.n_pages;
-          if (src_ok && dst_ok) {
-            const int at = atomicAdd(&s_n, 1);
-            s_dst[at] = (int64_t)page * a.pool.stride_page;
-            s_slots[at] = slots;
-          } else {
-            report(a.status, ACTKV_E_BADPAGE, src_ok ? d : src, src_ok ? page : src_page);
-          }
+  s.col = lp < a.tab.max_pages ? lp : a.tab.max_pages - 1;                 // (max_len may be beyond the table; no sound pair is)
+  s.page = a.tab.max_pages > 0 ? a.tab.page_table[(int64_t)s.src * a.tab.max_pages + s.col] : -1;
+  s.len = a.tab.seq_len[s.src];
+  return true;
+}
+// Branches among pairs j0 .. j0 + NT - 1 into sm: 1, none of them this CTA's business: 0, another CTA works for this source: -1.
+template <int NT>
+__device__ __forceinline__ int copy_branches(const CopyArgs& a, int i, int j0, int lp, bool first, const CopySource& s, CopySmem<NT>* sm) {
+  const int tid = threadIdx.x, P = a.pool.page_size;
+  __syncthreads();
+  if (tid == 0) sm->n = 0;
+  __syncthreads();
+  const int j = j0 + tid;
+  bool sound = false;
+  if (j < a.n_copy && (j == i || a.src[j] == s.src)) {
+    const int d = a.dst[j], n = a.length[j];
+    if ((uint32_t)d < (uint32_t)a.tab.n_req && d != s.src && n >= 0 && n <= a.max_len) {
+      const int dst_len = a.tab.seq_len[d], page = a.tab.max_pages > 0 ? a.tab.page_table[(int64_t)d * a.tab.max_pages + s.col] : -1;
+      sound = n <= s.len && n <= dst_len && (n == 0 || (n - 1) / P < a.tab.max_pages);
+      const int slots = min(P, n - lp * P);
+      if (sound && j >= i && slots > 0) {
+        const bool src_ok = (uint32_t)s.page < (uint32_t)a.pool.n_pages, dst_ok = (uint32_t)page < (uint32_t)a.pool.n_pages;
+        if (src_ok && dst_ok) {
+          const int at = atomicAdd(&sm->n, 1);
+          sm->dst[at] = (int64_t)page * a.pool.stride_page;
+          sm->slots[at] = slots;
+        } else {
+          report(a.status, ACTKV_E_BADPAGE, src_ok ? d : s.src, src_ok ? page : s.page);
         }
       }
-      if (j == i && !sound && first) report(a.status, ACTKV_E_INVALID, i, n);
     }
-    // (an unsound pair copies nothing itself; when it comes first, the next sound one works for the rest)
-    if (__syncthreads_or((sound && j < i) || (j == i && !sound))) return;
-    if (j0 + CP_NT <= i) continue;
-    const int n = s_n;
+    if (j == i && !sound && first) report(a.status, ACTKV_E_INVALID, i, n);
+  }
+  // (an unsound pair copies nothing itself; when it comes first, the next sound one works for the rest)
+  if (__syncthreads_or((sound && j < i) || (j == i && !sound))) return -1;
+  return j0 + NT > i && sm->n > 0 ? 1 : 0;
+}
+__device__ __forceinline__ __nv_bfloat16* copy_base(const CopyArgs& a) {
+  return const_cast<__nv_bfloat16*>(a.pool.base) + (int64_t)(a.layer_begin + (blockIdx.z >> 1)) * a.pool.stride_layer +
+         ((blockIdx.z & 1) ? a.pool.stride_kv : 0);
+}
+
+// Pages whose tokens' rows are one run of bytes: through shared memory by bulk copies, up to CB_BYTES of a page per CTA.
+// grid: (logical page * parts + part, pair, layer * 2 + kv).
+constexpr int CB_NT = 32, CB_BYTES = 16384;
+__global__ void __launch_bounds__(CB_NT) copy_bulk_kernel(const __grid_constant__ CopyArgs a, const int parts) {
+  pdl_begin();
+  __shared__ __align__(128) uint8_t buf[CB_BYTES];
+  __shared__ CopySmem<CB_NT> sm;
+  __shared__ uint64_t bar;
+  const int lp = blockIdx.x / parts, part = blockIdx.x - lp * parts, i = blockIdx.y;
+  const bool first = blockIdx.x == 0 && blockIdx.z == 0;
+  if (threadIdx.x == 0) {
+    tc::mbar_init(tc::smem_u32(&bar), 1);
+    tc::fence_barrier_init();
+  }
+  CopySource s;
+  if (!copy_source<CB_NT>(a, i, lp, first, s)) return;
+  const int slot_bytes = a.pool.n_kv_heads * a.pool.head_dim * 2, begin = part * CB_BYTES;
+  __nv_bfloat16* base = copy_base(a);
+  const int held = min(CB_BYTES, min(a.pool.page_size, s.len - lp * a.pool.page_size) * slot_bytes - begin);    // bytes of the source
+  bool here = false, lost = false;
+  for (int j0 = 0; j0 < a.n_copy; j0 += CB_NT) {
+    const int what = copy_branches<CB_NT>(a, i, j0, lp, first, s, &sm);
+    if (what < 0) break;
+    if (what == 0 || threadIdx.x != 0 || held <= 0 || lost) continue;
+    if (!here) {                                               // once: all of the part that the source has
+      const uint32_t b = tc::smem_u32(&bar);
+      tc::mbar_expect_tx(b, (uint32_t)held);
+      asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(tc::smem_u32(buf)),
+                   "l"((const uint8_t*)(base + (int64_t)s.page * a.pool.stride_page) + begin), "r"(held), "r"(b) : "memory");
+      here = tc::mbar_wait(b, 0, nullptr, tc::WAIT_LIMIT_CYCLES);
+      if (!here) {
+        lost = true;
+        report(a.status, ACTKV_E_TIMEOUT, i, lp);
+        tc::mbar_wait(b, 0, nullptr, tc::DRAIN_LIMIT_CYCLES);
+        continue;
+      }
+    }
+    for (int k = 0; k < sm.n; ++k) {
+      const int bytes = min(CB_BYTES, sm.slots[k] * slot_bytes - begin);
+      if (bytes > 0)
+        asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"((uint8_t*)(base + sm.dst[k]) + begin),
+                     "r"(tc::smem_u32(buf)), "r"(bytes) : "memory");
+    }
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+  }
+  if (threadIdx.x == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+}
+
+// Any layout.  grid: (logical page, pair, layer * 2 + kv).
+template <bool VEC>
+__global__ void __launch_bounds__(CP_NT) copy_kernel(const __grid_constant__ CopyArgs a) {
+  pdl_begin();
+  __shared__ CopySmem<CP_NT> sm;
+  const int tid = threadIdx.x, lp = blockIdx.x, i = blockIdx.y;
+  const int H = a.pool.n_kv_heads, D = a.pool.head_dim;
+  const bool first = blockIdx.x == 0 && blockIdx.z == 0;
+  CopySource s;
+  if (!copy_source<CP_NT>(a, i, lp, first, s)) return;
+  __nv_bfloat16* base = copy_base(a);
+  for (int j0 = 0; j0 < a.n_copy; j0 += CP_NT) {
+    const int what = copy_branches<CP_NT>(a, i, j0, lp, first, s, &sm);
+    if (what < 0) return;
+    if (what == 0) continue;
+    const int n = sm.n;
     int most = 0;
-    for (int b = 0; b < n; ++b) most = max(most, s_slots[b]);
-    const __nv_bfloat16* from = base + (int64_t)src_page * a.pool.stride_page;
+    for (int b = 0; b < n; ++b) most = max(most, sm.slots[b]);
+    const __nv_bfloat16* from = base + (int64_t)s.page * a.pool.stride_page;
     constexpr int E = VEC ? 8 : 1, U = VEC ? 4 : 1;
     const int per_row = D / E, per_slot = H * per_row, items = most * per_slot;
     for (int it0 = tid; it0 < items; it0 += CP_NT * U) {
       uint4 v[U];
       __nv_bfloat16 w[U];
       int64_t off[U];
-      int slot[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int it = it0 + u * CP_NT;
-        slot[u] = it < items ? it / per_slot : P;
-        const int rem = it - slot[u] * per_slot, h = rem / per_row;
-        off[u] = (int64_t)slot[u] * a.pool.stride_slot + (int64_t)h * a.pool.stride_head + (rem - h * per_row) * E;
+        const int slot = it / per_slot, rem = it - slot * per_slot, h = rem / per_row;
+        off[u] = (int64_t)slot * a.pool.stride_slot + (int64_t)h * a.pool.stride_head + (rem - h * per_row) * E;
         if (it < items) {
           if (VEC) v[u] = *reinterpret_cast<const uint4*>(from + off[u]);
           else w[u] = from[off[u]];
         }
       }
       for (int b = 0; b < n; ++b) {
-        __nv_bfloat16* to = base + s_dst[b];
+        __nv_bfloat16* to = base + sm.dst[b];
+        const int end = sm.slots[b] * per_slot;
 #pragma unroll
         for (int u = 0; u < U; ++u)
-          if (slot[u] < s_slots[b]) {
+          if (it0 + u * CP_NT < end) {
             if (VEC) *reinterpret_cast<uint4*>(to + off[u]) = v[u];
             else to[off[u]] = w[u];
           }
       }
     }
-    __syncthreads();
   }
 }
 
@@ -346,8 +420,16 @@ int actkv_copy(const actkv_pool_t* pool, const actkv_tables_t* tables, int32_t l
   a.status = status;
   const bool vec = ((uintptr_t)pool->base & 15) == 0 && pool->head_dim % 8 == 0 && pool->stride_layer % 8 == 0 &&
                    pool->stride_kv % 8 == 0 && pool->stride_page % 8 == 0 && pool->stride_slot % 8 == 0 && pool->stride_head % 8 == 0;
-  const dim3 grid((unsigned)((max_len - 1) / pool->page_size + 1), (unsigned)n_copy, (unsigned)nls * 2);
-  launch_pdl(vec ? copy_kernel<true> : copy_kernel<false>, grid, CP_NT, 0, (cudaStream_t)stream, a);
+  const int64_t pages = (max_len - 1) / pool->page_size + 1, slot_bytes = (int64_t)pool->n_kv_heads * pool->head_dim * 2;
+  const int64_t parts = (pool->page_size * slot_bytes + CB_BYTES - 1) / CB_BYTES;
+  // rows of a page's tokens in one run: 6 layers of 35000 tokens into 3 branches 292 us by vectors
+  if (vec && pool->stride_head == pool->head_dim && pool->stride_slot * 2 == slot_bytes && pages * parts <= 0x7fffffff &&
+      pool->page_size * slot_bytes <= 0x7fffffff) {
+    launch_pdl(copy_bulk_kernel, dim3((unsigned)(pages * parts), (unsigned)n_copy, (unsigned)nls * 2), CB_NT, 0, (cudaStream_t)stream, a, (int)parts);
+  } else {
+    const dim3 grid((unsigned)pages, (unsigned)n_copy, (unsigned)nls * 2);
+    launch_pdl(vec ? copy_kernel<true> : copy_kernel<false>, grid, CP_NT, 0, (cudaStream_t)stream, a);
+  }
   ACTKV_CHECK_LAUNCH();
   return ACTKV_OK;
 }

@@ -27,6 +27,7 @@
 #include "pool_map.cuh"
 #include "score_tc_lse.cuh"
 #include "score_tc_pool.cuh"
+#include "stall_hook.cuh"
 
 namespace actkv {
 namespace tc {
@@ -102,14 +103,6 @@ inline bool make_qmap(const actkv_pool_t* pool, const void* q, int nls, int sum_
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Fault-injection hook of the bounded waits (actkv_debug_inject_stall): while stall_tile >= 0 the K-tile
-// producers of every tensor-core score launch issue no tile from that one on, and every wait gives up after
-// `wait_cycles`.  Process-wide, read at launch.
-struct StallHook {
-  std::atomic<int32_t> stall_tile{-1};
-  std::atomic<long long> wait_cycles{WAIT_LIMIT_CYCLES};
-};
-inline StallHook& stall_hook() { static StallHook h; return h; }
 inline void apply_hook(TcArgs& ta) {
   ta.stall_tile = stall_hook().stall_tile.load();
   ta.wait_cycles = stall_hook().wait_cycles.load();

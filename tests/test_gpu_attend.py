@@ -75,7 +75,7 @@ def _check(inst, out, lse, window_left=0, layers=None):
     assert np.isfinite(got).all()
     over = np.abs(got - want) - tol
     assert over.max(initial=-1.0) <= 0, f"out beyond tolerance by {over.max()} at {np.unravel_index(over.argmax(), over.shape)}"
-    d = np.abs(glse - wlse)[~empty] - (dp + n * 2.0 ** -24 + np.abs(wlse[~empty]) * 2.0 ** -22)
+    d = np.abs(glse[~empty] - wlse[~empty]) - (dp + n * 2.0 ** -24 + np.abs(wlse[~empty]) * 2.0 ** -22)
     assert d.max(initial=-1.0) <= 0, f"lse beyond tolerance by {d.max()}"
     # and all of it together is a float32 computation rounded once: half a bf16 step is uniform, 2^-9 / sqrt(3) of the value
     if want.size > 4000:
@@ -270,3 +270,23 @@ def test_two_calls_at_once_with_a_workspace_each():
                 got.append(_attend(x)[0])
         torch.cuda.synchronize()
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("D,lens,after", [(64, [900, 1500], 0), (128, [900, 1500], 0), (64, [50000, 1500], 1), (128, [50000, 1500], 3)])
+def test_a_wait_that_runs_out_is_reported(D, lens, after):
+    # the hook lets the first `after` tiles of every stretch arrive and no other (short requests: a stretch is one tile); the waits
+    # give up after 5 ms and every role leaves
+    inst = _make(lens, [4, 3], hkv=2, G=8, D=D, seed=D)
+    want, wlse, dec = _attend(inst)
+    dec.check_status()
+    B.actkv_debug_inject_stall(after, 5000)
+    try:
+        _attend(inst, dec=dec)
+        torch.cuda.synchronize()
+    finally:
+        B.actkv_debug_inject_stall(-1, 0)
+    assert dec.status.cpu().tolist()[0] == B.E_TIMEOUT
+    dec.status.zero_()
+    out, lse, _ = _attend(inst, dec=dec)
+    dec.check_status()
+    assert torch.equal(out, want) and torch.equal(lse, wlse)
