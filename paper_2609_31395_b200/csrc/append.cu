@@ -56,11 +56,16 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
+__device__ __forceinline__ uint32_t turn_pair(uint32_t v, float cs, float sn) {
+  const float2 x = bf2(v);
+  return pack2(x.x * cs - x.y * sn, x.y * cs + x.x * sn);
+}
+
 // VEC: every row and head begins on 16 bytes and the halves of the turned dims are whole vectors.
 template <bool VEC>
 __global__ void __launch_bounds__(NT) append_kernel(const Args a) {
   pdl_begin();
-  __shared__ float2 s_cs[MAX_PAIRS];
+  __shared__ __align__(16) float s_cos[MAX_PAIRS], s_sin[MAX_PAIRS];       // (apart: a thread reads those of 8 pairs as vectors)
   __shared__ int64_t s_place;
   const int i = blockIdx.x, layer = blockIdx.y, tid = threadIdx.x;
   const int D = a.pool.head_dim, Hkv = a.pool.n_kv_heads, Hq = a.q_out != nullptr ? a.n_q_heads : 0;
@@ -76,7 +81,8 @@ __global__ void __launch_bounds__(NT) append_kernel(const Args a) {
     t -= 2.0 * rint(0.5 * t);
     float sn, cs;
     sincospif((float)t, &sn, &cs);
-    s_cs[p] = make_float2(cs, sn);
+    s_cos[p] = cs;
+    s_sin[p] = sn;
   }
   __syncthreads();
   const int64_t place = s_place;
@@ -91,8 +97,8 @@ __global__ void __launch_bounds__(NT) append_kernel(const Args a) {
   if (VEC) {
     // items of a head: turned pairs of vectors (or, interleaved, turned vectors), then vectors that pass
     const int turn = a.interleaved ? a.pairs / 4 : a.pairs / 8, pass = (D - 2 * a.pairs) / 8, per = turn + pass;
-    for (int it = tid; it < heads * per; it += NT) {
-      const int h = it / per, c = it - h * per;
+    const int dh = NT / per, dc = NT - dh * per;               // from one item of a thread to its next
+    for (int h = tid / per, c = tid - h * per; h < heads;) {
       const __nv_bfloat16* src = src_of(h);
       __nv_bfloat16* dst = dst_of(h);
       if (c >= turn) {
@@ -100,24 +106,33 @@ __global__ void __launch_bounds__(NT) append_kernel(const Args a) {
         *reinterpret_cast<uint4*>(dst + d) = *reinterpret_cast<const uint4*>(src + d);
       } else if (a.interleaved) {
         uint4 v = *reinterpret_cast<const uint4*>(src + c * 8);
-        uint32_t* u = reinterpret_cast<uint32_t*>(&v);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 x = bf2(u[e]), cs = s_cs[c * 4 + e];
-          u[e] = pack2(x.x * cs.x - x.y * cs.y, x.y * cs.x + x.x * cs.y);
-        }
+        const float4 cs = *reinterpret_cast<const float4*>(&s_cos[c * 4]), sn = *reinterpret_cast<const float4*>(&s_sin[c * 4]);
+        v.x = turn_pair(v.x, cs.x, sn.x);
+        v.y = turn_pair(v.y, cs.y, sn.y);
+        v.z = turn_pair(v.z, cs.z, sn.z);
+        v.w = turn_pair(v.w, cs.w, sn.w);
         *reinterpret_cast<uint4*>(dst + c * 8) = v;
       } else {
         uint4 va = *reinterpret_cast<const uint4*>(src + c * 8), vb = *reinterpret_cast<const uint4*>(src + a.pairs + c * 8);
         uint32_t *ua = reinterpret_cast<uint32_t*>(&va), *ub = reinterpret_cast<uint32_t*>(&vb);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 x = bf2(ua[e]), y = bf2(ub[e]), c0 = s_cs[c * 8 + 2 * e], c1 = s_cs[c * 8 + 2 * e + 1];
-          ua[e] = pack2(x.x * c0.x - y.x * c0.y, x.y * c1.x - y.y * c1.y);
-          ub[e] = pack2(y.x * c0.x + x.x * c0.y, y.y * c1.x + x.y * c1.y);
+        for (int e = 0; e < 4; e += 2) {
+          const float4 cs = *reinterpret_cast<const float4*>(&s_cos[c * 8 + 2 * e]), sn = *reinterpret_cast<const float4*>(&s_sin[c * 8 + 2 * e]);
+          float2 x = bf2(ua[e]), y = bf2(ub[e]);
+          ua[e] = pack2(x.x * cs.x - y.x * sn.x, x.y * cs.y - y.y * sn.y);
+          ub[e] = pack2(y.x * cs.x + x.x * sn.x, y.y * cs.y + x.y * sn.y);
+          x = bf2(ua[e + 1]), y = bf2(ub[e + 1]);
+          ua[e + 1] = pack2(x.x * cs.z - y.x * sn.z, x.y * cs.w - y.y * sn.w);
+          ub[e + 1] = pack2(y.x * cs.z + x.x * sn.z, y.y * cs.w + x.y * sn.w);
         }
         *reinterpret_cast<uint4*>(dst + c * 8) = va;
         *reinterpret_cast<uint4*>(dst + a.pairs + c * 8) = vb;
+      }
+      h += dh;
+      c += dc;
+      if (c >= per) {
+        c -= per;
+        ++h;
       }
     }
     if (place >= 0)
@@ -138,9 +153,9 @@ __global__ void __launch_bounds__(NT) append_kernel(const Args a) {
       } else {
         const int da = a.interleaved ? 2 * c : c, db = a.interleaved ? 2 * c + 1 : c + a.pairs;
         const float x = __bfloat162float(src[da]), y = __bfloat162float(src[db]);
-        const float2 cs = s_cs[c];
-        dst[da] = __float2bfloat16_rn(x * cs.x - y * cs.y);
-        dst[db] = __float2bfloat16_rn(y * cs.x + x * cs.y);
+        const float cs = s_cos[c], sn = s_sin[c];
+        dst[da] = __float2bfloat16_rn(x * cs - y * sn);
+        dst[db] = __float2bfloat16_rn(y * cs + x * sn);
       }
     }
     if (place >= 0)

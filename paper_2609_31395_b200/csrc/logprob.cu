@@ -1,7 +1,10 @@
 // actkv_logprob: log probabilities of given tokens, entropy and the top alternatives of every logits row, in one sweep.
 //
-// Per thread, with m the largest logit it has met: S = sum exp(x - m), T = sum exp(x - m) (x - m); when m moves by d,
-// S' = S e^-d and T' = (T - d S) e^-d.  Joined over the row: lse = m + ln S, log P(t) = (x_t - m) - ln S, entropy = ln S - T / S.
+// Per thread, with m the largest logit it has met, c = log2 e and r = c m rounded: y = c x - r (one fused operation), S = sum 2^y,
+// T = sum 2^y y; when r moves by d, S' = S 2^-d and T' = (T - d S) 2^-d.  Behind the sweep both are taken from r to c m itself (by the
+// remainder c m - r), so that nothing is lost to the size of the logits, and joined over the row: s = ln 2 log2 S, lse = m + s,
+// log P(t) = (x_t - m) - s, entropy = s - ln 2 T / S.  Sums go in pairs (two-lane instructions), 3.5 instructions a logit instead of 7 (1500 rows,
+// 20 alternatives: 172 -> 166 us).  Logits beyond 10^37 and -inf take a longer way to the same sums.
 //
 // Top alternatives.  While it streams, a thread notes the maximum of every 16 logits (a slot).  Behind the sweep the CTA has 128
 // groups of threads; the top_k-th largest of the groups' maxima is a bound that top_k logits reach, so only they and the few
@@ -26,7 +29,8 @@ constexpr int SLOTS = 24;                 // maxima that a thread notes, at most
 constexpr int LIST = 1024;                // candidates ranked against each other
 constexpr int TIGHT = 256;                // second reading: candidates that stay between two steps, at most
 constexpr float NO_REF = -3.402823466e38f;
-constexpr float FAR = -1e4f;              // exp of it is 0
+constexpr float FAR = -1e4f;              // 2 to its power is 0
+constexpr float HUGE_LOGIT = 1e37f;
 
 struct Args {
   const void* logits;
@@ -45,6 +49,22 @@ __device__ __forceinline__ uint32_t okey(float x) {
 }
 __device__ __forceinline__ float okey_inv(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k); }
 __device__ __forceinline__ uint64_t key_of(float x, uint32_t token) { return ((uint64_t)okey(x) << 32) | (0xffffffffu - token); }
+
+__device__ __forceinline__ void fma2(float& d0, float& d1, float a0, float a1, float b0, float b1, float c0, float c1) {
+  uint64_t a, b, c, d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(a) : "f"(a0), "f"(a1));
+  asm("mov.b64 %0, {%1, %2};" : "=l"(b) : "f"(b0), "f"(b1));
+  asm("mov.b64 %0, {%1, %2};" : "=l"(c) : "f"(c0), "f"(c1));
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(d0), "=f"(d1) : "l"(d));
+}
+__device__ __forceinline__ void add2(float& s0, float& s1, float a0, float a1) {
+  uint64_t s, a;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(s) : "f"(s0), "f"(s1));
+  asm("mov.b64 %0, {%1, %2};" : "=l"(a) : "f"(a0), "f"(a1));
+  asm("add.rn.f32x2 %0, %0, %1;" : "+l"(s) : "l"(a));
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(s0), "=f"(s1) : "l"(s));
+}
 
 template <typename T> struct Vec;
 template <> struct Vec<float> {
@@ -177,9 +197,9 @@ __device__ __noinline__ void cut(Smem<NT>* sm, uint64_t* cand, int n, int k) {
 
 __device__ __forceinline__ float4 join(float4 a, float4 b) {               // (m, S, T)
   const float m = fmaxf(a.x, b.x);
-  // (distances of up to 2^128 are cut where the exponential is 0 long since: no infinity meets that 0)
-  const float da = fmaxf(a.x - m, FAR), db = fmaxf(b.x - m, FAR);
-  const float fa = exp2f(da * kLog2e), fb = exp2f(db * kLog2e);
+  // (distances of up to 2^128 are cut where the power is 0 long since: no infinity meets that 0)
+  const float da = fmaxf((a.x - m) * kLog2e, FAR), db = fmaxf((b.x - m) * kLog2e, FAR);
+  const float fa = exp2f(da), fb = exp2f(db);
   return make_float4(m, a.y * fa + b.y * fb, (a.z + da * a.y) * fa + (b.z + db * b.y) * fb, 0.f);
 }
 
@@ -265,7 +285,8 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprob_kernel(const Args a) {
   }
 
   const int steps = (v1 - v0 + NT * U - 1) / (NT * U), per_slot = (steps + SLOTS - 1) / SLOTS;
-  float m = NO_REF, S = 0.f, Tt = 0.f;
+  float m = NO_REF, r = 0.f, S0 = 0.f, S1 = 0.f, T0 = 0.f, T1 = 0.f;
+  bool big = true;                                                         // m is too large for r
   float tm = -INFINITY, slot_max = -INFINITY;                              // of the thread's logits, of the slot's
   int slot = 0, in_slot = 0;
   for (int vb = v0; vb < v1; vb += NT * U) {
@@ -276,9 +297,12 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprob_kernel(const Args a) {
 #pragma unroll
       for (int u = 0; u < U; ++u) next[u] = read(vb + NT * U + u * NT + tid);
     }
-    float mx = x[0];
+    float mx = x[0], mn = x[0];
 #pragma unroll
-    for (int e = 1; e < PER; ++e) mx = fmaxf(mx, x[e]);
+    for (int e = 1; e < PER; ++e) {
+      mx = fmaxf(mx, x[e]);
+      mn = fminf(mn, x[e]);
+    }
     slot_max = fmaxf(slot_max, mx);
     if (++in_slot == per_slot) {
       sm->slot[slot++][tid] = slot_max;
@@ -287,20 +311,33 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprob_kernel(const Args a) {
       in_slot = 0;
     }
     if (mx > m) {
-      const float d = fmaxf(m - mx, FAR), f = exp2f(d * kLog2e);
-      Tt = (Tt + d * S) * f;
-      S *= f;
+      const bool far = fabsf(mx) > HUGE_LOGIT;
+      const float to = mx * kLog2e, d = fmaxf(far || big ? (m - mx) * kLog2e : r - to, FAR), f = exp2f(d);
+      T0 = (T0 + d * S0) * f;
+      T1 = (T1 + d * S1) * f;
+      S0 *= f;
+      S1 *= f;
       m = mx;
+      r = to;
+      big = far;
     }
-    float bs = 0.f;
+    if (!big && mn > -HUGE_LOGIT) {
 #pragma unroll
-    for (int e = 0; e < PER; ++e) {
-      const float y = x[e] - m;
-      const float p = exp2f(y * kLog2e);
-      bs += p;
-      Tt = fmaf(p, fmaxf(y, FAR), Tt);
+      for (int e = 0; e < PER; e += 2) {
+        float y0, y1;
+        fma2(y0, y1, x[e], x[e + 1], kLog2e, kLog2e, -r, -r);
+        const float p0 = exp2f(y0), p1 = exp2f(y1);
+        add2(S0, S1, p0, p1);
+        fma2(T0, T1, p0, p1, y0, y1, T0, T1);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < PER; ++e) {
+        const float y = big ? (x[e] - m) * kLog2e : fmaf(x[e], kLog2e, -r), p = exp2f(y);
+        S0 += p;
+        T0 = fmaf(p, fmaxf(y, FAR), T0);                                   // (p is 0 long before; -inf must not meet it)
+      }
     }
-    S += bs;
   }
   if (in_slot > 0) {
     sm->slot[slot++][tid] = slot_max;
@@ -308,7 +345,11 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprob_kernel(const Args a) {
   }
 
   // ---- (m, S, T) of the warps; maxima of the groups ----
-  float4 mst = make_float4(m, S, Tt, 0.f);
+  float4 mst;
+  {
+    const float S = S0 + S1, rest = big ? 0.f : fmaf(m, kLog2e, -r), f = exp2f(-rest);
+    mst = make_float4(m, S * f, (T0 + T1 - rest * S) * f, 0.f);
+  }
 #pragma unroll
   for (int o = 16; o >= 1; o >>= 1) {
     const float4 b = make_float4(__shfl_xor_sync(0xffffffffu, mst.x, o), __shfl_xor_sync(0xffffffffu, mst.y, o),
@@ -444,12 +485,12 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprob_kernel(const Args a) {
   }
 
   // ---- results ----
-  const float ls = logf(mst.y);
   const bool none = mst.y == 0.f;
+  const float ls = kLn2 * log2f(mst.y);
   auto lp_of = [&](float v) { return none ? -INFINITY : (v - mst.x) - ls; };
   if (tid == 0) {
     if (a.lse != nullptr) a.lse[row] = none ? -INFINITY : mst.x + ls;
-    if (a.entropy != nullptr) a.entropy[row] = none ? 0.f : ls - mst.z / mst.y;
+    if (a.entropy != nullptr) a.entropy[row] = none ? 0.f : ls - kLn2 * (mst.z / mst.y);
   }
   for (int j = tid; j < k; j += NT) {
     const uint64_t key = j < n_top ? sm->list[j] : 0;
