@@ -588,7 +588,8 @@ int actkv_debug_inject_stall(int32_t after_tile, int32_t wait_limit_us);
  * cache and its block table, Section 7.1 takes the LSE from the attention backend.)
  */
 
-/* actkv_attend — attention of the newest tokens of every request over its cached entries
+/* ---------------------------------------------------------------------------------------
+ * actkv_attend — attention of the newest tokens of every request over its cached entries
  * (Section 2.3), read through the block table, split over the cache's length and joined.
  *
  * For layer l, request r, window row w < W_r and q-head qh of KV head h = qh / G, over the keys
@@ -600,7 +601,8 @@ int actkv_debug_inject_stall(int32_t after_tile, int32_t wait_limit_us);
  * layers): only the S keys up to the row's own position count, as in actkv_score_sliding.
  * A row that sees no key (W_r > L_r, L_r = 0), or whose logits are all -inf, gets out = 0 and
  * lse = -inf.  What a masked or unused slot holds (infinities and NaN too) does not reach any row.  A
- * logit that is NaN or +inf makes its row NaN.
+ * logit that is NaN or +inf makes its row NaN; a visible V entry that is infinite or NaN makes its dim of the row
+ * infinite or NaN.
  * Logits, maxima, sums and the output's accumulation are float32; the probabilities enter the
  * product with V as two bf16 summands (16 bits of mantissa), so that the output is as good as a
  * float32 computation rounded once.  The result does not depend on anything but the arguments and
@@ -613,7 +615,9 @@ int actkv_debug_inject_stall(int32_t after_tile, int32_t wait_limit_us);
  * does not fit the host's bounds is reported as ACTKV_E_INVALID and its rows are left as they were; a page id
  * out of range is reported and replaced by page 0 for the read.
  * head_dim a multiple of 8, at most 256; any page size; strides multiples of 8 elements; base, q and out
- * 16-byte aligned.
+ * 16-byte aligned; at most 32 q-heads per KV head.  More than 8 window x group rows per request and KV head with
+ * head_dim 64 or 128 and pages of 16, 32, 64 or 128 tokens run on tcgen05 (whose waits are bounded: ACTKV_E_TIMEOUT in
+ * status), everything else on warp-level matrix instructions.
  */
 size_t actkv_attend_workspace_bytes(const actkv_pool_t* pool /* host */, int32_t n_req, int32_t n_layers_sub,
                                     int32_t n_q_heads, int32_t max_win, int32_t max_tok);
@@ -644,7 +648,8 @@ typedef struct {
   const float* inv_freq;        /* device, float32 [rotary_dim/2] */
 } actkv_rope_t;
 
-/* actkv_append — the new tokens' keys and values into their slots, queries and keys turned to their
+/* ---------------------------------------------------------------------------------------
+ * actkv_append — the new tokens' keys and values into their slots, queries and keys turned to their
  * positions on the way (Section 2.5: the block table places logical token j; positions are an input
  * because after a compression a token's position is no longer its index in the cache).
  *
@@ -667,7 +672,8 @@ int actkv_append(const actkv_pool_t* pool /* host */, const actkv_tables_t* tabl
                  const actkv_rope_t* rope /* host */, const int32_t* positions, void* q_out,
                  int32_t sum_win, int32_t* status, actkv_stream_t stream);
 
-/* actkv_resize — requests grow, are cut back or freed: pages from and to the free list (Section 2.5;
+/* ---------------------------------------------------------------------------------------
+ * actkv_resize — requests grow, are cut back or freed: pages from and to the free list (Section 2.5;
  * Section 7.2, last paragraph, for the freed blocks).
  *
  * For every request with new_len[r] >= 0 (negative: left as it is), Y_r and X_r pages before and after:
@@ -678,12 +684,13 @@ int actkv_append(const actkv_pool_t* pool /* host */, const actkv_tables_t* tabl
  * All or nothing: a free list too short (ACTKV_E_NOFREE), a length beyond the table row, a free count or
  * a page id out of range (ACTKV_E_INVALID, ACTKV_E_BADPAGE) is reported and nothing is modified; the same
  * when status is already set.
- * Only page_size and n_pages of the pool are used.  One launch of one cluster; no workspace.
+ * Only page_size and n_pages of the pool are used.  n_req * max_pages below 2^31.  One launch; no workspace.
  */
 int actkv_resize(const actkv_pool_t* pool /* host */, const actkv_tables_t* tables /* host */,
                  const int32_t* new_len, int32_t* status, actkv_stream_t stream);
 
-/* actkv_copy — branches of a trace: K and V rows of the first length[i] tokens of request src[i] into
+/* ---------------------------------------------------------------------------------------
+ * actkv_copy — branches of a trace: K and V rows of the first length[i] tokens of request src[i] into
  * the slots of request dst[i], i < n_copy, layers [layer_begin, layer_end).  The slots must exist: fork = actkv_resize
  * (dst from 0 to length) + actkv_copy.  Every branch has pages of its own, as the compaction calls
  * require.  Tables are not touched.  Pairs that share a source read it once.
@@ -697,7 +704,8 @@ int actkv_copy(const actkv_pool_t* pool /* host */, const actkv_tables_t* tables
                const int32_t* src, const int32_t* dst, const int32_t* length, int32_t n_copy, int32_t max_len,
                int32_t* status, actkv_stream_t stream);
 
-/* actkv_logprob — log probabilities of given tokens, entropy and the most probable alternatives of every
+/* ---------------------------------------------------------------------------------------
+ * actkv_logprob — log probabilities of given tokens, entropy and the most probable alternatives of every
  * logits row, in one pass over the row (log P as in Section 6.1, whose monitor reads the same logits).
  *
  * lse_i = log sum_t exp(z_it);  logprob[i, g] = z[i, given[i, g]] - lse_i;
@@ -709,8 +717,8 @@ int actkv_copy(const actkv_pool_t* pool /* host */, const actkv_tables_t* tables
  * logprob, entropy, lse, top_logprob: float32, entropy / lse may be NULL; top_index int32.  0 <= top_k <= 64;
  *         places past the vocabulary: index -1, log probability -inf.
  * Masked tokens (logit -inf) have probability 0.  A row with nothing but -inf: lse = -inf, log probabilities
- * -inf, entropy 0.  A NaN, or a logit of +inf, makes lse, entropy and every log probability NaN; the index order then
- * takes logits by their bit patterns (NaN with sign 0 above +inf).
+ * -inf, entropy 0.  A NaN, or a logit of +inf, makes lse, entropy and every log probability of its row NaN; the
+ * alternatives are then some tokens of the row.
  */
 #define ACTKV_F32   0
 #define ACTKV_BF16  1

@@ -131,6 +131,22 @@ def test_a_row_with_nothing_allowed():
     assert o.lse[1].item() == -float("inf") and o.entropy[1].item() == 0 and o.top_index[1].tolist() == [0, 1, 2, 3, 4, 5]
 
 
+@pytest.mark.parametrize("rows", [2, 300])
+def test_logits_near_the_end_of_the_type(rows):
+    # differences of such logits are multiples of 2^103 or zero: equal ones share the mass, the others have none
+    z = torch.full((rows, 9001), -3.4e38, device=DEV)
+    z[:, 700], z[:, 5], z[:, 8000] = 3.0e38, 3.0e38, 1.0e38
+    z[1, :] = -3.0e38
+    given = torch.tensor([[5, 8000, 9]] * rows, dtype=torch.int32, device=DEV)
+    o = _run(z, given, 3)
+    # lse 3e38 + ln 2 is 3e38 in float32
+    assert (o.lse[0] == 3.0e38).item() and (o.lse[1] == -3.0e38).item()
+    got = o.logprob.double().cpu().numpy()
+    assert abs(got[0, 0] + np.log(2)) < 1e-6 and got[0, 1] < -1e38 and np.abs(got[1] + np.log(9001)).max() < 1e-5
+    assert abs(o.entropy[0].item() - np.log(2)) < 1e-6 and abs(o.entropy[1].item() - np.log(9001)) < 1e-4
+    assert o.top_index[0].tolist() == [5, 700, 8000] and o.top_index[1].tolist() == [0, 1, 2]
+
+
 def test_signed_zeros_are_equal():
     z = torch.full((1, 100), -1.0, device=DEV)
     z[0, 10], z[0, 20], z[0, 30] = -0.0, 0.0, -0.0
