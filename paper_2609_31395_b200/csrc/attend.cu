@@ -21,6 +21,8 @@
 // of fences and reads by one CTA takes longer than a launch whose start is already behind it.)
 // Within a CTA the groups of RG warps take the tiles of a piece in turn; the warps of a group share a ring of tiles
 // in shared memory and have 8 NT rows each.
+#include <cooperative_groups.h>
+
 #include <algorithm>
 
 #include "attend_tc.cuh"
@@ -63,8 +65,8 @@ struct Cfg {
   static constexpr int NG = NW / RG;
   static constexpr int RB = 8 * NT * RG;                                   // rows of a block
   static constexpr int TILE = KT * DP * 2 * 2;                             // bytes: K and V
-  // CTAs per SM, as many as registers allow without spilling.  They share what the ring may take: with 2, 3 and 4 of them 8 rows of
-  // 35000 x 8 tokens at head_dim 128 took 98.8, 95 and - us, 16000 x 16 at head_dim 64 121, - and 94 us.
+  // CTAs per SM, as many as registers allow without spilling; they share what the rings may take.  (8 rows, 35000 x 8 tokens of 128 dims:
+  // 98.8 us with two, 95 with three; 16000 x 16 of 64 dims: 121 with two, 94 with four.)
   static constexpr int CTAS = DP > 128 ? 1 : NT > 1 ? 2 : DP == 64 ? 4 : 3;
   static constexpr int RING_MAX = 192 / CTAS * 1024;
   static constexpr int STAGES = RING_MAX / (NG * TILE) > 16 ? 16 : RING_MAX / (NG * TILE);
@@ -73,7 +75,7 @@ struct Cfg {
   static_assert(RED <= RING, "the join of the warps reuses the ring");
 };
 
-template <int DP, int NT, int RG>
+template <int DP, int NT, int RG, int CL>
 __global__ void __launch_bounds__(NTH, (Cfg<DP, NT, RG>::CTAS)) attend_kernel(const __grid_constant__ Args a) {
   using C = Cfg<DP, NT, RG>;
   pdl_begin();
@@ -83,9 +85,29 @@ __global__ void __launch_bounds__(NTH, (Cfg<DP, NT, RG>::CTAS)) attend_kernel(co
   const int grp = warp / RG, part = warp % RG;
   const int G = a.group, D = a.pool.head_dim, P = a.pool.page_size;
 
-  Line<KT, C::RB, MIN_TILES> line(a, blockIdx.x == 0 && warp == 0);
-  if (line.x >= line.x1) return;
-  const int h = line.h;
+  using L1 = Line<KT, C::RB, MIN_TILES>;
+  Seg sg;
+  int h;
+  if constexpr (CL > 1) {                                                  // a cluster per unit, equal shares of its tiles
+    const int unit = blockIdx.x / CL, rank = blockIdx.x % CL, lr = unit / a.rb_max, Hkv = a.pool.n_kv_heads;
+    sg.rb = unit - lr * a.rb_max;
+    sg.r = lr % a.tab.n_req;
+    sg.layer = lr / a.tab.n_req / Hkv;
+    h = lr / a.tab.n_req - sg.layer * Hkv;
+    sg.q = load_req<KT>(a, sg.r, unit < a.tab.n_req * a.rb_max && sg.rb == 0 && rank == 0 && warp == 0);
+    if (sg.rb * C::RB >= sg.q.W * G) return;                               // (the whole cluster)
+    const int share = (sg.q.tiles + CL - 1) / CL;
+    sg.t_in = rank * share;
+    sg.n_tiles = max(0, min(share, sg.q.tiles - sg.t_in));
+  }
+  std::conditional_t<(CL > 1), int, L1> line = [&]() {
+    if constexpr (CL > 1) return 0;
+    else return L1(a, blockIdx.x == 0 && warp == 0);
+  }();
+  if constexpr (CL == 1) {
+    if (line.x >= line.x1) return;
+    h = line.h;
+  }
 
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(at_smem) + grp * C::STAGES * C::TILE;
   const int g = lane >> 2, t2 = (lane & 3) * 2;
@@ -103,8 +125,17 @@ __global__ void __launch_bounds__(NTH, (Cfg<DP, NT, RG>::CTAS)) attend_kernel(co
     else asm volatile("bar.sync %0, %1;" ::"r"(1 + grp), "n"(RG * 32) : "memory");
   };
 
-  Seg sg;
-  while (line.next(sg)) {
+  bool more = true;
+  auto next = [&]() {
+    if constexpr (CL > 1) {
+      const bool now = more;
+      more = false;
+      return now;
+    } else {
+      return line.next(sg);
+    }
+  };
+  while (next()) {
     const Req& q = sg.q;
     const int r = sg.r, rb = sg.rb, t_in = sg.t_in, n_tiles = sg.n_tiles, layer = sg.layer;
     const int L = q.L, rows = q.W * G;
@@ -324,10 +355,17 @@ __global__ void __launch_bounds__(NTH, (Cfg<DP, NT, RG>::CTAS)) attend_kernel(co
         if (lane < 4) s_ml[warp][n * 8 + t2 + c] = make_float2(m[n][c], l[n][c]);
       }
     __syncthreads();                                                       // ... and nobody reads the rings any more
-    const bool whole = sg.b0 == sg.b1;
-    const int64_t slot = line.slot(sg);
-    if (t_in == 0 && tid == 0) a.desc[line.unit(sg)] = make_int2(sg.b0, sg.b1);
+    bool whole = false;
+    int64_t slot = 0;
+    if constexpr (CL == 1) {
+      whole = sg.b0 == sg.b1;
+      slot = line.slot(sg);
+      if (t_in == 0 && tid == 0) a.desc[line.unit(sg)] = make_int2(sg.b0, sg.b1);
+    }
     float* red = reinterpret_cast<float*>(at_smem);
+    // (a cluster: the CTA's share of the unit's rows, for the others to read)
+    float* mine = reinterpret_cast<float*>(at_smem + C::RED);
+    float2* mine_ml = reinterpret_cast<float2*>(mine + C::RB * DP);
     constexpr int RS = DP + 4;
 #pragma unroll 1
     for (int n = 0; n < NT; ++n) {
@@ -365,7 +403,10 @@ __global__ void __launch_bounds__(NTH, (Cfg<DP, NT, RG>::CTAS)) attend_kernel(co
           const float4 v = *reinterpret_cast<const float4*>(red + ((k * RG + pt) * 8 + row) * RS + d);
           o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w;
         }
-        if (whole) {
+        if (CL > 1) {
+          *reinterpret_cast<float4*>(mine + in_block * DP + d) = o;
+          if (d == 0) mine_ml[in_block] = make_float2(M, sum);
+        } else if (whole) {
           const int w = rho / G;
           const int64_t at = (qrow + w) * a.n_q_heads + h * G + (rho - w * G);
           store_row(a, at, d, o, sum, M, D);
@@ -375,6 +416,43 @@ __global__ void __launch_bounds__(NTH, (Cfg<DP, NT, RG>::CTAS)) attend_kernel(co
         }
       }
       __syncthreads();
+    }
+    if constexpr (CL > 1) {
+      static_assert(C::RED + C::RB * (DP * 4 + 8) <= C::RING, "the shares fit behind the join of the warps");
+      namespace cg = cooperative_groups;
+      cg::cluster_group cl = cg::this_cluster();
+      cl.sync();
+      for (int row = (int)cl.block_rank(); row < C::RB; row += CL) {
+        const int rho = rb * C::RB + row;
+        if (rho >= rows) break;
+        float M = NO_REF, sum = 0.f, f[CL];
+        float2 ml[CL];
+#pragma unroll
+        for (int c = 0; c < CL; ++c) ml[c] = cl.map_shared_rank(mine_ml, c)[row];
+#pragma unroll
+        for (int c = 0; c < CL; ++c) M = fmaxf(M, ml[c].x);
+#pragma unroll
+        for (int c = 0; c < CL; ++c) {
+          f[c] = exp2f(ml[c].x - M);
+          sum = fmaf(ml[c].y, f[c], sum);
+        }
+        const int w = rho / G;
+        const int64_t at = (qrow + w) * a.n_q_heads + h * G + (rho - w * G);
+        for (int d = tid * 4; d < DP; d += NTH * 4) {
+          float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+          for (int c = 0; c < CL; ++c) {
+            const float4 v = *reinterpret_cast<const float4*>(cl.map_shared_rank(mine, c) + row * DP + d);
+            o.x = fmaf(v.x, f[c], o.x);
+            o.y = fmaf(v.y, f[c], o.y);
+            o.z = fmaf(v.z, f[c], o.z);
+            o.w = fmaf(v.w, f[c], o.w);
+          }
+          store_row(a, at, d, o, sum, M, D);
+        }
+      }
+      cl.sync();                                                           // (the others' shares have been read)
+      return;
     }
     // (dims past head_dim: the join has written over their zeros)
     if (D < DP) {
@@ -392,7 +470,8 @@ __global__ void __launch_bounds__(NTH, (Cfg<DP, NT, RG>::CTAS)) attend_kernel(co
 constexpr int JN = 256;
 template <int DP>
 __global__ void __launch_bounds__(JN) attend_join_kernel(const __grid_constant__ Args a, int32_t RB) {
-  pdl_begin();
+  // (no early start of the next kernel: 8000 x 1 14.8 us with it, 13.6 without; see below)
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   __shared__ float2 s_ml[MAX_CTAS];
   __shared__ float s_red[JN / 32][DP];
   __shared__ float s_r[JN / 32];
@@ -468,8 +547,8 @@ __global__ void __launch_bounds__(JN) attend_join_kernel(const __grid_constant__
 // The same with a warp per row, eight rows of a unit per CTA: for launches with more rows than CTAs of the kernel above fit on the SMs.
 template <int DP>
 __global__ void __launch_bounds__(JN) attend_join_rows_kernel(const __grid_constant__ Args a, int32_t RB) {
-  // (The next kernel may start when this one has ended, not before: CTAs of the next attention call that were placed beside
-  // waiting ones of this kernel found an SM each other's pieces did not: 64 requests of 8K-32K 474 us, so 366.)
+  // (The next kernel may start when this one has ended, not before: with CTAs of the next call placed among those of this kernel,
+  // calls one behind another took 474 us, so 366: 64 requests of 8K-32K.)
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int lane = threadIdx.x & 31, row = blockIdx.y * (JN / 32) + (threadIdx.x >> 5);
   const int64_t unit = blockIdx.x;
@@ -562,12 +641,40 @@ int launch_join(const Args& a, int64_t pieces, int64_t units, int RB, cudaStream
 inline int64_t pieces_of(int64_t tiles_bound, int Hkv, int per_sm, int min_tiles) {
   return std::max<int64_t>(1, std::min<int64_t>(SMS * per_sm / Hkv, (tiles_bound / Hkv + min_tiles - 1) / min_tiles));
 }
+// Requests that are short and few: a cluster of CLUSTER CTAs per unit, joined through distributed shared memory, one launch (1000 tokens:
+// see the head of this file) while all of them fit on the SMs at once.  Longer ones need more CTAs than a cluster has.
+constexpr int CLUSTER = 8, CLUSTER_TOKENS = CLUSTER * NW * KT * 4;
+template <int DP>
+int launch_cluster(const Args& a, int64_t units, cudaStream_t s) {
+  using C = Cfg<DP, 1, 1>;
+  auto kernel = attend_kernel<DP, 1, 1, CLUSTER>;
+  if (ensure_dyn_smem(kernel, C::RING) != cudaSuccess) return ACTKV_E_CUDA;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)units * CLUSTER);
+  cfg.blockDim = dim3(NTH);
+  cfg.dynamicSmemBytes = C::RING;
+  cfg.stream = s;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = CLUSTER;
+  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  (void)cudaLaunchKernelEx(&cfg, kernel, a);
+  ACTKV_CHECK_LAUNCH();
+  return ACTKV_OK;
+}
 template <int DP, int NT, int RG>
 int launch(const Args& a, int64_t tiles_bound, int64_t units, cudaStream_t s) {
   using C = Cfg<DP, NT, RG>;
-  if (ensure_dyn_smem(attend_kernel<DP, NT, RG>, C::RING) != cudaSuccess) return ACTKV_E_CUDA;
+  if constexpr (NT == 1 && RG == 1) {
+    if (a.max_tok <= CLUSTER_TOKENS && units * CLUSTER <= SMS * C::CTAS) return launch_cluster<DP>(a, units, s);
+  }
+  if (ensure_dyn_smem(attend_kernel<DP, NT, RG, 1>, C::RING) != cudaSuccess) return ACTKV_E_CUDA;
   const int64_t pieces = pieces_of(tiles_bound, a.pool.n_kv_heads, C::CTAS, MIN_TILES);
-  launch_pdl(attend_kernel<DP, NT, RG>, (unsigned)(pieces * a.pool.n_kv_heads), NTH, C::RING, s, a);
+  launch_pdl(attend_kernel<DP, NT, RG, 1>, (unsigned)(pieces * a.pool.n_kv_heads), NTH, C::RING, s, a);
   ACTKV_CHECK_LAUNCH();
   return launch_join<DP>(a, pieces, units, C::RB, s);
 }
@@ -615,7 +722,8 @@ int actkv_attend(const actkv_pool_t* pool, const actkv_tables_t* tables, int32_t
   if (R == 0 || nls == 0 || sum_win == 0) return ACTKV_OK;
   if (!q || !win_indptr || !out || max_win == 0 || !tables->seq_len) return ACTKV_E_INVALID;
   if (!tables->page_table || tables->max_pages < 0) return ACTKV_E_INVALID;
-  if (q == out || (int64_t)max_win * G > (1 << 24)) return ACTKV_E_INVALID;
+  if (q == out) return ACTKV_E_INVALID;
+  if (max_tok > (1 << 30) || (int64_t)max_win * G > (1 << 24)) return ACTKV_E_TOOBIG;
   const WsLayout lay = ws_layout(Hkv, D, pool->page_size, R, nls, G, max_win);
   if (!ws || ws_bytes < lay.total) return ACTKV_E_WORKSPACE;
   if (lay.units > 0x7fffffff || (int64_t)R * lay.rb_max * std::max<int64_t>(1, ((int64_t)max_tok + KT - 1) / KT) > 0x7fffffff)
