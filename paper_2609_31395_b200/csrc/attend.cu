@@ -18,7 +18,7 @@
 // (head_dim 64, 8 heads: 137 us with one line through all heads, 100 so).
 // A unit that lies in several pieces leaves (m, l, O) partials, joined by attend_join_kernel in piece order.  (Joined by the CTA that finishes
 // last instead, found by marks in the workspace, a launch fewer: 10.1 us against 8.3 for 1000 tokens, 21.7 against 15.1 for 8000; a chain
-// of fences and reads by one CTA takes longer than a launch whose start is already behind it.)
+// of fences and reads by one CTA takes longer than a launch whose start is already behind it.)  Short and few requests: launch_cluster.
 // Within a CTA the groups of RG warps take the tiles of a piece in turn; the warps of a group share a ring of tiles
 // in shared memory and have 8 NT rows each.
 #include <cooperative_groups.h>
@@ -30,7 +30,6 @@
 namespace actkv {
 namespace at {
 
-constexpr int NW = 4, NTH = NW * 32;
 constexpr int KT = 16;                    // keys per tile
 constexpr int MIN_TILES = 4;              // fewest tiles of a CTA's piece
 
@@ -60,14 +59,16 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
 }
 
 // What a launch variant is made of.  NT: row tiles of 8 per warp; RG: warps that share a ring (and have different rows).
-template <int DP, int NT, int RG>
+// PER_SM, WARPS: 0 for the usual numbers.
+template <int DP, int NT, int RG, int PER_SM = 0, int WARPS = 0>
 struct Cfg {
+  static constexpr int NW = WARPS > 0 ? WARPS : 4, NTH = NW * 32;
   static constexpr int NG = NW / RG;
   static constexpr int RB = 8 * NT * RG;                                   // rows of a block
   static constexpr int TILE = KT * DP * 2 * 2;                             // bytes: K and V
   // CTAs per SM, as many as registers allow without spilling; they share what the rings may take.  (8 rows, 35000 x 8 tokens of 128 dims:
   // 98.8 us with two, 95 with three; 16000 x 16 of 64 dims: 121 with two, 94 with four.)
-  static constexpr int CTAS = DP > 128 ? 1 : NT > 1 ? 2 : DP == 64 ? 4 : 3;
+  static constexpr int CTAS = PER_SM > 0 ? PER_SM : DP > 128 ? 1 : NT > 1 ? 2 : DP == 64 ? 4 : 3;
   static constexpr int RING_MAX = 192 / CTAS * 1024;
   static constexpr int STAGES = RING_MAX / (NG * TILE) > 16 ? 16 : RING_MAX / (NG * TILE);
   static constexpr int RING = NG * STAGES * TILE;
@@ -75,9 +76,11 @@ struct Cfg {
   static_assert(RED <= RING, "the join of the warps reuses the ring");
 };
 
-template <int DP, int NT, int RG, int CL>
-__global__ void __launch_bounds__(NTH, (Cfg<DP, NT, RG>::CTAS)) attend_kernel(const __grid_constant__ Args a) {
-  using C = Cfg<DP, NT, RG>;
+template <int DP, int NT, int RG, int CL, int PER_SM = 0, int WARPS = 0>
+__global__ void __launch_bounds__((Cfg<DP, NT, RG, PER_SM, WARPS>::NTH), (Cfg<DP, NT, RG, PER_SM, WARPS>::CTAS))
+    attend_kernel(const __grid_constant__ Args a) {
+  using C = Cfg<DP, NT, RG, PER_SM, WARPS>;
+  constexpr int NW = C::NW, NTH = C::NTH;
   pdl_begin();
   extern __shared__ __align__(128) uint8_t at_smem[];
   __shared__ float2 s_ml[NW][8 * NT];
@@ -641,17 +644,19 @@ int launch_join(const Args& a, int64_t pieces, int64_t units, int RB, cudaStream
 inline int64_t pieces_of(int64_t tiles_bound, int Hkv, int per_sm, int min_tiles) {
   return std::max<int64_t>(1, std::min<int64_t>(SMS * per_sm / Hkv, (tiles_bound / Hkv + min_tiles - 1) / min_tiles));
 }
-// Requests that are short and few: a cluster of CLUSTER CTAs per unit, joined through distributed shared memory, one launch (1000 tokens:
-// see the head of this file) while all of them fit on the SMs at once.  Longer ones need more CTAs than a cluster has.
-constexpr int CLUSTER = 8, CLUSTER_TOKENS = CLUSTER * NW * KT * 4;
-template <int DP>
+// Requests that are short and few: a cluster of CLUSTER CTAs per unit, joined through distributed shared memory, one launch; while all CTAs fit
+// on the SMs at once, and up to CLUSTER_TOKENS.  Measured, us with a line per head and with clusters, 4 heads of 128 dims and 8 rows, 1, 3,
+// 6 and 12 requests: 500 tokens 7.9 8.4 9.1 11.2, 6.2 6.7 6.6 7.6; 2000 tokens 8.5 12.7 15.0 21.0, 7.7 8.3 10.2 14.2; 4000 tokens
+// 10.9 14.5 19.8 27.9, 9.3 10.2 17.3 21.9; 8000 tokens 13.6 19.5 26.7 41.8, 14.3 16.4 29.1 36.6 (and unequal lengths are the line's).
+constexpr int CLUSTER = 8, CLUSTER_TOKENS = 4096;
+template <int DP, int PER_SM, int WARPS>
 int launch_cluster(const Args& a, int64_t units, cudaStream_t s) {
-  using C = Cfg<DP, 1, 1>;
-  auto kernel = attend_kernel<DP, 1, 1, CLUSTER>;
+  using C = Cfg<DP, 1, 1, PER_SM, WARPS>;
+  auto kernel = attend_kernel<DP, 1, 1, CLUSTER, PER_SM, WARPS>;
   if (ensure_dyn_smem(kernel, C::RING) != cudaSuccess) return ACTKV_E_CUDA;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)units * CLUSTER);
-  cfg.blockDim = dim3(NTH);
+  cfg.blockDim = dim3(C::NTH);
   cfg.dynamicSmemBytes = C::RING;
   cfg.stream = s;
   cudaLaunchAttribute at[2];
@@ -670,11 +675,17 @@ template <int DP, int NT, int RG>
 int launch(const Args& a, int64_t tiles_bound, int64_t units, cudaStream_t s) {
   using C = Cfg<DP, NT, RG>;
   if constexpr (NT == 1 && RG == 1) {
-    if (a.max_tok <= CLUSTER_TOKENS && units * CLUSTER <= SMS * C::CTAS) return launch_cluster<DP>(a, units, s);
+    if (a.max_tok <= CLUSTER_TOKENS && units * CLUSTER <= SMS * C::CTAS) {
+      // one CTA per SM: as many warps as three (head_dim 64: four) small ones would have
+      if constexpr (DP <= 128) {
+        if (units * CLUSTER <= SMS) return launch_cluster<DP, 1, DP == 64 ? 16 : 12>(a, units, s);
+      }
+      return launch_cluster<DP, C::CTAS, C::NW>(a, units, s);
+    }
   }
   if (ensure_dyn_smem(attend_kernel<DP, NT, RG, 1>, C::RING) != cudaSuccess) return ACTKV_E_CUDA;
   const int64_t pieces = pieces_of(tiles_bound, a.pool.n_kv_heads, C::CTAS, MIN_TILES);
-  launch_pdl(attend_kernel<DP, NT, RG, 1>, (unsigned)(pieces * a.pool.n_kv_heads), NTH, C::RING, s, a);
+  launch_pdl(attend_kernel<DP, NT, RG, 1>, (unsigned)(pieces * a.pool.n_kv_heads), C::NTH, C::RING, s, a);
   ACTKV_CHECK_LAUNCH();
   return launch_join<DP>(a, pieces, units, C::RB, s);
 }
