@@ -615,9 +615,10 @@ int actkv_debug_inject_stall(int32_t after_tile, int32_t wait_limit_us);
  * does not fit the host's bounds is reported as ACTKV_E_INVALID and its rows are left as they were; a page id
  * out of range is reported and replaced by page 0 for the read.
  * head_dim a multiple of 8, at most 256; any page size; strides multiples of 8 elements; base, q and out
- * 16-byte aligned; at most 32 q-heads per KV head.  More than 8 window x group rows per request and KV head with
- * head_dim 64 or 128 and pages of 16, 32, 64 or 128 tokens run on tcgen05 (whose waits are bounded: ACTKV_E_TIMEOUT in
- * status), everything else on warp-level matrix instructions.
+ * 16-byte aligned; at most 32 q-heads per KV head.  Calls with more than 8 window x group rows per request and KV head
+ * and, by the host's bounds, work enough run on tcgen05 when head_dim is 64 or 128 and a page 16, 32, 64 or 128 tokens
+ * (the waits of that kernel are bounded: ACTKV_E_TIMEOUT in status), everything else on warp-level matrix
+ * instructions.  The workspace serves either.
  */
 size_t actkv_attend_workspace_bytes(const actkv_pool_t* pool /* host */, int32_t n_req, int32_t n_layers_sub,
                                     int32_t n_q_heads, int32_t max_win, int32_t max_tok);

@@ -600,14 +600,19 @@ __global__ void __launch_bounds__(JN) attend_join_rows_kernel(const __grid_const
   if (lane == 0 && a.lse != nullptr) a.lse[at] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
 }
 
-// The tensor-core kernel takes what has more rows than one instruction of the warp-level one holds.
-// Its loads are boxes of a page's rows: pages of 16 to 128 tokens.
-inline bool use_tc(int D, int P, int64_t rows) {
-  return (D == 64 || D == 128) && (P == 16 || P == 32 || P == 64 || P == 128) && rows > 8;
+// The tensor-core kernel takes more rows than one instruction of the warp-level one holds, its loads are boxes of a page's rows (pages of 16
+// to 128 tokens), and its start and end (12 us of a call at 32 rows, 27 at 64, most of it code that is run once) want work to stand against.
+// By rows and (key, KV head) pairs of the launch, as the host bounds them; us with the warp-level and the tensor-core kernel, 4 heads:
+//   16 rows, 128 dims:  1 x 8000 14.6 15.8, 8 x 8000 38.2 40.8, 16 x 16000 105 100;
+//   32 rows, 128 dims:  8 x 500 17.8 17.5, 1 x 8000 18.4 15.9, 8 x 2000 31.6 22.7, 16 x 16000 153 101; 64 dims: 8 x 500 14.2 16.3, 1 x 8000 15.6 15.3;
+//   64 rows, 128 dims:  1 x 8000 23.0 31.3, 8 x 2000 42.4 31.1, 16 x 16000 248 129; 64 dims: 1 x 8000 18.5 30.0, 8 x 2000 27.7 26.2.
+inline bool use_tc(int D, int P, int64_t rows, int64_t pairs) {
+  if ((D != 64 && D != 128) || (P != 16 && P != 32 && P != 64 && P != 128) || rows <= 8) return false;
+  return rows <= 16 ? pairs >= (512 << 10) : rows <= 32 ? pairs >= (24 << 10) : pairs * ((rows + 63) / 64) >= (64 << 10);
 }
 // rows of a block for this many rows per request at most: the smallest variant that holds them
-inline int block_rows(int D, int P, int64_t rows) {
-  if (use_tc(D, P, rows)) return rows <= 32 ? 32 : 64;
+inline int block_rows(int D, int64_t rows, bool tc) {
+  if (tc) return rows <= 32 ? 32 : 64;
   if (D > 128) return rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
   return rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
 }
@@ -618,9 +623,9 @@ struct WsLayout {
   int RB, DP;
   int64_t rb_max, units;
 };
-inline WsLayout ws_layout(int Hkv, int D, int P, int64_t n_req, int64_t nls, int G, int64_t max_win) {
+inline WsLayout ws_layout(int Hkv, int D, int64_t n_req, int64_t nls, int G, int64_t max_win, bool tc) {
   WsLayout l;
-  l.RB = block_rows(D, P, max_win * G);
+  l.RB = block_rows(D, max_win * G, tc);
   l.DP = padded_dim(D);
   l.rb_max = std::max<int64_t>(1, (max_win * G + l.RB - 1) / l.RB);
   l.units = nls * Hkv * n_req * l.rb_max;
@@ -710,7 +715,11 @@ size_t actkv_attend_workspace_bytes(const actkv_pool_t* pool, int32_t n_req, int
   if (!pool || pool->n_kv_heads <= 0 || pool->head_dim <= 0 || n_req < 0 || n_layers_sub < 0 || n_q_heads <= 0 ||
       max_win < 0 || max_tok < 0)
     return 0;
-  return actkv::at::ws_layout(pool->n_kv_heads, pool->head_dim, pool->page_size, n_req, n_layers_sub, n_q_heads / pool->n_kv_heads, max_win).total;
+  // (either kernel: a call on fewer layers, or with a smaller bound, may take the other one)
+  size_t most = 0;
+  for (bool tc : {false, true})
+    most = std::max(most, actkv::at::ws_layout(pool->n_kv_heads, pool->head_dim, n_req, n_layers_sub, n_q_heads / pool->n_kv_heads, max_win, tc).total);
+  return most;
 }
 
 int actkv_attend(const actkv_pool_t* pool, const actkv_tables_t* tables, int32_t layer_begin, int32_t layer_end, const void* q,
@@ -735,7 +744,8 @@ int actkv_attend(const actkv_pool_t* pool, const actkv_tables_t* tables, int32_t
   if (!tables->page_table || tables->max_pages < 0) return ACTKV_E_INVALID;
   if (q == out) return ACTKV_E_INVALID;
   if (max_tok > (1 << 30) || (int64_t)max_win * G > (1 << 24)) return ACTKV_E_TOOBIG;
-  const WsLayout lay = ws_layout(Hkv, D, pool->page_size, R, nls, G, max_win);
+  const bool tc = use_tc(D, pool->page_size, (int64_t)max_win * G, (int64_t)R * nls * Hkv * max_tok);
+  const WsLayout lay = ws_layout(Hkv, D, R, nls, G, max_win, tc);
   if (!ws || ws_bytes < lay.total) return ACTKV_E_WORKSPACE;
   if (lay.units > 0x7fffffff || (int64_t)R * lay.rb_max * std::max<int64_t>(1, ((int64_t)max_tok + KT - 1) / KT) > 0x7fffffff)
     return ACTKV_E_TOOBIG;
@@ -764,7 +774,7 @@ int actkv_attend(const actkv_pool_t* pool, const actkv_tables_t* tables, int32_t
   a.win_left = window_left;
   const int64_t bound = lay.units * std::max<int64_t>(1, ((int64_t)max_tok + KT - 1) / KT);
   cudaStream_t s = (cudaStream_t)stream;
-  if (use_tc(D, pool->page_size, (int64_t)max_win * G))
+  if (tc)
     return D == 64 ? launch_wide<64>(a, pool, max_tok, bound, lay.units, lay.RB, s) : launch_wide<128>(a, pool, max_tok, bound, lay.units, lay.RB, s);
   if (lay.DP == 256) {
     switch (lay.RB) {

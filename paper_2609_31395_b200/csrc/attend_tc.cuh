@@ -1,5 +1,5 @@
 // actkv_attend on the tensor cores of the fifth generation (tcgen05): 9 and more rows per request and KV head (drafted tokens, chunks,
-// large groups), head_dim 64 or 128.
+// large groups), head_dim 64 or 128, and work enough (use_tc in attend.cu).
 //
 // Why a second kernel.  Of every key the warp-level kernel loads fragments for each 8 rows and carries every instruction of the softmax
 // in the warps that feed the matrix pipe: 32 rows took 1.8 times, 64 rows 3.0 times what 8 rows take (16 requests of 16000 tokens, 4 heads of

@@ -22,6 +22,7 @@ import parity_util as U
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
+MANY = 1 << 19            # a bound on the lengths by which any number of rows above 8 is work for the tensor-core kernel
 
 
 def _make(lens, wins, hkv=2, G=4, D=64, page=16, layers=1, causal=True, seed=0, head_major=False):
@@ -110,9 +111,32 @@ def test_head_dims_and_groups(D, G, wins):
 
 
 @pytest.mark.parametrize("D", [64, 128, 256])
-def test_more_rows_than_a_block(D):
+@pytest.mark.parametrize("max_tok", [400, MANY])
+def test_more_rows_than_a_block(D, max_tok):
     inst = _make([400, 90], [37, 21], hkv=1, G=8, D=D, seed=3)
-    out, lse, dec = _attend(inst)
+    out, lse, dec = _attend(inst, max_tok=max_tok)
+    dec.check_status()
+    _check(inst, out, lse)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("G,wins", [(4, (3, 4)), (7, (4, 1)), (8, (8, 5)), (8, (9, 16)), (32, (4, 3)), (12, (0, 2)), (1, (60, 9))])
+@pytest.mark.parametrize("lens", [(300, 77), (1, 5000), (0, 129)])
+@pytest.mark.parametrize("S", [0, 40])
+def test_the_tensor_core_kernel(D, G, wins, lens, S):
+    # a large bound on the lengths takes the call there, as in a captured graph
+    inst = _make(lens, wins, hkv=2, G=G, D=D, seed=D + G)
+    out, lse, dec = _attend(inst, S, max_tok=MANY)
+    dec.check_status()
+    _check(inst, out, lse, S)
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+@pytest.mark.parametrize("head_major", [False, True])
+@pytest.mark.parametrize("causal", [True, False])
+def test_pages_and_strides_of_the_tensor_core_kernel(page, head_major, causal):
+    inst = _make([500, 129, 0, 16], [5, 3, 2, 4], D=128, page=page, layers=2, seed=page, head_major=head_major, causal=causal)
+    out, lse, dec = _attend(inst, max_tok=MANY)
     dec.check_status()
     _check(inst, out, lse)
 
@@ -173,7 +197,8 @@ def test_offsets_beyond_32_bits():
 
 
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
-def test_masked_slots_do_not_reach_a_row(value):
+@pytest.mark.parametrize("max_tok", [220, MANY])
+def test_masked_slots_do_not_reach_a_row(value, max_tok):
     # window rows 0 and 1 must not see the last two keys; with a sliding window of 50 nor the first ones
     inst = _make([220], [3], hkv=1, G=4, D=128)
     P = inst.wl.page_size
@@ -185,7 +210,7 @@ def test_masked_slots_do_not_reach_a_row(value):
     plant(218)
     for j in (0, 100, 160, 166):
         plant(j)
-    out, lse, dec = _attend(inst, 50)
+    out, lse, dec = _attend(inst, 50, max_tok=max_tok)
     inst.pool = clean
     wl = inst.wl
     want, wlse = O.attend(U.bits(clean), inst.page_table.cpu().numpy(), [220], U.bits(inst.q), [0, 3], 4, wl.sm_scale, True, 50)
@@ -277,7 +302,7 @@ def test_a_wait_that_runs_out_is_reported(D, lens, after):
     # the hook lets the first `after` tiles of every stretch arrive and no other (short requests: a stretch is one tile); the waits
     # give up after 5 ms and every role leaves
     inst = _make(lens, [4, 3], hkv=2, G=8, D=D, seed=D)
-    want, wlse, dec = _attend(inst)
+    want, wlse, dec = _attend(inst, max_tok=MANY)
     dec.check_status()
     B.actkv_debug_inject_stall(after, 5000)
     try:
