@@ -26,7 +26,7 @@ namespace lp {
 constexpr int GROUPS = 128;               // groups of threads whose maxima give the bound
 constexpr int PER = 16;                   // logits of a thread per step
 constexpr int SLOTS = 24;                 // maxima that a thread notes, at most (longer rows: of several steps each)
-constexpr int LIST = 1024;                // candidates ranked against each other
+constexpr int LIST = 1024;                // candidates kept
 constexpr int TIGHT = 256;                // second reading: candidates that stay between two steps, at most
 constexpr float NO_REF = -3.402823466e38f;
 constexpr float FAR = -1e4f;              // 2 to its power is 0
@@ -104,7 +104,7 @@ struct Smem {
   int n_best;
   uint32_t item[LIST];                    // slots that are read again
   uint32_t n_cand, n_item, thr;
-  uint32_t pick[2];
+  uint32_t pick[3];
 };
 
 template <int NT, int W>
@@ -126,11 +126,13 @@ template <int NT>
 __device__ __noinline__ void cut(Smem<NT>* sm, uint64_t* cand, int n, int k) {
   constexpr int CAP = Smem<NT>::CAP;
   const int tid = threadIdx.x;
-  if (n > LIST) {
-    // the k-th largest key, digit by digit; then only what is not smaller stays (k keys: they are all different)
+  if (n > NT / 2 && n > k) {
+    // the k-th largest key, digit by digit, until what shares its digits is wanted whole; then only what is not smaller stays (all keys are
+    // different).  (1009 candidates of a short, masked row: ranked against each other 30 us.)
     uint64_t prefix = 0;
     uint32_t left = (uint32_t)k;
-    for (int shift = 56; shift >= 0; shift -= 8) {
+    int shift = 56;
+    for (;; shift -= 8) {
       for (int i = tid; i < 256; i += NT) sm->hist[i] = 0;
       __syncthreads();
       for (int i = tid; i < n; i += NT) {
@@ -138,27 +140,44 @@ __device__ __noinline__ void cut(Smem<NT>* sm, uint64_t* cand, int n, int k) {
         if (shift == 56 || (key >> (shift + 8)) == prefix) atomicAdd(&sm->hist[(uint32_t)(key >> shift) & 255u], 1u);
       }
       __syncthreads();
-      if (tid == 0) {
-        uint32_t above = 0;
-        int d = 255;
-        for (; d > 0; --d) {
-          if (above + sm->hist[d] >= left) break;
-          above += sm->hist[d];
+      if (tid < 32) {                                          // lane t has digits 255 - 8 t downwards
+        uint32_t h[8], mine = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          h[j] = sm->hist[255 - 8 * tid - j];
+          mine += h[j];
         }
-        sm->pick[0] = (uint32_t)d;
-        sm->pick[1] = left - above;
+        uint32_t incl = mine;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const uint32_t t = __shfl_up_sync(0xffffffffu, incl, d);
+          if (tid >= d) incl += t;
+        }
+        uint32_t above = incl - mine;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (above < left && above + h[j] >= left) {
+            sm->pick[0] = (uint32_t)(255 - 8 * tid - j);
+            sm->pick[1] = left - above;
+            sm->pick[2] = h[j];
+          }
+          above += h[j];
+        }
       }
       __syncthreads();
       prefix = (prefix << 8) | sm->pick[0];
       left = sm->pick[1];
+      const bool done = sm->pick[2] == left || shift == 0;
       __syncthreads();
+      if (done) break;
     }
+    const uint64_t least = prefix << shift;
     uint64_t mine[(CAP + NT - 1) / NT];
 #pragma unroll
     for (int j = 0; j < (CAP + NT - 1) / NT; ++j) {
       const int i = tid + j * NT;
       mine[j] = i < n ? cand[i] : 0;
-      if (!(i < n && mine[j] >= prefix)) mine[j] = 0;                      // (no key is 0: a token is below 2^31)
+      if (!(i < n && mine[j] >= least)) mine[j] = 0;                       // (no key is 0: a token is below 2^31)
     }
     if (tid == 0) sm->pick[0] = 0;
     __syncthreads();
@@ -172,27 +191,7 @@ __device__ __noinline__ void cut(Smem<NT>* sm, uint64_t* cand, int n, int k) {
   // ranks by counting; with few candidates several lanes share one
   if (n <= NT / 8) return rank_few<NT, 8>(cand, n, k);
   if (n <= NT / 4) return rank_few<NT, 4>(cand, n, k);
-  if (n <= NT / 2) return rank_few<NT, 2>(cand, n, k);
-  uint64_t a[LIST / NT];
-  int rank[LIST / NT];
-#pragma unroll
-  for (int j = 0; j < LIST / NT; ++j) {
-    const int i = tid + j * NT;
-    rank[j] = 0x7fffffff;
-    a[j] = 0;
-    if (i < n) {
-      a[j] = cand[i];
-      int r = 0;
-#pragma unroll 4
-      for (int o = 0; o < n; ++o) r += cand[o] > a[j] ? 1 : 0;
-      rank[j] = r;
-    }
-  }
-  __syncthreads();
-#pragma unroll
-  for (int j = 0; j < LIST / NT; ++j)
-    if (rank[j] < k) cand[rank[j]] = a[j];
-  __syncthreads();
+  rank_few<NT, 2>(cand, n, k);
 }
 
 __device__ __forceinline__ float4 join(float4 a, float4 b) {               // (m, S, T)
