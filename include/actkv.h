@@ -605,8 +605,8 @@ int actkv_debug_inject_stall(int32_t after_tile, int32_t wait_limit_us);
  * infinite or NaN.
  * Logits, maxima, sums and the output's accumulation are float32; the probabilities enter the
  * product with V as two bf16 summands (16 bits of mantissa), so that the output is as good as a
- * float32 computation rounded once.  The result does not depend on anything but the arguments and
- * the number of SMs: no atomics, a fixed order of the sums.
+ * float32 computation rounded once.  Equal arguments (the host's bounds among them, which decide how the work is
+ * split) give equal bits: no atomics, a fixed order of the sums.
  * q, out     bf16 [NLs, sum_win, n_q_heads, head_dim], NLs = layer_end - layer_begin; may not overlap.
  * win_indptr int32 [n_req+1]; W_r = 0: the request is skipped.  lse_out float32 [NLs, sum_win, n_q_heads].
  * sum_win, max_win, max_tok: host copies (upper bounds are accepted) of win_indptr[n_req], max W_r, max L_r:

@@ -49,6 +49,13 @@ def test_attend_refuses_a_short_workspace_and_takes_empty_calls():
     assert B.actkv_attend_workspace_bytes(_pool(), 2, 1, 8, 2, 50) > 0
 
 
+def test_sizes_beyond_the_index_types_are_refused():
+    assert _attend(max_tok=(1 << 30) + 1) == B.E_TOOBIG
+    assert _attend(max_win=1 << 23, rows=1 << 23) == B.E_TOOBIG
+    assert _attend(tab=_tab(n_req=4096), max_tok=1 << 30) == B.E_TOOBIG
+    assert B.load().actkv_resize(_pool(), _tab(n_req=1 << 16, max_pages=1 << 16), P, N, N) == B.E_TOOBIG
+
+
 def test_attend_workspace_of_a_layer_range_serves_fewer_layers():
     size = [B.actkv_attend_workspace_bytes(_pool(), 3, n, 8, 5, 50) for n in (1, 2, 4)]
     assert size == sorted(size)
