@@ -35,19 +35,25 @@ struct Args {
 // Where row i goes: element offset of its K slot within a layer and head 0, -1 when it is dropped.  One warp calls it.
 __device__ __forceinline__ int64_t place_of(const Args& a, int i) {
   const int lane = threadIdx.x & 31, R = a.tab.n_req;
+  const int32_t code = status_code(a.status);
   int n = 0;                                     // requests 1 .. R - 1 that begin at or before the row (empty ones among them)
   for (int r = 1 + lane; r < R; r += 32) n += a.win_indptr[r] <= i ? 1 : 0;
   const int r = (int)__reduce_add_sync(0xffffffffu, (uint32_t)n);
   const int w0 = a.win_indptr[r], w1 = a.win_indptr[r + 1], L = a.tab.seq_len[r];
   if (i < w0 || i >= w1) return -1;              // a row of no request
+  if (refused(a.status, code)) return -1;        // (L does not count the new tokens, after a resize that did nothing)
   const int64_t j = (int64_t)L - w1 + i;
   const int P = a.pool.page_size;
   if (j < 0 || j / P >= a.tab.max_pages) {
-    if (lane == 0) report(a.status, ACTKV_E_INVALID, r, L);
+    if (lane == 0) report_row(a.status, ACTKV_E_INVALID, r, L);
     return -1;
   }
-  const int page = page_or_neg(a.tab, a.pool.n_pages, r, (int)(j / P), a.status);
-  return page < 0 ? -1 : (int64_t)page * a.pool.stride_page + (j % P) * a.pool.stride_slot;
+  const int32_t page = a.tab.page_table[(int64_t)r * a.tab.max_pages + (int)(j / P)];
+  if ((uint32_t)page >= (uint32_t)a.pool.n_pages) {
+    if (lane == 0) report_row(a.status, ACTKV_E_BADPAGE, r, page);
+    return -1;
+  }
+  return (int64_t)page * a.pool.stride_page + (j % P) * a.pool.stride_slot;
 }
 
 __device__ __forceinline__ float2 bf2(uint32_t v) { return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)); }

@@ -37,6 +37,26 @@ __device__ __forceinline__ bool status_set(const int32_t* status) {
   return status != nullptr && *((const volatile int32_t*)status) != 0;
 }
 
+// actkv_append and actkv_copy drop single rows and pages and carry out the rest, in one launch: an error that a CTA finds there must not
+// stop the CTAs that begin after it, one of an earlier call must stop them all.  status[3] tells the two apart: ACTKV_STATUS_ROWS while
+// status[0] comes from a dropped row or page (written before the code, looked at behind it).  actkv_resize writes 0 there, so that nothing
+// that relies on a resize that did nothing is written either.  `code`: status[0], read beside the CTA's other first loads.
+__device__ __forceinline__ int32_t status_code(const int32_t* status) {
+  return status != nullptr ? *((const volatile int32_t*)status) : ACTKV_OK;
+}
+__device__ __forceinline__ bool refused(const int32_t* status, int32_t code) {
+  if (code == ACTKV_OK) return false;
+  __threadfence();
+  return ((const volatile int32_t*)status)[3] != ACTKV_STATUS_ROWS;
+}
+// (only by calls that were not refused: status[0] is 0 or another row's error)
+__device__ __forceinline__ void report_row(int32_t* status, int32_t code, int32_t where, int32_t what) {
+  if (status == nullptr) return;
+  ((volatile int32_t*)status)[3] = ACTKV_STATUS_ROWS;
+  __threadfence();
+  report(status, code, where, what);
+}
+
 // Programmatic dependent launch.  A step is a chain of kernels of which many take a few microseconds; every one of them (but
 // the in-place copy, compact_inplace.cu) is launched while its predecessor on the stream still runs and begins here: it waits until that one has finished and its
 // writes are visible (and has, by the same rule, all kernels before it behind it), then allows the next launch.  What

@@ -181,6 +181,7 @@ __global__ void __launch_bounds__(NT) resize_kernel(TablesView tab, int32_t P, i
       }
     if (rank == 0 && tid == 0) *tab.free_count = (int32_t)(fc - pops + pushes);
   }
+  if (rank == 0 && tid == 0 && status != nullptr) status[3] = 0;
   if constexpr (CS > 1) cg::this_cluster().sync();                        // (flags are read from one another's shared memory)
 }
 
@@ -223,20 +224,23 @@ struct CopySmem {
 };
 struct CopySource {
   int src, len, page, col;
+  bool stop;                     // an earlier call has failed (each thread's own look: copy_branches makes it the CTA's)
 };
 // The source of pair i, for logical page lp; false: nothing to do.  `first`: one CTA of every pair, which reports what is wrong with it.
 template <int NT>
 __device__ __forceinline__ bool copy_source(const CopyArgs& a, int i, int lp, bool first, CopySource& s) {
   const int tid = threadIdx.x;
+  const int32_t code = status_code(a.status);
   s.src = a.src[i];
+  s.stop = refused(a.status, code);
   if ((uint32_t)s.src >= (uint32_t)a.tab.n_req) {
-    if (first && tid == 0) report(a.status, ACTKV_E_INVALID, i, s.src);
+    if (first && tid == 0 && !s.stop) report_row(a.status, ACTKV_E_INVALID, i, s.src);
     return false;
   }
-  if (first) {
+  if (first && !s.stop) {
     const int d = a.dst[i];
     for (int j = tid; j < a.n_copy; j += NT)
-      if (j != i && (a.dst[j] == d || a.src[j] == d)) report(a.status, ACTKV_E_INVALID, i, d);
+      if (j != i && (a.dst[j] == d || a.src[j] == d)) report_row(a.status, ACTKV_E_INVALID, i, d);
   }
   s.col = lp < a.tab.max_pages ? lp : a.tab.max_pages - 1;                 // (max_len may be beyond the table; no sound pair is)
   s.page = a.tab.max_pages > 0 ? a.tab.page_table[(int64_t)s.src * a.tab.max_pages + s.col] : -1;
@@ -252,7 +256,7 @@ __device__ __forceinline__ int copy_branches(const CopyArgs& a, int i, int j0, i
   __syncthreads();
   const int j = j0 + tid;
   bool sound = false;
-  if (j < a.n_copy && (j == i || a.src[j] == s.src)) {
+  if (!s.stop && j < a.n_copy && (j == i || a.src[j] == s.src)) {
     const int d = a.dst[j], n = a.length[j];
     if ((uint32_t)d < (uint32_t)a.tab.n_req && d != s.src && n >= 0 && n <= a.max_len) {
       const int dst_len = a.tab.seq_len[d], page = a.tab.max_pages > 0 ? a.tab.page_table[(int64_t)d * a.tab.max_pages + s.col] : -1;
@@ -265,14 +269,14 @@ __device__ __forceinline__ int copy_branches(const CopyArgs& a, int i, int j0, i
           sm->dst[at] = (int64_t)page * a.pool.stride_page;
           sm->slots[at] = slots;
         } else {
-          report(a.status, ACTKV_E_BADPAGE, src_ok ? d : s.src, src_ok ? page : s.page);
+          report_row(a.status, ACTKV_E_BADPAGE, src_ok ? d : s.src, src_ok ? page : s.page);
         }
       }
     }
-    if (j == i && !sound && first) report(a.status, ACTKV_E_INVALID, i, n);
+    if (j == i && !sound && first) report_row(a.status, ACTKV_E_INVALID, i, n);
   }
   // (an unsound pair copies nothing itself; when it comes first, the next sound one works for the rest)
-  if (__syncthreads_or((sound && j < i) || (j == i && !sound))) return -1;
+  if (__syncthreads_or(s.stop || (sound && j < i) || (j == i && !sound))) return -1;
   return j0 + NT > i && sm->n > 0 ? 1 : 0;
 }
 __device__ __forceinline__ __nv_bfloat16* copy_base(const CopyArgs& a) {
