@@ -771,7 +771,7 @@ int actkv_attend(const actkv_pool_t* pool, const actkv_tables_t* tables, int32_t
   a.page_shift = (pool->page_size & (pool->page_size - 1)) == 0 ? __builtin_ctz((unsigned)pool->page_size) : -1;
   a.scale_log2 = sm_scale * kLog2e;
   a.causal = causal;
-  a.win_left = window_left;
+  a.win_left = std::min(window_left, max_tok + max_win);                   // (no row looks back further, and positions minus this stay in 32 bits)
   const int64_t bound = lay.units * std::max<int64_t>(1, ((int64_t)max_tok + KT - 1) / KT);
   cudaStream_t s = (cudaStream_t)stream;
   if (tc)
