@@ -606,7 +606,7 @@ int actkv_debug_inject_stall(int32_t after_tile, int32_t wait_limit_us);
  * A row that sees no key (W_r > L_r, L_r = 0), or whose logits are all -inf, gets out = 0 and
  * lse = -inf.  What a masked or unused slot holds (infinities and NaN too) does not reach any row.  A
  * logit that is NaN or +inf makes its row NaN; a visible V entry that is infinite or NaN makes its dim of the row
- * infinite or NaN.
+ * infinite or NaN, also where the entry's probability is 0 in float32 or its logit is -inf.
  * Logits, maxima, sums and the output's accumulation are float32; the probabilities enter the
  * product with V as two bf16 summands (16 bits of mantissa), so that the output is as good as a
  * float32 computation rounded once.  Equal arguments (the host's bounds among them, which decide how the work is

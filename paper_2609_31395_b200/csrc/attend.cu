@@ -247,6 +247,7 @@ __global__ void __launch_bounds__((Cfg<DP, NT, RG, PER_SM, WARPS>::NTH), (Cfg<DP
         for (int c = 0; c < 4; ++c) s[n][c] *= a.scale_log2;
       const int key0 = tile * KT;
       const bool masked = key0 + KT - 1 > all_hi || key0 < all_lo;
+      uint32_t hidden = 0;                                                 // bit 4 n + c: s[n][c] is of a key that its row does not see
       if (masked) {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -254,7 +255,10 @@ __global__ void __launch_bounds__((Cfg<DP, NT, RG, PER_SM, WARPS>::NTH), (Cfg<DP
           for (int c = 0; c < 4; ++c) {
             const int key = key0 + g + (c >> 1) * 8;
             const int pos = pos0 + step * ((row0 + n * 8 + t2 + (c & 1)) / G);
-            if (key > pos || (a.win_left > 0 && key <= pos - a.win_left)) s[n][c] = -INFINITY;
+            if (key > pos || (a.win_left > 0 && key <= pos - a.win_left)) {
+              s[n][c] = -INFINITY;
+              hidden |= 1u << (4 * n + c);
+            }
           }
       }
       // the references, when some logit has left them behind
@@ -289,7 +293,8 @@ __global__ void __launch_bounds__((Cfg<DP, NT, RG, PER_SM, WARPS>::NTH), (Cfg<DP
           s[n][c] = exp2f(s[n][c] - m[n][c & 1]);
           l[n][c & 1] += s[n][c];
         }
-      // V of a tile that not every row sees whole: an infinity or NaN there must not meet a probability of 0 in a product
+      // V of a tile that not every row sees whole: an infinity or NaN there must not meet a hidden key's 0 in a product.  (A row that
+      // sees the key takes it whatever its probability: one that is 0 in float32 makes a NaN, as it does in every other tile.)
       const uint32_t vs_addr = ks_addr + C::TILE / 2;
       if (masked) {
         bool odd = false;
@@ -302,6 +307,7 @@ __global__ void __launch_bounds__((Cfg<DP, NT, RG, PER_SM, WARPS>::NTH), (Cfg<DP
         if (__any_sync(0xffffffffu, odd)) {
 #pragma unroll 1
           for (int kk = 0; kk < KT; ++kk) {
+            const uint32_t hid = __shfl_sync(0xffffffffu, hidden, (kk & 7) * 4 + (lane & 3)) >> (kk < 8 ? 0 : 2);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
               const float p0 = __shfl_sync(0xffffffffu, kk < 8 ? s[n][0] : s[n][2], (kk & 7) * 4 + (lane & 3));
@@ -313,8 +319,8 @@ __global__ void __launch_bounds__((Cfg<DP, NT, RG, PER_SM, WARPS>::NTH), (Cfg<DP
                   uint16_t raw;
                   asm volatile("ld.shared.u16 %0, [%1];" : "=h"(raw) : "r"(vs_addr + kk * DP * 2 + (((2 * mt + hf) ^ (kk & 7)) << 4) + g * 2) : "memory");
                   const float v = __uint_as_float((uint32_t)raw << 16);
-                  if (p0 != 0.f) acc[mt][n][2 * hf] = fmaf(p0, v, acc[mt][n][2 * hf]);
-                  if (p1 != 0.f) acc[mt][n][2 * hf + 1] = fmaf(p1, v, acc[mt][n][2 * hf + 1]);
+                  if (!(hid >> (4 * n) & 1u)) acc[mt][n][2 * hf] = fmaf(p0, v, acc[mt][n][2 * hf]);
+                  if (!(hid >> (4 * n) & 2u)) acc[mt][n][2 * hf + 1] = fmaf(p1, v, acc[mt][n][2 * hf + 1]);
                 }
             }
           }

@@ -286,7 +286,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tc_kernel(const __grid_cons
         }
         if (masked) {
           // V of a key that some row must not see, or of a slot behind the end: infinities and NaN leave the product; what they make of the
-          // rows that do see the key is noted
+          // rows that do see the key, whatever its probability there, is noted
           const uint32_t sl = t % T::STAGES;
           // (unguarded by the others: a wait of this thread alone; the entry stays until this tile's product)
           if (!mbar_wait(smem_u32(&ctl->full[1][sl]), (t / T::STAGES) & 1, abort_flag, limit)) dead = true;
@@ -303,9 +303,10 @@ __global__ void __launch_bounds__(THREADS, 1) attend_tc_kernel(const __grid_cons
               *el = 0;
               const bool nan = (bits & 0x7fu) != 0, neg = (bits & 0x8000u) != 0;
               const int d = c * 8 + k;
-#pragma unroll
+#pragma unroll 1
               for (int n = 0; n < NR; ++n) {
-                if (!(x[n] > 0.f)) continue;
+                const int pos = ctl->pos[n];
+                if (key > pos || (a.win_left > 0 && key <= pos - a.win_left)) continue;
                 if (nan || !neg) atomicOr(&ctl->poison[0][n][d >> 5], 1u << (d & 31));
                 if (nan || neg) atomicOr(&ctl->poison[1][n][d >> 5], 1u << (d & 31));
                 ctl->poisoned = 1;
