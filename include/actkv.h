@@ -603,8 +603,8 @@ int actkv_debug_inject_stall(int32_t after_tile, int32_t wait_limit_us);
  * causal != 0: the window is the last W_r cached tokens (append them first), row w sees
  * j <= L_r - W_r + w; causal == 0: every row sees every key.  window_left = S > 0 (sliding-window
  * layers): only the S keys up to the row's own position count, as in actkv_score_sliding.
- * A row that sees no key (W_r > L_r, L_r = 0), or whose logits are all -inf, gets out = 0 and
- * lse = -inf.  What a masked or unused slot holds (infinities and NaN too) does not reach any row.  A
+ * A row that sees no key (W_r > L_r, L_r = 0), or whose logits are all -inf, gets lse = -inf and, over finite V entries,
+ * out = 0.  What a masked or unused slot holds (infinities and NaN too) does not reach any row.  A
  * logit that is NaN or +inf makes its row NaN; a visible V entry that is infinite or NaN makes its dim of the row
  * infinite or NaN, also where the entry's probability is 0 in float32 or its logit is -inf.
  * Logits, maxima, sums and the output's accumulation are float32; the probabilities enter the

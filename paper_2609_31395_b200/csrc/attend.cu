@@ -548,7 +548,7 @@ __global__ void __launch_bounds__(JN) attend_join_kernel(const __grid_constant__
     float v = 0.f;
 #pragma unroll
     for (int k = 0; k < JN / 32; ++k) v += s_red[k][tid];
-    a.out[at * D + tid] = __float2bfloat16_rn(sum == 0.f ? 0.f : v / sum);
+    a.out[at * D + tid] = __float2bfloat16_rn(sum == 0.f ? v * 0.f : v / sum);    // (0, or NaN where V has it)
   }
   if (tid == 0 && a.lse != nullptr) a.lse[at] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
 }
