@@ -226,6 +226,10 @@ struct CopySource {
   int src, len, page, col;
   bool stop;                     // an earlier call has failed (each thread's own look: copy_branches makes it the CTA's)
 };
+__device__ __forceinline__ bool sound_pair(const CopyArgs& a, int src, int src_len, int dst, int n) {
+  return (uint32_t)dst < (uint32_t)a.tab.n_req && dst != src && n >= 0 && n <= a.max_len && n <= src_len && n <= a.tab.seq_len[dst] &&
+         (n == 0 || (n - 1) / a.pool.page_size < a.tab.max_pages);
+}
 // The source of pair i, for logical page lp; false: nothing to do.  `first`: one CTA of every pair, which reports what is wrong with it.
 template <int NT>
 __device__ __forceinline__ bool copy_source(const CopyArgs& a, int i, int lp, bool first, CopySource& s) {
@@ -237,19 +241,20 @@ __device__ __forceinline__ bool copy_source(const CopyArgs& a, int i, int lp, bo
     if (first && tid == 0 && !s.stop) report_row(a.status, ACTKV_E_INVALID, i, s.src);
     return false;
   }
-  if (first && !s.stop) {
-    const int d = a.dst[i];
-    for (int j = tid; j < a.n_copy; j += NT)
-      if (j != i && (a.dst[j] == d || a.src[j] == d)) report_row(a.status, ACTKV_E_INVALID, i, d);
-  }
   s.col = lp < a.tab.max_pages ? lp : a.tab.max_pages - 1;                 // (max_len may be beyond the table; no sound pair is)
   s.page = a.tab.max_pages > 0 ? a.tab.page_table[(int64_t)s.src * a.tab.max_pages + s.col] : -1;
   s.len = a.tab.seq_len[s.src];
+  if (first && !s.stop) {                                                  // (here, not where branches are looked for: that ends early)
+    const int d = a.dst[i], n = a.length[i];
+    if (tid == 0 && !sound_pair(a, s.src, s.len, d, n)) report_row(a.status, ACTKV_E_INVALID, i, n);
+    for (int j = tid; j < a.n_copy; j += NT)
+      if (j != i && (a.dst[j] == d || a.src[j] == d)) report_row(a.status, ACTKV_E_INVALID, i, d);
+  }
   return true;
 }
 // Branches among pairs j0 .. j0 + NT - 1 into sm: 1, none of them this CTA's business: 0, another CTA works for this source: -1.
 template <int NT>
-__device__ __forceinline__ int copy_branches(const CopyArgs& a, int i, int j0, int lp, bool first, const CopySource& s, CopySmem<NT>* sm) {
+__device__ __forceinline__ int copy_branches(const CopyArgs& a, int i, int j0, int lp, const CopySource& s, CopySmem<NT>* sm) {
   const int tid = threadIdx.x, P = a.pool.page_size;
   __syncthreads();
   if (tid == 0) sm->n = 0;
@@ -258,9 +263,9 @@ __device__ __forceinline__ int copy_branches(const CopyArgs& a, int i, int j0, i
   bool sound = false;
   if (!s.stop && j < a.n_copy && (j == i || a.src[j] == s.src)) {
     const int d = a.dst[j], n = a.length[j];
-    if ((uint32_t)d < (uint32_t)a.tab.n_req && d != s.src && n >= 0 && n <= a.max_len) {
-      const int dst_len = a.tab.seq_len[d], page = a.tab.max_pages > 0 ? a.tab.page_table[(int64_t)d * a.tab.max_pages + s.col] : -1;
-      sound = n <= s.len && n <= dst_len && (n == 0 || (n - 1) / P < a.tab.max_pages);
+    if ((uint32_t)d < (uint32_t)a.tab.n_req) {
+      const int page = a.tab.max_pages > 0 ? a.tab.page_table[(int64_t)d * a.tab.max_pages + s.col] : -1;     // (beside its length)
+      sound = sound_pair(a, s.src, s.len, d, n);
       const int slots = min(P, n - lp * P);
       if (sound && j >= i && slots > 0) {
         const bool src_ok = (uint32_t)s.page < (uint32_t)a.pool.n_pages, dst_ok = (uint32_t)page < (uint32_t)a.pool.n_pages;
@@ -273,7 +278,6 @@ __device__ __forceinline__ int copy_branches(const CopyArgs& a, int i, int j0, i
         }
       }
     }
-    if (j == i && !sound && first) report_row(a.status, ACTKV_E_INVALID, i, n);
   }
   // (an unsound pair copies nothing itself; when it comes first, the next sound one works for the rest)
   if (__syncthreads_or(s.stop || (sound && j < i) || (j == i && !sound))) return -1;
@@ -305,7 +309,7 @@ __global__ void __launch_bounds__(CB_NT) copy_bulk_kernel(const __grid_constant_
   const int held = min(CB_BYTES, min(a.pool.page_size, s.len - lp * a.pool.page_size) * slot_bytes - begin);    // bytes of the source
   bool here = false, lost = false;
   for (int j0 = 0; j0 < a.n_copy; j0 += CB_NT) {
-    const int what = copy_branches<CB_NT>(a, i, j0, lp, first, s, &sm);
+    const int what = copy_branches<CB_NT>(a, i, j0, lp, s, &sm);
     if (what < 0) break;
     if (what == 0 || threadIdx.x != 0 || held <= 0 || lost) continue;
     if (!here) {                                               // once: all of the part that the source has
@@ -344,7 +348,7 @@ __global__ void __launch_bounds__(CP_NT) copy_kernel(const __grid_constant__ Cop
   if (!copy_source<CP_NT>(a, i, lp, first, s)) return;
   __nv_bfloat16* base = copy_base(a);
   for (int j0 = 0; j0 < a.n_copy; j0 += CP_NT) {
-    const int what = copy_branches<CP_NT>(a, i, j0, lp, first, s, &sm);
+    const int what = copy_branches<CP_NT>(a, i, j0, lp, s, &sm);
     if (what < 0) return;
     if (what == 0) continue;
     const int n = sm.n;
