@@ -639,21 +639,35 @@ def actkv_copy(pool: PoolDesc, tables: TablesDesc, layer_begin, layer_end, src, 
 _LOGIT_TYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 
+def _result_rows(t, n, width, name):
+    """The width of a result buffer [n or more, width] (width None: any); [n] is [n, 1]."""
+    shape = None if t is None else t.shape
+    if shape == (n,):
+        shape = (n, 1)
+    if shape is None or len(shape) != 2 or shape[0] < n or (width is not None and shape[1] != width):
+        raise ValueError(f"{name}: expected [{n} or more, {'any' if width is None else width}], got {None if shape is None else list(shape)}")
+    return shape[1]
+
+
 def actkv_logprob(logits, given, logprob, entropy, lse, top_logprob, top_index, status, stream=None):
-    """logits [rows, vocab] float32 or bf16, rows any distance apart; given int32 [rows, n] or None; top_logprob /
-    top_index [rows, k] or None."""
+    """logits [rows, vocab] float32 or bf16, rows any distance apart; given int32 [rows, n] or None.  Results: logprob [rows, n],
+    entropy and lse [rows], top_logprob and top_index [rows, k], each with room for that many rows or more, or None."""
     i = _cuda_index(logits, "logits")
     kind = _LOGIT_TYPES.get(logits.dtype)
     st = logits.stride()
     if kind is None or len(st) != 2 or (st[1] != 1 and logits.shape[1] != 1):
         raise TypeError("logits: expected float32 or bf16 [rows, vocab] with contiguous rows")
     n, vocab = logits.shape
-    n_given = 0 if given is None or n == 0 else given.numel() // n
-    top_k = 0 if top_index is None or n == 0 else top_index.numel() // n
-    if n_given and (given.numel() != n * n_given or logprob is None or logprob.numel() != given.numel()):
-        raise ValueError("given, logprob: expected [rows, n]")
-    if top_k and (top_index.numel() != n * top_k or top_logprob is None or top_logprob.numel() != top_index.numel()):
-        raise ValueError("top_logprob, top_index: expected [rows, k]")
+    n_given = top_k = 0
+    if given is not None:
+        n_given = _result_rows(given, n, None, "given")
+        if given.shape[0] != n:
+            raise ValueError(f"given: {given.shape[0]} rows for {n} rows of logits")
+        if n_given:
+            _result_rows(logprob, n, n_given, "logprob")
+    if top_index is not None or top_logprob is not None:
+        top_k = _result_rows(top_index, n, None, "top_index")
+        _result_rows(top_logprob, n, top_k, "top_logprob")
     _call("actkv_logprob", i, stream, logits.data_ptr(), kind, n, vocab, st[0] if n > 1 else vocab,
           _arg(given, torch.int32, i, 0, "given"), n_given, top_k, _arg(logprob, torch.float32, i, 0, "logprob"),
           _arg(entropy, torch.float32, i, n, "entropy"), _arg(lse, torch.float32, i, n, "lse"),
