@@ -47,6 +47,7 @@ __device__ __forceinline__ uint32_t okey(float x) {
   if (b == 0x80000000u) b = 0u;                                            // -0 and +0 are equal
   return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
 }
+constexpr uint32_t LEAST_ZERO = ~0x807fffffu;                              // okey of the negative subnormal furthest from 0
 __device__ __forceinline__ float okey_inv(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? (k & 0x7fffffffu) : ~k); }
 __device__ __forceinline__ uint64_t key_of(float x, uint32_t token) { return ((uint64_t)okey(x) << 32) | (0xffffffffu - token); }
 
@@ -381,7 +382,8 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprob_kernel(const Args a) {
       }
 #pragma unroll
       for (int d = 1; d < TG; d <<= 1) rank += __shfl_xor_sync(0xffffffffu, rank, d);
-      if (rank == k - 1 && tid % TG == 0) sm->thr = v == -INFINITY ? 0u : okey(v);
+      // (maxima are flushed: one that is 0 may stand for any subnormal logit, while candidates are compared by their bits)
+      if (rank == k - 1 && tid % TG == 0) sm->thr = v == -INFINITY ? 0u : v == 0.f ? LEAST_ZERO : okey(v);
     }
     __syncthreads();
     const uint32_t thr = sm->thr;
