@@ -664,6 +664,7 @@ typedef struct {
  *   q_out[l, i, qh, :] = rotate(q[l, i, qh, :]).
  * The angle is formed and reduced to half a turn in float64, sine and cosine in float32; products in float32,
  * rounded once to bf16.
+ * Rows of no request (a padded batch: sum_win above win_indptr[n_req]) are left as they are, in q_out too.
  * q may be NULL (then q_out is not written); q_out bf16 [NLs, sum_win, n_q_heads, head_dim], which may be
  * the memory of q when q lies that way, and overlaps nothing else.  rope NULL: nothing turns, positions
  * is not read.  positions int32 [n_axes, sum_win].

@@ -32,7 +32,9 @@ struct Args {
   int32_t pairs, interleaved, n_axes, sec_end[4];
 };
 
-// Where row i goes: element offset of its K slot within a layer and head 0, -1 when it is dropped.  One warp calls it.
+// Where row i goes: element offset of its K slot within a layer and head 0, -1 when it is dropped, NO_ROW for a row of no request.
+// One warp calls it.
+constexpr int64_t NO_ROW = -2;
 __device__ __forceinline__ int64_t place_of(const Args& a, int i) {
   const int lane = threadIdx.x & 31, R = a.tab.n_req;
   const int32_t code = status_code(a.status);
@@ -40,7 +42,7 @@ __device__ __forceinline__ int64_t place_of(const Args& a, int i) {
   for (int r = 1 + lane; r < R; r += 32) n += a.win_indptr[r] <= i ? 1 : 0;
   const int r = (int)__reduce_add_sync(0xffffffffu, (uint32_t)n);
   const int w0 = a.win_indptr[r], w1 = a.win_indptr[r + 1], L = a.tab.seq_len[r];
-  if (i < w0 || i >= w1) return -1;              // a row of no request
+  if (i < w0 || i >= w1) return NO_ROW;
   if (refused(a.status, code)) return -1;        // (L does not count the new tokens, after a resize that did nothing)
   const int64_t j = (int64_t)L - w1 + i;
   const int P = a.pool.page_size;
@@ -92,6 +94,7 @@ __global__ void __launch_bounds__(NT) append_kernel(const Args a) {
   }
   __syncthreads();
   const int64_t place = s_place;
+  if (place == NO_ROW) return;
   const __nv_bfloat16* qr = a.q.base + (int64_t)layer * a.q.stride_layer + (int64_t)i * a.q.stride_row;
   const __nv_bfloat16* kr = a.k.base + (int64_t)layer * a.k.stride_layer + (int64_t)i * a.k.stride_row;
   const __nv_bfloat16* vr = a.v.base + (int64_t)layer * a.v.stride_layer + (int64_t)i * a.v.stride_row;
