@@ -43,16 +43,13 @@ __device__ __forceinline__ int64_t place_of(const Args& a, int i) {
   const int r = (int)__reduce_add_sync(0xffffffffu, (uint32_t)n);
   const int w0 = a.win_indptr[r], w1 = a.win_indptr[r + 1], L = a.tab.seq_len[r];
   if (i < w0 || i >= w1) return NO_ROW;
-  if (refused(a.status, code)) return -1;        // (L does not count the new tokens, after a resize that did nothing)
   const int64_t j = (int64_t)L - w1 + i;
   const int P = a.pool.page_size;
-  if (j < 0 || j / P >= a.tab.max_pages) {
-    if (lane == 0) report_row(a.status, ACTKV_E_INVALID, r, L);
-    return -1;
-  }
-  const int32_t page = a.tab.page_table[(int64_t)r * a.tab.max_pages + (int)(j / P)];
+  const bool out = j < 0 || j / P >= a.tab.max_pages;
+  const int32_t page = out ? -1 : a.tab.page_table[(int64_t)r * a.tab.max_pages + (int)(j / P)];
+  if (refused(a.status, code)) return -1;        // (after a resize that did nothing L does not count the new tokens)
   if ((uint32_t)page >= (uint32_t)a.pool.n_pages) {
-    if (lane == 0) report_row(a.status, ACTKV_E_BADPAGE, r, page);
+    if (lane == 0) report_row(a.status, out ? ACTKV_E_INVALID : ACTKV_E_BADPAGE, r, out ? L : page);
     return -1;
   }
   return (int64_t)page * a.pool.stride_page + (j % P) * a.pool.stride_slot;

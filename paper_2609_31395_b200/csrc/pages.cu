@@ -224,29 +224,29 @@ struct CopySmem {
 };
 struct CopySource {
   int src, len, page, col;
-  bool stop;                     // an earlier call has failed (each thread's own look: copy_branches makes it the CTA's)
+  int32_t code;                  // status_code
 };
-__device__ __forceinline__ bool sound_pair(const CopyArgs& a, int src, int src_len, int dst, int n) {
-  return (uint32_t)dst < (uint32_t)a.tab.n_req && dst != src && n >= 0 && n <= a.max_len && n <= src_len && n <= a.tab.seq_len[dst] &&
-         (n == 0 || (n - 1) / a.pool.page_size < a.tab.max_pages);
+// (dst is a request, of dst_len tokens)
+__device__ __forceinline__ bool sound_pair(const CopyArgs& a, int src, int src_len, int dst, int dst_len, int n) {
+  return dst != src && n >= 0 && n <= a.max_len && n <= src_len && n <= dst_len && (n == 0 || (n - 1) / a.pool.page_size < a.tab.max_pages);
 }
 // The source of pair i, for logical page lp; false: nothing to do.  `first`: one CTA of every pair, which reports what is wrong with it.
 template <int NT>
 __device__ __forceinline__ bool copy_source(const CopyArgs& a, int i, int lp, bool first, CopySource& s) {
   const int tid = threadIdx.x;
-  const int32_t code = status_code(a.status);
+  s.code = status_code(a.status);
   s.src = a.src[i];
-  s.stop = refused(a.status, code);
   if ((uint32_t)s.src >= (uint32_t)a.tab.n_req) {
-    if (first && tid == 0 && !s.stop) report_row(a.status, ACTKV_E_INVALID, i, s.src);
+    if (first && tid == 0 && !refused(a.status, s.code)) report_row(a.status, ACTKV_E_INVALID, i, s.src);
     return false;
   }
   s.col = lp < a.tab.max_pages ? lp : a.tab.max_pages - 1;                 // (max_len may be beyond the table; no sound pair is)
   s.page = a.tab.max_pages > 0 ? a.tab.page_table[(int64_t)s.src * a.tab.max_pages + s.col] : -1;
   s.len = a.tab.seq_len[s.src];
-  if (first && !s.stop) {                                                  // (here, not where branches are looked for: that ends early)
+  if (first && !refused(a.status, s.code)) {                                                  // (here, not where branches are looked for: that ends early)
     const int d = a.dst[i], n = a.length[i];
-    if (tid == 0 && !sound_pair(a, s.src, s.len, d, n)) report_row(a.status, ACTKV_E_INVALID, i, n);
+    const bool known = (uint32_t)d < (uint32_t)a.tab.n_req;
+    if (tid == 0 && !(known && sound_pair(a, s.src, s.len, d, a.tab.seq_len[d], n))) report_row(a.status, ACTKV_E_INVALID, i, n);
     for (int j = tid; j < a.n_copy; j += NT)
       if (j != i && (a.dst[j] == d || a.src[j] == d)) report_row(a.status, ACTKV_E_INVALID, i, d);
   }
@@ -261,11 +261,11 @@ __device__ __forceinline__ int copy_branches(const CopyArgs& a, int i, int j0, i
   __syncthreads();
   const int j = j0 + tid;
   bool sound = false;
-  if (!s.stop && j < a.n_copy && (j == i || a.src[j] == s.src)) {
+  if (j < a.n_copy && (j == i || a.src[j] == s.src)) {
     const int d = a.dst[j], n = a.length[j];
     if ((uint32_t)d < (uint32_t)a.tab.n_req) {
-      const int page = a.tab.max_pages > 0 ? a.tab.page_table[(int64_t)d * a.tab.max_pages + s.col] : -1;     // (beside its length)
-      sound = sound_pair(a, s.src, s.len, d, n);
+      const int dst_len = a.tab.seq_len[d], page = a.tab.max_pages > 0 ? a.tab.page_table[(int64_t)d * a.tab.max_pages + s.col] : -1;
+      sound = sound_pair(a, s.src, s.len, d, dst_len, n);
       const int slots = min(P, n - lp * P);
       if (sound && j >= i && slots > 0) {
         const bool src_ok = (uint32_t)s.page < (uint32_t)a.pool.n_pages, dst_ok = (uint32_t)page < (uint32_t)a.pool.n_pages;
@@ -273,14 +273,14 @@ __device__ __forceinline__ int copy_branches(const CopyArgs& a, int i, int j0, i
           const int at = atomicAdd(&sm->n, 1);
           sm->dst[at] = (int64_t)page * a.pool.stride_page;
           sm->slots[at] = slots;
-        } else {
+        } else if (!refused(a.status, s.code)) {
           report_row(a.status, ACTKV_E_BADPAGE, src_ok ? d : s.src, src_ok ? page : s.page);
         }
       }
     }
   }
   // (an unsound pair copies nothing itself; when it comes first, the next sound one works for the rest)
-  if (__syncthreads_or(s.stop || (sound && j < i) || (j == i && !sound))) return -1;
+  if (__syncthreads_or((sound && j < i) || (j == i && !sound) || refused(a.status, s.code))) return -1;
   return j0 + NT > i && sm->n > 0 ? 1 : 0;
 }
 __device__ __forceinline__ __nv_bfloat16* copy_base(const CopyArgs& a) {
