@@ -66,7 +66,8 @@ struct Cfg {
   static constexpr int NG = NW / RG;
   static constexpr int RB = 8 * NT * RG;                                   // rows of a block
   static constexpr int TILE = KT * DP * 2 * 2;                             // bytes: K and V
-  // CTAs per SM, as many as registers allow without spilling; they share what the rings may take.  (8 rows, 35000 x 8 tokens of 128 dims:
+  // CTAs per SM, as many as registers allow (the variants of 32 rows a warp at 128 dims, and of 16 at 256, spill 20 to 44 bytes at the
+  // 255 that a thread has at most); they share what the rings may take.  (8 rows, 35000 x 8 tokens of 128 dims:
   // 98.8 us with two, 95 with three; 16000 x 16 of 64 dims: 121 with two, 94 with four.)
   static constexpr int CTAS = PER_SM > 0 ? PER_SM : DP > 128 ? 1 : NT > 1 ? 2 : DP == 64 ? 4 : 3;
   static constexpr int RING_MAX = 192 / CTAS * 1024;

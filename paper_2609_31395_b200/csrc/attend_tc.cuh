@@ -17,8 +17,10 @@
 // those for O, warps 12-15 load.  K and V have a ring each, S and P two buffers, one for each warpgroup; S runs ahead of the softmax by up
 // to two tiles.  All waits are bounded; one that gives up raises a flag that ends every role (ACTKV_E_TIMEOUT).
 //
-// What bounds it: reading K and V (up to 64 rows and 128 dims).  Shared memory comes next: a tile's operands are read by the MMAs
-// once each (64 rows, 128 dims: 1150 cycles of 2850 that the tile's bytes take to arrive).
+// What bounds it: reading K and V up to 32 rows (128 dims: 101 us where 8 rows in the other kernel take 89); beyond, the softmax: a warpgroup
+// takes 4250 cycles for a tile of 64 columns, 2100 with two of them, against 1425 (64 dims) that the tile's bytes take to arrive.  8192
+// exponentials are 512 of those cycles; the columns behind the last row of a block are computed all the same (a block of 33 rows costs
+// as much as one of 64), and the 64-row variants spill (412 to 420 bytes stored, 244 to 248 loaded per thread; 32 rows: none).
 #pragma once
 
 #include "attend_line.cuh"

@@ -203,10 +203,10 @@ __device__ __forceinline__ float4 join(float4 a, float4 b) {               // (m
   return make_float4(m, a.y * fa + b.y * fb, (a.z + da * a.y) * fa + (b.z + db * b.y) * fb, 0.f);
 }
 
-// Second reading of a row's part, for the top k of rows whose candidates do not fit the list: a vector per thread and step, the list
-// cut to the k largest whenever more than TIGHT are in it.  Logits below the image `thr` are none of them.
+// Second reading of a row's part, for the top k of rows whose candidates do not fit the list: the logits of a vector per thread and step,
+// one by one, the list cut to the k largest whenever more than TIGHT are in it.  Logits below the image `thr` are none of them.
 template <int NT, typename T>
-__device__ __noinline__ int top_again(Smem<NT>* sm, const T* z, const uint4* zv, int mis, int vocab, int v0, int v1, int k, uint32_t thr) {
+__device__ __noinline__ int top_again(Smem<NT>* sm, const T* z, int mis, int vocab, int v0, int v1, int k, uint32_t thr) {
   constexpr int VE = Vec<T>::N;
   const int tid = threadIdx.x;
   static_assert(NT * VE + TIGHT <= Smem<NT>::CAP, "a step fits");
@@ -418,7 +418,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprob_kernel(const Args a) {
       cut<NT>(sm, sm->list, (int)n, k);
       n_top = min((int)n, k);
     } else {
-      n_top = top_again<NT, T>(sm, z, zv, mis, vocab, v0, v1, k, thr);
+      n_top = top_again<NT, T>(sm, z, mis, vocab, v0, v1, k, thr);
     }
   }
   if constexpr (C > 1) {
