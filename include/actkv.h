@@ -23,9 +23,9 @@
  *     replaced by page 0 for the read and reported; a copy whose source or destination page id is
  *     out of range is dropped and reported (nothing is read from or written to a page the request
  *     does not own).  Once status[0] is set, actkv_select and the compaction calls of the same
- *     step do nothing, actkv_resize modifies nothing, and actkv_append and actkv_copy leave the cache as it
- *     is, unless the error is a row, pair or page that one of these two dropped itself (status[3] is then
- *     ACTKV_STATUS_ROWS, and no resize has been refused since).  The caller clears all four words together.  When the plan step of actkv_compact reports ACTKV_E_NOFREE the copy and
+ *     step do nothing and actkv_resize is refused; behind a refused resize (status[3] is then
+ *     ACTKV_STATUS_REFUSED) actkv_append and actkv_copy leave the cache as it is, until a resize is carried
+ *     out or the status cleared.  The caller clears all four words together.  When the plan step of actkv_compact reports ACTKV_E_NOFREE the copy and
  *     table-update steps of that call do nothing, so pool and tables stay unmodified.
  *   - All indices are int32.  Strides are in ELEMENTS (bf16), the head dimension is contiguous.
  *   - "unit" = one (layer, KV head, request); units are independent in score and select.
@@ -52,7 +52,7 @@ extern "C" {
 #define ACTKV_E_TIMEOUT    -7   /* device: a bounded wait inside a kernel gave up                */
 #define ACTKV_E_TOOBIG     -8   /* sizes beyond the fixed scratch of a *_noalloc entry point    */
 
-#define ACTKV_STATUS_ROWS   1   /* status[3]: status[0] is a row, pair or page dropped by actkv_append or actkv_copy */
+#define ACTKV_STATUS_REFUSED 1  /* status[3]: the last actkv_resize modified nothing             */
 
 /* CUDA stream handle (identical to cudaStream_t; spelled out so the header needs no CUDA). */
 typedef struct CUstream_st* actkv_stream_t;
@@ -669,9 +669,9 @@ typedef struct {
  * the memory of q when q lies that way, and overlaps nothing else.  rope NULL: nothing turns, positions
  * is not read.  positions int32 [n_axes, sum_win].
  * A row whose token falls outside its request (W_r > L_r) or table, or whose page id is out of range, is reported and
- * its K and V dropped; the other rows are carried out, in this call and in later ones.  When an earlier call has set
- * status[0] to anything else (an actkv_resize that was refused: seq_len does not count the new tokens), no K and V is
- * written; q_out is.  k, v and the pool may not overlap.
+ * its K and V dropped; the other rows are carried out.  Behind an actkv_resize that was refused (seq_len does not count the
+ * new tokens) no K and V is written; q_out is.  Other errors that status holds change nothing: on the next layers the
+ * tokens are needed all the same.  k, v and the pool may not overlap.
  */
 int actkv_append(const actkv_pool_t* pool /* host */, const actkv_tables_t* tables /* host */,
                  int32_t layer_begin, int32_t layer_end,
@@ -704,8 +704,8 @@ int actkv_resize(const actkv_pool_t* pool /* host */, const actkv_tables_t* tabl
  * require.  Tables are not touched.  Pairs that share a source read it once.
  * src, dst, length int32 [n_copy] (device); max_len: host upper bound on length.
  * A pair whose src, dst or length is out of range (length > seq_len of either, > max_len), with src == dst, or with
- * a bad page id is reported and dropped (a bad page: only that page); the others are carried out.  When an earlier call has
- * set status[0] to anything else, nothing is copied.  A request that occurs twice as dst, or both
+ * a bad page id is reported and dropped (a bad page: only that page); the others are carried out.  Behind an
+ * actkv_resize that was refused nothing is copied.  max_len = 0: nothing is looked at.  A request that occurs twice as dst, or both
  * as src and dst, is reported as ACTKV_E_INVALID; what its rows hold afterwards is unspecified.
  */
 int actkv_copy(const actkv_pool_t* pool /* host */, const actkv_tables_t* tables /* host */,

@@ -37,7 +37,7 @@ struct Args {
 constexpr int64_t NO_ROW = -2;
 __device__ __forceinline__ int64_t place_of(const Args& a, int i) {
   const int lane = threadIdx.x & 31, R = a.tab.n_req;
-  const int32_t code = status_code(a.status);
+  const int32_t stop = refused(a.status);
   int n = 0;                                     // requests 1 .. R - 1 that begin at or before the row (empty ones among them)
   for (int r = 1 + lane; r < R; r += 32) n += a.win_indptr[r] <= i ? 1 : 0;
   const int r = (int)__reduce_add_sync(0xffffffffu, (uint32_t)n);
@@ -47,9 +47,9 @@ __device__ __forceinline__ int64_t place_of(const Args& a, int i) {
   const int P = a.pool.page_size;
   const bool out = j < 0 || j / P >= a.tab.max_pages;
   const int32_t page = out ? -1 : a.tab.page_table[(int64_t)r * a.tab.max_pages + (int)(j / P)];
-  if (refused(a.status, code)) return -1;        // (after a resize that did nothing L does not count the new tokens)
+  if (stop) return -1;                           // (L does not count the new tokens)
   if ((uint32_t)page >= (uint32_t)a.pool.n_pages) {
-    if (lane == 0) report_row(a.status, out ? ACTKV_E_INVALID : ACTKV_E_BADPAGE, r, out ? L : page);
+    if (lane == 0) report(a.status, out ? ACTKV_E_INVALID : ACTKV_E_BADPAGE, r, out ? L : page);
     return -1;
   }
   return (int64_t)page * a.pool.stride_page + (j % P) * a.pool.stride_slot;

@@ -37,25 +37,13 @@ __device__ __forceinline__ bool status_set(const int32_t* status) {
   return status != nullptr && *((const volatile int32_t*)status) != 0;
 }
 
-// actkv_append and actkv_copy drop single rows and pages and carry out the rest, in one launch: an error that a CTA finds there must not
-// stop the CTAs that begin after it, one of an earlier call must stop them all.  status[3] tells the two apart: ACTKV_STATUS_ROWS while
-// status[0] comes from a dropped row or page (written before the code, looked at behind it).  actkv_resize writes 0 there, so that nothing
-// that relies on a resize that did nothing is written either.  `code`: status[0], read beside the CTA's other first loads and looked at
-// behind them.  (An ordinary load, as those are: it may miss an error of the same launch, which is not to stop anybody.  6 layers of 35000
-// tokens into 3 branches 279.1 us, without the look 276.7, with a volatile load that is looked at first 281.2; 8400 rows appended 38.9, 38.5
-// and 39.1.)
-__device__ __forceinline__ int32_t status_code(const int32_t* status) { return status != nullptr ? *status : ACTKV_OK; }
-__device__ __forceinline__ bool refused(const int32_t* status, int32_t code) {
-  if (code == ACTKV_OK) return false;
-  __threadfence();
-  return ((const volatile int32_t*)status)[3] != ACTKV_STATUS_ROWS;
-}
-// (only by calls that were not refused: status[0] is 0 or another row's error)
-__device__ __forceinline__ void report_row(int32_t* status, int32_t code, int32_t where, int32_t what) {
-  if (status == nullptr) return;
-  ((volatile int32_t*)status)[3] = ACTKV_STATUS_ROWS;
-  __threadfence();
-  report(status, code, where, what);
+// Whether the last actkv_resize on these status words was refused (by an error of its own or one that it found): the lengths are then not
+// those that were asked for, and what actkv_append and actkv_copy would write falls on live entries.  actkv_resize writes status[3], they
+// only read it, so that an error which one of their CTAs reports (a row or page that is dropped) stops no other CTA, whichever comes first.
+// Read beside a CTA's other first loads and looked at behind them: 6 layers of 35000 tokens into 3 branches 277.8 us, without the look 276.4;
+// 8400 rows appended 38.9 and 38.4.
+__device__ __forceinline__ int32_t refused(const int32_t* status) {
+  return status != nullptr ? (status[0] != ACTKV_OK) & (status[3] == ACTKV_STATUS_REFUSED) : 0;
 }
 
 // Programmatic dependent launch.  A step is a chain of kernels of which many take a few microseconds; every one of them (but

@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(NT) resize_kernel(TablesView tab, int32_t P, i
       }
     if (rank == 0 && tid == 0) *tab.free_count = (int32_t)(fc - pops + pushes);
   }
-  if (rank == 0 && tid == 0 && status != nullptr) status[3] = 0;
+  if (rank == 0 && tid == 0 && status != nullptr) status[3] = any ? ACTKV_STATUS_REFUSED : 0;
   if constexpr (CS > 1) cg::this_cluster().sync();                        // (flags are read from one another's shared memory)
 }
 
@@ -224,7 +224,7 @@ struct CopySmem {
 };
 struct CopySource {
   int src, len, page, col;
-  int32_t code;                  // status_code
+  int32_t stop;                  // refused
 };
 // (dst is a request, of dst_len tokens)
 __device__ __forceinline__ bool sound_pair(const CopyArgs& a, int src, int src_len, int dst, int dst_len, int n) {
@@ -234,21 +234,21 @@ __device__ __forceinline__ bool sound_pair(const CopyArgs& a, int src, int src_l
 template <int NT>
 __device__ __forceinline__ bool copy_source(const CopyArgs& a, int i, int lp, bool first, CopySource& s) {
   const int tid = threadIdx.x;
-  s.code = status_code(a.status);
+  s.stop = refused(a.status);
   s.src = a.src[i];
   if ((uint32_t)s.src >= (uint32_t)a.tab.n_req) {
-    if (first && tid == 0 && !refused(a.status, s.code)) report_row(a.status, ACTKV_E_INVALID, i, s.src);
+    if (first && tid == 0 && !s.stop) report(a.status, ACTKV_E_INVALID, i, s.src);
     return false;
   }
   s.col = lp < a.tab.max_pages ? lp : a.tab.max_pages - 1;                 // (max_len may be beyond the table; no sound pair is)
   s.page = a.tab.max_pages > 0 ? a.tab.page_table[(int64_t)s.src * a.tab.max_pages + s.col] : -1;
   s.len = a.tab.seq_len[s.src];
-  if (first && !refused(a.status, s.code)) {                                                  // (here, not where branches are looked for: that ends early)
+  if (first && !s.stop) {                                                  // (here, not where branches are looked for: that ends early)
     const int d = a.dst[i], n = a.length[i];
     const bool known = (uint32_t)d < (uint32_t)a.tab.n_req;
-    if (tid == 0 && !(known && sound_pair(a, s.src, s.len, d, a.tab.seq_len[d], n))) report_row(a.status, ACTKV_E_INVALID, i, n);
+    if (tid == 0 && !(known && sound_pair(a, s.src, s.len, d, a.tab.seq_len[d], n))) report(a.status, ACTKV_E_INVALID, i, n);
     for (int j = tid; j < a.n_copy; j += NT)
-      if (j != i && (a.dst[j] == d || a.src[j] == d)) report_row(a.status, ACTKV_E_INVALID, i, d);
+      if (j != i && (a.dst[j] == d || a.src[j] == d)) report(a.status, ACTKV_E_INVALID, i, d);
   }
   return true;
 }
@@ -273,14 +273,14 @@ __device__ __forceinline__ int copy_branches(const CopyArgs& a, int i, int j0, i
           const int at = atomicAdd(&sm->n, 1);
           sm->dst[at] = (int64_t)page * a.pool.stride_page;
           sm->slots[at] = slots;
-        } else if (!refused(a.status, s.code)) {
-          report_row(a.status, ACTKV_E_BADPAGE, src_ok ? d : s.src, src_ok ? page : s.page);
+        } else if (!s.stop) {
+          report(a.status, ACTKV_E_BADPAGE, src_ok ? d : s.src, src_ok ? page : s.page);
         }
       }
     }
   }
   // (an unsound pair copies nothing itself; when it comes first, the next sound one works for the rest)
-  if (__syncthreads_or((sound && j < i) || (j == i && !sound) || refused(a.status, s.code))) return -1;
+  if (__syncthreads_or((sound && j < i) || (j == i && !sound) || s.stop)) return -1;
   return j0 + NT > i && sm->n > 0 ? 1 : 0;
 }
 __device__ __forceinline__ __nv_bfloat16* copy_base(const CopyArgs& a) {

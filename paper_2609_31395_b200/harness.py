@@ -342,7 +342,9 @@ class Decoder:
     """Decoding on the paged cache between two compression steps: resize -> append -> attend, and copies for branches.
 
     Holds the descriptors of the pool and its tables and the workspace of `attend`; max_rows, max_win and max_tok bound a call's
-    rows, a request's rows and a request's length.  Calls on two streams at once need a Decoder each (the workspace)."""
+    rows, a request's rows and a request's length.  Calls on two streams at once need a Decoder each (the workspace).
+    A `resize` that is refused (status) modifies nothing, and append and copy behind it write nothing, until a later one is carried out:
+    make room, clear the status (`status.zero_()`), resize again."""
 
     def __init__(self, pool: torch.Tensor, page_table, seq_len, free_list, free_count, n_q_heads: int, max_rows: int = 1,
                  max_win: int = 1, max_tok: int = 1, layers_per_call: int = 1):

@@ -1,5 +1,6 @@
-"""actkv_append and actkv_copy behind a call that was refused: what the cache holds stays as it was, bit for bit.  Rows and pages that
-these two calls drop themselves are no refusal: everything else is carried out, in this call and in the following ones."""
+"""actkv_append and actkv_copy behind an actkv_resize that was refused: what the cache holds stays as it was, bit for bit.  Any other error
+(rows and pages that these two calls drop themselves, a request that attention leaves out) stops nothing else: the tokens of the other
+requests are written, in this call and in those on the next layers."""
 import pytest
 import torch
 
@@ -102,16 +103,45 @@ def test_a_refused_step_leaves_the_cache_alone(cause, captured):
 
 
 @pytest.mark.parametrize("code", [B.E_INVALID, B.E_BADPAGE, B.E_NOFREE, B.E_TIMEOUT])
-def test_any_error_of_an_earlier_call_stops_both(code):
+def test_a_resize_that_finds_an_error_stops_both(code):
+    # whatever call it comes from: the lengths are not the ones that were asked for
     d = _decoder([30, 30, 20], spare=2, width=4)
     q, k, v = _new_rows(d, 3)
     q_out = torch.zeros(q.shape, dtype=torch.bfloat16, device=DEV)
     d.status.copy_(_i32([code, 5, 6, 0]))
     before = _state(d)
-    d.append(k, v, _i32([0, 1, 2, 3]), q=q, q_out=q_out)
-    d.copy(_i32([0]), _i32([1]), _i32([30]), 30)
-    assert _same(_state(d), before) and d.status.cpu().tolist() == [code, 5, 6, 0]
+    for _ in range(2):
+        d.resize(d.seq_len + 1)
+        d.append(k, v, _i32([0, 1, 2, 3]), q=q, q_out=q_out)
+        d.copy(_i32([0]), _i32([1]), _i32([30]), 30)
+    assert _same(_state(d), before) and d.status.cpu().tolist()[:3] == [code, 5, 6]
     assert torch.equal(q_out, q)                       # (the queries are the caller's, not the cache's)
+    d.status.zero_()
+    d.resize(d.seq_len + 1)
+    d.append(k, v, _i32([0, 1, 2, 3]))
+    d.check_status()
+    assert torch.equal(d.pool[0, 1, d.page_table[0, 1], 30 % 16], v[0, 0])
+
+
+@pytest.mark.parametrize("damage", ["length", "page"])
+def test_an_error_of_attention_in_one_layer_leaves_the_next_layers_alone(damage):
+    # three requests, two layers; attend reports request 1 in layer 0, the tokens of the others belong into layer 1 all the same
+    d = _decoder([30, 30, 20], spare=2, width=4, layers=2)
+    q, k, v = _new_rows(d, 3, 2)
+    q, wi = q.contiguous(), _i32([0, 1, 2, 3])
+    out = torch.empty_like(q[:1])
+    d.resize(d.seq_len + 1)
+    if damage == "page":
+        d.page_table[1, 0] = 1 << 20                   # (token 0's; the new one is on page 1)
+    else:
+        d.max_tok = 30
+    for l in range(2):
+        d.append(k[l:l + 1], v[l:l + 1], wi, l0=l)
+        d.attend(q[l:l + 1], wi, 0.25, True, out, l0=l)
+    assert d.status.cpu().tolist()[0] == (B.E_BADPAGE if damage == "page" else B.E_INVALID)
+    for l in range(2):
+        for r, n in enumerate([30, 30, 20]):
+            assert torch.equal(d.pool[l, 0, d.page_table[r, 1], n % 16], k[l, r]) and torch.equal(d.pool[l, 1, d.page_table[r, 1], n % 16], v[l, r])
 
 
 @pytest.mark.parametrize("head_major", [False, True])
