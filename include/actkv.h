@@ -586,8 +586,8 @@ int actkv_debug_inject_stall(int32_t after_tile, int32_t wait_limit_us);
 
 /* ---------------------------------------------------------------------------------------
  * Decoding on the cache between two compression steps: actkv_resize -> actkv_append ->
- * actkv_attend (whose LSE is the lse_in of actkv_score / actkv_score_accumulate) -> actkv_logprob,
- * and actkv_copy for the branches of a trace.
+ * actkv_attend (whose LSE is the lse_in of actkv_score / actkv_score_accumulate) -> actkv_penalize -> actkv_sample ->
+ * actkv_logprob, actkv_copy for the branches of a trace, and actkv_reposition behind a compression.
  * (The paper leaves these to the serving system: Section 2.3 defines the attention, Section 2.5 the paged
  * cache and its block table, Section 7.1 takes the LSE from the attention backend.)
  */
@@ -736,6 +736,105 @@ int actkv_logprob(const void* logits, int32_t dtype, int32_t n_rows, int32_t voc
                   const int32_t* given, int32_t n_given, int32_t top_k,
                   float* logprob, float* entropy, float* lse, float* top_logprob, int32_t* top_index,
                   int32_t* status, actkv_stream_t stream);
+
+/* ---------------------------------------------------------------------------------------
+ * actkv_reposition — cached keys carried from one rotary position to another, or from one table of frequencies to another, in
+ * place.  (Positions are the model's business in the paper.  Behind a compression every layer and KV head holds tokens with gaps between
+ * their positions; this call closes the gaps, so that the positions of a long trace stay in the range that the model was trained on, or
+ * goes over to frequencies scaled for longer contexts.)
+ *
+ * For request r, its first n_r = tok_indptr[r+1] - tok_indptr[r] tokens j, layer l, KV head h, unit o = (l - layer_begin) * n_kv_heads + h,
+ * and the pairs i of dims that rope turns (the pairs, axes and layouts of actkv_append):
+ *   pair i of K[l, slot(r, j), h, :] turns by  to(o, j)[axis] * to_inv_freq[i] - from(o, j)[axis] * rope->inv_freq[i].
+ * from, to: where the key is and where it goes; the position of token j on an axis is
+ *   base[axis*stride_axis + o*stride_unit + tok_indptr[r] + j],  int32;
+ * a stride of 0: all axes or units alike.  from or to NULL, or its base NULL: the position is j, the token's index in the cache.  So, behind
+ * actkv_compact, from = { sel_idx, 0, sel_stride }, to = NULL and tok_indptr = keep_indptr move the survivors up when positions were indices before.
+ * to_inv_freq float32 [rotary_dim/2], NULL: the frequencies stay.  Then keys whose positions stay are left as they are (their bits too).
+ * The angle is exact modulo a turn but for the rounding of inv_freq / 2 pi in float64; sine and cosine in float32; the result is rounded once to
+ * bf16, so that a key that is moved many times gathers a rounding each time.
+ * V, other dims, tokens from n_r on and free pages are not touched.  sum_tok, max_tok: host upper bounds on tok_indptr[n_req]
+ * (what the positions hold) and n_r.
+ * All or nothing: a request with n_r outside [0, min(seq_len, max_tok)], beyond sum_tok or its table row (ACTKV_E_INVALID), or a page id out of
+ * range (ACTKV_E_BADPAGE), is reported and no key of the call is turned; the same when status is already set (a compaction that was not carried
+ * out must not be followed by turns).  With status NULL tokens on bad pages, and the requests above, are left out.
+ * head_dim a multiple of 8, at most 256.  Two launches; no workspace.
+ */
+typedef struct {
+  const int32_t* base;          /* device, or NULL */
+  int64_t stride_axis, stride_unit;
+} actkv_positions_t;
+int actkv_reposition(const actkv_pool_t* pool /* host */, const actkv_tables_t* tables /* host */,
+                     int32_t layer_begin, int32_t layer_end,
+                     const actkv_rope_t* rope /* host */, const float* to_inv_freq,
+                     const actkv_positions_t* from /* host */, const actkv_positions_t* to /* host */,
+                     const int32_t* tok_indptr, int32_t sum_tok, int32_t max_tok, int32_t* status, actkv_stream_t stream);
+
+/* ---------------------------------------------------------------------------------------
+ * actkv_penalize — what a request's rules make of its logits before a token is drawn: biases, penalties for tokens that its history
+ * holds, masks.  (The paper's agents act through tool calls, Section 8.1; how their tokens are drawn is left to the serving system.)
+ *
+ * Rows win_indptr[r] .. win_indptr[r+1] of the logits belong to request r; row w of W_r stands behind the first
+ * hist_len[r] - (W_r - 1 - w) tokens of the request (none where that is negative): all of them for the newest row, fewer for those before it, as
+ * in actkv_attend.  For token t of the row, in this order, in float32:
+ *   z += bias(t);
+ *   t among these tokens:                        z = z > 0 ? z / repetition : z * repetition
+ *   n > 0 times among those from prompt_len on:  z -= frequency * n + presence
+ *   t not allowed:                               z = -inf
+ * and rounded once to the logits' type.  out == logits: in place (row strides equal); otherwise every logit of these rows is written, and
+ * logits and out may not overlap.  Rows of no request (sum_win above win_indptr[n_req]) are left as they are.
+ * Tokens of the history outside [0, vocab) count for nothing.
+ * The rules (struct read during the call; every pointer on the device; NULL: off):
+ *   tokens int32 [n_req, token_stride], hist_len int32 [n_req] (needed with tokens), prompt_len int32 [n_req] (NULL: 0);
+ *   repetition, frequency, presence float32 [n_req] (NULL: 1, 0, 0);
+ *   bias_token int32, bias_value float32 [n_bias]: a request's entries, from bias_indptr[r] to bias_indptr[r+1], its tokens ascending; values finite or -inf;
+ *   allow uint32 [n_allow, allow_stride]: bit t % 32 of word t / 32; allow_row int32 [sum_win] the row of allow for each row of logits, negative:
+ *   everything is allowed (NULL: row i has row i).
+ * Reported, the rows concerned left as they are (ACTKV_E_INVALID): repetition not positive and finite, frequency or presence not finite, hist_len outside
+ * [0, min(max_hist, token_stride)], rows that do not fit max_win or sum_win,
+ * a bias_indptr outside [0, n_bias]; (ACTKV_E_BADINDEX): biases out of order or range, allow_row beyond
+ * n_allow.  max_win, max_hist: host upper bounds on W_r and hist_len.  One launch; no workspace.
+ */
+typedef struct {
+  const int32_t*  tokens;
+  int64_t         token_stride;
+  const int32_t  *hist_len, *prompt_len;
+  const float    *repetition, *frequency, *presence;
+  const int32_t  *bias_indptr, *bias_token;
+  const float*    bias_value;
+  int32_t         n_bias;       /* entries of bias_token and bias_value */
+  const uint32_t* allow;
+  int64_t         allow_stride; /* words */
+  int32_t         n_allow;
+  const int32_t*  allow_row;
+} actkv_logit_rules_t;
+int actkv_penalize(const void* logits, int32_t dtype, int32_t vocab, int64_t row_stride,
+                   const int32_t* win_indptr, int32_t n_req, int32_t sum_win, int32_t max_win, int32_t max_hist,
+                   const actkv_logit_rules_t* rules /* host */, void* out, int64_t out_stride,
+                   int32_t* status, actkv_stream_t stream);
+
+/* ---------------------------------------------------------------------------------------
+ * actkv_sample — a token per row of logits, from what temperature, top-k, top-p and min-p leave.  (Section 8.1 samples actions
+ * at a temperature; how is left to the serving system.)
+ *
+ * Tokens in order: logits descending, among equal ones the lower token first; those with logit -inf are none.  With T = temperature[i] > 0,
+ * w(t) = exp((z_t - z_max) / T):
+ *   the first top_k[i] of them (<= 0: all);
+ *   of these the shortest prefix with at least top_p[i] of their sum of w (>= 1: all; at least one token);
+ *   of these the ones with w >= min_p[i] (above 1 counts as 1).
+ * The token drawn is the first one, in the order of the vocabulary, up to which the sum of w over the kept tokens exceeds u[i] times their sum
+ * S; logprob = log(w / S) (NULL to skip), kept = how many tokens were kept (NULL to skip).  T = 0: the first token in order, logprob 0, kept 1.
+ * u in [0, 1] is the row's random number (1: the last kept token).  Weights are formed in float64 and summed as whole multiples of 2^-45
+ * (weights below 2^-46 are 0 in the sums), so that equal arguments give equal results.
+ * temperature, top_p, min_p float32, top_k int32 [n_rows], NULL: 1, 1, 0, 0 for every row.
+ * A row with nothing but -inf, a NaN or +inf: token -1, logprob -inf, kept 0.  The same, reported as ACTKV_E_INVALID, for a temperature that is
+ * negative, infinite or NaN, top_p or min_p NaN, u outside [0, 1].
+ * logits [n_rows, vocab] with row_stride elements between rows, ACTKV_F32 or ACTKV_BF16; vocab at most ACTKV_SAMPLE_MAX_VOCAB.
+ */
+#define ACTKV_SAMPLE_MAX_VOCAB 344064
+int actkv_sample(const void* logits, int32_t dtype, int32_t n_rows, int32_t vocab, int64_t row_stride,
+                 const float* u, const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+                 int32_t* token, float* logprob, int32_t* kept, int32_t* status, actkv_stream_t stream);
 
 /* Library version string (host pointer to static storage). */
 const char* actkv_version(void);

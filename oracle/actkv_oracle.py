@@ -25,6 +25,7 @@ and the x-axis of the line fit.
 from __future__ import annotations
 
 import math
+from collections import Counter
 from dataclasses import dataclass
 
 import numpy as np
@@ -613,3 +614,65 @@ def log_probabilities(logits: np.ndarray):
 def top_tokens(logits: np.ndarray, k: int) -> np.ndarray:
     """The k largest logits of every row, descending, equal ones by token: int [rows, min(k, vocab)]."""
     return np.argsort(-np.asarray(logits, dtype=np.float64), axis=1, kind="stable")[:, :k]
+
+
+# --------------------------------------------------------------------------------------------
+# Cached keys to other positions; rules on logits; drawn tokens (left to the model and the serving system by the paper)
+
+
+def turn(x: np.ndarray, angle: np.ndarray, interleaved: bool) -> np.ndarray:
+    """x float64 [..., D]; pair i turns by angle[..., i] (its dims: i and i + pairs, or 2i and 2i + 1)."""
+    y = np.array(x, dtype=np.float64)
+    half = angle.shape[-1]
+    a, b = (slice(0, 2 * half, 2), slice(1, 2 * half, 2)) if interleaved else (slice(0, half), slice(half, 2 * half))
+    c, s = np.cos(angle), np.sin(angle)
+    y[..., a] = x[..., a] * c - x[..., b] * s
+    y[..., b] = x[..., b] * c + x[..., a] * s
+    return y
+
+
+def reposition_unit(k: np.ndarray, from_pos, to_pos, inv_freq, to_inv_freq, sections, interleaved: bool) -> np.ndarray:
+    """Keys k float64 [n, D] of one (layer, request, KV head); from_pos, to_pos int [axes, n]; inv_freq [pairs] before and after."""
+    axis = np.repeat(np.arange(len(sections)), sections)
+    was = np.asarray(from_pos, dtype=np.float64)[axis].T * np.asarray(inv_freq, dtype=np.float64)
+    will = np.asarray(to_pos, dtype=np.float64)[axis].T * np.asarray(to_inv_freq, dtype=np.float64)
+    return turn(k, will - was, interleaved)
+
+
+def penalize_row(z, past, n_prompt: int, repetition: float, frequency: float, presence: float, bias, allowed) -> np.ndarray:
+    """One row of logits, float64 [vocab]; past: the tokens it stands behind; bias {token: value}; allowed bool [vocab] or None."""
+    z = np.array(z, dtype=np.float64)
+    for t, b in bias.items():
+        z[t] += b
+    past = np.asarray(past, dtype=np.int64)
+    made = Counter(past[n_prompt:].tolist())
+    for t in set(past.tolist()):
+        if 0 <= t < len(z):
+            z[t] = z[t] / repetition if z[t] > 0 else z[t] * repetition
+            if made[t] > 0:
+                z[t] -= frequency * made[t] + presence
+    if allowed is not None:
+        z[~allowed] = -np.inf
+    return z
+
+
+def sample_row(z, u: float, temperature: float, top_k: int, top_p: float, min_p: float):
+    """(token, log probability, kept tokens) of one row of float64 logits; (-1, -inf, 0) where there is no token."""
+    z = np.asarray(z, dtype=np.float64)
+    if np.isnan(z).any() or np.isposinf(z).any() or np.isneginf(z).all():
+        return -1, -np.inf, 0
+    order = np.argsort(-z, kind="stable")
+    order = order[z[order] > -np.inf]
+    if temperature == 0:
+        return int(order[0]), 0.0, 1
+    if top_k > 0:
+        order = order[:top_k]
+    w = np.exp((z[order] - z[order[0]]) / temperature)
+    if top_p < 1:
+        order = order[:max(1, int(np.searchsorted(np.cumsum(w), top_p * w.sum())) + 1)]
+        w = w[:len(order)]
+    order = np.sort(order[w >= min(min_p, 1.0)])
+    w = np.exp((z[order] - z.max()) / temperature)
+    c = np.cumsum(w)
+    at = min(int(np.searchsorted(c, u * c[-1], side="right")), len(order) - 1)
+    return int(order[at]), float(np.log(w[at] / c[-1])), len(order)

@@ -31,7 +31,7 @@ EXPORTS = ["actkv_budget_workspace_bytes", "actkv_budget", "actkv_score_workspac
            "actkv_compact_deferred_workspace_bytes", "actkv_compact_begin", "actkv_compact_end", "actkv_score_overlap", "actkv_compact_stats",
            "actkv_compact_inplace_deferred_workspace_bytes", "actkv_compact_inplace_begin", "actkv_compact_inplace_end",
            "actkv_attend_workspace_bytes", "actkv_attend", "actkv_append", "actkv_resize", "actkv_copy", "actkv_logprob",
-           "actkv_version"]
+           "actkv_reposition", "actkv_penalize", "actkv_sample", "actkv_version"]
 
 
 class ActKVError(RuntimeError):
@@ -76,6 +76,19 @@ class RopeDesc(C.Structure):
     """actkv_rope_t: which dims turn, by which axis, how fast."""
     _fields_ = [("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("n_axes", C.c_int32), ("section", C.c_int32 * 4),
                 ("inv_freq", C.c_void_p)]
+
+
+class PositionsDesc(C.Structure):
+    """actkv_positions_t: a position per (axis, unit, token)."""
+    _fields_ = [("base", C.c_void_p), ("stride_axis", C.c_int64), ("stride_unit", C.c_int64)]
+
+
+class LogitRulesDesc(C.Structure):
+    """actkv_logit_rules_t: history, penalties, biases and masks of all requests."""
+    _fields_ = [("tokens", C.c_void_p), ("token_stride", C.c_int64), ("hist_len", C.c_void_p), ("prompt_len", C.c_void_p),
+                ("repetition", C.c_void_p), ("frequency", C.c_void_p), ("presence", C.c_void_p), ("bias_indptr", C.c_void_p),
+                ("bias_token", C.c_void_p), ("bias_value", C.c_void_p), ("n_bias", C.c_int32), ("allow", C.c_void_p), ("allow_stride", C.c_int64),
+                ("n_allow", C.c_int32), ("allow_row", C.c_void_p)]
 
 
 class HostStep(C.Structure):
@@ -201,6 +214,13 @@ def load():
     lib.actkv_copy.argtypes = [C.POINTER(PoolDesc), C.POINTER(TablesDesc), i32, i32, vp, vp, vp, i32, i32, vp, vp]
     lib.actkv_logprob.restype = i32
     lib.actkv_logprob.argtypes = [vp, i32, i32, i32, i64, vp, i32, i32, vp, vp, vp, vp, vp, vp, vp]
+    lib.actkv_reposition.restype = i32
+    lib.actkv_reposition.argtypes = [C.POINTER(PoolDesc), C.POINTER(TablesDesc), i32, i32, C.POINTER(RopeDesc), vp,
+                                     C.POINTER(PositionsDesc), C.POINTER(PositionsDesc), vp, i32, i32, vp, vp]
+    lib.actkv_penalize.restype = i32
+    lib.actkv_penalize.argtypes = [vp, i32, i32, i64, vp, i32, i32, i32, i32, C.POINTER(LogitRulesDesc), vp, i64, vp, vp]
+    lib.actkv_sample.restype = i32
+    lib.actkv_sample.argtypes = [vp, i32, i32, i32, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.actkv_debug_inject_stall.restype = i32
     lib.actkv_debug_inject_stall.argtypes = [i32, i32]
     _lib = lib
@@ -673,3 +693,98 @@ def actkv_logprob(logits, given, logprob, entropy, lse, top_logprob, top_index, 
           _arg(entropy, torch.float32, i, n, "entropy"), _arg(lse, torch.float32, i, n, "lse"),
           _arg(top_logprob, torch.float32, i, 0, "top_logprob"), _arg(top_index, torch.int32, i, 0, "top_index"),
           _arg(status, torch.int32, i, 4, "status"))
+
+
+def positions_desc(t: torch.Tensor, n_axes: int, n_units: int, name: str = "positions"):
+    """Descriptor of int32 positions and the number of tokens that they hold: [tokens] (the same on every axis and for every unit),
+    [axes, tokens], or [axes, units, tokens]; one axis or unit stands for all.  The last dim contiguous."""
+    if t.dtype is not torch.int32:
+        raise TypeError(f"{name}: expected torch.int32, got {t.dtype}")
+    shape, st = t.shape, t.stride()
+    d = len(shape)
+    if not 1 <= d <= 3 or (d > 1 and shape[0] not in (1, n_axes)) or (d == 3 and shape[1] not in (1, n_units)):
+        raise ValueError(f"{name}: {list(shape)}, expected [tokens], [{n_axes}, tokens] or [{n_axes}, {n_units}, tokens]")
+    if st[-1] != 1 and shape[-1] > 1:
+        raise TypeError(f"{name}: expected a contiguous last dimension")
+    return PositionsDesc(t.data_ptr(), st[0] if d > 1 and shape[0] > 1 else 0, st[1] if d == 3 and shape[1] > 1 else 0), shape[-1]
+
+
+def actkv_reposition(pool: PoolDesc, tables: TablesDesc, layer_begin, layer_end, rope: RopeDesc, to_inv_freq, from_pos, to_pos,
+                     tok_indptr, max_tok, status, stream=None):
+    """from_pos, to_pos: int32 positions (positions_desc), None: a token's index; to_inv_freq float32 [pairs], None: as before.
+    tok_indptr [n_req + 1]: where each request's tokens begin in the positions, and how many of them are moved."""
+    i = _cuda_index(tok_indptr, "tok_indptr")
+    units = (layer_end - layer_begin) * pool.n_kv_heads
+    desc, sum_tok = [None, None], 0x7fffffff
+    for at, (t, name) in enumerate(((from_pos, "from_pos"), (to_pos, "to_pos"))):
+        if t is not None:
+            if t.get_device() != i:
+                raise TypeError(f"{name}: on {t.device}, expected cuda:{i}")
+            desc[at], n = positions_desc(t, rope.n_axes, units, name)
+            sum_tok = min(sum_tok, n)
+    _call("actkv_reposition", i, stream, pool, tables, layer_begin, layer_end, rope,
+          _arg(to_inv_freq, torch.float32, i, rope.rotary_dim // 2, "to_inv_freq"), desc[0], desc[1],
+          _arg(tok_indptr, torch.int32, i, tables.n_req + 1, "tok_indptr"), sum_tok, max_tok, _arg(status, torch.int32, i, 4, "status"))
+
+
+def logit_rules_desc(n_req, tokens=None, hist_len=None, prompt_len=None, repetition=None, frequency=None, presence=None,
+                     bias_indptr=None, bias_token=None, bias_value=None, allow=None, allow_row=None) -> LogitRulesDesc:
+    """tokens int32 [n_req, any]; allow int32 or uint32 [rows, words], 32 tokens a word; the others as actkv_logit_rules_t has them."""
+    given = [t for t in (tokens, hist_len, prompt_len, repetition, frequency, presence, bias_indptr, bias_token, bias_value, allow, allow_row)
+             if t is not None]
+    if not given:
+        return LogitRulesDesc()
+    i = _cuda_index(given[0], "rules")
+    if tokens is not None and (len(tokens.shape) != 2 or tokens.shape[0] != n_req):
+        raise ValueError(f"tokens: {list(tokens.shape)}, expected [{n_req}, any]")
+    if allow is not None and len(allow.shape) != 2:
+        raise ValueError(f"allow: {list(allow.shape)}, expected [rows, words]")
+    if tokens is not None and hist_len is None:
+        raise ValueError("hist_len: expected with tokens")
+    if bias_indptr is not None and (bias_token is None or bias_value is None or bias_token.numel() != bias_value.numel()):
+        raise ValueError("bias_token, bias_value: expected with bias_indptr, one value per token")
+    if allow is not None and allow.dtype is torch.uint32:
+        allow = allow.view(torch.int32)
+    return LogitRulesDesc(_arg(tokens, torch.int32, i, 0, "tokens"), 0 if tokens is None else tokens.shape[1],
+                          _arg(hist_len, torch.int32, i, n_req, "hist_len"), _arg(prompt_len, torch.int32, i, n_req, "prompt_len"),
+                          _arg(repetition, torch.float32, i, n_req, "repetition"), _arg(frequency, torch.float32, i, n_req, "frequency"),
+                          _arg(presence, torch.float32, i, n_req, "presence"), _arg(bias_indptr, torch.int32, i, n_req + 1, "bias_indptr"),
+                          _arg(bias_token, torch.int32, i, 0, "bias_token"), _arg(bias_value, torch.float32, i, 0, "bias_value"), 0 if bias_value is None else bias_value.numel(),
+                          _arg(allow, torch.int32, i, 0, "allow"), 0 if allow is None else allow.shape[1], 0 if allow is None else allow.shape[0],
+                          _arg(allow_row, torch.int32, i, 0, "allow_row"))
+
+
+def _logit_rows(t, index, name):
+    """Type code, rows, vocabulary and row stride of logits on this device."""
+    kind, st = _LOGIT_TYPES.get(t.dtype), t.stride()
+    if kind is None or len(st) != 2 or (st[1] != 1 and t.shape[1] != 1):
+        raise TypeError(f"{name}: expected float32 or bf16 [rows, vocab] with contiguous rows")
+    if t.get_device() != index:
+        raise TypeError(f"{name}: on {t.device}, expected cuda:{index}")
+    n, vocab = t.shape
+    return kind, n, vocab, st[0] if n > 1 else vocab
+
+
+def actkv_penalize(logits, win_indptr, n_req, rules: LogitRulesDesc, max_win, max_hist, out, status, stream=None):
+    """logits [rows, vocab] float32 or bf16, rows any distance apart; out: the same tensor (in place), or one of its shape and type."""
+    i = _cuda_index(logits, "logits")
+    kind, n, vocab, stride = _logit_rows(logits, i, "logits")
+    to, out_stride = logits.data_ptr(), stride
+    if out is not logits:
+        if out.dtype is not logits.dtype or out.shape != logits.shape:
+            raise ValueError(f"out: expected {logits.dtype} {list(logits.shape)}, got {out.dtype} {list(out.shape)}")
+        to, out_stride = out.data_ptr(), _logit_rows(out, i, "out")[3]
+    _call("actkv_penalize", i, stream, logits.data_ptr(), kind, vocab, stride, _arg(win_indptr, torch.int32, i, n_req + 1, "win_indptr"), n_req,
+          n, max_win, max_hist, rules, to, out_stride, _arg(status, torch.int32, i, 4, "status"))
+
+
+def actkv_sample(logits, u, temperature, top_k, top_p, min_p, token, logprob, kept, status, stream=None):
+    """logits [rows, vocab] float32 or bf16, rows any distance apart; u, temperature, top_p, min_p float32 and top_k int32 [rows] (None: 1, 1, 0,
+    0); results token int32, logprob float32, kept int32 with room for that many rows (the last two may be None)."""
+    i = _cuda_index(logits, "logits")
+    kind, n, vocab, stride = _logit_rows(logits, i, "logits")
+    f32, i32 = torch.float32, torch.int32
+    _call("actkv_sample", i, stream, logits.data_ptr(), kind, n, vocab, stride, _arg(u, f32, i, n, "u"),
+          _arg(temperature, f32, i, n, "temperature"), _arg(top_k, i32, i, n, "top_k"), _arg(top_p, f32, i, n, "top_p"),
+          _arg(min_p, f32, i, n, "min_p"), _arg(token, i32, i, n, "token"), _arg(logprob, f32, i, n, "logprob"), _arg(kept, i32, i, n, "kept"),
+          _arg(status, i32, i, 4, "status"))

@@ -384,6 +384,58 @@ class Decoder:
         """The first length[i] tokens of request src[i] into the pages of request dst[i]."""
         B.actkv_copy(self.pd, self.td, l0, self.pd.n_layers if l1 is None else l1, src, dst, length, max_len, self.status, stream)
 
+    def reposition(self, rope: Rope, tok_indptr, max_tok, from_pos=None, to_pos=None, to_inv_freq=None, l0=0, l1=None, stream=None):
+        """Cached keys from their positions to others (None: a token's index), or to other frequencies.  Behind a compaction that kept
+        sel_idx [units, any] of tokens whose positions were their indices: from_pos = sel_idx[None], tok_indptr = keep_indptr."""
+        B.actkv_reposition(self.pd, self.td, l0, self.pd.n_layers if l1 is None else l1, rope.desc, to_inv_freq, from_pos, to_pos, tok_indptr,
+                           max_tok, self.status, stream)
+
+    def check_status(self):
+        st = self.status.cpu().tolist()
+        if st[0] != 0:
+            raise B.ActKVError(f"device status {st}", st[0])
+
+
+class LogitRules:
+    """History, penalties, biases and masks of a set of requests (actkv_logit_rules_t); every argument may be None.  Holds the tensors, whose
+    contents may change from call to call."""
+
+    def __init__(self, tokens=None, hist_len=None, prompt_len=None, repetition=None, frequency=None, presence=None, bias_indptr=None,
+                 bias_token=None, bias_value=None, allow=None, allow_row=None, n_req: Optional[int] = None):
+        self.tensors = (tokens, hist_len, prompt_len, repetition, frequency, presence, bias_indptr, bias_token, bias_value, allow, allow_row)
+        if n_req is None:
+            by = next((t for t in (tokens, hist_len, prompt_len, repetition, frequency, presence) if t is not None), None)
+            n_req = by.shape[0] if by is not None else bias_indptr.shape[0] - 1 if bias_indptr is not None else 0
+        self.n_req = n_req
+        self.rows = None if allow is None else allow.shape[0] if allow_row is None else allow_row.shape[0]
+        self.words = None if allow is None else allow.shape[1]
+        self.desc = B.logit_rules_desc(n_req, *self.tensors)
+
+
+class Sampler:
+    """Draws tokens from logits: result buffers and status for up to `rows` rows."""
+
+    def __init__(self, rows: int, device):
+        B.load()
+        self.token = torch.empty(rows, dtype=torch.int32, device=device)
+        self.logprob = torch.empty(rows, dtype=torch.float32, device=device)
+        self.kept = torch.empty(rows, dtype=torch.int32, device=device)
+        self.status = torch.zeros(4, dtype=torch.int32, device=device)
+
+    def penalize(self, logits, win_indptr, rules: LogitRules, max_win=1, max_hist=0, out=None, stream=None):
+        """The rules' biases, penalties and masks on logits [rows, vocab], in place or into out; rows of request r are
+        win_indptr[r] .. win_indptr[r + 1]."""
+        n_req = win_indptr.shape[0] - 1
+        if rules.n_req not in (0, n_req):
+            raise ValueError(f"rules: of {rules.n_req} requests, win_indptr: of {n_req}")
+        if rules.rows is not None and rules.rows < logits.shape[0]:
+            raise ValueError(f"allow: masks for {rules.rows} rows, logits: {logits.shape[0]}")
+        B.actkv_penalize(logits, win_indptr, n_req, rules.desc, max_win, max_hist, logits if out is None else out, self.status, stream)
+
+    def sample(self, logits, u, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
+        """A token per row into self.token, its log probability and the number of tokens that it was drawn from beside it."""
+        B.actkv_sample(logits, u, temperature, top_k, top_p, min_p, self.token, self.logprob, self.kept, self.status, stream)
+
     def check_status(self):
         st = self.status.cpu().tolist()
         if st[0] != 0:
