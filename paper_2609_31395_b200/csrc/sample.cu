@@ -34,11 +34,18 @@ constexpr int CAP = 1024;                  // tokens that are sorted
 constexpr int MAX_CLUSTER = 8;
 constexpr int MAX_SLICE = 43008;           // tokens of a CTA
 constexpr double MAGIC = 6755399441055744.0;          // 1.5 * 2^52: adding it rounds to a whole number in the low bits
-constexpr double MAGIC45 = 192.0;                     // 1.5 * 2^7: the same in steps of 2^-45
 constexpr float OCTAVES = 47.f;                       // weights below 2^-47 are 0
 constexpr int NT = 512, NW = NT / 32, BPT = NB / NT;
-constexpr int GROUPS = 256;                // of a row's tokens, for the bound of a small top-k
-constexpr int SMALL_K = GROUPS / 2;
+constexpr int GROUPS = 128;                // of a row's tokens, for the bound of a small top-k
+constexpr int SMALL_K = 96;
+constexpr int FEW = NT / 4;                // tokens of a short list
+
+// 2^(-i / 16)
+__constant__ double ROOTS[16] = {
+    0x1.0000000000000p+0, 0x1.ea4afa2a490dap-1, 0x1.d5818dcfba487p-1, 0x1.c199bdd85529cp-1,
+    0x1.ae89f995ad3adp-1, 0x1.9c49182a3f090p-1, 0x1.8ace5422aa0dbp-1, 0x1.7a11473eb0187p-1,
+    0x1.6a09e667f3bcdp-1, 0x1.5ab07dd485429p-1, 0x1.4bfdad5362a27p-1, 0x1.3dea64c123422p-1,
+    0x1.306fe0a31b715p-1, 0x1.2387a6e756238p-1, 0x1.172b83c7d517bp-1, 0x1.0b5586cf9890fp-1};
 
 struct Args {
   const void* logits;
@@ -61,9 +68,10 @@ __device__ __forceinline__ float okey_inv(uint32_t k) { return __uint_as_float((
 __device__ __forceinline__ uint64_t key_of(float x, uint32_t token) { return ((uint64_t)okey(x) << 32) | (0xffffffffu - token); }
 __device__ __forceinline__ float logit_of(uint64_t key) { return okey_inv((uint32_t)(key >> 32)); }
 
-// Parts that are not live together share their place.  What another CTA writes may arrive as soon as this one has joined the barrier before: the
-// joint list lies over the own histogram (given away before the barrier in front of the list), the own list over the inbox, the sorted list over the joint
-// histogram.
+// Parts that are not live together share their place.  What another CTA writes may arrive as soon as this one has joined the barrier before; so
+// over the own histogram, which is given away before the barrier in front of them, lies what comes with or behind the lists; over the inbox,
+// read before the barrier behind it, the own list, given away before its barrier, and the last sums; over the joint histogram, written behind a
+// barrier, what comes with the first one.
 struct Hist {
   uint32_t cnt[NB], lo[NB], hi[NB];        // tokens, mass in two words
 };
@@ -76,17 +84,21 @@ struct Shared {
   union {
     Hist inbox;                            // [CTA][its share of the steps], written by the others
     uint64_t list[CAP];
+    ulonglong2 end[MAX_CLUSTER][NW];       // mass and number of every warp's kept tokens, written by the others
   };
   union {
     Hist sum;                              // all tokens, written by the others
-    uint64_t sorted[CAP];
+    struct {
+      int2 ends[MAX_CLUSTER][NW];          // largest and smallest logit of every warp as ordered(), written by the others
+      uint64_t sent[CAP];                  // short lists, written by the others (perhaps while the ends are read)
+    };
+    uint64_t mass[2][FEW];                 // of a short list
   };
   double tab[16][16];                      // 2^(-i/16), sixteen times, so that no two lanes of a half warp meet on a bank
   uint64_t scan[2][NW];
   uint64_t found[4];
-  int32_t high[MAX_CLUSTER], low[MAX_CLUSTER];         // largest and smallest logit as ordered(), written by the others
-  uint64_t total[MAX_CLUSTER], range[MAX_CLUSTER][2];
-  uint32_t kept[MAX_CLUSTER], few[MAX_CLUSTER];
+  uint64_t range[MAX_CLUSTER][2];          // written by the others
+  uint32_t few[MAX_CLUSTER];
   uint32_t n_list, n_all;
 };
 
@@ -105,10 +117,16 @@ constexpr int32_t POS_INF = 0x7f800000, NEG_INF = (int32_t)0x807fffff;
 
 struct Scale {                             // of a row
   double top, c;                           // largest logit; 16 log2(e) / T
+  int limit;                               // high word of a gap of 47 octaves and a little, whose weight rounds to 0
 };
-// 2^(-y / 16) for y in [0, 2^14], scaled and shifted into the low bits of `onto`.
-__device__ __forceinline__ double power(double y, double onto, const double (*tab)[16]) {
-  const double k = y + MAGIC, r = y - (k - MAGIC);
+// top - z, at most a limit (its high word) and a little.
+__device__ __forceinline__ double gap_of(float z, double top, int limit) {
+  const double d = top - (double)z;
+  return __hiloint2double(min(__double2hiint(d), limit), __double2loint(d));
+}
+// onto + 2^(-d c / 16), d c in [0, 2^14]
+__device__ __forceinline__ double power(double d, double c, double onto, const double (*tab)[16]) {
+  const double k = fma(d, c, MAGIC), r = fma(d, c, MAGIC - k);
   const int ki = __double2loint(k);
   double p = fma(r, -0x1.5d897e525c216p-30, 0x1.3b2c9b8a6caeap-23);
   p = fma(p, r, -0x1.c6b08d6f2a289p-17);
@@ -116,17 +134,15 @@ __device__ __forceinline__ double power(double y, double onto, const double (*ta
   p = fma(p, r, -0x1.62e42fefa39f3p-5);
   p = fma(p, r, 1.0);
   const double t = tab[ki & 15][threadIdx.x & 15];
-  return fma(__hiloint2double(__double2hiint(t) - ((ki >> 4) << 20), __double2loint(t)), p, onto);
+  return fma(__hiloint2double(__double2hiint(t) - (ki & ~15) * 65536, __double2loint(t)), p, onto);
 }
-// y of a logit, at most `most` (the high word of a limit) and a little.
-__device__ __forceinline__ double steps_below(float z, const Scale& s, int most) {
-  const double y = (s.top - (double)z) * s.c;
-  return __hiloint2double(min(__double2hiint(y), most), __double2loint(y));
+// Between 128 and 256 a float64 goes in steps of 2^-45: what is added to it is rounded to them, and up to 127 weights can be.
+constexpr double SUM45 = 128.0;
+__device__ __forceinline__ double add45(double sum, float z, const Scale& s, const double (*tab)[16]) {
+  return power(gap_of(z, s.top, s.limit), s.c, sum, tab);
 }
-// The weight in steps of 2^-45.  From y = 752 on it rounds to 0.
-__device__ __forceinline__ uint64_t weight45(float z, const Scale& s, const double (*tab)[16]) {
-  return (uint64_t)__double_as_longlong(power(steps_below(z, s, 0x40878000), MAGIC45, tab)) - 0x4068000000000000ull;
-}
+__device__ __forceinline__ uint64_t of_sum45(double sum) { return (uint64_t)__double_as_longlong(sum) - 0x4060000000000000ull; }
+__device__ __forceinline__ uint64_t weight45(float z, const Scale& s, const double (*tab)[16]) { return of_sum45(add45(SUM45, z, s, tab)); }
 
 __device__ __forceinline__ uint64_t warp_scan(uint64_t v) {                 // inclusive
   const int lane = threadIdx.x & 31;
@@ -135,6 +151,11 @@ __device__ __forceinline__ uint64_t warp_scan(uint64_t v) {                 // i
     const uint64_t t = __shfl_up_sync(0xffffffffu, v, o);
     if (lane >= o) v += t;
   }
+  return v;
+}
+__device__ __forceinline__ uint64_t warp_sum(uint64_t v) {
+#pragma unroll
+  for (int o = 16; o >= 1; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
 // Sums of two numbers over the threads before this one, and of all.
@@ -182,19 +203,115 @@ template <> struct Vec<__nv_bfloat16> {
 __device__ __forceinline__ float to_f(float x) { return x; }
 __device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
 
-// The step of a histogram in which a token falls, -1: none.  First equal steps of z, of the tokens that reach `border`; then equal steps of the
+// Tokens that reach a key in order: by the logit as a number, and where that is equal by the key.
+struct Border {
+  uint64_t key;
+  int32_t hi, lo;                          // over hi: yes, below lo: no
+  __device__ __forceinline__ explicit Border(uint64_t k) : key(k), hi(NEG_INF), lo(INT32_MAX) {
+    if (k != 0) {
+      hi = ordered(logit_of(k));
+      lo = hi == 0 ? -1 : hi;
+    }
+  }
+  __device__ __forceinline__ bool keeps(float x, uint32_t token) const {
+    const int32_t o = ordered(x);
+    return o > hi || (o >= lo && key_of(x, token) >= key);
+  }
+};
+// The step of a histogram in which a token falls, -1: none.  First equal steps of z, of the tokens that a border keeps; then equal steps of the
 // keys from hi down to lo.
 struct Where {
   bool linear;
   float top, scale;
-  uint64_t border, lo, hi;
+  uint64_t lo, hi;
   int shift;
-  __device__ __forceinline__ int operator()(float z, uint32_t token) const {
+  // Smallest and largest z of the steps a .. b, and a little more.
+  __device__ __forceinline__ float2 around(int a, int b) const {
+    if (!linear) return make_float2(logit_of(lo), logit_of(hi));
+    if (scale == 0.f) return make_float2(-FLT_MAX, top);
+    const float from = b == NB - 1 ? -FLT_MAX : top - (float)(b + 1) / scale, to = top - (float)a / scale, slack = 1e-6f * fmaxf(fabsf(from), fabsf(to)) + 1e-30f;
+    return make_float2(fmaxf(from - slack - 1e-5f * (float)(b + 1) / scale, -FLT_MAX), to + slack + 1e-5f * (float)a / scale);
+  }
+  __device__ __forceinline__ int by_logit(float z) const { return (int)fminf((top - z) * scale, (float)(NB - 1)); }
+  __device__ __forceinline__ int by_logit(float z, uint32_t token, const Border& border) const {
+    return border.keeps(z, token) ? by_logit(z) : -1;
+  }
+  __device__ __forceinline__ int by_key(float z, uint32_t token) const {
     const uint64_t k = key_of(z, token);
-    if (linear) return z == -INFINITY || k < border ? -1 : (int)fminf((top - z) * scale, (float)(NB - 1));
     return k < lo || k > hi ? -1 : (int)((hi - k) >> shift);
   }
+  __device__ __forceinline__ int operator()(float z, uint32_t token, const Border& border) const {
+    return linear ? by_logit(z, token, border) : by_key(z, token);
+  }
 };
+
+__device__ __forceinline__ uint64_t lds64(const uint64_t* p) {
+  uint64_t v;
+  asm volatile("ld.shared.u64 %0, [%1];" : "=l"(v) : "r"((uint32_t)__cvta_generic_to_shared(p)) : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts64(uint64_t* p, uint64_t v) {
+  asm volatile("st.shared.u64 [%0], %1;" ::"r"((uint32_t)__cvta_generic_to_shared(p)), "l"(v) : "memory");
+}
+__device__ __forceinline__ void larger_first(uint64_t& x, uint64_t& y, bool descending) {
+  if ((x < y) == descending) {
+    const uint64_t t = x;
+    x = y;
+    y = t;
+  }
+}
+// a[0 .. n) in shared memory, different and not 0, into descending order; a has CAP places.  Bitonic: a warp has 64 places in registers, and what lies further
+// apart is exchanged in shared memory.
+__device__ __noinline__ void sort_descending(uint64_t* a, int n) {
+  static_assert(CAP == NT * 2, "64 places per warp");
+  const int tid = threadIdx.x, lane = tid & 31, base = tid / 32 * 64;
+  int size = 64;
+  while (size < n) size *= 2;
+  const bool mine = base < size;                                           // (of the warp)
+  uint64_t x = base + lane < n ? lds64(a + base + lane) : 0, y = base + 32 + lane < n ? lds64(a + base + 32 + lane) : 0;
+  auto inside = [&](int len) {                                             // distances up to 32
+    if (len >= 64) larger_first(x, y, ((base + lane) & len) == 0);
+#pragma unroll
+    for (int d = 16; d >= 1; d /= 2) {
+      if (d >= len) continue;
+      const uint64_t ox = __shfl_xor_sync(0xffffffffu, x, d), oy = __shfl_xor_sync(0xffffffffu, y, d);
+      const bool first = (lane & d) == 0;
+      x = (x > ox) == (first == (((base + lane) & len) == 0)) ? x : ox;
+      y = (y > oy) == (first == (((base + 32 + lane) & len) == 0)) ? y : oy;
+    }
+  };
+  if (mine)
+    for (int len = 2; len <= 64; len *= 2) inside(len);
+  for (int len = 128; len <= size; len *= 2) {
+    if (mine) {
+      sts64(a + base + lane, x);
+      sts64(a + base + 32 + lane, y);
+    }
+    for (int d = len / 2; d >= 64; d /= 2) {
+      __syncthreads();
+      if (tid < size / 2) {
+        const int i = 2 * tid - (tid & (d - 1));
+        uint64_t u = lds64(a + i), v = lds64(a + i + d);
+        if ((u < v) == ((i & len) == 0)) {
+          sts64(a + i, v);
+          sts64(a + i + d, u);
+        }
+      }
+    }
+    __syncthreads();
+    if (mine) {
+      x = lds64(a + base + lane);
+      y = lds64(a + base + 32 + lane);
+      inside(len);
+    }
+  }
+  __syncthreads();
+  if (mine) {
+    sts64(a + base + lane, x);
+    sts64(a + base + 32 + lane, y);
+  }
+  __syncthreads();
+}
 
 template <typename T>
 __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ Args a) {
@@ -237,7 +354,7 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
     low = min(low, o);
   };
   if (tid < head) see(z[tid] = to_f(src[tid]));
-#pragma unroll 4
+#pragma unroll 8
   for (int i = tid; i < vecs; i += NT) {
     float x[N];
     Vec<T>::open(*reinterpret_cast<const uint4*>(src + head + i * N), x);
@@ -250,47 +367,52 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
     const int i = head + vecs * N + tid;
     if (i < n_own) see(z[i] = to_f(src[i]));
   }
-  if (tid < 256) sh.tab[tid >> 4][tid & 15] = exp2(-(tid >> 4) / 16.0);
+  if (tid < 256) sh.tab[tid >> 4][tid & 15] = ROOTS[tid >> 4];
   if (tid == 0) sh.n_list = sh.n_all = 0;
   const bool greedy = __float_as_uint(t) << 1 == 0u || k == 1, by_k = k > 0 && k < a.vocab, by_p = p < 1.f;
   const bool bounded = by_k && k <= SMALL_K;                               // a bound for the k-th largest
+  double temp = 1.0, below = 0.0;                                          // temperature, and how far below the largest logit m reaches
+  Scale scale;
+  if (!greedy) {
+    temp = exact_double(t);
+    if (m > 0.f && m < 1.f) below = temp * log(exact_double(m));
+    scale.c = 16.0 * 1.4426950408889634074 / temp;
+    scale.limit = __double2hiint(temp * (47.0 * 0.69314718055994530942)) + 1;
+  }
   cluster_wait();
-  if (bounded && !greedy) {                                                // maxima of 2 C lanes, GROUPS over the cluster
+  if (bounded && !greedy) {                                                // maxima of 4 C lanes, GROUPS over the cluster
     int32_t g = high;
-    for (int o = 1; o < 2 * C; o <<= 1) g = max(g, __shfl_xor_sync(0xffffffffu, g, o));
-    if (lane % (2 * C) == 0)
-      for (int c = 0; c < C; ++c) cl.map_shared_rank(&sh, c)->group[rank * (GROUPS / C) + tid / (2 * C)] = g;
+    for (int o = 1; o < 4 * C; o <<= 1) g = max(g, __shfl_xor_sync(0xffffffffu, g, o));
+    g = __shfl_sync(0xffffffffu, g, lane / C * 4 * C);
+    if (lane < 8) cl.map_shared_rank(&sh, lane % C)->group[rank * (GROUPS / C) + warp * (8 / C) + lane / C] = g;
   }
   {
     const int32_t h = __reduce_max_sync(0xffffffffu, high), l = __reduce_min_sync(0xffffffffu, low);
-    if (lane == 0) sh.scan[0][warp] = ((uint64_t)(uint32_t)h << 32) | (uint32_t)l;
-    __syncthreads();
-    if (warp == 0) {
-      const uint64_t v = sh.scan[0][lane & (NW - 1)];
-      high = __reduce_max_sync(0xffffffffu, (int32_t)(v >> 32));
-      low = __reduce_min_sync(0xffffffffu, (int32_t)(uint32_t)v);
-      if (lane < C) {
-        Shared* to = cl.map_shared_rank(&sh, lane);
-        to->high[rank] = high;
-        to->low[rank] = low;
-      }
-    }
+    if (lane < C) cl.map_shared_rank(&sh, lane)->ends[rank][warp] = make_int2(h, l);
   }
   cluster_barrier();
   high = INT32_MIN, low = INT32_MAX;
-  int leader = 0;                                                          // the first CTA that has the largest logit
-  for (int c = C - 1; c >= 0; --c) {
-    const int32_t h = sh.high[c] == -1 ? 0 : sh.high[c];                   // (-0 and +0 are equal)
-    if (h >= high) high = h, leader = c;
-    low = min(low, sh.low[c]);
+  for (int i = lane; i < C * NW; i += 32) {
+    const int2 v = (&sh.ends[0][0])[i];
+    high = max(high, v.x);
+    low = min(low, v.y);
   }
+  high = __reduce_max_sync(0xffffffffu, high);
+  low = __reduce_min_sync(0xffffffffu, low);
+  if (high == -1) high = 0;                                                // (-0 and +0 are equal)
   if (high >= POS_INF || high <= NEG_INF || low < NEG_INF) {
     if (rank == 0 && tid == 0) result(-1, -INFINITY, 0);
     return;
   }
   const float top = __int_as_float(high ^ ((high >> 31) & 0x7fffffff));
   if (greedy) {
-    if (rank != leader) return;
+    // the first CTA that has the largest logit looks for it
+    int leader = C * NW;
+    for (int i = lane; i < C * NW; i += 32) {
+      const int32_t h = (&sh.ends[0][0])[i].x;
+      if ((h == -1 ? 0 : h) == high) leader = min(leader, i);
+    }
+    if (rank != __reduce_min_sync(0xffffffffu, leader) / NW) return;
     uint32_t at = ~0u;
     const uint32_t want = okey(top);
     for (int i = tid; i < n_own; i += NT)
@@ -304,17 +426,14 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
     }
     return;
   }
-  Scale scale;
   scale.top = (double)top;
-  const double temp = exact_double(t);
-  scale.c = 16.0 * 1.4426950408889634074 / temp;
   auto log_of = [&](float x, uint64_t S) { return (float)(((double)x - scale.top) / temp - log((double)S * 0x1p-45)); };
   uint64_t by_m = 0;                                                       // key of the smallest logit with w >= m
   if (m > 0.f) {
-    const uint32_t near = okey((float)(scale.top + (m < 1.f ? temp * log(exact_double(m)) : 0.0)));
+    const uint32_t near = okey((float)(scale.top + below));
     const uint32_t mine = near + lane < 16u ? 0u : near + lane - 16u;
     const float x = okey_inv(mine);
-    const double w = power(steps_below(x <= top ? x : top, scale, 0x40d00000), 0.0, sh.tab);
+    const double w = power(gap_of(x <= top ? x : top, scale.top, __double2hiint(temp * 690.0)), scale.c, 0.0, sh.tab);
     const uint32_t hit = __ballot_sync(0xffffffffu, x == x && x >= -FLT_MAX && w >= (m < 1.f ? exact_double(m) : 1.0));
     // (near a logit of 0 floats lie closer than weights are told apart: any of these is right to 2^-46)
     by_m = (uint64_t)(hit == 0 ? near : near + (uint32_t)__ffs((int)hit) - 17u) << 32;
@@ -324,21 +443,54 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
   // All that can be kept is a list of nn tokens in the first CTA, which sorts it, cuts it and draws from it.  cut_k: the list is to be cut to k; then
   // the mass that p is a part of is the list's.
   auto draw_from_list = [&](int nn, bool cut_k, uint64_t target) {
-    for (int i = tid; i < nn; i += NT) {
-      const uint64_t key = sh.all[i];
-      int before = 0;
-#pragma unroll 4
-      for (int o = 0; o < nn; ++o) before += sh.all[o] > key ? 1 : 0;
-      sh.sorted[before] = key;
+    if (nn <= FEW) {                                                       // by counting, four threads a token
+      const int i = tid >> 2, q = tid & 3;
+      const uint64_t key = i < nn ? sh.all[i] : 0;
+      if (tid < nn) sh.mass[0][tid] = weight45(logit_of(sh.all[tid]), scale, sh.tab);
+      __syncthreads();
+      const uint64_t w = i < nn ? sh.mass[0][i] : 0;
+      int place = 0;                                                       // in order, and the mass in front
+      uint64_t front = 0;
+      for (int o = q; o < nn; o += 4)
+        if (sh.all[o] > key) ++place, front += sh.mass[0][o];
+      front += __shfl_xor_sync(0xffffffffu, front, 1);
+      front += __shfl_xor_sync(0xffffffffu, front, 2);
+      place += __shfl_xor_sync(0xffffffffu, place, 1);
+      place += __shfl_xor_sync(0xffffffffu, place, 2);
+      bool keep = i < nn && (!cut_k || place < k) && key >= by_m;
+      if (by_p) {
+        if (cut_k) {
+          // (the last of the first k knows their mass)
+          if (q == 0 && i < nn && place == min(k, nn) - 1) sh.found[0] = front + w;
+          __syncthreads();
+          target = p > 0.f ? max((uint64_t)1, (uint64_t)ceil((double)p * (double)sh.found[0])) : 1;
+        }
+        keep = keep && front < target;
+      }
+      if (q == 0 && i < nn) sh.mass[1][i] = keep ? w : 0;
+      const int nk = __syncthreads_count(keep && q == 0);
+      uint64_t at = 0, S = 0;                                              // in the order of the vocabulary (the lower half: 2^32 - 1 - token)
+      for (int o = q; o < nn; o += 4) {
+        const uint64_t v = sh.mass[1][o];
+        S += v;
+        if ((uint32_t)sh.all[o] > (uint32_t)key) at += v;
+      }
+      at += __shfl_xor_sync(0xffffffffu, at, 1);
+      at += __shfl_xor_sync(0xffffffffu, at, 2);
+      S += __shfl_xor_sync(0xffffffffu, S, 1);
+      S += __shfl_xor_sync(0xffffffffu, S, 2);
+      const uint64_t goal = min((uint64_t)((double)u * (double)S), S - 1);
+      if (q == 0 && keep && goal >= at && goal < at + w) result((int32_t)(0xffffffffu - (uint32_t)key), log_of(logit_of(key), S), nk);
+      return;
     }
-    __syncthreads();
+    sort_descending(sh.all, nn);
     constexpr int PER = CAP / NT;
     const int most = cut_k ? min(nn, k) : nn;
     uint64_t w[PER], mine = 0, ones = 0, all, none;
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
       const int i = tid * PER + e;
-      w[e] = i < most ? weight45(logit_of(sh.sorted[i]), scale, sh.tab) : 0;
+      w[e] = i < most ? weight45(logit_of(sh.all[i]), scale, sh.tab) : 0;
       mine += w[e];
     }
     block_before(sh, mine, ones, all, none);
@@ -348,21 +500,17 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
       const int i = tid * PER + e;
-      if (i < most && (!by_p || run < target) && sh.sorted[i] >= by_m) ++kept;
+      if (i < most && (!by_p || run < target) && sh.all[i] >= by_m) ++kept;
       run += w[e];
     }
     uint64_t before_kept = kept, all_kept_n, zero = 0, zeros;
     block_before(sh, before_kept, zero, all_kept_n, zeros);
     const int nk = (int)all_kept_n;
-    // in the order of the vocabulary
-    for (int i = tid; i < nk; i += NT) {
-      const uint64_t key = sh.sorted[i];
-      const uint32_t token = (uint32_t)key;
-      int before = 0;
-#pragma unroll 4
-      for (int o = 0; o < nk; ++o) before += (uint32_t)sh.sorted[o] > token ? 1 : 0;    // (the lower half: 2^32 - 1 - token)
-      sh.all[before] = key;
-    }
+    // in the order of the vocabulary: the halves of the keys (logit; 2^32 - 1 - token) change places
+    for (int i = tid; i < nk; i += NT) sh.all[i] = sh.all[i] << 32 | sh.all[i] >> 32;
+    __syncthreads();
+    sort_descending(sh.all, nk);
+    for (int i = tid; i < nk; i += NT) sh.all[i] = sh.all[i] << 32 | sh.all[i] >> 32;
     __syncthreads();
     mine = 0;
 #pragma unroll
@@ -389,41 +537,69 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
   Where where;
   where.top = top;
   const float range = fminf(top - __int_as_float(low ^ ((low >> 31) & 0x7fffffff)), OCTAVES * kLn2 * t);
-  where.scale = range > 1e-30f ? (float)NB / range : 0.f;
-  where.border = 0;
+  Border border(0);
   if (bounded) {
-    if (tid < GROUPS) {
-      const int32_t g = sh.group[tid];
-      int before = 0;
-#pragma unroll 8
-      for (int o = 0; o < GROUPS; ++o) {
-        const int32_t x = sh.group[o];
-        before += x > g || (x == g && o < tid) ? 1 : 0;
+    // the smallest of the groups' maxima that fewer than k exceed: the k-th largest
+    if (tid == 0) sh.found[0] = 0x7fffffff;
+    {
+      const int32_t g = sh.group[tid >> 2];
+      int over = 0;
+#pragma unroll 2
+      for (int o = 0; o < GROUPS / 4; o += 4) {
+        const int4 x = *reinterpret_cast<const int4*>(sh.group + (tid & 3) * (GROUPS / 4) + o);
+        over += (x.x > g ? 1 : 0) + (x.y > g ? 1 : 0) + (x.z > g ? 1 : 0) + (x.w > g ? 1 : 0);
       }
-      if (before == k - 1) sh.found[0] = (uint32_t)(g == 0 ? -1 : g);       // (-0 is as large as +0)
+      over += __shfl_xor_sync(0xffffffffu, over, 1);
+      over += __shfl_xor_sync(0xffffffffu, over, 2);
+      const int32_t least = __reduce_min_sync(0xffffffffu, over < k ? g : INT32_MAX);
+      __syncthreads();
+      if (lane == 0) atomicMin((int32_t*)&sh.found[0], least);
     }
     __syncthreads();
-    const int32_t bound = (int32_t)(uint32_t)sh.found[0];
-    for (int i = tid; i < n_own; i += NT) {
-      const int32_t o = ordered(z[i]);
-      if (o >= bound && o > NEG_INF) {
-        const uint32_t at = atomicAdd(&sh.n_list, 1u);
-        if (at < CAP) sh.list[at] = key_of(z[i], first + i);
+    // (as a number; of subnormal ones all may pass for 0 and so for as large as the bound, and none is lost)
+    const int32_t b = (int32_t)(uint32_t)sh.found[0];
+    const float bound = b <= NEG_INF ? -FLT_MAX : __int_as_float(b ^ ((b >> 31) & 0x7fffffff));
+    auto take = [&](int i) {
+      const uint32_t at = atomicAdd(&sh.n_list, 1u);
+      if (at < CAP) sh.list[at] = key_of(z[i], first + i);
+    };
+    int i = tid;
+    for (; i + 3 * NT < n_own; i += 4 * NT) {
+      const float x0 = z[i], x1 = z[i + NT], x2 = z[i + 2 * NT], x3 = z[i + 3 * NT];
+      if (x0 >= bound || x1 >= bound || x2 >= bound || x3 >= bound) {
+        if (x0 >= bound) take(i);
+        if (x1 >= bound) take(i + NT);
+        if (x2 >= bound) take(i + 2 * NT);
+        if (x3 >= bound) take(i + 3 * NT);
       }
     }
+    for (; i < n_own; i += NT)
+      if (z[i] >= bound) take(i);
     __syncthreads();
-    if (tid < C) cl.map_shared_rank(&sh, tid)->few[rank] = sh.n_list;
+    const int room = CAP / C, own = (int)sh.n_list;
+    if (tid < C) cl.map_shared_rank(&sh, tid)->few[rank] = own;
+    if (own <= room) {
+      Shared* to = cl.map_shared_rank(&sh, 0);
+      for (int o = tid; o < own; o += NT) to->sent[rank * room + o] = sh.list[o];
+    }
     cluster_barrier();
-    uint32_t at = 0, n = 0;
+    int n = 0;
+    bool fits = true;
     for (int c = 0; c < C; ++c) {
-      at += c < rank ? sh.few[c] : 0;
+      fits = fits && (int)sh.few[c] <= room;
       n += sh.few[c];
     }
-    if (n <= CAP) {
-      Shared* to = cl.map_shared_rank(&sh, 0);
-      for (int i = tid; i < (int)sh.n_list; i += NT) to->all[at + i] = sh.list[i];
-      cluster_barrier();
-      if (rank == 0) draw_from_list((int)n, true, 0);
+    if (fits) {
+      if (rank != 0) return;
+      for (int o = tid; o < CAP; o += NT) {
+        const int c = o / room, i = o % room;
+        if (i >= (int)sh.few[c]) continue;
+        int at = i;
+        for (int x = 0; x < c; ++x) at += sh.few[x];
+        sh.all[at] = sh.sent[o];
+      }
+      __syncthreads();
+      draw_from_list(n, true, 0);
       return;
     }
     __syncthreads();
@@ -438,21 +614,45 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
     uint32_t n = 0;
     bool all_kept = false;
     where.linear = true;
+    // (the tokens below (1 - p) / vocab have less than 1 - p together, so that the last one to be kept is none of them)
+    const float reach = mass ? fminf(range, t * (__logf((float)a.vocab / (1.f - p)) + 0.1f)) : range;
+    where.scale = reach > 1e-30f ? (float)NB / reach : 0.f;
 #pragma unroll 1
     for (;;) {
       // the joint histogram
       for (int i = tid; i < NB; i += NT) sh.own.cnt[i] = sh.own.lo[i] = sh.own.hi[i] = 0;
       __syncthreads();
-      for (int i = tid; i < n_own; i += NT) {
-        const float x = z[i];
-        const int b = where(x, first + i);
-        if (b >= 0) {
-          atomicAdd(&sh.own.cnt[b], 1u);
-          if (mass) {
-            const uint64_t w = weight45(x, scale, sh.tab);
-            const uint32_t wl = (uint32_t)w, old = atomicAdd(&sh.own.lo[b], wl);
-            atomicAdd(&sh.own.hi[b], (uint32_t)(w >> 32) + (old + wl < old ? 1u : 0u));
+      // four at a time, so that they do not wait for one another; the mass of the last step, where p leaves most tokens, is added up here
+      uint64_t rest = 0;
+      auto count = [&](auto&& step_of) {
+        for (int i = tid; i < n_own; i += 4 * NT) {
+          int b[4];
+          uint64_t w[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float x = i + e * NT < n_own ? z[i + e * NT] : -INFINITY;
+            b[e] = step_of(x, first + i + e * NT);
+            w[e] = mass ? weight45(x, scale, sh.tab) : 0;
           }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if (b[e] >= 0) atomicAdd(&sh.own.cnt[b[e]], 1u);
+            if (b[e] == NB - 1) rest += w[e];
+            if (mass && (uint32_t)b[e] < NB - 1) {
+              const uint32_t wl = (uint32_t)w[e], old = atomicAdd(&sh.own.lo[b[e]], wl);
+              atomicAdd(&sh.own.hi[b[e]], (uint32_t)(w[e] >> 32) + (old + wl < old ? 1u : 0u));
+            }
+          }
+        }
+      };
+      if (!where.linear) count([&](float x, uint32_t token) { return where.by_key(x, token); });
+      else if (border.key != 0) count([&](float x, uint32_t token) { return where.by_logit(x, token, border); });
+      else count([&](float x, uint32_t) { return x >= -FLT_MAX ? where.by_logit(x) : -1; });
+      if (mass) {
+        rest = warp_sum(rest);
+        if (lane == 0) {
+          const uint32_t wl = (uint32_t)rest, old = atomicAdd(&sh.own.lo[NB - 1], wl);
+          atomicAdd(&sh.own.hi[NB - 1], (uint32_t)(rest >> 32) + (old + wl < old ? 1u : 0u));
         }
       }
       __syncthreads();
@@ -522,12 +722,13 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
 
       if (where.linear && upto <= CAP) {
         // All that can be kept is a short list: the first CTA sorts it, cuts it and draws from it.
+        Shared* to = cl.map_shared_rank(&sh, 0);
+        const float2 near = where.around(0, step);
+#pragma unroll 4
         for (int i = tid; i < n_own; i += NT) {
-          const int b = where(z[i], first + i);
-          if (b >= 0 && b <= step) {
-            Shared* to = cl.map_shared_rank(&sh, 0);
-            to->all[atomicAdd(&to->n_all, 1u)] = key_of(z[i], first + i);
-          }
+          if (z[i] < near.x) continue;
+          const int b = where(z[i], first + i, border);
+          if (b >= 0 && b <= step) to->all[atomicAdd(&to->n_all, 1u)] = key_of(z[i], first + i);
         }
         cluster_barrier();
         if (rank == 0) draw_from_list((int)upto, pass == 0, target);
@@ -537,7 +738,7 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
       if (where.linear) {                                                  // the keys between which the step's tokens lie
         uint64_t lo = ~0ull, hi = 0;
         for (int i = tid; i < n_own; i += NT) {
-          if (where(z[i], first + i) == step) {
+          if (where(z[i], first + i, border) == step) {
             const uint64_t key = key_of(z[i], first + i);
             lo = min(lo, key);
             hi = max(hi, key);
@@ -573,8 +774,10 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
     }
     if (all_kept) continue;
     // the step's tokens, in every CTA, and sorted
+    const float2 near = where.around(step, step);
+#pragma unroll 4
     for (int i = tid; i < n_own; i += NT)
-      if (where(z[i], first + i) == step) sh.list[atomicAdd(&sh.n_list, 1u)] = key_of(z[i], first + i);
+      if (z[i] >= near.x && z[i] <= near.y && where(z[i], first + i, border) == step) sh.list[atomicAdd(&sh.n_list, 1u)] = key_of(z[i], first + i);
     __syncthreads();
     {
       const int own = (int)sh.n_list;
@@ -587,73 +790,81 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
       }
     }
     cluster_barrier();
-    for (int i = tid; i < (int)n; i += NT) {
-      const uint64_t key = sh.all[i];
-      int before = 0;
-#pragma unroll 4
-      for (int o = 0; o < (int)n; ++o) before += sh.all[o] > key ? 1 : 0;
-      sh.sorted[before] = key;
-    }
-    __syncthreads();
+    sort_descending(sh.all, (int)n);
     if (!mass) {
-      if (tid == 0) sh.found[0] = sh.sorted[target - above - 1];
+      if (tid == 0) sh.found[0] = sh.all[target - above - 1];
     } else {
       constexpr int PER = CAP / NT;
       uint64_t w[PER], at = 0, zero = 0, all, zeros;
 #pragma unroll
       for (int e = 0; e < PER; ++e) {
         const int i = tid * PER + e;
-        w[e] = i < (int)n ? weight45(logit_of(sh.sorted[i]), scale, sh.tab) : 0;
+        w[e] = i < (int)n ? weight45(logit_of(sh.all[i]), scale, sh.tab) : 0;
         at += w[e];
       }
       block_before(sh, at, zero, all, zeros);
       at += above;
 #pragma unroll
       for (int e = 0; e < PER; ++e) {
-        if (at < target && at + w[e] >= target) sh.found[0] = sh.sorted[tid * PER + e];
+        if (at < target && at + w[e] >= target) sh.found[0] = sh.all[tid * PER + e];
         at += w[e];
       }
     }
     if (tid == 0) sh.n_list = sh.n_all = 0;
     __syncthreads();
-    where.border = max(where.border, sh.found[0]);
+    border = Border(max(border.key, sh.found[0]));
     __syncthreads();
   }
 
   // ---- the draw, in the order of the vocabulary ----
-  where.border = max(where.border, by_m);
+  border = Border(max(border.key, by_m));
   const int sub = ((n_own + NT - 1) / NT) | 1, i0 = min(n_own, tid * sub), i1 = min(n_own, i0 + sub);   // (odd: no two lanes on one bank)
-  uint64_t mine = 0, kept = 0, own, own_kept;
-  if (where.border == 0) {
-    int n = 0;
-#pragma unroll 4
-    for (int i = i0; i < i1; ++i) {
-      const float x = z[i];
-      mine += weight45(x, scale, sh.tab);                                  // (0 for -inf)
-      n += x != -INFINITY ? 1 : 0;
+  double sum[4] = {SUM45, SUM45, SUM45, SUM45};
+  uint32_t kept = i1 - i0;
+  const bool some = border.key != 0 || low <= NEG_INF;                     // not all tokens
+  if (some) kept = 0;
+  if (!some) {
+    for (int i = i0; i < i1; i += 4) {
+      float x[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = i + e < i1 ? z[i + e] : -INFINITY;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] = add45(sum[e], x[e], scale, sh.tab);        // (nothing for -inf)
     }
-    kept = n;
   } else {
-    for (int i = i0; i < i1; ++i) {
-      const float x = z[i];
-      if (key_of(x, first + i) >= where.border && x != -INFINITY) mine += weight45(x, scale, sh.tab), ++kept;
+    for (int base = i0; base < i1; base += 32) {                           // which are kept, then their weights
+      uint32_t bits = 0;
+#pragma unroll 4
+      for (int i = min(base + 32, i1) - 1; i >= base; --i) bits = bits * 2 + (border.keeps(z[i], first + i) ? 1 : 0);
+      kept += __popc(bits);
+      while (bits != 0) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          sum[e] = add45(sum[e], bits != 0 ? z[base + __ffs((int)bits) - 1] : -INFINITY, scale, sh.tab);
+          bits &= bits - 1;
+        }
+      }
     }
   }
-  uint64_t run = mine;
-  block_before(sh, run, kept, own, own_kept);
-  if (tid < C) {
-    Shared* to = cl.map_shared_rank(&sh, tid);
-    to->total[rank] = own;
-    to->kept[rank] = (uint32_t)own_kept;
+  static_assert(MAX_SLICE / NT + 2 < 127, "a thread's sum stays below 128");
+  const uint64_t mine = of_sum45(sum[0]) + of_sum45(sum[1]) + of_sum45(sum[2]) + of_sum45(sum[3]), upto = warp_scan(mine);
+  kept = __reduce_add_sync(0xffffffffu, kept);
+  {
+    const uint64_t all = __shfl_sync(0xffffffffu, upto, 31);
+    if (lane < C) cl.map_shared_rank(&sh, lane)->end[rank][warp] = make_ulonglong2(all, kept);
   }
   cluster_barrier();
-  uint64_t S = 0;
+  uint64_t S = 0, run = 0;
   uint32_t n_kept = 0;
-  for (int c = 0; c < C; ++c) {
-    run += c < rank ? sh.total[c] : 0;
-    S += sh.total[c];
-    n_kept += sh.kept[c];
+  for (int i = lane; i < C * NW; i += 32) {
+    const ulonglong2 v = (&sh.end[0][0])[i];
+    S += v.x;
+    run += i < rank * NW + warp ? v.x : 0;
+    n_kept += (uint32_t)v.y;
   }
+  S = warp_sum(S);
+  run = warp_sum(run) + upto - mine;
+  n_kept = __reduce_add_sync(0xffffffffu, n_kept);
   const uint64_t goal = min((uint64_t)((double)u * (double)S), S - 1);
   const uint32_t here = __ballot_sync(0xffffffffu, goal >= run && goal < run + mine);
   if (here != 0) {                                                         // one warp of the cluster, along the tokens of one of its lanes
@@ -662,7 +873,7 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
     for (int j = __shfl_sync(0xffffffffu, i0, lead); j < j1; j += 32) {
       const int i = j + lane;
       const float x = i < j1 ? z[i] : -INFINITY;
-      const uint64_t w = x != -INFINITY && key_of(x, first + i) >= where.border ? weight45(x, scale, sh.tab) : 0, up = at + warp_scan(w);
+      const uint64_t w = border.keeps(x, first + i) ? weight45(x, scale, sh.tab) : 0, up = at + warp_scan(w);
       if (goal < up && goal >= up - w) result(first + i, log_of(x, S), (int32_t)n_kept);
       at = __shfl_sync(0xffffffffu, up, 31);
     }
