@@ -1,7 +1,7 @@
 // actkv_penalize: biases, penalties for tokens that the history holds, and masks on logits, before a token is drawn.
 //
 // A CTA has a slice of the vocabulary and some consecutive rows of one request.  It keeps a word per token of the slice in shared memory
-// (bit 31: in the prompt, bit 30: has a bias, below: how often it was generated), counts the history into it once, and adds the one token by
+// (bit 31: has a bias, bit 30: in the prompt, below: how often it was generated), counts the history into it once, and adds the one token by
 // which each further row has seen more.  Integer counts: the same in every order.  Then it goes over the slice: in place, only tokens whose word is set are
 // read, and what the mask takes away is written without being read; out of place every logit is read and written once.
 //
@@ -15,7 +15,7 @@ namespace actkv {
 namespace pn {
 
 constexpr int NT = 512;
-constexpr uint32_t PROMPT = 1u << 31, BIAS = 1u << 30, COUNT = BIAS - 1;
+constexpr uint32_t BIAS = 1u << 31, PROMPT = 1u << 30, COUNT = PROMPT - 1;
 constexpr int MAX_SLICE = 24576;           // tokens of a CTA: 96 KB, two CTAs on an SM
 
 struct Args {
@@ -26,112 +26,172 @@ struct Args {
   actkv_logit_rules_t q;
   int32_t* status;
   int32_t vocab, n_req, sum_win, max_win, max_hist;
-  int32_t slice, n_slices, groups, rows_per, in_place;
+  int32_t slice, n_slices, groups, rows_per, in_place, alike;              // alike: all rows begin at the same place of a vector
 };
 
 struct Rules {                             // of one request
-  float theta, freq, pres;
-  const int32_t* bias_token;
-  const float* bias_value;
-  int n_bias;
+  float theta, inverse, freq, pres;        // (z / theta as a product: a rounding more)
 };
 
-__device__ __forceinline__ float apply(float z, uint32_t word, int token, const Rules& q) {
-  if (word & BIAS) {
-    int lo = 0, hi = q.n_bias - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (q.bias_token[mid] < token) lo = mid + 1;
-      else hi = mid;
-    }
-    z += q.bias_value[lo];
-  }
-  if (word & ~BIAS) z = z > 0.f ? __fdiv_rn(z, q.theta) : z * q.theta;
-  if (word & COUNT) z -= q.freq * (float)(word & COUNT) + q.pres;
-  return z;
+// Penalties by a token's word, 0 where none; no branches.
+__device__ __forceinline__ float penalty(float z, uint32_t word, const Rules& q) {
+  const float turned = z * (z > 0.f ? q.inverse : q.theta);
+  z = word & ~BIAS ? turned : z;
+  const uint32_t n = word & COUNT;
+  const float less = z - fmaf(q.freq, __uint_as_float(0x4b000000u | n) - 8388608.f, q.pres);         // (n below 2^23 as a float32)
+  return n != 0 ? less : z;
 }
 
-template <typename T> struct Io;
-template <> struct Io<float> {
-  using V4 = float4;
-  static __device__ __forceinline__ float load(const float* p) { return *p; }
-  static __device__ __forceinline__ void store(float* p, float x) { *p = x; }
-  static __device__ __forceinline__ void open(const V4& v, float (&x)[4]) { x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w; }
-  static __device__ __forceinline__ V4 close(const float (&x)[4]) { return make_float4(x[0], x[1], x[2], x[3]); }
-};
-template <> struct Io<__nv_bfloat16> {
-  using V4 = uint2;
-  static __device__ __forceinline__ float load(const __nv_bfloat16* p) { return __bfloat162float(*p); }
-  static __device__ __forceinline__ void store(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
-  static __device__ __forceinline__ void open(const V4& v, float (&x)[4]) {
-    x[0] = __uint_as_float(v.x << 16); x[1] = __uint_as_float(v.x & 0xffff0000u);
-    x[2] = __uint_as_float(v.y << 16); x[3] = __uint_as_float(v.y & 0xffff0000u);
+__device__ __forceinline__ float load1(const float* p) { return *p; }
+__device__ __forceinline__ float load1(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+__device__ __forceinline__ void store1(float* p, float x) { *p = x; }
+__device__ __forceinline__ void store1(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
+
+// 16 bytes of logits.  rules: tokens with a bias are left as they are.
+template <typename T> struct Vec;
+template <> struct Vec<float> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ uint4 none() { return make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u); }
+  static __device__ __forceinline__ void rules(uint4& v, const uint32_t (&w)[4], const Rules& q) {
+    v.x = (int32_t)w[0] > 0 ? __float_as_uint(penalty(__uint_as_float(v.x), w[0], q)) : v.x;
+    v.y = (int32_t)w[1] > 0 ? __float_as_uint(penalty(__uint_as_float(v.y), w[1], q)) : v.y;
+    v.z = (int32_t)w[2] > 0 ? __float_as_uint(penalty(__uint_as_float(v.z), w[2], q)) : v.z;
+    v.w = (int32_t)w[3] > 0 ? __float_as_uint(penalty(__uint_as_float(v.w), w[3], q)) : v.w;
   }
-  static __device__ __forceinline__ V4 close(const float (&x)[4]) {
-    const __nv_bfloat162 a = __floats2bfloat162_rn(x[0], x[1]), b = __floats2bfloat162_rn(x[2], x[3]);
-    return make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+  static __device__ __forceinline__ void mask(uint4& v, uint32_t bits) {
+    v.x = bits & 1u ? v.x : 0xff800000u;
+    v.y = bits & 2u ? v.y : 0xff800000u;
+    v.z = bits & 4u ? v.z : 0xff800000u;
+    v.w = bits & 8u ? v.w : 0xff800000u;
+  }
+};
+template <> struct Vec<__nv_bfloat16> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ uint4 none() { return make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }
+  static __device__ __forceinline__ uint32_t two_rules(uint32_t v, uint32_t w0, uint32_t w1, const Rules& q) {
+    const __nv_bfloat162 r = __floats2bfloat162_rn(penalty(__uint_as_float(v << 16), w0, q), penalty(__uint_as_float(v & 0xffff0000u), w1, q));
+    const uint32_t n = *reinterpret_cast<const uint32_t*>(&r);
+    return ((int32_t)w0 > 0 ? n & 0xffffu : v & 0xffffu) | ((int32_t)w1 > 0 ? n & 0xffff0000u : v & 0xffff0000u);
+  }
+  static __device__ __forceinline__ void rules(uint4& v, const uint32_t (&w)[8], const Rules& q) {
+    v.x = two_rules(v.x, w[0], w[1], q);
+    v.y = two_rules(v.y, w[2], w[3], q);
+    v.z = two_rules(v.z, w[4], w[5], q);
+    v.w = two_rules(v.w, w[6], w[7], q);
+  }
+  static __device__ __forceinline__ uint32_t two(uint32_t v, uint32_t bits) {
+    v = bits & 1u ? v : (v & 0xffff0000u) | 0xff80u;
+    return bits & 2u ? v : (v & 0xffffu) | 0xff800000u;
+  }
+  static __device__ __forceinline__ void mask(uint4& v, uint32_t bits) {
+    v.x = two(v.x, bits);
+    v.y = two(v.y, bits >> 2);
+    v.z = two(v.z, bits >> 4);
+    v.w = two(v.w, bits >> 6);
   }
 };
 
-// One token.  word: 0 where no rule but the mask looks at it.
-template <typename T>
-__device__ __forceinline__ void one(const T* in, T* out, int v, uint32_t word, bool allowed, bool in_place, const Rules& q) {
-  if (!allowed) Io<T>::store(out + v, -INFINITY);
-  else if (word) Io<T>::store(out + v, apply(Io<T>::load(in + v), word, v, q));
-  else if (!in_place) out[v] = in[v];
-}
+constexpr int BATCH = 4, READ = 8;         // vectors that a thread has in flight, of logits and of the history
 
-// The row's logits of tokens [v0, v1).
+// How a row's logits of tokens [v0, v1) are walked over: vectors a0 .. a1 of N, and single tokens at the ends (all of them when in and out begin at
+// different places of a vector).
 template <typename T>
-__device__ __forceinline__ void sweep(const T* in, T* out, const uint32_t* word, bool words, const uint32_t* allow, int v0, int v1, bool in_place,
-                                      const Rules& q) {
-  using V4 = typename Io<T>::V4;
-  const int tid = threadIdx.x;
-  const bool whole = (((uintptr_t)(in + v0) | (uintptr_t)(out + v0)) & (sizeof(V4) - 1)) == 0;
-  int v = v0;
-  if (whole) {
-    const int end = v0 + ((v1 - v0) & ~3);
-#pragma unroll 4
-    for (v = v0 + tid * 4; v < end; v += NT * 4) {
-      uint4 w = make_uint4(0, 0, 0, 0);
-      if (words) w = *reinterpret_cast<const uint4*>(word + (v - v0));
-      const uint32_t nib = allow != nullptr ? allow[v >> 5] >> (v & 31) & 15u : 15u;
-      const uint32_t any = w.x | w.y | w.z | w.w;
-      if (in_place && nib == 15u && any == 0u) continue;
-      if (nib == 0u) {
-        const float none[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        *reinterpret_cast<V4*>(out + v) = Io<T>::close(none);
-      } else if (!in_place) {
-        const V4 raw = *reinterpret_cast<const V4*>(in + v);
-        if (nib == 15u && any == 0u) {
-          *reinterpret_cast<V4*>(out + v) = raw;
-          continue;
-        }
-        float x[4];
-        Io<T>::open(raw, x);
-        const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+struct Walk {
+  static constexpr int N = Vec<T>::N;
+  int head, vecs;
+  __device__ __forceinline__ Walk(const T* in, const T* out, int n) {      // (of the slice's first token)
+    const bool whole = (((uintptr_t)in ^ (uintptr_t)out) & 15) == 0;
+    head = whole ? min(n, (N - (int)(((uintptr_t)in & 15) / sizeof(T))) % N) : 0;
+    vecs = whole ? (n - head) / N : 0;
+  }
+  __device__ __forceinline__ int thread_of(int at) const {                 // which thread has the slice's token `at`
+    const int in = at - head, end = vecs * N;
+    return in < 0 ? at : in < end ? in / N % NT : (in - end) % NT;
+  }
+};
+
+// Batches of vectors, whose loads stand before any store (the compiler cannot know that out is not read again); the masks of the next batch are on their way
+// while one is worked on.  Logits of tokens with a bias are carried over, if they are allowed.
+template <typename T>
+__device__ __forceinline__ void sweep(const T* in, T* out, const Walk<T>& walk, const uint32_t* word, bool words, const uint32_t* allow, int last_word,
+                                      int v0, int v1, bool in_place, const Rules& q) {
+  constexpr int N = Vec<T>::N;
+  constexpr uint32_t ALL = (1u << N) - 1;
+  const int tid = threadIdx.x, head = walk.head, vecs = walk.vecs, a0 = v0 + head, a1 = a0 + vecs * N;
+  auto one = [&](int v) {
+    const uint32_t w = words ? word[v - v0] : 0u;
+    if (allow != nullptr && !(allow[v >> 5] >> (v & 31) & 1u)) store1(out + v, -INFINITY);
+    else if ((int32_t)w > 0) store1(out + v, penalty(load1(in + v), w, q));
+    else if (!in_place) out[v] = in[v];
+  };
+  if (tid < head) one(v0 + tid);
+  // the words of a vector, and what they have set
+  auto words_of = [&](int v, uint32_t (&w)[N]) {
+    uint32_t any = 0;
+    if (head % 4 == 0) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (ww[e]) x[e] = apply(x[e], ww[e], v + e, q);
-          if (!(nib >> e & 1u)) x[e] = -INFINITY;
-        }
-        *reinterpret_cast<V4*>(out + v) = Io<T>::close(x);
-      } else {
-        const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) one(in, out, v + e, ww[e], nib >> e & 1u, true, q);
+      for (int e = 0; e < N; e += 4) {
+        const uint4 x = *reinterpret_cast<const uint4*>(word + (v - v0) + e);
+        w[e] = x.x, w[e + 1] = x.y, w[e + 2] = x.z, w[e + 3] = x.w;
       }
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e) w[e] = word[v - v0 + e];
     }
-    v = end;
+#pragma unroll
+    for (int e = 0; e < N; ++e) any |= w[e];
+    return any;
+  };
+  auto masks = [&](int base, uint32_t (&bits)[BATCH]) {
+#pragma unroll
+    for (int u = 0; u < BATCH; ++u) {
+      const int i = base + u * NT, v = a0 + i * N;
+      bits[u] = ALL;
+      if (allow != nullptr && i < vecs) bits[u] &= __funnelshift_r(allow[v >> 5], allow[min((v >> 5) + 1, last_word)], v & 31);
+    }
+  };
+  uint32_t bits[BATCH], ahead[BATCH];
+  masks(tid, bits);
+  for (int base = tid; base < vecs; base += BATCH * NT) {
+    uint4 raw[BATCH];
+    uint32_t hit[BATCH];
+#pragma unroll
+    for (int u = 0; u < BATCH; ++u) {
+      const int i = base + u * NT, v = a0 + i * N;
+      hit[u] = 0;
+      if (i >= vecs) continue;
+      uint32_t w[N];
+      if (words) hit[u] = words_of(v, w);
+      if (bits[u] != 0 && (hit[u] != 0 || !in_place)) raw[u] = *reinterpret_cast<const uint4*>(in + v);
+    }
+    if (base + BATCH * NT < vecs) masks(base + BATCH * NT, ahead);
+#pragma unroll
+    for (int u = 0; u < BATCH; ++u) {
+      const int i = base + u * NT, v = a0 + i * N;
+      if (i >= vecs) continue;
+      if (bits[u] == 0) {
+        *reinterpret_cast<uint4*>(out + v) = Vec<T>::none();
+      } else if (hit[u] != 0 || !in_place) {
+        if (hit[u] != 0) {
+          uint32_t w[N];
+          (void)words_of(v, w);
+          Vec<T>::rules(raw[u], w, q);
+        }
+        if (bits[u] != ALL) Vec<T>::mask(raw[u], bits[u]);
+        *reinterpret_cast<uint4*>(out + v) = raw[u];
+      } else if (bits[u] != ALL) {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          if (!(bits[u] >> e & 1u)) store1(out + v + e, -INFINITY);
+      }
+      bits[u] = ahead[u];
+    }
   }
-  for (v += tid; v < v1; v += NT) {
-    const bool allowed = allow == nullptr || (allow[v >> 5] >> (v & 31) & 1u);
-    one(in, out, v, words ? word[v - v0] : 0u, allowed, in_place, q);
-  }
+  for (int v = a1 + tid; v < v1; v += NT) one(v);
 }
 
 template <typename T>
-__global__ void __launch_bounds__(NT) penalize_kernel(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(NT, 2) penalize_kernel(const __grid_constant__ Args a) {
   pdl_begin();
   extern __shared__ __align__(16) uint32_t s_word[];
   const int tid = threadIdx.x;
@@ -146,6 +206,7 @@ __global__ void __launch_bounds__(NT) penalize_kernel(const __grid_constant__ Ar
   if (i0 >= i1) return;
   Rules q;
   q.theta = a.q.repetition != nullptr ? a.q.repetition[r] : 1.f;
+  q.inverse = __frcp_rn(q.theta);
   q.freq = a.q.frequency != nullptr ? a.q.frequency[r] : 0.f;
   q.pres = a.q.presence != nullptr ? a.q.presence[r] : 0.f;
   const int hist = a.q.tokens != nullptr ? a.q.hist_len[r] : 0;
@@ -155,11 +216,9 @@ __global__ void __launch_bounds__(NT) penalize_kernel(const __grid_constant__ Ar
     if (first) report(a.status, ACTKV_E_INVALID, r, hist);
     return;
   }
-  q.bias_token = a.q.bias_token + b0;
-  q.bias_value = a.q.bias_value + b0;
-  q.n_bias = b1 - b0;
+  const int n_bias = b1 - b0;
   const int v0 = sl * a.slice, v1 = min(a.vocab, v0 + a.slice);
-  const bool counts = hist > 0 && (q.theta != 1.f || q.freq != 0.f || q.pres != 0.f), words = counts || q.n_bias > 0;
+  const bool counts = hist > 0 && (q.theta != 1.f || q.freq != 0.f || q.pres != 0.f), words = counts || n_bias > 0;
   const int32_t* tokens = a.q.tokens + (int64_t)r * a.q.token_stride;
   const int prompt = counts && a.q.prompt_len != nullptr ? a.q.prompt_len[r] : 0;
   auto count = [&](int at, int32_t token) {
@@ -174,22 +233,27 @@ __global__ void __launch_bounds__(NT) penalize_kernel(const __grid_constant__ Ar
     for (int i = tid * 4; i < v1 - v0; i += NT * 4) *reinterpret_cast<uint4*>(s_word + i) = make_uint4(0, 0, 0, 0);
     __syncthreads();
     bool bad = false;
-    for (int i = tid; i < q.n_bias; i += NT) {
-      const int32_t t = q.bias_token[i];
-      bad |= (uint32_t)t >= (uint32_t)a.vocab || (i > 0 && q.bias_token[i - 1] >= t);
+    for (int i = tid; i < n_bias; i += NT) {
+      const int32_t t = a.q.bias_token[b0 + i];
+      bad |= (uint32_t)t >= (uint32_t)a.vocab || (i > 0 && a.q.bias_token[b0 + i - 1] >= t);
       if (t >= v0 && t < v1) atomicOr(&s_word[t - v0], BIAS);
     }
     if (counts) {
       const int head = min(seen, (int)((0u - (uint32_t)(uintptr_t)tokens & 15u) / 4)), vecs = (seen - head) / 4;
       if (tid < head) count(tid, tokens[tid]);
-#pragma unroll 4
-      for (int i = tid; i < vecs; i += NT) {
-        const int at = head + i * 4;
-        const int4 t = *reinterpret_cast<const int4*>(tokens + at);
-        count(at, t.x);
-        count(at + 1, t.y);
-        count(at + 2, t.z);
-        count(at + 3, t.w);
+      for (int base = tid; base < vecs; base += READ * NT) {
+        int4 t[READ];
+#pragma unroll
+        for (int u = 0; u < READ; ++u)
+          t[u] = base + u * NT < vecs ? *reinterpret_cast<const int4*>(tokens + head + (base + u * NT) * 4) : make_int4(-1, -1, -1, -1);
+#pragma unroll
+        for (int u = 0; u < READ; ++u) {
+          const int at = head + (base + u * NT) * 4;
+          count(at, t[u].x);
+          count(at + 1, t[u].y);
+          count(at + 2, t[u].z);
+          count(at + 3, t[u].w);
+        }
       }
       const int at = head + vecs * 4 + tid;
       if (at < seen) count(at, tokens[at]);
@@ -212,14 +276,30 @@ __global__ void __launch_bounds__(NT) penalize_kernel(const __grid_constant__ Ar
         allow = a.q.allow + (int64_t)m * a.q.allow_stride;
       }
     }
+    const T* in = (const T*)a.logits + row * a.in_stride;
+    T* out = (T*)a.out + row * a.out_stride;
+    const Walk<T> walk(in + v0, out + v0, v1 - v0);
     if (!skip && (words || allow != nullptr || !a.in_place))
-      sweep<T>((const T*)a.logits + row * a.in_stride, (T*)a.out + row * a.out_stride, s_word, words, allow, v0, v1, a.in_place != 0, q);
+      sweep<T>(in, out, walk, s_word, words, allow, (a.vocab - 1) >> 5, v0, v1, a.in_place != 0, q);
+    if (n_bias > 0 && !skip) {
+      __syncthreads();                                                     // (what the sweep carried over is there)
+      for (int k = tid; k < n_bias; k += NT) {
+        const int32_t t = a.q.bias_token[b0 + k];
+        if (t < v0 || t >= v1 || (allow != nullptr && !(allow[t >> 5] >> (t & 31) & 1u))) continue;
+        store1(out + t, penalty(load1(in + t) + a.q.bias_value[b0 + k], s_word[t - v0], q));
+      }
+    }
     if (counts && i + 1 < i1) {
+      // One token more for the next row, counted by the thread that alone looks at its word; with biases, or rows that lie differently, in between.
       const int next = max(0, hist - (W - 2 - i));
-      __syncthreads();
-      if (tid == 0 && next > seen) count(seen, tokens[seen]);
+      const bool apart = n_bias > 0 || !a.alike;
+      if (apart) __syncthreads();
+      if (next > seen) {
+        const int32_t token = tokens[seen];
+        if (token >= v0 && token < v1 && tid == walk.thread_of(token - v0)) count(seen, token);
+      }
       seen = next;
-      __syncthreads();
+      if (apart) __syncthreads();
     }
   }
 }
@@ -242,7 +322,7 @@ extern "C" int actkv_penalize(const void* logits, int32_t dtype, int32_t vocab, 
   const int item = dtype == ACTKV_BF16 ? 2 : 4;
   if (!logits || !out || !win_indptr || max_win == 0 || ((uintptr_t)logits | (uintptr_t)out) % item != 0) return ACTKV_E_INVALID;
   if (logits == out && sum_win > 1 && row_stride != out_stride) return ACTKV_E_INVALID;
-  if (max_hist >= (int32_t)BIAS) return ACTKV_E_TOOBIG;
+  if (max_hist >= (1 << 23)) return ACTKV_E_TOOBIG;                        // (counts as float32)
   Args a = {};
   a.logits = logits;
   a.out = out;
@@ -257,9 +337,10 @@ extern "C" int actkv_penalize(const void* logits, int32_t dtype, int32_t vocab, 
   a.max_win = std::min(max_win, sum_win);
   a.max_hist = max_hist;
   a.in_place = logits == out;
+  a.alike = row_stride * item % 16 == 0 && out_stride * item % 16 == 0;
   // slices: at least as many as shared memory asks for, more while the SMs have not two CTAs each; rows of a request apart for the same reason
   const int64_t want = 148 * 2, least = (vocab + MAX_SLICE - 1) / MAX_SLICE;
-  const int64_t slices = std::max(least, std::min<int64_t>((want + n_req - 1) / n_req, (vocab + 4095) / 4096));
+  const int64_t rows = (int64_t)n_req * a.max_win, slices = std::max(least, std::min<int64_t>((want + rows - 1) / rows, (vocab + 4095) / 4096));
   a.slice = (int32_t)(((vocab + slices - 1) / slices + 31) / 32 * 32);
   a.n_slices = (vocab + a.slice - 1) / a.slice;
   const int64_t groups = std::max<int64_t>(1, std::min<int64_t>(a.max_win, 2 * want / ((int64_t)n_req * a.n_slices)));

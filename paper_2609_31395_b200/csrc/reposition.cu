@@ -20,6 +20,7 @@ namespace actkv {
 namespace rp {
 
 constexpr int NT = 256;
+constexpr int MAX_PAIRS = 128;
 constexpr int UNROLL = 4;                  // heads of a token that a thread has in flight
 
 struct Positions {
@@ -37,7 +38,8 @@ struct Args {
   const int32_t* tok_indptr;
   int32_t* status;
   int32_t layer_begin, sum_tok, max_tok, pairs, n_axes, interleaved, sec_end[4];
-  int32_t lanes, steps, head_groups, heads_per, shared;
+  int32_t lanes, lane_step, second;        // lanes of a key, elements from one to the next, and from the first dims of its pairs to the second
+  int32_t steps, head_groups, heads_per, shared;
 };
 
 __device__ __forceinline__ bool bad_request(const Args& a, int r, int32_t& n) {
@@ -65,15 +67,46 @@ __device__ __forceinline__ uint64_t turns64(float f) {                      // f
   t -= floor(t);
   return __double2ull_rz(t * 18446744073709551616.0);
 }
-__device__ __forceinline__ void sincos_of(uint64_t phase, float& sn, float& cs) {
-  const float t = (float)(int32_t)(phase >> 32) * 1.4629180792671596e-9f;   // 2 pi 2^-32: in [-pi, pi)
+// The upper half of p F modulo 2^64: a position times the frequency, in steps of 2^-32 turns.
+__device__ __forceinline__ uint32_t phase_of(uint32_t p, uint64_t F) { return p * (uint32_t)(F >> 32) + __umulhi(p, (uint32_t)F); }
+__device__ __forceinline__ uint32_t phase_of(int32_t p, uint64_t F) { return phase_of((uint32_t)p, F) - (p < 0 ? (uint32_t)F : 0u); }
+__device__ __forceinline__ void sincos_of(uint32_t phase, float& sn, float& cs) {
+  const float t = (float)(int32_t)phase * 1.4629180792671596e-9f;           // 2 pi 2^-32: in [-pi, pi)
   sn = __sinf(t);
   cs = __cosf(t);
 }
+__device__ __forceinline__ float bf1(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
 __device__ __forceinline__ float2 bf2(uint32_t v) { return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)); }
+// (x, y) (u, v) + (a, b), lane by lane
+__device__ __forceinline__ float2 fma2(float2 x, float2 u, float2 a) {
+  uint64_t p, q, c, d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(x.x), "f"(x.y));
+  asm("mov.b64 %0, {%1, %2};" : "=l"(q) : "f"(u.x), "f"(u.y));
+  asm("mov.b64 %0, {%1, %2};" : "=l"(c) : "f"(a.x), "f"(a.y));
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(p), "l"(q), "l"(c));
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(d));
+  return r;
+}
+__device__ __forceinline__ float2 mul2(float2 x, float2 u) {
+  uint64_t p, q, d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(x.x), "f"(x.y));
+  asm("mov.b64 %0, {%1, %2};" : "=l"(q) : "f"(u.x), "f"(u.y));
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(p), "l"(q));
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(d));
+  return r;
+}
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// a == b ? x : y, as an instruction: of a chain of them the compiler makes an array in local memory
+__device__ __forceinline__ int32_t where_equal(int32_t a, int32_t b, int32_t x, int32_t y) {
+  int32_t v;
+  asm("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %1, %2;\n\tselp.s32 %0, %3, %4, p;\n\t}" : "=r"(v) : "r"(a), "r"(b), "r"(x), "r"(y));
+  return v;
 }
 
 // Where the token's keys lie, within a layer and head 0; -1: nowhere.
@@ -83,34 +116,53 @@ __device__ __forceinline__ int64_t place_of(const Args& a, int r, int j) {
   return (uint32_t)page < (uint32_t)a.pool.n_pages ? (int64_t)page * a.pool.stride_page + (int64_t)(j % P) * a.pool.stride_slot : -1;
 }
 
-// HALF: a lane has 8 pairs, dims 8 c .. 8 c + 7 and those half a turned part further on; else 4 pairs side by side, dims 8 c .. 8 c + 7.
-// TWO: the frequencies change.  AXES: more than one axis.
-template <bool HALF, bool TWO, bool AXES>
-__global__ void __launch_bounds__(NT) turn_kernel(const __grid_constant__ Args a) {
+template <int BYTES> struct Raw;
+template <> struct Raw<16> { using T = uint4; };
+template <> struct Raw<8> { using T = uint2; };
+template <> struct Raw<4> { using T = uint32_t; };
+template <> struct Raw<2> { using T = uint16_t; };
+template <int N> union Elems {             // N bf16
+  typename Raw<2 * N>::T raw;
+  uint16_t e[N];
+  uint32_t pair[(N + 1) / 2];
+};
+
+// A lane has E pairs: HALF: E dims and as many `second` elements further on; else 2 E dims side by side.  TWO: the frequencies
+// may change.  AXES: there may be more than one axis.  (E below a whole vector: only with both.)
+template <bool HALF, int E, bool TWO, bool AXES>
+__global__ void __launch_bounds__(NT, HALF && E == 8 ? 2 : 4) turn_kernel(const __grid_constant__ Args a) {
   pdl_begin();
-  constexpr int E = HALF ? 8 : 4, V = HALF ? 2 : 1, U = AXES ? 1 : UNROLL, NA = AXES ? 4 : 1;
+  __shared__ __align__(16) uint64_t s_turns[TWO ? 2 : 1][MAX_PAIRS];
+  constexpr int V = HALF ? 2 : 1, W = HALF ? E : 2 * E, NA = AXES ? 4 : 1;  // vectors, elements of one
+  constexpr int U = AXES ? UNROLL / 2 : UNROLL;
+  using Vec = typename Raw<2 * W>::T;
   const int tid = threadIdx.x, per = NT / a.lanes, slot = tid / a.lanes, c = tid - slot * a.lanes;
   const int r = blockIdx.y, layer = blockIdx.z / a.head_groups, hg = blockIdx.z - layer * a.head_groups;
+  const bool same = !TWO || a.to_freq == nullptr;
   int32_t n;
   const bool stop = status_set(a.status);
-  if (bad_request(a, r, n) || stop) return;
   const int tok0 = blockIdx.x * per * a.steps;
-  if (tok0 >= n || slot >= per) return;
+  if (bad_request(a, r, n) || stop || tok0 >= n) return;                   // (all threads)
+  for (int p = tid; p < a.pairs; p += NT) {
+    s_turns[0][p] = turns64(a.freq[p]);
+    if (TWO) s_turns[TWO ? 1 : 0][p] = turns64(same ? a.freq[p] : a.to_freq[p]);
+  }
+  __syncthreads();
+  if (slot >= per) return;
   const int t0 = a.tok_indptr[r], H = a.pool.n_kv_heads, h0 = hg * a.heads_per, h1 = min(H, h0 + a.heads_per);
   uint64_t F[E], G[TWO ? E : 1];
   int axis[AXES ? E : 1];
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    const int p = c * E + e;
-    F[e] = turns64(a.freq[p]);
-    if (TWO) G[e] = turns64(a.to_freq[p]);
+    F[e] = s_turns[0][c * E + e];
+    if (TWO) G[e] = s_turns[TWO ? 1 : 0][c * E + e];
     if (AXES) {
-      axis[e] = 0;
-      while (p >= a.sec_end[axis[e]]) ++axis[e];
+      int x = 0;
+      while (c * E + e >= a.sec_end[x]) ++x;
+      axis[e] = x;
     }
   }
-  __nv_bfloat16* base = const_cast<__nv_bfloat16*>(a.pool.base) + (int64_t)(a.layer_begin + layer) * a.pool.stride_layer + c * 8;
-  const int dv = a.pairs;
+  __nv_bfloat16* base = const_cast<__nv_bfloat16*>(a.pool.base) + (int64_t)(a.layer_begin + layer) * a.pool.stride_layer + c * a.lane_step;
 #pragma unroll 1
   for (int st = 0; st < a.steps; ++st) {
     const int j = tok0 + st * per + slot;
@@ -125,26 +177,24 @@ __global__ void __launch_bounds__(NT) turn_kernel(const __grid_constant__ Args a
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int64_t unit = (int64_t)layer * H + min(hb + u, h1 - 1);
-        move[u] = false;
+        move[u] = !same;
 #pragma unroll
         for (int x = 0; x < NA; ++x) {
-          if (AXES && x >= a.n_axes) {
-            pf[u][x] = pt[u][x] = 0;
-            continue;
-          }
+          pf[u][x] = pt[u][x] = 0;
+          if (AXES && x >= a.n_axes) continue;
           pf[u][x] = a.from.at(x, unit, off, j);
           pt[u][x] = a.to.at(x, unit, off, j);
-          move[u] |= TWO || pf[u][x] != pt[u][x];
+          move[u] |= pf[u][x] != pt[u][x];
         }
         move[u] = move[u] && hb + u < h1;
       }
-      uint4 v[U][V];
+      Elems<W> v[U][V];
 #pragma unroll
       for (int u = 0; u < U; ++u)
         if (move[u]) {
-          const uint4* src = reinterpret_cast<const uint4*>(base + place + (int64_t)(hb + u) * a.pool.stride_head);
-          v[u][0] = src[0];
-          if (HALF) v[u][V - 1] = *reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(src) + dv);
+          const __nv_bfloat16* src = base + place + (int64_t)(hb + u) * a.pool.stride_head;
+#pragma unroll
+          for (int x = 0; x < V; ++x) v[u][x].raw = *reinterpret_cast<const Vec*>(src + x * a.second);
         }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -156,66 +206,38 @@ __global__ void __launch_bounds__(NT) turn_kernel(const __grid_constant__ Args a
             if (AXES) {
 #pragma unroll
               for (int x = 1; x < NA; ++x)
-                if (axis[e] == x) f = pf[u][x], t = pt[u][x];
+                f = where_equal(axis[e], x, pf[u][x], f), t = where_equal(axis[e], x, pt[u][x], t);
             }
-            const uint64_t ph = TWO ? (uint64_t)(int64_t)t * G[TWO ? e : 0] - (uint64_t)(int64_t)f * F[e] : (uint64_t)((int64_t)t - f) * F[e];
+            // (one table: the positions' distance, which fits 32 bits beside its sign)
+            const uint32_t up = phase_of((uint32_t)t - (uint32_t)f, F[e]), ph = TWO ? phase_of(t, G[TWO ? e : 0]) - phase_of(f, F[e]) : t >= f ? up : up - (uint32_t)F[e];
             sincos_of(ph, sn[e], cs[e]);
           }
         }
-        uint4* dst = reinterpret_cast<uint4*>(base + place + (int64_t)(hb + u) * a.pool.stride_head);
-        if (HALF) {
-          uint32_t *ua = reinterpret_cast<uint32_t*>(&v[u][0]), *ub = reinterpret_cast<uint32_t*>(&v[u][V - 1]);
+        __nv_bfloat16* dst = base + place + (int64_t)(hb + u) * a.pool.stride_head;
+        if (HALF && E == 1) {
+          const float x = bf1(v[u][0].e[0]), y = bf1(v[u][V - 1].e[0]);
+          v[u][0].pair[0] = pack2(x * cs[0] - y * sn[0], 0.f);
+          v[u][V - 1].pair[0] = pack2(y * cs[0] + x * sn[0], 0.f);
+        } else if (HALF) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float2 x = bf2(ua[e]), y = bf2(ub[e]);
-            ua[e] = pack2(x.x * cs[2 * e] - y.x * sn[2 * e], x.y * cs[(2 * e + 1) % E] - y.y * sn[(2 * e + 1) % E]);
-            ub[e] = pack2(y.x * cs[2 * e] + x.x * sn[2 * e], y.y * cs[(2 * e + 1) % E] + x.y * sn[(2 * e + 1) % E]);
+          for (int e = 0; e + 1 < E; e += 2) {
+            const float2 x = bf2(v[u][0].pair[e / 2]), y = bf2(v[u][V - 1].pair[e / 2]);
+            const float2 co = make_float2(cs[e], cs[e + 1]), si = make_float2(sn[e], sn[e + 1]), no = make_float2(-sn[e], -sn[e + 1]);
+            const float2 p = fma2(x, co, mul2(y, no)), q = fma2(y, co, mul2(x, si));
+            v[u][0].pair[e / 2] = pack2(p.x, p.y);
+            v[u][V - 1].pair[e / 2] = pack2(q.x, q.y);
           }
-          dst[0] = v[u][0];
-          *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(dst) + dv) = v[u][V - 1];
         } else {
-          uint32_t* ua = reinterpret_cast<uint32_t*>(&v[u][0]);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float2 x = bf2(ua[e]);
-            ua[e] = pack2(x.x * cs[e] - x.y * sn[e], x.y * cs[e] + x.x * sn[e]);
+          for (int e = 0; e < E; ++e) {
+            const float2 x = bf2(v[u][0].pair[e]);
+            v[u][0].pair[e] = pack2(x.x * cs[e] - x.y * sn[e], x.y * cs[e] + x.x * sn[e]);
           }
-          dst[0] = v[u][0];
         }
+#pragma unroll
+        for (int x = 0; x < V; ++x) *reinterpret_cast<Vec*>(dst + x * a.second) = v[u][x].raw;
       }
     }
-  }
-}
-
-// The same, a pair at a time, for strides and halves that are not whole 16-byte vectors.
-__global__ void __launch_bounds__(NT) turn_pairs_kernel(const __grid_constant__ Args a) {
-  pdl_begin();
-  const int r = blockIdx.y, layer = blockIdx.z;
-  int32_t n;
-  const bool stop = status_set(a.status);
-  if (bad_request(a, r, n) || stop) return;
-  const int t0 = a.tok_indptr[r], H = a.pool.n_kv_heads, j0 = blockIdx.x * a.steps, j1 = min(n, j0 + a.steps);
-  __nv_bfloat16* base = const_cast<__nv_bfloat16*>(a.pool.base) + (int64_t)(a.layer_begin + layer) * a.pool.stride_layer;
-  const int items = (j1 - j0) * H * a.pairs;
-  for (int i = threadIdx.x; i < items; i += NT) {
-    const int p = i % a.pairs, row = i / a.pairs, h = row % H, j = j0 + row / H;
-    const int64_t place = place_of(a, r, j);
-    if (place < 0) continue;
-    bool move = a.to_freq != nullptr;
-    const int64_t unit = (int64_t)layer * H + h, off = (int64_t)t0 + j;
-    for (int x = 0; x < a.n_axes; ++x) move |= a.from.at(x, unit, off, j) != a.to.at(x, unit, off, j);
-    if (!move) continue;
-    int axis = 0;
-    while (p >= a.sec_end[axis]) ++axis;
-    const uint64_t F = turns64(a.freq[p]), G = a.to_freq != nullptr ? turns64(a.to_freq[p]) : F;
-    const uint64_t ph = (uint64_t)(int64_t)a.to.at(axis, unit, off, j) * G - (uint64_t)(int64_t)a.from.at(axis, unit, off, j) * F;
-    float sn, cs;
-    sincos_of(ph, sn, cs);
-    __nv_bfloat16* k = base + place + (int64_t)h * a.pool.stride_head;
-    const int da = a.interleaved ? 2 * p : p, db = a.interleaved ? 2 * p + 1 : p + a.pairs;
-    const float x = __bfloat162float(k[da]), y = __bfloat162float(k[db]);
-    k[da] = __float2bfloat16_rn(x * cs - y * sn);
-    k[db] = __float2bfloat16_rn(y * cs + x * sn);
   }
 }
 
@@ -266,15 +288,14 @@ extern "C" int actkv_reposition(const actkv_pool_t* pool, const actkv_tables_t* 
   const int64_t pages = ((int64_t)max_tok + pool->page_size - 1) / pool->page_size;
   launch_pdl(check_kernel, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(16, (pages + NT - 1) / NT)), (unsigned)R), NT, 0, s, a);
   ACTKV_CHECK_LAUNCH();
-  const bool vec = a.pairs % (a.interleaved ? 4 : 8) == 0 && ((uintptr_t)pool->base & 15) == 0 && pool->stride_layer % 8 == 0 &&
-                   pool->stride_page % 8 == 0 && pool->stride_slot % 8 == 0 && pool->stride_head % 8 == 0;
-  if (!vec) {
-    a.steps = std::max(1, 4096 / (H * a.pairs));
-    launch_pdl(turn_pairs_kernel, dim3((unsigned)((max_tok + a.steps - 1) / a.steps), (unsigned)R, (unsigned)nls), NT, 0, s, a);
-    ACTKV_CHECK_LAUNCH();
-    return ACTKV_OK;
-  }
-  a.lanes = a.interleaved ? a.pairs / 4 : a.pairs / 8;
+  // pairs of a lane: as many as make a vector of up to 16 bytes on which all rows, heads and halves begin
+  int per_lane = a.interleaved ? 4 : 8;
+  const int64_t all = (int64_t)((uintptr_t)pool->base / 2) | pool->stride_layer | pool->stride_page | pool->stride_slot | pool->stride_head;
+  while (per_lane > 1 && (a.pairs % per_lane != 0 || all % (a.interleaved ? 2 * per_lane : per_lane) != 0)) per_lane /= 2;
+  const bool side_by_side = a.interleaved && all % 2 == 0;                  // (else element by element)
+  a.lanes = a.pairs / per_lane;
+  a.lane_step = a.interleaved ? 2 * per_lane : per_lane;
+  a.second = a.interleaved ? 1 : a.pairs;
   const int per = NT / a.lanes;
   // heads apart while there are few tokens, together (and several steps per CTA, for whose sake a thread forms its frequencies once) when
   // there are CTAs enough for every SM to have eight
@@ -286,12 +307,17 @@ extern "C" int actkv_reposition(const actkv_pool_t* pool, const actkv_tables_t* 
   const dim3 grid((unsigned)((max_tok + per * a.steps - 1) / (per * a.steps)), (unsigned)R, (unsigned)(nls * a.head_groups));
   const bool two = to_inv_freq != nullptr, axes = a.n_axes > 1;
   auto go = [&](auto kernel) { launch_pdl(kernel, grid, NT, 0, s, a); };
-  if (!a.interleaved) {
-    if (two) axes ? go(turn_kernel<true, true, true>) : go(turn_kernel<true, true, false>);
-    else axes ? go(turn_kernel<true, false, true>) : go(turn_kernel<true, false, false>);
+  if (!side_by_side) {
+    if (per_lane == 8) two ? (axes ? go(turn_kernel<true, 8, true, true>) : go(turn_kernel<true, 8, true, false>))
+                           : (axes ? go(turn_kernel<true, 8, false, true>) : go(turn_kernel<true, 8, false, false>));
+    else if (per_lane == 4) go(turn_kernel<true, 4, true, true>);
+    else if (per_lane == 2) go(turn_kernel<true, 2, true, true>);
+    else go(turn_kernel<true, 1, true, true>);
   } else {
-    if (two) axes ? go(turn_kernel<false, true, true>) : go(turn_kernel<false, true, false>);
-    else axes ? go(turn_kernel<false, false, true>) : go(turn_kernel<false, false, false>);
+    if (per_lane == 4) two ? (axes ? go(turn_kernel<false, 4, true, true>) : go(turn_kernel<false, 4, true, false>))
+                           : (axes ? go(turn_kernel<false, 4, false, true>) : go(turn_kernel<false, 4, false, false>));
+    else if (per_lane == 2) go(turn_kernel<false, 2, true, true>);
+    else go(turn_kernel<false, 1, true, true>);
   }
   ACTKV_CHECK_LAUNCH();
   return ACTKV_OK;
