@@ -161,7 +161,7 @@ __device__ __forceinline__ void sweep(const T* in, T* out, const Walk<T>& walk, 
       hit[u] = 0;
       if (i >= vecs) continue;
       uint32_t w[N];
-      if (words) hit[u] = words_of(v, w);
+      if (words && bits[u] != 0) hit[u] = words_of(v, w);
       if (bits[u] != 0 && (hit[u] != 0 || !in_place)) raw[u] = *reinterpret_cast<const uint4*>(in + v);
     }
     if (base + BATCH * NT < vecs) masks(base + BATCH * NT, ahead);
@@ -197,66 +197,72 @@ __global__ void __launch_bounds__(NT, 2) penalize_kernel(const __grid_constant__
   const int tid = threadIdx.x;
   const int sl = blockIdx.x % a.n_slices, unit = blockIdx.x / a.n_slices, grp = unit % a.groups, r = unit / a.groups;
   const bool first = sl == 0 && grp == 0 && tid == 0;
+  // (all loads that hang on nothing else before the first look at one)
+  const bool has_history = a.q.tokens != nullptr, has_bias = a.q.bias_indptr != nullptr;
   const int w0 = a.win_indptr[r], w1 = a.win_indptr[r + 1], W = w1 - w0;
+  Rules q;
+  q.theta = a.q.repetition != nullptr ? a.q.repetition[r] : 1.f;
+  q.freq = a.q.frequency != nullptr ? a.q.frequency[r] : 0.f;
+  q.pres = a.q.presence != nullptr ? a.q.presence[r] : 0.f;
+  const int hist = has_history ? a.q.hist_len[r] : 0;
+  const int prompt = has_history && a.q.prompt_len != nullptr ? a.q.prompt_len[r] : 0;
+  const int b0 = has_bias ? a.q.bias_indptr[r] : 0, b1 = has_bias ? a.q.bias_indptr[r + 1] : 0, n_bias = b1 - b0;
   if (w0 < 0 || w1 < w0 || w1 > a.sum_win || W > a.max_win) {
     if (first) report(a.status, ACTKV_E_INVALID, r, W);
     return;
   }
   const int i0 = grp * a.rows_per, i1 = min(W, i0 + a.rows_per);
   if (i0 >= i1) return;
-  Rules q;
-  q.theta = a.q.repetition != nullptr ? a.q.repetition[r] : 1.f;
-  q.inverse = __frcp_rn(q.theta);
-  q.freq = a.q.frequency != nullptr ? a.q.frequency[r] : 0.f;
-  q.pres = a.q.presence != nullptr ? a.q.presence[r] : 0.f;
-  const int hist = a.q.tokens != nullptr ? a.q.hist_len[r] : 0;
-  const int b0 = a.q.bias_indptr != nullptr ? a.q.bias_indptr[r] : 0, b1 = a.q.bias_indptr != nullptr ? a.q.bias_indptr[r + 1] : 0;
   if (!(q.theta > 0.f && q.theta < INFINITY) || !(fabsf(q.freq) < INFINITY) || !(fabsf(q.pres) < INFINITY) || hist < 0 || hist > a.max_hist ||
       hist > a.q.token_stride || b0 < 0 || b1 < b0 || b1 > a.q.n_bias) {
     if (first) report(a.status, ACTKV_E_INVALID, r, hist);
     return;
   }
-  const int n_bias = b1 - b0;
+  q.inverse = __frcp_rn(q.theta);
   const int v0 = sl * a.slice, v1 = min(a.vocab, v0 + a.slice);
   const bool counts = hist > 0 && (q.theta != 1.f || q.freq != 0.f || q.pres != 0.f), words = counts || n_bias > 0;
   const int32_t* tokens = a.q.tokens + (int64_t)r * a.q.token_stride;
-  const int prompt = counts && a.q.prompt_len != nullptr ? a.q.prompt_len[r] : 0;
-  auto count = [&](int at, int32_t token) {
-    const uint32_t v = (uint32_t)token - (uint32_t)v0;
-    if (v < (uint32_t)(v1 - v0)) {
-      if (at < prompt) atomicOr(&s_word[v], PROMPT);
-      else atomicAdd(&s_word[v], 1u);
+  // f of the slice's tokens among the history's [lo, hi), by their place in the slice
+  auto history = [&](int lo, int hi, auto&& f) {
+    auto see = [&](int32_t token) {
+      const uint32_t v = (uint32_t)token - (uint32_t)v0;
+      if (v < (uint32_t)(v1 - v0)) f(v);
+    };
+    const int head = min(hi - lo, (int)((0u - (uint32_t)(uintptr_t)(tokens + lo) & 15u) / 4)), vecs = (hi - lo - head) / 4;
+    if (tid < head) see(tokens[lo + tid]);
+    for (int base = tid; base < vecs; base += READ * NT) {
+      int4 t[READ];
+#pragma unroll
+      for (int u = 0; u < READ; ++u)
+        t[u] = base + u * NT < vecs ? *reinterpret_cast<const int4*>(tokens + lo + head + (base + u * NT) * 4) : make_int4(-1, -1, -1, -1);
+#pragma unroll
+      for (int u = 0; u < READ; ++u) {
+        see(t[u].x);
+        see(t[u].y);
+        see(t[u].z);
+        see(t[u].w);
+      }
     }
+    const int at = lo + head + vecs * 4 + tid;
+    if (at < hi) see(tokens[at]);
   };
   int seen = max(0, hist - (W - 1 - i0));                                  // tokens that the row stands behind
   if (words) {
     for (int i = tid * 4; i < v1 - v0; i += NT * 4) *reinterpret_cast<uint4*>(s_word + i) = make_uint4(0, 0, 0, 0);
     __syncthreads();
     bool bad = false;
+    if (counts) {
+      const int mid = min(max(prompt, 0), seen);
+      if (mid > 0) {
+        history(0, mid, [&](uint32_t v) { s_word[v] = PROMPT; });          // (the same from whichever thread)
+        __syncthreads();
+      }
+      history(mid, seen, [&](uint32_t v) { atomicAdd(&s_word[v], 1u); });
+    }
     for (int i = tid; i < n_bias; i += NT) {
       const int32_t t = a.q.bias_token[b0 + i];
       bad |= (uint32_t)t >= (uint32_t)a.vocab || (i > 0 && a.q.bias_token[b0 + i - 1] >= t);
       if (t >= v0 && t < v1) atomicOr(&s_word[t - v0], BIAS);
-    }
-    if (counts) {
-      const int head = min(seen, (int)((0u - (uint32_t)(uintptr_t)tokens & 15u) / 4)), vecs = (seen - head) / 4;
-      if (tid < head) count(tid, tokens[tid]);
-      for (int base = tid; base < vecs; base += READ * NT) {
-        int4 t[READ];
-#pragma unroll
-        for (int u = 0; u < READ; ++u)
-          t[u] = base + u * NT < vecs ? *reinterpret_cast<const int4*>(tokens + head + (base + u * NT) * 4) : make_int4(-1, -1, -1, -1);
-#pragma unroll
-        for (int u = 0; u < READ; ++u) {
-          const int at = head + (base + u * NT) * 4;
-          count(at, t[u].x);
-          count(at + 1, t[u].y);
-          count(at + 2, t[u].z);
-          count(at + 3, t[u].w);
-        }
-      }
-      const int at = head + vecs * 4 + tid;
-      if (at < seen) count(at, tokens[at]);
     }
     if (__syncthreads_or(bad)) {
       if (first) report(a.status, ACTKV_E_BADINDEX, r, b0);
@@ -296,7 +302,10 @@ __global__ void __launch_bounds__(NT, 2) penalize_kernel(const __grid_constant__
       if (apart) __syncthreads();
       if (next > seen) {
         const int32_t token = tokens[seen];
-        if (token >= v0 && token < v1 && tid == walk.thread_of(token - v0)) count(seen, token);
+        if (token >= v0 && token < v1 && tid == walk.thread_of(token - v0)) {
+          if (seen < prompt) s_word[token - v0] |= PROMPT;
+          else s_word[token - v0] += 1;
+        }
       }
       seen = next;
       if (apart) __syncthreads();
@@ -322,7 +331,7 @@ extern "C" int actkv_penalize(const void* logits, int32_t dtype, int32_t vocab, 
   const int item = dtype == ACTKV_BF16 ? 2 : 4;
   if (!logits || !out || !win_indptr || max_win == 0 || ((uintptr_t)logits | (uintptr_t)out) % item != 0) return ACTKV_E_INVALID;
   if (logits == out && sum_win > 1 && row_stride != out_stride) return ACTKV_E_INVALID;
-  if (max_hist >= (1 << 23)) return ACTKV_E_TOOBIG;                        // (counts as float32)
+  if (max_hist >= (1 << 23) || vocab > (1 << 30)) return ACTKV_E_TOOBIG;                        // (counts as float32)
   Args a = {};
   a.logits = logits;
   a.out = out;

@@ -70,8 +70,10 @@ __device__ __forceinline__ uint64_t turns64(float f) {                      // f
 // The upper half of p F modulo 2^64: a position times the frequency, in steps of 2^-32 turns.
 __device__ __forceinline__ uint32_t phase_of(uint32_t p, uint64_t F) { return p * (uint32_t)(F >> 32) + __umulhi(p, (uint32_t)F); }
 __device__ __forceinline__ uint32_t phase_of(int32_t p, uint64_t F) { return phase_of((uint32_t)p, F) - (p < 0 ? (uint32_t)F : 0u); }
+// (The upper 23 bits as a float32 in [1, 2), without a conversion: those share the special function units with sine and cosine, 24 operations of a lane's 8
+// pairs, and 16 so.)
 __device__ __forceinline__ void sincos_of(uint32_t phase, float& sn, float& cs) {
-  const float t = (float)(int32_t)phase * 1.4629180792671596e-9f;           // 2 pi 2^-32: in [-pi, pi)
+  const float t = (__uint_as_float((phase >> 9 ^ 0x400000u) | 0x3f800000u) - 1.5f) * 6.283185307179586f;       // in [-pi, pi), steps of 2^-23 turns
   sn = __sinf(t);
   cs = __cosf(t);
 }
@@ -163,11 +165,13 @@ __global__ void __launch_bounds__(NT, HALF && E == 8 ? 2 : 4) turn_kernel(const 
     }
   }
   __nv_bfloat16* base = const_cast<__nv_bfloat16*>(a.pool.base) + (int64_t)(a.layer_begin + layer) * a.pool.stride_layer + c * a.lane_step;
+  int64_t next_place = tok0 + slot < n ? place_of(a, r, tok0 + slot) : -1;
 #pragma unroll 1
   for (int st = 0; st < a.steps; ++st) {
     const int j = tok0 + st * per + slot;
     if (j >= n) return;
-    const int64_t place = place_of(a, r, j), off = (int64_t)t0 + j;
+    const int64_t place = next_place, off = (int64_t)t0 + j;
+    next_place = j + per < n ? place_of(a, r, j + per) : -1;               // (its page is looked up while these keys are turned)
     if (place < 0) continue;
     float cs[E], sn[E];
 #pragma unroll 1
