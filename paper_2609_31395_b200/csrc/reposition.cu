@@ -79,26 +79,6 @@ __device__ __forceinline__ void sincos_of(uint32_t phase, float& sn, float& cs) 
 }
 __device__ __forceinline__ float bf1(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
 __device__ __forceinline__ float2 bf2(uint32_t v) { return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)); }
-// (x, y) (u, v) + (a, b), lane by lane
-__device__ __forceinline__ float2 fma2(float2 x, float2 u, float2 a) {
-  uint64_t p, q, c, d;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(x.x), "f"(x.y));
-  asm("mov.b64 %0, {%1, %2};" : "=l"(q) : "f"(u.x), "f"(u.y));
-  asm("mov.b64 %0, {%1, %2};" : "=l"(c) : "f"(a.x), "f"(a.y));
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(p), "l"(q), "l"(c));
-  float2 r;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(d));
-  return r;
-}
-__device__ __forceinline__ float2 mul2(float2 x, float2 u) {
-  uint64_t p, q, d;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(x.x), "f"(x.y));
-  asm("mov.b64 %0, {%1, %2};" : "=l"(q) : "f"(u.x), "f"(u.y));
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(p), "l"(q));
-  float2 r;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(d));
-  return r;
-}
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&v);
@@ -129,15 +109,37 @@ template <int N> union Elems {             // N bf16
   uint32_t pair[(N + 1) / 2];
 };
 
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void* dst, const void* src) {
+  static_assert(BYTES == 4 || BYTES == 8 || BYTES == 16, "");
+  const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst);
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d), "l"(src) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(d), "l"(src), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void copy_wait_one() { asm volatile("cp.async.wait_group 1;" ::: "memory"); }
+
 // A lane has E pairs: HALF: E dims and as many `second` elements further on; else 2 E dims side by side.  TWO: the frequencies
 // may change.  AXES: there may be more than one axis.  (E below a whole vector: only with both.)
+// A thread goes through items of U heads of one token: it turns the keys of one while those of the next are on their way into shared memory (places that
+// only this thread reads) and the positions and the page of the one behind that into registers.
 template <bool HALF, int E, bool TWO, bool AXES>
-__global__ void __launch_bounds__(NT, HALF && E == 8 ? 2 : 4) turn_kernel(const __grid_constant__ Args a) {
-  pdl_begin();
-  __shared__ __align__(16) uint64_t s_turns[TWO ? 2 : 1][MAX_PAIRS];
-  constexpr int V = HALF ? 2 : 1, W = HALF ? E : 2 * E, NA = AXES ? 4 : 1;  // vectors, elements of one
-  constexpr int U = AXES ? UNROLL / 2 : UNROLL;
+struct Shape {
+  static constexpr int V = HALF ? 2 : 1, W = HALF ? E : 2 * E, NA = AXES ? 4 : 1;           // vectors, elements of one, axes
+  static constexpr int U = AXES ? UNROLL / 2 : UNROLL;
+  static constexpr int CTAS = 2;
   using Vec = typename Raw<2 * W>::T;
+  static constexpr size_t SMEM = W > 1 ? (size_t)2 * U * V * NT * sizeof(Vec) : 16;
+};
+template <bool HALF, int E, bool TWO, bool AXES>
+__global__ void __launch_bounds__(NT, (Shape<HALF, E, TWO, AXES>::CTAS)) turn_kernel(const __grid_constant__ Args a) {
+  using S = Shape<HALF, E, TWO, AXES>;
+  constexpr int V = S::V, W = S::W, NA = S::NA, U = S::U;
+  using Vec = typename S::Vec;
+  pdl_begin();
+  extern __shared__ __align__(16) uint8_t rp_smem[];
+  __shared__ __align__(16) uint64_t s_turns[TWO ? 2 : 1][MAX_PAIRS];
+  Vec* buf = reinterpret_cast<Vec*>(rp_smem) + threadIdx.x;                // [stage][head][vector][thread]
   const int tid = threadIdx.x, per = NT / a.lanes, slot = tid / a.lanes, c = tid - slot * a.lanes;
   const int r = blockIdx.y, layer = blockIdx.z / a.head_groups, hg = blockIdx.z - layer * a.head_groups;
   const bool same = !TWO || a.to_freq == nullptr;
@@ -165,85 +167,126 @@ __global__ void __launch_bounds__(NT, HALF && E == 8 ? 2 : 4) turn_kernel(const 
     }
   }
   __nv_bfloat16* base = const_cast<__nv_bfloat16*>(a.pool.base) + (int64_t)(a.layer_begin + layer) * a.pool.stride_layer + c * a.lane_step;
-  int64_t next_place = tok0 + slot < n ? place_of(a, r, tok0 + slot) : -1;
-#pragma unroll 1
-  for (int st = 0; st < a.steps; ++st) {
-    const int j = tok0 + st * per + slot;
-    if (j >= n) return;
-    const int64_t place = next_place, off = (int64_t)t0 + j;
-    next_place = j + per < n ? place_of(a, r, j + per) : -1;               // (its page is looked up while these keys are turned)
-    if (place < 0) continue;
-    float cs[E], sn[E];
-#pragma unroll 1
-    for (int hb = h0; hb < h1; hb += U) {
-      int32_t pf[U][NA], pt[U][NA];
-      bool move[U];
+  const int end = min(n, tok0 + a.steps * per);
+
+  struct Item {
+    int64_t place;                         // of the token's keys, with the item's first head
+    int32_t f[U][NA], t[U][NA];
+    uint32_t move;                         // heads whose key moves
+    bool first;                            // ... of the token
+  };
+  int j = tok0 + slot, h = h0;                                             // the next item to fetch
+  // positions and page of the next item; no heads left: move stays 0
+  auto fetch = [&](Item& it) {
+    it.move = 0;
+    it.place = -1;
+    it.first = h == h0;
+    if (j >= end) return;
+    const int64_t off = (int64_t)t0 + j, place = place_of(a, r, j);
+    it.place = place < 0 ? -1 : place + (int64_t)h * a.pool.stride_head;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int64_t unit = (int64_t)layer * H + min(hb + u, h1 - 1);
-        move[u] = !same;
+    for (int u = 0; u < U; ++u) {
+      const int64_t unit = (int64_t)layer * H + min(h + u, h1 - 1);
 #pragma unroll
-        for (int x = 0; x < NA; ++x) {
-          pf[u][x] = pt[u][x] = 0;
-          if (AXES && x >= a.n_axes) continue;
-          pf[u][x] = a.from.at(x, unit, off, j);
-          pt[u][x] = a.to.at(x, unit, off, j);
-          move[u] |= pf[u][x] != pt[u][x];
-        }
-        move[u] = move[u] && hb + u < h1;
+      for (int x = 0; x < NA; ++x) {
+        it.f[u][x] = it.t[u][x] = 0;
+        if (AXES && x >= a.n_axes) continue;
+        it.f[u][x] = a.from.at(x, unit, off, j);
+        it.t[u][x] = a.to.at(x, unit, off, j);
       }
-      Elems<W> v[U][V];
+      if (h + u < h1) it.move |= 1u << u;
+    }
+    h += U;
+    if (h >= h1) {
+      h = h0;
+      j += per;
+    }
+  };
+  // which keys move, and these on their way
+  auto issue = [&](Item& it, int stage) {
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (move[u]) {
-          const __nv_bfloat16* src = base + place + (int64_t)(hb + u) * a.pool.stride_head;
+    for (int u = 0; u < U; ++u) {
+      bool move = !same;
 #pragma unroll
-          for (int x = 0; x < V; ++x) v[u][x].raw = *reinterpret_cast<const Vec*>(src + x * a.second);
+      for (int x = 0; x < NA; ++x) move |= it.f[u][x] != it.t[u][x];
+      if (it.place < 0 || !move) it.move &= ~(1u << u);
+      if constexpr (W > 1) {
+        if (it.move >> u & 1u) {
+          const __nv_bfloat16* src = base + it.place + (int64_t)u * a.pool.stride_head;
+#pragma unroll
+          for (int x = 0; x < V; ++x) copy_async<2 * W>(buf + ((stage * U + u) * V + x) * NT, src + x * a.second);
         }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (!move[u]) continue;
-        if (!a.shared || (hb == h0 && u == 0)) {
-#pragma unroll
-          for (int e = 0; e < E; ++e) {
-            int32_t f = pf[u][0], t = pt[u][0];
-            if (AXES) {
-#pragma unroll
-              for (int x = 1; x < NA; ++x)
-                f = where_equal(axis[e], x, pf[u][x], f), t = where_equal(axis[e], x, pt[u][x], t);
-            }
-            // (one table: the positions' distance, which fits 32 bits beside its sign)
-            const uint32_t up = phase_of((uint32_t)t - (uint32_t)f, F[e]), ph = TWO ? phase_of(t, G[TWO ? e : 0]) - phase_of(f, F[e]) : t >= f ? up : up - (uint32_t)F[e];
-            sincos_of(ph, sn[e], cs[e]);
-          }
-        }
-        __nv_bfloat16* dst = base + place + (int64_t)(hb + u) * a.pool.stride_head;
-        if (HALF && E == 1) {
-          const float x = bf1(v[u][0].e[0]), y = bf1(v[u][V - 1].e[0]);
-          v[u][0].pair[0] = pack2(x * cs[0] - y * sn[0], 0.f);
-          v[u][V - 1].pair[0] = pack2(y * cs[0] + x * sn[0], 0.f);
-        } else if (HALF) {
-#pragma unroll
-          for (int e = 0; e + 1 < E; e += 2) {
-            const float2 x = bf2(v[u][0].pair[e / 2]), y = bf2(v[u][V - 1].pair[e / 2]);
-            const float2 co = make_float2(cs[e], cs[e + 1]), si = make_float2(sn[e], sn[e + 1]), no = make_float2(-sn[e], -sn[e + 1]);
-            const float2 p = fma2(x, co, mul2(y, no)), q = fma2(y, co, mul2(x, si));
-            v[u][0].pair[e / 2] = pack2(p.x, p.y);
-            v[u][V - 1].pair[e / 2] = pack2(q.x, q.y);
-          }
-        } else {
-#pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const float2 x = bf2(v[u][0].pair[e]);
-            v[u][0].pair[e] = pack2(x.x * cs[e] - x.y * sn[e], x.y * cs[e] + x.x * sn[e]);
-          }
-        }
-#pragma unroll
-        for (int x = 0; x < V; ++x) *reinterpret_cast<Vec*>(dst + x * a.second) = v[u][x].raw;
       }
     }
+    copy_commit();
+  };
+  Item now, next, later;
+  fetch(now);
+  fetch(next);
+  issue(now, 0);
+  float cs[E], sn[E];
+  int stage = 0;
+#pragma unroll 1
+  while (now.place != -1 || next.place != -1 || j < end) {
+    issue(next, stage ^ 1);
+    fetch(later);
+    copy_wait_one();
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (!(now.move >> u & 1u)) continue;
+      __nv_bfloat16* key = base + now.place + (int64_t)u * a.pool.stride_head;
+      Elems<W> v[V];
+#pragma unroll
+      for (int x = 0; x < V; ++x) {
+        if constexpr (W > 1) v[x].raw = buf[((stage * U + u) * V + x) * NT];
+        else v[x].raw = *reinterpret_cast<const Vec*>(key + x * a.second);
+      }
+      if (!a.shared || (now.first && u == 0)) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          int32_t f = now.f[u][0], t = now.t[u][0];
+          if (AXES) {
+#pragma unroll
+            for (int x = 1; x < NA; ++x)
+              f = where_equal(axis[e], x, now.f[u][x], f), t = where_equal(axis[e], x, now.t[u][x], t);
+          }
+          // (one table: the positions' distance, which fits 32 bits beside its sign)
+          const uint32_t up = phase_of((uint32_t)t - (uint32_t)f, F[e]), ph = TWO ? phase_of(t, G[TWO ? e : 0]) - phase_of(f, F[e]) : t >= f ? up : up - (uint32_t)F[e];
+          sincos_of(ph, sn[e], cs[e]);
+        }
+      }
+      if (HALF && E == 1) {
+        const float x = bf1(v[0].e[0]), y = bf1(v[V - 1].e[0]);
+        v[0].pair[0] = pack2(x * cs[0] - y * sn[0], 0.f);
+        v[V - 1].pair[0] = pack2(y * cs[0] + x * sn[0], 0.f);
+      } else if (HALF) {
+#pragma unroll
+        for (int e = 0; e + 1 < E; e += 2) {
+          const float2 x = bf2(v[0].pair[e / 2]), y = bf2(v[V - 1].pair[e / 2]);
+          v[0].pair[e / 2] = pack2(x.x * cs[e] - y.x * sn[e], x.y * cs[e + 1] - y.y * sn[e + 1]);
+          v[V - 1].pair[e / 2] = pack2(y.x * cs[e] + x.x * sn[e], y.y * cs[e + 1] + x.y * sn[e + 1]);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const float2 x = bf2(v[0].pair[e]);
+          v[0].pair[e] = pack2(x.x * cs[e] - x.y * sn[e], x.y * cs[e] + x.x * sn[e]);
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < V; ++x) *reinterpret_cast<Vec*>(key + x * a.second) = v[x].raw;
+    }
+    now = next;
+    next = later;
+    stage ^= 1;
   }
 }
+
+template <bool HALF, int E, bool TWO, bool AXES>
+struct Kernel {
+  static constexpr auto kernel = turn_kernel<HALF, E, TWO, AXES>;
+  static constexpr size_t smem = Shape<HALF, E, TWO, AXES>::SMEM;
+};
 
 }  // namespace rp
 }  // namespace actkv
@@ -307,22 +350,22 @@ extern "C" int actkv_reposition(const actkv_pool_t* pool, const actkv_tables_t* 
   a.heads_per = blocks * ((H + UNROLL - 1) / UNROLL) < 148 * 4 ? 1 : UNROLL;
   if (a.shared && blocks >= 148 * 8) a.heads_per = H;
   a.head_groups = (H + a.heads_per - 1) / a.heads_per;
-  a.steps = (int32_t)std::max<int64_t>(1, std::min<int64_t>(4, blocks * a.head_groups / (148 * 8)));
+  a.steps = (int32_t)std::max<int64_t>(1, std::min<int64_t>(8, blocks * a.head_groups / (148 * 8)));
   const dim3 grid((unsigned)((max_tok + per * a.steps - 1) / (per * a.steps)), (unsigned)R, (unsigned)(nls * a.head_groups));
   const bool two = to_inv_freq != nullptr, axes = a.n_axes > 1;
-  auto go = [&](auto kernel) { launch_pdl(kernel, grid, NT, 0, s, a); };
+  auto go = [&](auto shape) {
+    using S = decltype(shape);
+    if (ensure_dyn_smem(S::kernel, S::smem) != cudaSuccess) return ACTKV_E_CUDA;
+    launch_pdl(S::kernel, grid, NT, S::smem, s, a);
+    ACTKV_CHECK_LAUNCH();
+    return ACTKV_OK;
+  };
   if (!side_by_side) {
-    if (per_lane == 8) two ? (axes ? go(turn_kernel<true, 8, true, true>) : go(turn_kernel<true, 8, true, false>))
-                           : (axes ? go(turn_kernel<true, 8, false, true>) : go(turn_kernel<true, 8, false, false>));
-    else if (per_lane == 4) go(turn_kernel<true, 4, true, true>);
-    else if (per_lane == 2) go(turn_kernel<true, 2, true, true>);
-    else go(turn_kernel<true, 1, true, true>);
-  } else {
-    if (per_lane == 4) two ? (axes ? go(turn_kernel<false, 4, true, true>) : go(turn_kernel<false, 4, true, false>))
-                           : (axes ? go(turn_kernel<false, 4, false, true>) : go(turn_kernel<false, 4, false, false>));
-    else if (per_lane == 2) go(turn_kernel<false, 2, true, true>);
-    else go(turn_kernel<false, 1, true, true>);
+    if (per_lane == 8) return two ? (axes ? go(Kernel<true, 8, true, true>{}) : go(Kernel<true, 8, true, false>{}))
+                                  : (axes ? go(Kernel<true, 8, false, true>{}) : go(Kernel<true, 8, false, false>{}));
+    return per_lane == 4 ? go(Kernel<true, 4, true, true>{}) : per_lane == 2 ? go(Kernel<true, 2, true, true>{}) : go(Kernel<true, 1, true, true>{});
   }
-  ACTKV_CHECK_LAUNCH();
-  return ACTKV_OK;
+  if (per_lane == 4) return two ? (axes ? go(Kernel<false, 4, true, true>{}) : go(Kernel<false, 4, true, false>{}))
+                                : (axes ? go(Kernel<false, 4, false, true>{}) : go(Kernel<false, 4, false, false>{}));
+  return per_lane == 2 ? go(Kernel<false, 2, true, true>{}) : go(Kernel<false, 1, true, true>{});
 }
