@@ -202,21 +202,29 @@ template <> struct Vec<__nv_bfloat16> {
 };
 __device__ __forceinline__ float to_f(float x) { return x; }
 __device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
+// The largest and the smallest of three, subnormal ones too; the largest is NaN if one is.
+__device__ __forceinline__ float larger(float x, float y, float z) {
+  float v;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(v) : "f"(x), "f"(y), "f"(z));
+  return v;
+}
+__device__ __forceinline__ float smaller(float x, float y, float z) {
+  float v;
+  asm("min.f32 %0, %1, %2, %3;" : "=f"(v) : "f"(x), "f"(y), "f"(z));
+  return v;
+}
+template <typename T>
+__device__ __forceinline__ void see(T x, float& most, float& least) {
+  most = larger(most, to_f(x), to_f(x));
+  least = smaller(least, to_f(x), to_f(x));
+}
 
 // Tokens that reach a key in order: by the logit as a number, and where that is equal by the key.
 struct Border {
   uint64_t key;
-  int32_t hi, lo;                          // over hi: yes, below lo: no
-  __device__ __forceinline__ explicit Border(uint64_t k) : key(k), hi(NEG_INF), lo(INT32_MAX) {
-    if (k != 0) {
-      hi = ordered(logit_of(k));
-      lo = hi == 0 ? -1 : hi;
-    }
-  }
-  __device__ __forceinline__ bool keeps(float x, uint32_t token) const {
-    const int32_t o = ordered(x);
-    return o > hi || (o >= lo && key_of(x, token) >= key);
-  }
+  float at;                                // (comparisons take a subnormal logit for 0: among these, too, the key tells)
+  __device__ __forceinline__ explicit Border(uint64_t k) : key(k), at(k != 0 ? logit_of(k) : -FLT_MAX) {}
+  __device__ __forceinline__ bool keeps(float x, uint32_t token) const { return x > at || (x >= at && key_of(x, token) >= key); }
 };
 // The step of a histogram in which a token falls, -1: none.  First equal steps of z, of the tokens that a border keeps; then equal steps of the
 // keys from hi down to lo.
@@ -318,7 +326,7 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
   pdl_begin();
   extern __shared__ __align__(16) uint8_t sa_smem[];
   Shared& sh = *reinterpret_cast<Shared*>(sa_smem);
-  float* buf = reinterpret_cast<float*>(sa_smem + (sizeof(Shared) + 15) / 16 * 16);
+  T* buf = reinterpret_cast<T*>(sa_smem + (sizeof(Shared) + 15) / 16 * 16);
   cg::cluster_group cl = cg::this_cluster();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, C = (int)cl.num_blocks(), rank = (int)cl.block_rank();
   const int64_t r = blockIdx.x / C;
@@ -345,28 +353,28 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
   const T* src = (const T*)a.logits + r * a.row_stride + first;
   constexpr int N = Vec<T>::N;
   const int off = (int)(((uintptr_t)src & 15) / sizeof(T));                 // as far off a vector's beginning as in memory
-  float* z = buf + off;
+  T* row = buf + off;
+  auto z = [&](int i) { return to_f(row[i]); };
   const int head = min(n_own, (N - off) % N), vecs = (n_own - head) / N;
-  int32_t high = INT32_MIN, low = INT32_MAX;
-  auto see = [&](float x) {
-    const int32_t o = ordered(x);
-    high = max(high, o);
-    low = min(low, o);
-  };
-  if (tid < head) see(z[tid] = to_f(src[tid]));
+  float most = -INFINITY, least = INFINITY;                                 // NaN: there is one
+  if (tid < head) see(row[tid] = src[tid], most, least);
 #pragma unroll 8
   for (int i = tid; i < vecs; i += NT) {
+    const uint4 v = *reinterpret_cast<const uint4*>(src + head + i * N);
+    *reinterpret_cast<uint4*>(row + head + i * N) = v;
     float x[N];
-    Vec<T>::open(*reinterpret_cast<const uint4*>(src + head + i * N), x);
+    Vec<T>::open(v, x);
 #pragma unroll
-    for (int e = 0; e < N; e += 4) *reinterpret_cast<float4*>(z + head + i * N + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
-#pragma unroll
-    for (int e = 0; e < N; ++e) see(x[e]);
+    for (int e = 0; e < N; e += 2) {
+      most = larger(most, x[e], x[e + 1]);
+      least = smaller(least, x[e], x[e + 1]);
+    }
   }
   {
     const int i = head + vecs * N + tid;
-    if (i < n_own) see(z[i] = to_f(src[i]));
+    if (i < n_own) see(row[i] = src[i], most, least);
   }
+  int32_t high = ordered(most), low = ordered(least);
   if (tid < 256) sh.tab[tid >> 4][tid & 15] = ROOTS[tid >> 4];
   if (tid == 0) sh.n_list = sh.n_all = 0;
   const bool greedy = __float_as_uint(t) << 1 == 0u || k == 1, by_k = k > 0 && k < a.vocab, by_p = p < 1.f;
@@ -416,7 +424,7 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
     uint32_t at = ~0u;
     const uint32_t want = okey(top);
     for (int i = tid; i < n_own; i += NT)
-      if (okey(z[i]) == want) at = min(at, (uint32_t)i);
+      if (okey(z(i)) == want) at = min(at, (uint32_t)i);
     at = __reduce_min_sync(0xffffffffu, at);
     if (lane == 0) sh.scan[0][warp] = at;
     __syncthreads();
@@ -561,11 +569,11 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
     const float bound = b <= NEG_INF ? -FLT_MAX : __int_as_float(b ^ ((b >> 31) & 0x7fffffff));
     auto take = [&](int i) {
       const uint32_t at = atomicAdd(&sh.n_list, 1u);
-      if (at < CAP) sh.list[at] = key_of(z[i], first + i);
+      if (at < CAP) sh.list[at] = key_of(z(i), first + i);
     };
     int i = tid;
     for (; i + 3 * NT < n_own; i += 4 * NT) {
-      const float x0 = z[i], x1 = z[i + NT], x2 = z[i + 2 * NT], x3 = z[i + 3 * NT];
+      const float x0 = z(i), x1 = z(i + NT), x2 = z(i + 2 * NT), x3 = z(i + 3 * NT);
       if (x0 >= bound || x1 >= bound || x2 >= bound || x3 >= bound) {
         if (x0 >= bound) take(i);
         if (x1 >= bound) take(i + NT);
@@ -574,7 +582,7 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
       }
     }
     for (; i < n_own; i += NT)
-      if (z[i] >= bound) take(i);
+      if (z(i) >= bound) take(i);
     __syncthreads();
     const int room = CAP / C, own = (int)sh.n_list;
     if (tid < C) cl.map_shared_rank(&sh, tid)->few[rank] = own;
@@ -630,7 +638,7 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
           uint64_t w[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float x = i + e * NT < n_own ? z[i + e * NT] : -INFINITY;
+            const float x = i + e * NT < n_own ? z(i + e * NT) : -INFINITY;
             b[e] = step_of(x, first + i + e * NT);
             w[e] = mass ? weight45(x, scale, sh.tab) : 0;
           }
@@ -726,9 +734,9 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
         const float2 near = where.around(0, step);
 #pragma unroll 4
         for (int i = tid; i < n_own; i += NT) {
-          if (z[i] < near.x) continue;
-          const int b = where(z[i], first + i, border);
-          if (b >= 0 && b <= step) to->all[atomicAdd(&to->n_all, 1u)] = key_of(z[i], first + i);
+          if (z(i) < near.x) continue;
+          const int b = where(z(i), first + i, border);
+          if (b >= 0 && b <= step) to->all[atomicAdd(&to->n_all, 1u)] = key_of(z(i), first + i);
         }
         cluster_barrier();
         if (rank == 0) draw_from_list((int)upto, pass == 0, target);
@@ -738,8 +746,8 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
       if (where.linear) {                                                  // the keys between which the step's tokens lie
         uint64_t lo = ~0ull, hi = 0;
         for (int i = tid; i < n_own; i += NT) {
-          if (where(z[i], first + i, border) == step) {
-            const uint64_t key = key_of(z[i], first + i);
+          if (where(z(i), first + i, border) == step) {
+            const uint64_t key = key_of(z(i), first + i);
             lo = min(lo, key);
             hi = max(hi, key);
           }
@@ -777,7 +785,7 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
     const float2 near = where.around(step, step);
 #pragma unroll 4
     for (int i = tid; i < n_own; i += NT)
-      if (z[i] >= near.x && z[i] <= near.y && where(z[i], first + i, border) == step) sh.list[atomicAdd(&sh.n_list, 1u)] = key_of(z[i], first + i);
+      if (z(i) >= near.x && z(i) <= near.y && where(z(i), first + i, border) == step) sh.list[atomicAdd(&sh.n_list, 1u)] = key_of(z(i), first + i);
     __syncthreads();
     {
       const int own = (int)sh.n_list;
@@ -818,35 +826,35 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
 
   // ---- the draw, in the order of the vocabulary ----
   border = Border(max(border.key, by_m));
-  const int sub = ((n_own + NT - 1) / NT) | 1, i0 = min(n_own, tid * sub), i1 = min(n_own, i0 + sub);   // (odd: no two lanes on one bank)
+  const int words = 4 / (int)sizeof(T);                                    // tokens of a bank's word
+  const int sub = ((n_own + NT * words - 1) / (NT * words) | 1) * words, i0 = min(n_own, tid * sub), i1 = min(n_own, i0 + sub);   // (an odd number of words: no two lanes on one bank)
   double sum[4] = {SUM45, SUM45, SUM45, SUM45};
   uint32_t kept = i1 - i0;
   const bool some = border.key != 0 || low <= NEG_INF;                     // not all tokens
   if (some) kept = 0;
   if (!some) {
-    for (int i = i0; i < i1; i += 4) {
-      float x[4];
+    int i = i0;
+    for (; i + 3 < i1; i += 4) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = i + e < i1 ? z[i + e] : -INFINITY;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum[e] = add45(sum[e], x[e], scale, sh.tab);        // (nothing for -inf)
+      for (int e = 0; e < 4; ++e) sum[e] = add45(sum[e], z(i + e), scale, sh.tab);
     }
+    for (; i < i1; ++i) sum[0] = add45(sum[0], z(i), scale, sh.tab);
   } else {
     for (int base = i0; base < i1; base += 32) {                           // which are kept, then their weights
       uint32_t bits = 0;
 #pragma unroll 4
-      for (int i = min(base + 32, i1) - 1; i >= base; --i) bits = bits * 2 + (border.keeps(z[i], first + i) ? 1 : 0);
+      for (int i = min(base + 32, i1) - 1; i >= base; --i) bits = bits * 2 + (border.keeps(z(i), first + i) ? 1 : 0);
       kept += __popc(bits);
       while (bits != 0) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          sum[e] = add45(sum[e], bits != 0 ? z[base + __ffs((int)bits) - 1] : -INFINITY, scale, sh.tab);
+          sum[e] = add45(sum[e], bits != 0 ? z(base + __ffs((int)bits) - 1) : -INFINITY, scale, sh.tab);
           bits &= bits - 1;
         }
       }
     }
   }
-  static_assert(MAX_SLICE / NT + 2 < 127, "a thread's sum stays below 128");
+  static_assert(MAX_SLICE / NT + 4 < 127, "a thread's sum stays below 128");
   const uint64_t mine = of_sum45(sum[0]) + of_sum45(sum[1]) + of_sum45(sum[2]) + of_sum45(sum[3]), upto = warp_scan(mine);
   kept = __reduce_add_sync(0xffffffffu, kept);
   {
@@ -872,7 +880,7 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
     uint64_t at = __shfl_sync(0xffffffffu, run, lead);
     for (int j = __shfl_sync(0xffffffffu, i0, lead); j < j1; j += 32) {
       const int i = j + lane;
-      const float x = i < j1 ? z[i] : -INFINITY;
+      const float x = i < j1 ? z(i) : -INFINITY;
       const uint64_t w = border.keeps(x, first + i) ? weight45(x, scale, sh.tab) : 0, up = at + warp_scan(w);
       if (goal < up && goal >= up - w) result(first + i, log_of(x, S), (int32_t)n_kept);
       at = __shfl_sync(0xffffffffu, up, 31);
@@ -907,12 +915,13 @@ extern "C" int actkv_sample(const void* logits, int32_t dtype, int32_t n_rows, i
   a.status = status;
   a.vocab = vocab;
   // CTAs of a row: so many that two fit on an SM, more while the SMs have not two each
+  const int bytes = dtype == ACTKV_BF16 ? 2 : 4;
   int C = 1;
-  while (C < MAX_CLUSTER && (vocab > C * 19008 || (int64_t)n_rows * C * 2 <= 148)) C *= 2;
+  while (C < MAX_CLUSTER && ((int64_t)vocab * bytes > C * 76032 || (int64_t)n_rows * C * 2 <= 148)) C *= 2;
   a.slice = ((vocab + C - 1) / C + 7) / 8 * 8;
   cudaStream_t s = (cudaStream_t)stream;
   auto go = [&](auto kernel) {
-    const size_t smem = (sizeof(Shared) + 15) / 16 * 16 + (size_t)(a.slice + 8) * 4;
+    const size_t smem = (sizeof(Shared) + 15) / 16 * 16 + (size_t)(a.slice + 8) * bytes;
     if (ensure_dyn_smem(kernel, smem) != cudaSuccess) return ACTKV_E_CUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(n_rows * C));
