@@ -91,7 +91,7 @@ template <> struct Vec<__nv_bfloat16> {
   }
 };
 
-constexpr int BATCH = 4, READ = 8;         // vectors that a thread has in flight, of logits and of the history
+constexpr int BATCH = 2, READ = 4;         // vectors that a thread has in flight, of logits and of the history
 
 // How a row's logits of tokens [v0, v1) are walked over: vectors a0 .. a1 of N, and single tokens at the ends (all of them when in and out begin at
 // different places of a vector).
