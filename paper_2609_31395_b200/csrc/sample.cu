@@ -358,7 +358,7 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
   const int head = min(n_own, (N - off) % N), vecs = (n_own - head) / N;
   float most = -INFINITY, least = INFINITY;                                 // NaN: there is one
   if (tid < head) see(row[tid] = src[tid], most, least);
-#pragma unroll 8
+#pragma unroll 4
   for (int i = tid; i < vecs; i += NT) {
     const uint4 v = *reinterpret_cast<const uint4*>(src + head + i * N);
     *reinterpret_cast<uint4*>(row + head + i * N) = v;
