@@ -758,7 +758,8 @@ int actkv_logprob(const void* logits, int32_t dtype, int32_t n_rows, int32_t voc
  * All or nothing: a request with n_r outside [0, min(seq_len, max_tok)], beyond sum_tok or its table row (ACTKV_E_INVALID), or a page id out of
  * range (ACTKV_E_BADPAGE), is reported and no key of the call is turned; the same when status is already set (a compaction that was not carried
  * out must not be followed by turns).  With status NULL tokens on bad pages, and the requests above, are left out.
- * head_dim a multiple of 8, at most 256.  Two launches; no workspace.
+ * A page belongs to one request (as everywhere): the keys of a page that the tables hold twice would be turned twice.
+ * head_dim a multiple of 8, at most 256.  ACTKV_E_TOOBIG: more than 65535 requests or units, max_tok above 2^30.  Two launches; no workspace.
  */
 typedef struct {
   const int32_t* base;          /* device, or NULL */
@@ -778,7 +779,7 @@ int actkv_reposition(const actkv_pool_t* pool /* host */, const actkv_tables_t* 
  * hist_len[r] - (W_r - 1 - w) tokens of the request (none where that is negative): all of them for the newest row, fewer for those before it, as
  * in actkv_attend.  For token t of the row, in this order, in float32:
  *   z += bias(t);
- *   t among these tokens:                        z = z > 0 ? z / repetition : z * repetition
+ *   t among these tokens:                        z = z > 0 ? z / repetition : z * repetition     (z times the rounded 1 / repetition)
  *   n > 0 times among those from prompt_len on:  z -= frequency * n + presence
  *   t not allowed:                               z = -inf
  * and rounded once to the logits' type.  out == logits: in place (row strides equal); otherwise every logit of these rows is written, and
@@ -793,7 +794,8 @@ int actkv_reposition(const actkv_pool_t* pool /* host */, const actkv_tables_t* 
  * Reported, the rows concerned left as they are (ACTKV_E_INVALID): repetition not positive and finite, frequency or presence not finite, hist_len outside
  * [0, min(max_hist, token_stride)], rows that do not fit max_win or sum_win,
  * a bias_indptr outside [0, n_bias]; (ACTKV_E_BADINDEX): biases out of order or range, allow_row beyond
- * n_allow.  max_win, max_hist: host upper bounds on W_r and hist_len.  One launch; no workspace.
+ * n_allow.  max_win, max_hist: host upper bounds on W_r and hist_len.  ACTKV_E_TOOBIG: max_hist from 2^23 on (counts are exact in float32), vocab above
+ * 2^30.  One launch; no workspace.
  */
 typedef struct {
   const int32_t*  tokens;

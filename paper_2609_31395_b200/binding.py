@@ -745,13 +745,16 @@ def logit_rules_desc(n_req, tokens=None, hist_len=None, prompt_len=None, repetit
         raise ValueError("bias_token, bias_value: expected with bias_indptr, one value per token")
     if allow is not None and allow.dtype is torch.uint32:
         allow = allow.view(torch.int32)
-    return LogitRulesDesc(_arg(tokens, torch.int32, i, 0, "tokens"), 0 if tokens is None else tokens.shape[1],
+    desc = LogitRulesDesc(_arg(tokens, torch.int32, i, 0, "tokens"), 0 if tokens is None else tokens.shape[1],
                           _arg(hist_len, torch.int32, i, n_req, "hist_len"), _arg(prompt_len, torch.int32, i, n_req, "prompt_len"),
                           _arg(repetition, torch.float32, i, n_req, "repetition"), _arg(frequency, torch.float32, i, n_req, "frequency"),
                           _arg(presence, torch.float32, i, n_req, "presence"), _arg(bias_indptr, torch.int32, i, n_req + 1, "bias_indptr"),
                           _arg(bias_token, torch.int32, i, 0, "bias_token"), _arg(bias_value, torch.float32, i, 0, "bias_value"), 0 if bias_value is None else bias_value.numel(),
                           _arg(allow, torch.int32, i, 0, "allow"), 0 if allow is None else allow.shape[1], 0 if allow is None else allow.shape[0],
                           _arg(allow_row, torch.int32, i, 0, "allow_row"))
+    desc.index, desc.n_req = i, n_req                                       # (what only the tensors know)
+    desc.rows = None if allow is None else allow.shape[0] if allow_row is None else allow_row.numel()
+    return desc
 
 
 def _logit_rows(t, index, name):
@@ -769,6 +772,12 @@ def actkv_penalize(logits, win_indptr, n_req, rules: LogitRulesDesc, max_win, ma
     """logits [rows, vocab] float32 or bf16, rows any distance apart; out: the same tensor (in place), or one of its shape and type."""
     i = _cuda_index(logits, "logits")
     kind, n, vocab, stride = _logit_rows(logits, i, "logits")
+    if getattr(rules, "index", i) != i:
+        raise TypeError(f"rules: on cuda:{rules.index}, expected cuda:{i}")
+    if getattr(rules, "n_req", 0) not in (0, n_req):
+        raise ValueError(f"rules: of {rules.n_req} requests, win_indptr: of {n_req}")
+    if getattr(rules, "rows", None) is not None and rules.rows < n:
+        raise ValueError(f"allow: masks for {rules.rows} rows, logits: {n}")
     to, out_stride = logits.data_ptr(), stride
     if out is not logits:
         if out.dtype is not logits.dtype or out.shape != logits.shape:

@@ -406,9 +406,6 @@ class LogitRules:
         if n_req is None:
             by = next((t for t in (tokens, hist_len, prompt_len, repetition, frequency, presence) if t is not None), None)
             n_req = by.shape[0] if by is not None else bias_indptr.shape[0] - 1 if bias_indptr is not None else 0
-        self.n_req = n_req
-        self.rows = None if allow is None else allow.shape[0] if allow_row is None else allow_row.shape[0]
-        self.words = None if allow is None else allow.shape[1]
         self.desc = B.logit_rules_desc(n_req, *self.tensors)
 
 
@@ -425,12 +422,7 @@ class Sampler:
     def penalize(self, logits, win_indptr, rules: LogitRules, max_win=1, max_hist=0, out=None, stream=None):
         """The rules' biases, penalties and masks on logits [rows, vocab], in place or into out; rows of request r are
         win_indptr[r] .. win_indptr[r + 1]."""
-        n_req = win_indptr.shape[0] - 1
-        if rules.n_req not in (0, n_req):
-            raise ValueError(f"rules: of {rules.n_req} requests, win_indptr: of {n_req}")
-        if rules.rows is not None and rules.rows < logits.shape[0]:
-            raise ValueError(f"allow: masks for {rules.rows} rows, logits: {logits.shape[0]}")
-        B.actkv_penalize(logits, win_indptr, n_req, rules.desc, max_win, max_hist, logits if out is None else out, self.status, stream)
+        B.actkv_penalize(logits, win_indptr, win_indptr.shape[0] - 1, rules.desc, max_win, max_hist, logits if out is None else out, self.status, stream)
 
     def sample(self, logits, u, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
         """A token per row into self.token, its log probability and the number of tokens that it was drawn from beside it."""
