@@ -93,6 +93,7 @@ struct Shared {
       uint64_t sent[CAP];                  // short lists, written by the others (perhaps while the ends are read)
     };
     uint64_t mass[2][FEW];                 // of a short list
+    uint64_t weight[CAP];                  // of a stretch of a longer one
   };
   double tab[16][16];                      // 2^(-i/16), sixteen times, so that no two lanes of a half warp meet on a bank
   uint64_t scan[2][NW];
@@ -253,6 +254,10 @@ struct Where {
   }
 };
 
+__device__ __forceinline__ void add_mass(Hist& h, uint32_t b, uint64_t w) {
+  const uint32_t lo = (uint32_t)w, old = atomicAdd(&h.lo[b], lo);
+  atomicAdd(&h.hi[b], (uint32_t)(w >> 32) + (old + lo < old ? 1u : 0u));
+}
 __device__ __forceinline__ uint64_t lds64(const uint64_t* p) {
   uint64_t v;
   asm volatile("ld.shared.u64 %0, [%1];" : "=l"(v) : "r"((uint32_t)__cvta_generic_to_shared(p)) : "memory");
@@ -514,30 +519,50 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
     uint64_t before_kept = kept, all_kept_n, zero = 0, zeros;
     block_before(sh, before_kept, zero, all_kept_n, zeros);
     const int nk = (int)all_kept_n;
-    // in the order of the vocabulary: the halves of the keys (logit; 2^32 - 1 - token) change places
-    for (int i = tid; i < nk; i += NT) sh.all[i] = sh.all[i] << 32 | sh.all[i] >> 32;
+    // in the order of the vocabulary: the masses of stretches of tokens, then the tokens of the one in which u S falls
+    const int stretch = max(0, 32 - __clz(a.vocab - 1) - LOG_NB);
+    for (int i = tid; i < NB; i += NT) sh.sum.lo[i] = sh.sum.hi[i] = 0;
+    if (tid == 0) sh.n_list = 0;
     __syncthreads();
-    sort_descending(sh.all, nk);
-    for (int i = tid; i < nk; i += NT) sh.all[i] = sh.all[i] << 32 | sh.all[i] >> 32;
-    __syncthreads();
-    mine = 0;
+    auto token_at = [&](int i) { return 0xffffffffu - (uint32_t)sh.all[i]; };
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
       const int i = tid * PER + e;
-      w[e] = i < nk ? weight45(logit_of(sh.all[i]), scale, sh.tab) : 0;
-      mine += w[e];
+      if (i < nk) add_mass(sh.sum, token_at(i) >> stretch, w[e]);
     }
-    uint64_t at = mine, S;
+    __syncthreads();
+    uint64_t part[BPT], at = 0, S;
+#pragma unroll
+    for (int e = 0; e < BPT; ++e) {
+      part[e] = ((uint64_t)sh.sum.hi[tid * BPT + e] << 32) + sh.sum.lo[tid * BPT + e];
+      at += part[e];
+    }
     zero = 0;
     block_before(sh, at, zero, S, zeros);
     const uint64_t goal = min((uint64_t)((double)u * (double)S), S - 1);
 #pragma unroll
+    for (int e = 0; e < BPT; ++e) {
+      if (goal >= at && goal < at + part[e]) sh.found[0] = tid * BPT + e, sh.found[1] = at;
+      at += part[e];
+    }
+    __syncthreads();
+#pragma unroll
     for (int e = 0; e < PER; ++e) {
-      if (goal >= at && goal < at + w[e]) {
-        const uint64_t key = sh.all[tid * PER + e];
-        result((int32_t)(0xffffffffu - (uint32_t)key), log_of(logit_of(key), S), nk);
+      const int i = tid * PER + e;
+      if (i < nk && token_at(i) >> stretch == (uint32_t)sh.found[0]) {
+        const uint32_t to = atomicAdd(&sh.n_list, 1u);
+        sh.list[to] = sh.all[i];
+        sh.weight[to] = w[e];
       }
-      at += w[e];
+    }
+    __syncthreads();
+    const int members = (int)sh.n_list;
+    for (int i = tid; i < members; i += NT) {
+      const uint64_t key = sh.list[i];
+      uint64_t before = sh.found[1];
+      for (int o = 0; o < members; ++o)
+        if ((uint32_t)sh.list[o] > (uint32_t)key) before += sh.weight[o];  // (the lower half: 2^32 - 1 - token)
+      if (goal >= before && goal < before + sh.weight[i]) result((int32_t)(0xffffffffu - (uint32_t)key), log_of(logit_of(key), S), nk);
     }
   };
 
@@ -646,10 +671,7 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
           for (int e = 0; e < 4; ++e) {
             if (b[e] >= 0) atomicAdd(&sh.own.cnt[b[e]], 1u);
             if (b[e] == NB - 1) rest += w[e];
-            if (mass && (uint32_t)b[e] < NB - 1) {
-              const uint32_t wl = (uint32_t)w[e], old = atomicAdd(&sh.own.lo[b[e]], wl);
-              atomicAdd(&sh.own.hi[b[e]], (uint32_t)(w[e] >> 32) + (old + wl < old ? 1u : 0u));
-            }
+            if (mass && (uint32_t)b[e] < NB - 1) add_mass(sh.own, b[e], w[e]);
           }
         }
       };
@@ -658,10 +680,7 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
       else count([&](float x, uint32_t) { return x >= -FLT_MAX ? where.by_logit(x) : -1; });
       if (mass) {
         rest = warp_sum(rest);
-        if (lane == 0) {
-          const uint32_t wl = (uint32_t)rest, old = atomicAdd(&sh.own.lo[NB - 1], wl);
-          atomicAdd(&sh.own.hi[NB - 1], (uint32_t)(rest >> 32) + (old + wl < old ? 1u : 0u));
-        }
+        if (lane == 0) add_mass(sh.own, NB - 1, rest);
       }
       __syncthreads();
       const int share = NB / C;
