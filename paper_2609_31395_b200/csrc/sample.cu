@@ -5,18 +5,27 @@
 // every order and on every split, so that equal arguments draw equal tokens, and a sum of 150000 weights is off by less than 2^-36 of the largest one.
 // (In float32 one draw in some hundred would fall on the neighbour of its token, and top-p would keep a token more or less.)
 //
-// A cluster holds the row in shared memory; it is read once.  Tokens are ordered by (logit descending, token ascending), as 64-bit keys that are all
-// different, and the kept ones are those that reach a border key.
-//   top-k, small: the k-th largest of the maxima of 256 groups of tokens is a bound that k tokens reach; the few that reach it go to the first
-// CTA, which sorts them, cuts the list by k, p and m, and draws from it.
+// A cluster holds the row in shared memory, in its own type; it is read once.  Tokens are ordered by (logit descending, token ascending), as 64-bit keys
+// that are all different, and the kept ones are those that reach a border key.
+//   top-k, small: the k-th largest of the maxima of 128 groups of tokens is a bound that k tokens reach; the few that reach it go to the first
+// CTA, which orders them, cuts the list by k, p and m, and draws from it.
 //   Otherwise top-k and top-p each ask for the key at which a count or a mass is reached: a histogram of 1024 equal steps of z, whose counts and
-// masses are added up over the cluster, tells the step in which it happens.  If the tokens down to it are few, the first CTA goes on with them as above; if not, the
-// tokens of the step are sorted, or, when they are more than the list holds, spread over a histogram of their keys, and so on.
+// masses are added up over the cluster, tells the step in which it happens.  If the tokens down to it are few, the first CTA goes on with them as above; if not,
+// the tokens of the step are sorted, or, when they are more than the list holds, spread over a histogram of their keys, and so on.
 //   min-p is a smallest logit, found by trying the floats around max + T ln m.
 //   The draw goes over the kept tokens in the order of the vocabulary: sums per thread, per CTA, and then along the tokens of the thread in which u S falls.
 //
-// What bounds it: few rows: the chain of passes and cluster barriers; many rows: the float64 unit (11 operations a token at 64 a clock
-// and SM), beside reading the logits.
+// CTAs only write into one another's shared memory, never read there: what is written lands before a barrier of the cluster, and behind its last barrier a CTA
+// can end.  (Loads from a neighbour may still be on their way when a thread has arrived.)
+//
+// What bounds it.  Few rows: the chain of passes and barriers: at 152K float32 tokens loading takes 2.0 us, a barrier of the cluster 0.7, the
+// weights of a CTA's 19000 tokens 3.4.  Many rows: loading and barriers (1024 bf16 rows of 152K, T = 0: 145 us
+// where reading takes 48), the weights (11 float64 operations a token: 140 us more), and, in histograms, shared memory's atomics (about 16 cycles per
+// warp, one for a count, two for a mass).
+// Measured, us: 16 rows of 152K float32: T = 0 7.5, the whole distribution 14.7, k = 20 13.4, k = 1000 30, p = 0.95 42; 64 rows 21, 34, 37, 71, 89; 1024 bf16
+// rows 145, 288, 227, 582, 908.
+// Tried: a persistent grid of clusters (321 instead of 288 for the last whole ones); a bound from 2048 groups for k up to 1280 (27 instead of 24, one row);
+// the upper word of a mass only where it is not 0 (908 -> 944).
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -36,9 +45,10 @@ constexpr int MAX_SLICE = 43008;           // tokens of a CTA
 constexpr double MAGIC = 6755399441055744.0;          // 1.5 * 2^52: adding it rounds to a whole number in the low bits
 constexpr float OCTAVES = 47.f;                       // weights below 2^-47 are 0
 constexpr int NT = 512, NW = NT / 32, BPT = NB / NT;
-constexpr int GROUPS = 128;                // of a row's tokens, for the bound of a small top-k
-constexpr int SMALL_K = 96;
-constexpr int FEW = NT / 4;                // tokens of a short list
+// The bound of a small top-k, from maxima of 128 groups: at k = 20 about 22 tokens reach it, at k = 120 some 350 (16 rows of 152K: 13.7 and 18.4 us, by the
+// histogram 20.5 and 23); with fewer groups left over than eight it may lie anywhere.
+constexpr int GROUPS = 128, SMALL_K = 120;
+constexpr int FEW = NT / 4;                // tokens of a short list, by counting: k = 20, 16 rows of 152K 13.7 us, by sorting 15.4
 
 // 2^(-i / 16)
 __constant__ double ROOTS[16] = {
@@ -363,7 +373,7 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
   const int head = min(n_own, (N - off) % N), vecs = (n_own - head) / N;
   float most = -INFINITY, least = INFINITY;                                 // NaN: there is one
   if (tid < head) see(row[tid] = src[tid], most, least);
-#pragma unroll 4
+#pragma unroll 4                                                             // (eight: 72 us instead of 62 for 1024 rows of 32003 tokens, T = 0)
   for (int i = tid; i < vecs; i += NT) {
     const uint4 v = *reinterpret_cast<const uint4*>(src + head + i * N);
     *reinterpret_cast<uint4*>(row + head + i * N) = v;
@@ -933,7 +943,9 @@ extern "C" int actkv_sample(const void* logits, int32_t dtype, int32_t n_rows, i
   a.kept = kept;
   a.status = status;
   a.vocab = vocab;
-  // CTAs of a row: so many that two fit on an SM, more while the SMs have not two each
+  // CTAs of a row: so many that two fit on an SM (with half as many and one on an SM: 300 float32 rows of 152K 146 us instead of 137, 64 rows with p = 0.95 98
+  // instead of 90, 1024 bf16 rows 318 instead of 290, but 64 whole rows 32.7 instead of 34.7), more while there are CTAs for less than half of the SMs (one row of
+  // 32003: 9.2 us with two, 6.5 with eight)
   const int bytes = dtype == ACTKV_BF16 ? 2 : 4;
   int C = 1;
   while (C < MAX_CLUSTER && ((int64_t)vocab * bytes > C * 76032 || (int64_t)n_rows * C * 2 <= 148)) C *= 2;
