@@ -828,24 +828,20 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
     }
     cluster_barrier();
     sort_descending(sh.all, (int)n);
-    if (!mass) {
-      if (tid == 0) sh.found[0] = sh.all[target - above - 1];
-    } else {
-      constexpr int PER = CAP / NT;
-      uint64_t w[PER], at = 0, zero = 0, all, zeros;
+    constexpr int PER = CAP / NT;
+    uint64_t w[PER], at = 0, zero = 0, all, zeros;                       // (one each where k asks)
 #pragma unroll
-      for (int e = 0; e < PER; ++e) {
-        const int i = tid * PER + e;
-        w[e] = i < (int)n ? weight45(logit_of(sh.all[i]), scale, sh.tab) : 0;
-        at += w[e];
-      }
-      block_before(sh, at, zero, all, zeros);
-      at += above;
+    for (int e = 0; e < PER; ++e) {
+      const int i = tid * PER + e;
+      w[e] = i >= (int)n ? 0 : mass ? weight45(logit_of(sh.all[i]), scale, sh.tab) : 1;
+      at += w[e];
+    }
+    block_before(sh, at, zero, all, zeros);
+    at += above;
 #pragma unroll
-      for (int e = 0; e < PER; ++e) {
-        if (at < target && at + w[e] >= target) sh.found[0] = sh.all[tid * PER + e];
-        at += w[e];
-      }
+    for (int e = 0; e < PER; ++e) {
+      if (at < target && at + w[e] >= target) sh.found[0] = sh.all[tid * PER + e];
+      at += w[e];
     }
     if (tid == 0) sh.n_list = sh.n_all = 0;
     __syncthreads();
