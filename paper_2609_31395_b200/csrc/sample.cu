@@ -686,8 +686,7 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
         }
       };
       if (!where.linear) count([&](float x, uint32_t token) { return where.by_key(x, token); });
-      else if (border.key != 0) count([&](float x, uint32_t token) { return where.by_logit(x, token, border); });
-      else count([&](float x, uint32_t) { return x >= -FLT_MAX ? where.by_logit(x) : -1; });
+      else count([&](float x, uint32_t token) { return where.by_logit(x, token, border); });
       if (mass) {
         rest = warp_sum(rest);
         if (lane == 0) add_mass(sh.own, NB - 1, rest);
