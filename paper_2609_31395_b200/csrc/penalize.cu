@@ -115,14 +115,40 @@ struct Walk {
   }
 };
 
-// Batches of vectors, whose loads stand before any store (the compiler cannot know that out is not read again); the masks of the next batch are on their way
-// while one is worked on.  Logits of tokens with a bias are carried over, if they are allowed.
 template <typename T>
-__device__ __forceinline__ void sweep(const T* in, T* out, const Walk<T>& walk, const uint32_t* word, bool words, const uint32_t* allow, int last_word,
-                                      int v0, int v1, bool in_place, const Rules& q) {
+struct Row {
+  const T* in;                             // of token 0
+  T* out;
+  const uint32_t* allow;                   // null: no mask
+  Walk<T> walk;
+};
+
+// The words of the mask that hold a thread's next batch of vectors.
+struct Masks {
+  uint32_t lo[BATCH], hi[BATCH];
+};
+template <typename T>
+__device__ __forceinline__ void load_masks(const uint32_t* allow, const Walk<T>& walk, int base, int v0, int last_word, Masks& m) {
+#pragma unroll
+  for (int u = 0; u < BATCH; ++u) {
+    const int i = base + u * NT, at = (v0 + walk.head + i * Vec<T>::N) >> 5;
+    const bool some = allow != nullptr && i < walk.vecs;
+    m.lo[u] = some ? allow[at] : ~0u;
+    m.hi[u] = some ? allow[min(at + 1, last_word)] : ~0u;
+  }
+}
+
+// Batches of vectors, whose loads stand before any store (the compiler cannot know that out is not read again); ahead: the masks of the first batch, in the end those
+// of the next row's first, which like those of every next batch are on their way meanwhile.  Logits of tokens with a bias are carried over, if they are allowed.
+template <bool MASKED, typename T, typename Next>
+__device__ __forceinline__ void sweep(const Row<T>& row, Next&& next, const uint32_t* word, bool words, int last_word, int v0, int v1,
+                                      bool in_place, const Rules& q, Masks& ahead) {
+  const T* in = row.in;
+  T* out = row.out;
+  const uint32_t* allow = MASKED ? row.allow : nullptr;
   constexpr int N = Vec<T>::N;
   constexpr uint32_t ALL = (1u << N) - 1;
-  const int tid = threadIdx.x, head = walk.head, vecs = walk.vecs, a0 = v0 + head, a1 = a0 + vecs * N;
+  const int tid = threadIdx.x, head = row.walk.head, vecs = row.walk.vecs, a0 = v0 + head, a1 = a0 + vecs * N;
   auto one = [&](int v) {
     const uint32_t w = words ? word[v - v0] : 0u;
     if (allow != nullptr && !(allow[v >> 5] >> (v & 31) & 1u)) store1(out + v, -INFINITY);
@@ -147,34 +173,30 @@ __device__ __forceinline__ void sweep(const T* in, T* out, const Walk<T>& walk, 
     for (int e = 0; e < N; ++e) any |= w[e];
     return any;
   };
-  auto masks = [&](int base, uint32_t (&bits)[BATCH]) {
-#pragma unroll
-    for (int u = 0; u < BATCH; ++u) {
-      const int i = base + u * NT, v = a0 + i * N;
-      bits[u] = ALL;
-      if (allow != nullptr && i < vecs) bits[u] &= __funnelshift_r(allow[v >> 5], allow[min((v >> 5) + 1, last_word)], v & 31);
-    }
-  };
-  uint32_t bits[BATCH], ahead[BATCH];
-  masks(tid, bits);
-  for (int base = tid; base < vecs; base += BATCH * NT) {
+  int base = tid;
+#pragma unroll 1
+  for (bool more = true; more;) {
     uint4 raw[BATCH];
-    uint32_t hit[BATCH];
+    uint32_t hit[BATCH], bits[BATCH];
 #pragma unroll
     for (int u = 0; u < BATCH; ++u) {
       const int i = base + u * NT, v = a0 + i * N;
+      bits[u] = MASKED ? __funnelshift_r(ahead.lo[u], ahead.hi[u], v & 31) & ALL : ALL;
       hit[u] = 0;
       if (i >= vecs) continue;
       uint32_t w[N];
       if (words && bits[u] != 0) hit[u] = words_of(v, w);
       if (bits[u] != 0 && (hit[u] != 0 || !in_place)) raw[u] = *reinterpret_cast<const uint4*>(in + v);
     }
-    if (base + BATCH * NT < vecs) masks(base + BATCH * NT, ahead);
+    more = base + BATCH * NT < vecs;
+    if (MASKED && more) load_masks(allow, row.walk, base + BATCH * NT, v0, last_word, ahead);
+    else if (MASKED) next();
 #pragma unroll
     for (int u = 0; u < BATCH; ++u) {
       const int i = base + u * NT, v = a0 + i * N;
+      const uint32_t now = bits[u];
       if (i >= vecs) continue;
-      if (bits[u] == 0) {
+      if (now == 0) {
         *reinterpret_cast<uint4*>(out + v) = Vec<T>::none();
       } else if (hit[u] != 0 || !in_place) {
         if (hit[u] != 0) {
@@ -182,20 +204,21 @@ __device__ __forceinline__ void sweep(const T* in, T* out, const Walk<T>& walk, 
           (void)words_of(v, w);
           Vec<T>::rules(raw[u], w, q);
         }
-        if (bits[u] != ALL) Vec<T>::mask(raw[u], bits[u]);
+        if (now != ALL) Vec<T>::mask(raw[u], now);
         *reinterpret_cast<uint4*>(out + v) = raw[u];
-      } else if (bits[u] != ALL) {
+      } else if (now != ALL) {
 #pragma unroll
         for (int e = 0; e < N; ++e)
-          if (!(bits[u] >> e & 1u)) store1(out + v + e, -INFINITY);
+          if (!(now >> e & 1u)) store1(out + v + e, -INFINITY);
       }
-      bits[u] = ahead[u];
     }
+    base += BATCH * NT;
   }
   for (int v = a1 + tid; v < v1; v += NT) one(v);
 }
 
-template <typename T>
+// MASKED: there are masks.
+template <typename T, bool MASKED>
 __global__ void __launch_bounds__(NT, 2) penalize_kernel(const __grid_constant__ Args a) {
   pdl_begin();
   extern __shared__ __align__(16) uint32_t s_word[];
@@ -251,6 +274,22 @@ __global__ void __launch_bounds__(NT, 2) penalize_kernel(const __grid_constant__
     const int at = lo + head + vecs * 4 + tid;
     if (at < hi) see(tokens[at]);
   };
+  // the row of allow for a row, -1: none, -2: there is no such row
+  auto mask_of = [&](int i) {
+    if (!MASKED || i >= i1) return -1;
+    const int m = a.q.allow_row != nullptr ? a.q.allow_row[w0 + i] : w0 + i;
+    if (m < a.q.n_allow) return max(m, -1);
+    if (sl == 0 && tid == 0) report(a.status, ACTKV_E_BADINDEX, r, m);
+    return -2;
+  };
+  auto allow_of = [&](int m) { return m >= 0 ? a.q.allow + (int64_t)m * a.q.allow_stride : nullptr; };
+  auto walk_of = [&](int i) {
+    return Walk<T>((const T*)a.logits + (int64_t)(w0 + i) * a.in_stride + v0, (const T*)a.out + (int64_t)(w0 + i) * a.out_stride + v0, v1 - v0);
+  };
+  const int last_word = (a.vocab - 1) >> 5;
+  int mask = mask_of(i0);
+  Masks masks;
+  if (MASKED) load_masks<T>(allow_of(mask), walk_of(i0), tid, v0, last_word, masks);
   int seen = max(0, hist - (W - 1 - i0));                                  // tokens that the row stands behind
   if (words) {
     for (int i = tid * 4; i < v1 - v0; i += NT * 4) *reinterpret_cast<uint4*>(s_word + i) = make_uint4(0, 0, 0, 0);
@@ -275,29 +314,20 @@ __global__ void __launch_bounds__(NT, 2) penalize_kernel(const __grid_constant__
     }
   }
   for (int i = i0; i < i1; ++i) {
-    const int64_t row = w0 + i;
-    const uint32_t* allow = nullptr;
-    bool skip = false;
-    if (a.q.allow != nullptr) {
-      const int m = a.q.allow_row != nullptr ? a.q.allow_row[row] : (int)row;
-      if (m >= a.q.n_allow) {
-        if (sl == 0 && tid == 0) report(a.status, ACTKV_E_BADINDEX, r, m);
-        skip = true;
-      } else if (m >= 0) {
-        allow = a.q.allow + (int64_t)m * a.q.allow_stride;
-      }
-    }
-    const T* in = (const T*)a.logits + row * a.in_stride;
-    T* out = (T*)a.out + row * a.out_stride;
-    const Walk<T> walk(in + v0, out + v0, v1 - v0);
-    if (!skip && (words || allow != nullptr || !a.in_place))
-      sweep<T>(in, out, walk, s_word, words, allow, (a.vocab - 1) >> 5, v0, v1, a.in_place != 0, q);
+    const Row<T> row = {(const T*)a.logits + (int64_t)(w0 + i) * a.in_stride, (T*)a.out + (int64_t)(w0 + i) * a.out_stride, allow_of(mask), walk_of(i)};
+    const bool skip = mask == -2;
+    mask = mask_of(i + 1);
+    auto next = [&] {
+      if (MASKED) load_masks<T>(allow_of(mask), a.alike ? row.walk : walk_of(i + 1), tid, v0, last_word, masks);
+    };
+    if (!skip && (words || row.allow != nullptr || !a.in_place)) sweep<MASKED>(row, next, s_word, words, last_word, v0, v1, a.in_place != 0, q, masks);
+    else next();
     if (n_bias > 0 && !skip) {
       __syncthreads();                                                     // (what the sweep carried over is there)
       for (int k = tid; k < n_bias; k += NT) {
         const int32_t t = a.q.bias_token[b0 + k];
-        if (t < v0 || t >= v1 || (allow != nullptr && !(allow[t >> 5] >> (t & 31) & 1u))) continue;
-        store1(out + t, penalty(load1(in + t) + a.q.bias_value[b0 + k], s_word[t - v0], q));
+        if (t < v0 || t >= v1 || (row.allow != nullptr && !(row.allow[t >> 5] >> (t & 31) & 1u))) continue;
+        store1(row.out + t, penalty(load1(row.in + t) + a.q.bias_value[b0 + k], s_word[t - v0], q));
       }
     }
     if (counts && i + 1 < i1) {
@@ -307,7 +337,7 @@ __global__ void __launch_bounds__(NT, 2) penalize_kernel(const __grid_constant__
       if (apart) __syncthreads();
       if (next > seen) {
         const int32_t token = tokens[seen];
-        if (token >= v0 && token < v1 && tid == walk.thread_of(token - v0)) {
+        if (token >= v0 && token < v1 && tid == row.walk.thread_of(token - v0)) {
           if (seen < prompt) s_word[token - v0] |= PROMPT;
           else s_word[token - v0] += 1;
         }
@@ -370,5 +400,6 @@ extern "C" int actkv_penalize(const void* logits, int32_t dtype, int32_t vocab, 
     ACTKV_CHECK_LAUNCH();
     return ACTKV_OK;
   };
-  return dtype == ACTKV_BF16 ? go(penalize_kernel<__nv_bfloat16>) : go(penalize_kernel<float>);
+  if (a.q.allow != nullptr) return dtype == ACTKV_BF16 ? go(penalize_kernel<__nv_bfloat16, true>) : go(penalize_kernel<float, true>);
+  return dtype == ACTKV_BF16 ? go(penalize_kernel<__nv_bfloat16, false>) : go(penalize_kernel<float, false>);
 }
