@@ -30,7 +30,7 @@ struct Args {
   actkv_logit_rules_t q;
   int32_t* status;
   int32_t vocab, n_req, sum_win, max_win, max_hist;
-  int32_t slice, n_slices, groups, rows_per, in_place, alike;              // alike: all rows begin at the same place of a vector
+  int32_t slice, n_slices, groups, rows_per, alike;              // alike: all rows begin at the same place of a vector
 };
 
 struct Rules {                             // of one request
@@ -140,9 +140,9 @@ __device__ __forceinline__ void load_masks(const uint32_t* allow, const Walk<T>&
 
 // Batches of vectors, whose loads stand before any store (the compiler cannot know that out is not read again); ahead: the masks of the first batch, in the end those
 // of the next row's first, which like those of every next batch are on their way meanwhile.  Logits of tokens with a bias are carried over, if they are allowed.
-template <bool MASKED, typename T, typename Next>
+template <bool MASKED, bool in_place, typename T, typename Next>
 __device__ __forceinline__ void sweep(const Row<T>& row, Next&& next, const uint32_t* word, bool words, int last_word, int v0, int v1,
-                                      bool in_place, const Rules& q, Masks& ahead) {
+                                      const Rules& q, Masks& ahead) {
   const T* in = row.in;
   T* out = row.out;
   const uint32_t* allow = MASKED ? row.allow : nullptr;
@@ -218,7 +218,7 @@ __device__ __forceinline__ void sweep(const Row<T>& row, Next&& next, const uint
 }
 
 // MASKED: there are masks.
-template <typename T, bool MASKED>
+template <typename T, bool MASKED, bool IN_PLACE>
 __global__ void __launch_bounds__(NT, 2) penalize_kernel(const __grid_constant__ Args a) {
   pdl_begin();
   extern __shared__ __align__(16) uint32_t s_word[];
@@ -320,7 +320,7 @@ __global__ void __launch_bounds__(NT, 2) penalize_kernel(const __grid_constant__
     auto next = [&] {
       if (MASKED) load_masks<T>(allow_of(mask), a.alike ? row.walk : walk_of(i + 1), tid, v0, last_word, masks);
     };
-    if (!skip && (words || row.allow != nullptr || !a.in_place)) sweep<MASKED>(row, next, s_word, words, last_word, v0, v1, a.in_place != 0, q, masks);
+    if (!skip && (words || row.allow != nullptr || !IN_PLACE)) sweep<MASKED, IN_PLACE>(row, next, s_word, words, last_word, v0, v1, q, masks);
     else next();
     if (n_bias > 0 && !skip) {
       __syncthreads();                                                     // (what the sweep carried over is there)
@@ -380,7 +380,6 @@ extern "C" int actkv_penalize(const void* logits, int32_t dtype, int32_t vocab, 
   a.sum_win = sum_win;
   a.max_win = std::min(max_win, sum_win);
   a.max_hist = max_hist;
-  a.in_place = logits == out;
   a.alike = row_stride * item % 16 == 0 && out_stride * item % 16 == 0;
   // slices: at least as many as shared memory asks for, more while the SMs have not two CTAs each; rows of a request apart for the same reason
   const int64_t want = 148 * 2, least = (vocab + MAX_SLICE - 1) / MAX_SLICE;
@@ -400,6 +399,10 @@ extern "C" int actkv_penalize(const void* logits, int32_t dtype, int32_t vocab, 
     ACTKV_CHECK_LAUNCH();
     return ACTKV_OK;
   };
-  if (a.q.allow != nullptr) return dtype == ACTKV_BF16 ? go(penalize_kernel<__nv_bfloat16, true>) : go(penalize_kernel<float, true>);
-  return dtype == ACTKV_BF16 ? go(penalize_kernel<__nv_bfloat16, false>) : go(penalize_kernel<float, false>);
+  auto typed = [&](auto type) {
+    using T = decltype(type);
+    if (a.q.allow != nullptr) return logits == out ? go(penalize_kernel<T, true, true>) : go(penalize_kernel<T, true, false>);
+    return logits == out ? go(penalize_kernel<T, false, true>) : go(penalize_kernel<T, false, false>);
+  };
+  return dtype == ACTKV_BF16 ? typed(__nv_bfloat16{}) : typed(0.f);
 }
