@@ -7,10 +7,12 @@
 //
 // What bounds it: in place without masks the history (4 bytes a token, from L2 for all but the first CTA of a request; every CTA looks at all of it), else
 // writing, or reading and writing, the logits; in small calls the chain of loads and instructions that are not in the cache yet.
-// Measured: 16 requests of 2000-34000 tokens, in place, 152K: 13.3 us (the longest history: 17 rounds of a CTA); 64 requests, three quarters with masks: 33.5;
-// 4-8 bf16 rows for each of 16 requests, out of place: 32.8; 6 x 200-300 rows out of place: 442, 60 % of the rate of a copy (a batch's loads wait for its masks).
-// Tried: tokens dealt to the CTAs of a cluster, counted through distributed shared memory (25 us instead of 14 for the first case); masks of the next row ahead
-// (586 instead of 437 for the last); three CTAs on an SM (registers spill: 19 and 666); 1024 threads and one CTA (11.7 and 458).
+// Measured: 16 requests of 2000-34000 tokens, in place, 152K: 11.8 us (the longest history: 17 rounds of a CTA); 64 requests, three quarters with masks: 33.5;
+// 4-8 bf16 rows for each of 16 requests, out of place: 32.4; 6 x 200-300 rows out of place, a third with masks: 406, 66 % of the rate of a copy; 15 x 25-37 rows
+// without masks: 110, 80 %.
+// Tried: tokens dealt to the CTAs of a cluster, counted through distributed shared memory (25 us instead of 14 for the first case); three CTAs on an SM (registers spill: 19
+// and 666 instead of 14 and 437); 1024 threads and one CTA (11.7 and 458 instead of 13.3 and 442); slices chosen so that the last wave of CTAs is full
+// (single large rows 4 to 7 % faster, drafts and small ones 2 to 4 % slower).
 #include <algorithm>
 
 #include "common.cuh"
@@ -95,8 +97,10 @@ template <> struct Vec<__nv_bfloat16> {
   }
 };
 
-constexpr int BATCH = 2, READ = 4;         // vectors that a thread has in flight, of logits and of the history (4 and 8: 1 us more in every small call, 38 us instead of
-                                           // 33.5 for 64 requests, 437 instead of 442 for many rows; 1 and 4: 491 for these)
+constexpr int READ = 4;                    // vectors of the history that a thread has in flight (eight: 1 us more in every small call)
+// Vectors of logits in flight.  Out of place without masks: 15 x 25-37 rows 110 us, with two 128.  With masks, 6 x 200-300 rows: 406, with four, whose registers
+// spill, 425.  In place few vectors are read at all: 4.6 us in the smallest calls, with four 5.1.
+template <bool MASKED, bool IN_PLACE> constexpr int BATCH = !MASKED && !IN_PLACE ? 4 : 2;
 
 // How a row's logits of tokens [v0, v1) are walked over: vectors a0 .. a1 of N, and single tokens at the ends (all of them when in and out begin at
 // different places of a vector).
@@ -124,13 +128,14 @@ struct Row {
 };
 
 // The words of the mask that hold a thread's next batch of vectors.
+template <int B>
 struct Masks {
-  uint32_t lo[BATCH], hi[BATCH];
+  uint32_t lo[B], hi[B];
 };
-template <typename T>
-__device__ __forceinline__ void load_masks(const uint32_t* allow, const Walk<T>& walk, int base, int v0, int last_word, Masks& m) {
+template <typename T, int B>
+__device__ __forceinline__ void load_masks(const uint32_t* allow, const Walk<T>& walk, int base, int v0, int last_word, Masks<B>& m) {
 #pragma unroll
-  for (int u = 0; u < BATCH; ++u) {
+  for (int u = 0; u < B; ++u) {
     const int i = base + u * NT, at = (v0 + walk.head + i * Vec<T>::N) >> 5;
     const bool some = allow != nullptr && i < walk.vecs;
     m.lo[u] = some ? allow[at] : ~0u;
@@ -140,20 +145,20 @@ __device__ __forceinline__ void load_masks(const uint32_t* allow, const Walk<T>&
 
 // Batches of vectors, whose loads stand before any store (the compiler cannot know that out is not read again); ahead: the masks of the first batch, in the end those
 // of the next row's first, which like those of every next batch are on their way meanwhile.  Logits of tokens with a bias are carried over, if they are allowed.
-template <bool MASKED, bool in_place, typename T, typename Next>
+template <bool MASKED, bool IN_PLACE, typename T, typename Next>
 __device__ __forceinline__ void sweep(const Row<T>& row, Next&& next, const uint32_t* word, bool words, int last_word, int v0, int v1,
-                                      const Rules& q, Masks& ahead) {
+                                      const Rules& q, Masks<BATCH<MASKED, IN_PLACE>>& ahead) {
   const T* in = row.in;
   T* out = row.out;
   const uint32_t* allow = MASKED ? row.allow : nullptr;
-  constexpr int N = Vec<T>::N;
+  constexpr int N = Vec<T>::N, B = BATCH<MASKED, IN_PLACE>;
   constexpr uint32_t ALL = (1u << N) - 1;
   const int tid = threadIdx.x, head = row.walk.head, vecs = row.walk.vecs, a0 = v0 + head, a1 = a0 + vecs * N;
   auto one = [&](int v) {
     const uint32_t w = words ? word[v - v0] : 0u;
     if (allow != nullptr && !(allow[v >> 5] >> (v & 31) & 1u)) store1(out + v, -INFINITY);
     else if ((int32_t)w > 0) store1(out + v, penalty(load1(in + v), w, q));
-    else if (!in_place) out[v] = in[v];
+    else if (!IN_PLACE) out[v] = in[v];
   };
   if (tid < head) one(v0 + tid);
   // the words of a vector, and what they have set
@@ -176,29 +181,29 @@ __device__ __forceinline__ void sweep(const Row<T>& row, Next&& next, const uint
   int base = tid;
 #pragma unroll 1
   for (bool more = true; more;) {
-    uint4 raw[BATCH];
-    uint32_t hit[BATCH], bits[BATCH];
+    uint4 raw[B];
+    uint32_t hit[B], bits[B];
 #pragma unroll
-    for (int u = 0; u < BATCH; ++u) {
+    for (int u = 0; u < B; ++u) {
       const int i = base + u * NT, v = a0 + i * N;
       bits[u] = MASKED ? __funnelshift_r(ahead.lo[u], ahead.hi[u], v & 31) & ALL : ALL;
       hit[u] = 0;
       if (i >= vecs) continue;
       uint32_t w[N];
       if (words && bits[u] != 0) hit[u] = words_of(v, w);
-      if (bits[u] != 0 && (hit[u] != 0 || !in_place)) raw[u] = *reinterpret_cast<const uint4*>(in + v);
+      if (bits[u] != 0 && (hit[u] != 0 || !IN_PLACE)) raw[u] = *reinterpret_cast<const uint4*>(in + v);
     }
-    more = base + BATCH * NT < vecs;
-    if (MASKED && more) load_masks(allow, row.walk, base + BATCH * NT, v0, last_word, ahead);
+    more = base + B * NT < vecs;
+    if (MASKED && more) load_masks(allow, row.walk, base + B * NT, v0, last_word, ahead);
     else if (MASKED) next();
 #pragma unroll
-    for (int u = 0; u < BATCH; ++u) {
+    for (int u = 0; u < B; ++u) {
       const int i = base + u * NT, v = a0 + i * N;
       const uint32_t now = bits[u];
       if (i >= vecs) continue;
       if (now == 0) {
         *reinterpret_cast<uint4*>(out + v) = Vec<T>::none();
-      } else if (hit[u] != 0 || !in_place) {
+      } else if (hit[u] != 0 || !IN_PLACE) {
         if (hit[u] != 0) {
           uint32_t w[N];
           (void)words_of(v, w);
@@ -212,7 +217,7 @@ __device__ __forceinline__ void sweep(const Row<T>& row, Next&& next, const uint
           if (!(now >> e & 1u)) store1(out + v + e, -INFINITY);
       }
     }
-    base += BATCH * NT;
+    base += B * NT;
   }
   for (int v = a1 + tid; v < v1; v += NT) one(v);
 }
@@ -288,7 +293,7 @@ __global__ void __launch_bounds__(NT, 2) penalize_kernel(const __grid_constant__
   };
   const int last_word = (a.vocab - 1) >> 5;
   int mask = mask_of(i0);
-  Masks masks;
+  Masks<BATCH<MASKED, IN_PLACE>> masks;
   if (MASKED) load_masks<T>(allow_of(mask), walk_of(i0), tid, v0, last_word, masks);
   int seen = max(0, hist - (W - 1 - i0));                                  // tokens that the row stands behind
   if (words) {
