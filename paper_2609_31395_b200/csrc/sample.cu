@@ -463,9 +463,9 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
     by_m = min(by_m, (uint64_t)okey(top) << 32);
   }
 
-  // All that can be kept is a list of nn tokens in the first CTA, which sorts it, cuts it and draws from it.  cut_k: the list is to be cut to k; then
+  // All that can be kept is a list of nn tokens in the first CTA, which sorts it, cuts it and draws from it.  cut: the list is to be cut to k; then
   // the mass that p is a part of is the list's.
-  auto draw_from_list = [&](int nn, bool cut_k, uint64_t target) {
+  auto draw_from_list = [&](int nn, bool cut, uint64_t target) {
     if (nn <= FEW) {                                                       // by counting, four threads a token
       const int i = tid >> 2, q = tid & 3;
       const uint64_t key = i < nn ? sh.all[i] : 0;
@@ -480,9 +480,9 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
       front += __shfl_xor_sync(0xffffffffu, front, 2);
       place += __shfl_xor_sync(0xffffffffu, place, 1);
       place += __shfl_xor_sync(0xffffffffu, place, 2);
-      bool keep = i < nn && (!cut_k || place < k) && key >= by_m;
+      bool keep = i < nn && (!cut || place < k) && key >= by_m;
       if (by_p) {
-        if (cut_k) {
+        if (cut) {
           // (the last of the first k knows their mass)
           if (q == 0 && i < nn && place == min(k, nn) - 1) sh.found[0] = front + w;
           __syncthreads();
@@ -508,7 +508,7 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
     }
     sort_descending(sh.all, nn);
     constexpr int PER = CAP / NT;
-    const int most = cut_k ? min(nn, k) : nn;
+    const int most = cut ? min(nn, k) : nn;
     uint64_t w[PER], mine = 0, ones = 0, all, none;
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
@@ -517,7 +517,7 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
       mine += w[e];
     }
     block_before(sh, mine, ones, all, none);
-    if (cut_k && by_p) target = p > 0.f ? max((uint64_t)1, (uint64_t)ceil((double)p * (double)all)) : 1;
+    if (cut && by_p) target = p > 0.f ? max((uint64_t)1, (uint64_t)ceil((double)p * (double)all)) : 1;
     // kept: in front of the target, and not too small (a prefix both)
     uint64_t run = mine, kept = 0;
 #pragma unroll
@@ -581,6 +581,9 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
   where.top = top;
   const float range = fminf(top - __int_as_float(low ^ ((low >> 31) & 0x7fffffff)), OCTAVES * kLn2 * t);
   Border border(0);
+  int listed = -1;                                                         // all that can be kept: so many tokens in the first CTA's list, to be cut to k or not,
+  bool cut_k = false;                                                      // and the mass that p asks for
+  uint64_t list_target = 0;
   if (bounded) {
     // the smallest of the groups' maxima that fewer than k exceed: the k-th largest
     if (tid == 0) sh.found[0] = 0x7fffffff;
@@ -642,15 +645,16 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
         sh.all[at] = sh.sent[o];
       }
       __syncthreads();
-      draw_from_list(n, true, 0);
-      return;
+      listed = n;
+      cut_k = true;
+    } else {
+      __syncthreads();
+      if (tid == 0) sh.n_list = 0;                                         // (many equal logits, or the largest ones in few groups)
+      __syncthreads();
     }
-    __syncthreads();
-    if (tid == 0) sh.n_list = 0;                                           // (many equal logits, or the largest ones in few groups)
-    __syncthreads();
   }
 #pragma unroll 1
-  for (int pass = by_k ? 0 : 1; pass < (by_p ? 2 : 1); ++pass) {
+  for (int pass = by_k ? 0 : 1; pass < (by_p ? 2 : 1) && listed < 0; ++pass) {
     const bool mass = pass == 1;
     uint64_t target = (uint64_t)k, above = 0, total = 0;                   // above: what lies over the steps
     int step = 0;
@@ -767,8 +771,11 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
           if (b >= 0 && b <= step) to->all[atomicAdd(&to->n_all, 1u)] = key_of(z(i), first + i);
         }
         cluster_barrier();
-        if (rank == 0) draw_from_list((int)upto, pass == 0, target);
-        return;
+        if (rank != 0) return;
+        listed = (int)upto;
+        cut_k = pass == 0;
+        list_target = target;
+        break;
       }
       if (n <= CAP) break;
       if (where.linear) {                                                  // the keys between which the step's tokens lie
@@ -808,7 +815,7 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
       // (a step of more than one token spans more than one key: they are all different)
       where.shift = max(0, 64 - __clzll((long long)(where.hi - where.lo)) - LOG_NB);
     }
-    if (all_kept) continue;
+    if (all_kept || listed >= 0) continue;
     // the step's tokens, in every CTA, and sorted
     const float2 near = where.around(step, step);
 #pragma unroll 4
@@ -846,6 +853,11 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
     __syncthreads();
     border = Border(max(border.key, sh.found[0]));
     __syncthreads();
+  }
+
+  if (listed >= 0) {
+    draw_from_list(listed, cut_k, list_target);
+    return;
   }
 
   // ---- the draw, in the order of the vocabulary ----
