@@ -19,11 +19,11 @@
 // can end.  (Loads from a neighbour may still be on their way when a thread has arrived.)
 //
 // What bounds it.  Few rows: the chain of passes and barriers: at 152K float32 tokens loading takes 2.0 us, a barrier of the cluster 0.7, the
-// weights of a CTA's 19000 tokens 3.4.  Many rows: loading and barriers (1024 bf16 rows of 152K, T = 0: 145 us
-// where reading takes 48), the weights (11 float64 operations a token: 140 us more), and, in histograms, shared memory's atomics (about 16 cycles per
+// weights of a CTA's 19000 tokens 3.4.  Many rows: loading and barriers (1024 bf16 rows of 152K, T = 0: 140 us
+// where reading takes 48), the weights (11 float64 operations a token: 150 us more), and, in histograms, shared memory's atomics (about 16 cycles per
 // warp, one for a count, two for a mass).
-// Measured, us: 16 rows of 152K float32: T = 0 7.4, the whole distribution 14.5, k = 20 13.3, k = 1000 30, p = 0.95 42; 64 rows 20, 34, 36, 70, 89; 1024 bf16
-// rows 143, 288, 227, 581, 906.
+// Measured, us: 16 rows of 152K float32: T = 0 7.2, the whole distribution 14.6, k = 20 13.0, k = 1000 30, p = 0.95 43; 64 rows 20, 34, 35, 69, 91; 1024 bf16
+// rows 140, 290, 212, 567, 916.
 // Tried: a persistent grid of clusters (321 instead of 288 for the last whole ones); a bound from 2048 groups for k up to 1280 (27 instead of 24, one row);
 // the upper word of a mass only where it is not 0 (908 -> 944); a step's tokens ordered by counting (p = 0.95, 64 rows: 89 -> 101).
 #include <cooperative_groups.h>
