@@ -190,7 +190,7 @@ __device__ __forceinline__ void sweep(const Row<T>& row, Next&& next, const uint
       hit[u] = 0;
       if (i >= vecs) continue;
       uint32_t w[N];
-      if (words && bits[u] != 0) hit[u] = words_of(v, w);
+      if (IN_PLACE && words && bits[u] != 0) hit[u] = words_of(v, w);
       if (bits[u] != 0 && (hit[u] != 0 || !IN_PLACE)) raw[u] = *reinterpret_cast<const uint4*>(in + v);
     }
     more = base + B * NT < vecs;
@@ -204,9 +204,9 @@ __device__ __forceinline__ void sweep(const Row<T>& row, Next&& next, const uint
       if (now == 0) {
         *reinterpret_cast<uint4*>(out + v) = Vec<T>::none();
       } else if (hit[u] != 0 || !IN_PLACE) {
-        if (hit[u] != 0) {
-          uint32_t w[N];
-          (void)words_of(v, w);
+        uint32_t w[N];
+        if (IN_PLACE || (words && words_of(v, w) != 0)) {
+          if (IN_PLACE) (void)words_of(v, w);
           Vec<T>::rules(raw[u], w, q);
         }
         if (now != ALL) Vec<T>::mask(raw[u], now);
