@@ -115,7 +115,7 @@ struct Walk {
   }
   __device__ __forceinline__ int thread_of(int at) const {                 // which thread has the slice's token `at`
     const int in = at - head, end = vecs * N;
-    return in < 0 ? at : in < end ? in / N % NT : (in - end) % NT;
+    return in < 0 ? at : in < end ? in / N % NT : (head + in - end) % NT;
   }
 };
 
@@ -160,7 +160,6 @@ __device__ __forceinline__ void sweep(const Row<T>& row, Next&& next, const uint
     else if ((int32_t)w > 0) store1(out + v, penalty(load1(in + v), w, q));
     else if (!IN_PLACE) out[v] = in[v];
   };
-  if (tid < head) one(v0 + tid);
   // the words of a vector, and what they have set
   auto words_of = [&](int v, uint32_t (&w)[N]) {
     uint32_t any = 0;
@@ -219,7 +218,8 @@ __device__ __forceinline__ void sweep(const Row<T>& row, Next&& next, const uint
     }
     base += B * NT;
   }
-  for (int v = a1 + tid; v < v1; v += NT) one(v);
+#pragma unroll 1
+  for (int i = tid; i < head + v1 - a1; i += NT) one(i < head ? v0 + i : a1 + i - head);
 }
 
 // MASKED: there are masks.
