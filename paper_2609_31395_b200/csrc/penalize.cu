@@ -7,9 +7,9 @@
 //
 // What bounds it: in place without masks the history (4 bytes a token, from L2 for all but the first CTA of a request; every CTA looks at all of it), else
 // writing, or reading and writing, the logits; in small calls the chain of loads and instructions that are not in the cache yet.
-// Measured: 16 requests of 2000-34000 tokens, in place, 152K: 11.8 us (the longest history: 17 rounds of a CTA); 64 requests, three quarters with masks: 33.5;
-// 4-8 bf16 rows for each of 16 requests, out of place: 32.4; 6 x 200-300 rows out of place, a third with masks: 406, 66 % of the rate of a copy; 15 x 25-37 rows
-// without masks: 110, 80 %.
+// Measured: 16 requests of 2000-34000 tokens, in place, 152K: 11.6 us (the longest history: 17 rounds of a CTA); 64 requests, three quarters with masks: 32.1;
+// 4-8 bf16 rows for each of 16 requests, out of place: 31.3; 6 x 200-300 rows out of place, a third with masks: 383, 70 % of the rate of a copy; 15 x 25-37 rows
+// without masks: 108, 81 %.
 // Tried: tokens dealt to the CTAs of a cluster, counted through distributed shared memory (25 us instead of 14 for the first case); three CTAs on an SM (registers spill: 19
 // and 666 instead of 14 and 437); 1024 threads and one CTA (11.7 and 458 instead of 13.3 and 442); slices chosen so that the last wave of CTAs is full
 // (single large rows 4 to 7 % faster, drafts and small ones 2 to 4 % slower).
@@ -98,8 +98,8 @@ template <> struct Vec<__nv_bfloat16> {
 };
 
 constexpr int READ = 4;                    // vectors of the history that a thread has in flight (eight: 1 us more in every small call)
-// Vectors of logits in flight.  Out of place without masks: 15 x 25-37 rows 110 us, with two 128.  With masks, 6 x 200-300 rows: 406, with four, whose registers
-// spill, 425.  In place few vectors are read at all: 4.6 us in the smallest calls, with four 5.1.
+// Vectors of logits in flight.  Out of place without masks: 15 x 25-37 rows 108 us, with two 125.  With masks, 6 x 200-300 rows: 383, with one 437, with four, whose
+// registers spill, 405.  In place few vectors are read at all: 4.6 us in the smallest calls, with four 5.1.
 template <bool MASKED, bool IN_PLACE> constexpr int BATCH = !MASKED && !IN_PLACE ? 4 : 2;
 
 // How a row's logits of tokens [v0, v1) are walked over: vectors a0 .. a1 of N, and single tokens at the ends (all of them when in and out begin at
