@@ -757,7 +757,8 @@ int actkv_logprob(const void* logits, int32_t dtype, int32_t n_rows, int32_t voc
  * (what the positions hold) and n_r.
  * All or nothing: a request with n_r outside [0, min(seq_len, max_tok)], beyond sum_tok or its table row (ACTKV_E_INVALID), or a page id out of
  * range (ACTKV_E_BADPAGE), is reported and no key of the call is turned; the same when status is already set (a compaction that was not carried
- * out must not be followed by turns).  With status NULL tokens on bad pages, and the requests above, are left out.
+ * out must not be followed by turns: hand over the status words of the compaction itself).  With status NULL tokens on bad pages, and the
+ * requests above, are left out.
  * A page belongs to one request (as everywhere): the keys of a page that the tables hold twice would be turned twice.
  * head_dim a multiple of 8, at most 256.  ACTKV_E_TOOBIG: more than 65535 requests or units, max_tok above 2^30.  Two launches; no workspace.
  */

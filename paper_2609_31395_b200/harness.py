@@ -384,11 +384,16 @@ class Decoder:
         """The first length[i] tokens of request src[i] into the pages of request dst[i]."""
         B.actkv_copy(self.pd, self.td, l0, self.pd.n_layers if l1 is None else l1, src, dst, length, max_len, self.status, stream)
 
-    def reposition(self, rope: Rope, tok_indptr, max_tok, from_pos=None, to_pos=None, to_inv_freq=None, l0=0, l1=None, stream=None):
-        """Cached keys from their positions to others (None: a token's index), or to other frequencies.  Behind a compaction that kept
-        sel_idx [units, any] of tokens whose positions were their indices: from_pos = sel_idx[None], tok_indptr = keep_indptr."""
+    def reposition(self, rope: Rope, tok_indptr, max_tok, from_pos=None, to_pos=None, to_inv_freq=None, l0=0, l1=None, stream=None, status=None):
+        """Cached keys from their positions to others (None: a token's index), or to other frequencies.
+
+        status: the words that stop the call where they hold an error and that its own errors are reported to (None: this Decoder's).  Behind a
+        compaction they have to be the Compressor's: a compaction that was refused leaves keys and lengths as they were, and only its own status
+        tells.  Behind comp.step(...), where positions were the tokens' indices:
+            dec.reposition(rope, comp.keep_indptr, max_keep, from_pos=comp.sel_idx[None], status=comp.status)
+        comp.sel_idx holds the lists of the last layer group: the step has to have taken all layers at once (layers_per_call as by default)."""
         B.actkv_reposition(self.pd, self.td, l0, self.pd.n_layers if l1 is None else l1, rope.desc, to_inv_freq, from_pos, to_pos, tok_indptr,
-                           max_tok, self.status, stream)
+                           max_tok, self.status if status is None else status, stream)
 
     def check_status(self):
         st = self.status.cpu().tolist()
