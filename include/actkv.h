@@ -750,6 +750,8 @@ int actkv_logprob(const void* logits, int32_t dtype, int32_t n_rows, int32_t voc
  *   base[axis*stride_axis + o*stride_unit + tok_indptr[r] + j],  int32;
  * a stride of 0: all axes or units alike.  from or to NULL, or its base NULL: the position is j, the token's index in the cache.  So, behind
  * actkv_compact, from = { sel_idx, 0, sel_stride }, to = NULL and tok_indptr = keep_indptr move the survivors up when positions were indices before.
+ * Behind actkv_compact_inplace, whose survivors do not lie in ascending order, from = { new_order, 0, sel_stride }, and to holds the rank of
+ * every entry of new_order among those of its unit.
  * to_inv_freq float32 [rotary_dim/2], NULL: the frequencies stay.  Then keys whose positions stay are left as they are (their bits too).
  * The angle is exact modulo a turn but for the rounding of inv_freq / 2 pi in float64; sine and cosine in float32; the result is rounded once to
  * bf16, so that a key that is moved many times gathers a rounding each time.

@@ -132,12 +132,13 @@ class Compressor:
                           self.status, stream)
 
     def step(self, q, win_indptr, tok_indptr, budget, sm_scale, causal, lse_in=None, stream=None, marks=None,
-             lrfu: Optional["LrfuState"] = None, inplace: bool = False, fused_lrfu: bool = True):
+             lrfu: Optional["LrfuState"] = None, inplace: bool = False, fused_lrfu: bool = True, want_order: bool = False):
         """score -> select -> compact over all layers, `layers_per_call` layers at a time.
         Tables are rewritten by the last compact call; earlier calls see the old tables.
         `lrfu`: rank by the attention-aware LRFU keep-score instead of the raw pooled score
         (score -> keepscore + select in one launch, or as two with fused_lrfu=False -> gather keep-scores -> compact).
-        `inplace`: compact into the tail blocks of each request (Algorithm 4) instead of fresh pages.
+        `inplace`: compact into the tail blocks of each request (Algorithm 4) instead of fresh pages; `want_order`: `self.new_order` then
+        holds the survivors as they lie (with `lrfu` it always does).
         `marks`: optional callable(name) invoked between stages (the benchmark records CUDA events
         there); with it the LSE pass and the pooled-score pass run as two calls so that each can be
         timed on its own.  Returns the number of kernels launched."""
@@ -169,7 +170,7 @@ class Compressor:
                 self.run_gather_ks(lrfu, tok_indptr, l0, l1, stream)
             mark("select")
             if inplace:
-                self.run_compact_inplace(budget, l0, l1, stream, want_order=lrfu is not None)
+                self.run_compact_inplace(budget, l0, l1, stream, want_order=want_order or lrfu is not None)
                 if lrfu is not None:
                     self.run_gather_ks(lrfu, tok_indptr, l0, l1, stream, idx=self.new_order)
             else:
@@ -391,7 +392,14 @@ class Decoder:
         compaction they have to be the Compressor's: a compaction that was refused leaves keys and lengths as they were, and only its own status
         tells.  Behind comp.step(...), where positions were the tokens' indices:
             dec.reposition(rope, comp.keep_indptr, max_keep, from_pos=comp.sel_idx[None], status=comp.status)
-        comp.sel_idx holds the lists of the last layer group: the step has to have taken all layers at once (layers_per_call as by default)."""
+        Behind comp.step(..., inplace=True, want_order=True) the survivors do not lie in ascending order.  They come from comp.new_order and go to
+        their ranks among the survivors of their request (n = how many all requests keep, T above every length):
+            request = torch.searchsorted(comp.keep_indptr[1:], torch.arange(n, device=dev), right=True)
+            order = comp.new_order[:, :n] + T * request                      # (int64; every request's behind the one before)
+            rank = order.argsort(1).argsort(1) - comp.keep_indptr[request]
+            dec.reposition(rope, comp.keep_indptr, max_keep, from_pos=comp.new_order[None], to_pos=rank[None].int(), status=comp.status)
+        comp.sel_idx and comp.new_order hold the last layer group: the step has to have taken all layers at once (layers_per_call as by
+        default)."""
         B.actkv_reposition(self.pd, self.td, l0, self.pd.n_layers if l1 is None else l1, rope.desc, to_inv_freq, from_pos, to_pos, tok_indptr,
                            max_tok, self.status if status is None else status, stream)
 

@@ -64,7 +64,7 @@ class Cache:
                     raw = self.rows(self.before, self.old, l, h, r, self.lens[r])[was]
                     want = O.reposition_unit(raw, was[None], will[None], f, f, [D // 2], False)
                     # half a step of bf16, and 2^-19 of the pair for the angle, sine and cosine
-                    tol = 2.0 ** -8 * np.abs(want) + 2.0 ** -19 * 2 * np.abs(raw).max()
+                    tol = 2.0 ** -8 * np.abs(want) + 2.0 ** -19 * 2 * np.abs(raw).max(initial=0.0)
                     assert (np.abs(self.rows(now, table, l, h, r, n) - want) <= tol).all()
 
 
@@ -110,3 +110,47 @@ def test_an_error_of_the_call_goes_to_the_words_that_it_was_given():
     assert c.comp.status.tolist()[:2] == [B.E_INVALID, 0] and c.dec.status.tolist() == [0] * 4 and np.array_equal(U.bits(c.pool), bits)
     c.dec.reposition(c.rope, _i32([0, 100, 161, 289]), 128, from_pos=_i32(range(1, 290)))          # (the Decoder's own, which are clean)
     assert c.dec.status.tolist() == [0] * 4 and not np.array_equal(U.bits(c.pool), bits)
+
+
+def _ranks(comp, n, longest):
+    """The recipe of Decoder.reposition's documentation."""
+    request = torch.searchsorted(comp.keep_indptr[1:], torch.arange(n, device=DEV), right=True)
+    order = comp.new_order[:, :n] + longest * request
+    return order.argsort(1).argsort(1) - comp.keep_indptr[request]
+
+
+@pytest.mark.parametrize("lens,budget", [(LENS, BUDGET), ([300], [111]), ([33, 0, 16, 200], [1, 0, 16, 130]), ([70, 80], [70, 80])])
+def test_behind_a_compaction_in_place(lens, budget):
+    c = Cache(3, lens, budget)
+    c.step(inplace=True, want_order=True)
+    n = sum(budget)
+    c.dec.reposition(c.rope, c.comp.keep_indptr, max(budget), from_pos=c.comp.new_order[None], to_pos=_ranks(c.comp, n, 1 << 20)[None].int(), status=c.comp.status)
+    c.comp.check_status()
+    order, ind = c.comp.new_order.cpu().numpy(), c.comp.keep_indptr.cpu().tolist()
+    of, disordered = _lists(c), 0
+
+    def lies(unit, r):
+        nonlocal disordered
+        was = order[unit, ind[r]:ind[r + 1]]
+        assert np.array_equal(np.sort(was), of(unit, r))
+        disordered += int((np.diff(was) < 0).any())
+        return was, np.searchsorted(of(unit, r), was)
+    c.check(lies)
+    assert (disordered > 0) == any(b < n for b, n in zip(budget, lens))
+
+
+def test_a_step_in_place_without_the_order_is_as_before():
+    a, b = Cache(4), Cache(4)
+    a.step(inplace=True)
+    b.step(inplace=True, want_order=True)
+    assert getattr(a.comp, "new_order", None) is None and np.array_equal(U.bits(a.pool), U.bits(b.pool)) and torch.equal(a.table, b.table)
+
+
+def test_behind_a_compaction_in_place_that_was_refused():
+    c = Cache(5)
+    c.table[1, 2] = 10000                        # (a page that is not there)
+    c.step(inplace=True, want_order=True)
+    bits = U.bits(c.pool)
+    c.dec.reposition(c.rope, c.comp.keep_indptr, max(BUDGET), from_pos=c.comp.new_order[None], to_pos=_ranks(c.comp, sum(BUDGET), 1 << 20)[None].int(),
+                     status=c.comp.status)
+    assert c.comp.status[0].item() == B.E_BADPAGE and c.seq_len.cpu().tolist() == LENS and np.array_equal(U.bits(c.pool), bits)
