@@ -119,6 +119,12 @@ __device__ __forceinline__ double exact_double(float x) {
   return (b & 0x7f800000u) != 0 ? (double)x : (b & 0x80000000u ? -1.0 : 1.0) * (double)(int)(b & 0x7fffffu) * 0x1p-149;
 }
 
+// 0 (of either sign) <= x <= most (false for NaN), and x > 0 where x is no NaN, by the bits: float32 comparisons take a subnormal number for 0.
+__device__ __forceinline__ bool from_zero_to(float x, float most) {
+  return __float_as_uint(x) <= __float_as_uint(most) || __float_as_uint(x) == 0x80000000u;
+}
+__device__ __forceinline__ bool positive(float x) { return __float_as_int(x) > 0; }
+
 // Order of the logits as signed integers (-0 just below +0).  NaN lie outside the infinities.
 __device__ __forceinline__ int32_t ordered(float x) {
   const int32_t b = __float_as_int(x);
@@ -353,7 +359,7 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
     if (a.logprob != nullptr) a.logprob[r] = logprob;
     if (a.kept != nullptr) a.kept[r] = kept;
   };
-  if (!(t >= 0.f && t < INFINITY) || !(p == p) || !(m == m) || !(u >= 0.f && u <= 1.f)) {      // (the whole cluster)
+  if (!from_zero_to(t, FLT_MAX) || !(p == p) || !(m == m) || !from_zero_to(u, 1.f)) {          // (the whole cluster)
     if (rank == 0 && tid == 0) {
       report(a.status, ACTKV_E_INVALID, (int)r, k);
       result(-1, -INFINITY, 0);
@@ -398,7 +404,7 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
   Scale scale;
   if (!greedy) {
     temp = exact_double(t);
-    if (m > 0.f && m < 1.f) below = temp * log(exact_double(m));
+    if (positive(m) && m < 1.f) below = temp * log(exact_double(m));
     scale.c = 16.0 * 1.4426950408889634074 / temp;
     scale.limit = __double2hiint(temp * (47.0 * 0.69314718055994530942)) + 1;
   }
@@ -452,7 +458,7 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
   scale.top = (double)top;
   auto log_of = [&](float x, uint64_t S) { return (float)(((double)x - scale.top) / temp - log((double)S * 0x1p-45)); };
   uint64_t by_m = 0;                                                       // key of the smallest logit with w >= m
-  if (m > 0.f) {
+  if (positive(m)) {
     const uint32_t near = okey((float)(scale.top + below));
     const uint32_t mine = near + lane < 16u ? 0u : near + lane - 16u;
     const float x = okey_inv(mine);
