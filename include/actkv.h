@@ -785,7 +785,8 @@ int actkv_reposition(const actkv_pool_t* pool /* host */, const actkv_tables_t* 
  *   t among these tokens:                        z = z > 0 ? z / repetition : z * repetition     (z times the rounded 1 / repetition)
  *   n > 0 times among those from prompt_len on:  z -= frequency * n + presence
  *   t not allowed:                               z = -inf
- * and rounded once to the logits' type.  out == logits: in place (row strides equal); otherwise every logit of these rows is written, and
+ * and rounded once to the logits' type; numbers below 2^-126 on the way count as 0.  Logits that no rule touches keep their bits.
+ * out == logits: in place (row strides equal); otherwise every logit of these rows is written, and
  * logits and out may not overlap.  Rows of no request (sum_win above win_indptr[n_req]) are left as they are.
  * Tokens of the history outside [0, vocab) count for nothing.
  * The rules (struct read during the call; every pointer on the device; NULL: off):
@@ -794,8 +795,8 @@ int actkv_reposition(const actkv_pool_t* pool /* host */, const actkv_tables_t* 
  *   bias_token int32, bias_value float32 [n_bias]: a request's entries, from bias_indptr[r] to bias_indptr[r+1], its tokens ascending; values finite or -inf;
  *   allow uint32 [n_allow, allow_stride]: bit t % 32 of word t / 32; allow_row int32 [sum_win] the row of allow for each row of logits, negative:
  *   everything is allowed (NULL: row i has row i).
- * Reported, the rows concerned left as they are (ACTKV_E_INVALID): repetition not positive and finite, frequency or presence not finite, hist_len outside
- * [0, min(max_hist, token_stride)], rows that do not fit max_win or sum_win,
+ * Reported, the rows concerned left as they are (ACTKV_E_INVALID): repetition outside [2^-126, 2^126] (beyond, it or its reciprocal is no normal
+ * float32), frequency or presence not finite, hist_len outside [0, min(max_hist, token_stride)], rows that do not fit max_win or sum_win,
  * a bias_indptr outside [0, n_bias]; (ACTKV_E_BADINDEX): biases out of order or range, allow_row beyond
  * n_allow.  max_win, max_hist: host upper bounds on W_r and hist_len.  ACTKV_E_TOOBIG: max_hist from 2^23 on (counts are exact in float32), vocab above
  * 2^30.  One launch; no workspace.

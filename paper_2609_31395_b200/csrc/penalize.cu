@@ -246,12 +246,12 @@ __global__ void __launch_bounds__(NT, 2) penalize_kernel(const __grid_constant__
   }
   const int i0 = grp * a.rows_per, i1 = min(W, i0 + a.rows_per);
   if (i0 >= i1) return;
-  if (!(q.theta > 0.f && q.theta < INFINITY) || !(fabsf(q.freq) < INFINITY) || !(fabsf(q.pres) < INFINITY) || hist < 0 || hist > a.max_hist ||
+  if (!(q.theta >= 0x1p-126f && q.theta <= 0x1p126f) || !(fabsf(q.freq) < INFINITY) || !(fabsf(q.pres) < INFINITY) || hist < 0 || hist > a.max_hist ||
       hist > a.q.token_stride || b0 < 0 || b1 < b0 || b1 > a.q.n_bias) {
     if (first) report(a.status, ACTKV_E_INVALID, r, hist);
     return;
   }
-  q.inverse = __frcp_rn(q.theta);
+  q.inverse = __frcp_rn(q.theta);                                          // (in its range a normal number: a subnormal one would be taken for 0)
   const int v0 = sl * a.slice, v1 = min(a.vocab, v0 + a.slice);
   const bool counts = hist > 0 && (q.theta != 1.f || q.freq != 0.f || q.pres != 0.f), words = counts || n_bias > 0;
   const int32_t* tokens = a.q.tokens + (int64_t)r * a.q.token_stride;
