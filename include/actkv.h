@@ -795,10 +795,12 @@ int actkv_reposition(const actkv_pool_t* pool /* host */, const actkv_tables_t* 
  *   bias_token int32, bias_value float32 [n_bias]: a request's entries, from bias_indptr[r] to bias_indptr[r+1], its tokens ascending; values finite or -inf;
  *   allow uint32 [n_allow, allow_stride]: bit t % 32 of word t / 32; allow_row int32 [sum_win] the row of allow for each row of logits, negative:
  *   everything is allowed (NULL: row i has row i).
- * Reported, the rows concerned left as they are (ACTKV_E_INVALID): repetition outside [2^-126, 2^126] (beyond, it or its reciprocal is no normal
- * float32), frequency or presence not finite, hist_len outside [0, min(max_hist, token_stride)], rows that do not fit max_win or sum_win,
- * a bias_indptr outside [0, n_bias]; (ACTKV_E_BADINDEX): biases out of order or range, allow_row beyond
- * n_allow.  max_win, max_hist: host upper bounds on W_r and hist_len.  ACTKV_E_TOOBIG: max_hist from 2^23 on (counts are exact in float32), vocab above
+ * Reported (ACTKV_E_INVALID): repetition outside [2^-126, 2^126] (beyond, it or its reciprocal is no normal float32), frequency or presence not
+ * finite, hist_len outside [0, min(max_hist, token_stride)], rows that do not fit max_win or sum_win, a bias_indptr outside [0, n_bias];
+ * (ACTKV_E_BADINDEX): biases out of order or range, allow_row beyond n_allow.  The rows concerned (of the request; with allow_row the one row) are left
+ * as they are in place, so that a token drawn from them is drawn without the rules: look at status before it is used.  Out of place they are -inf
+ * throughout, and no token is drawn from them (actkv_sample: -1).  The others are carried out.
+ * max_win, max_hist: host upper bounds on W_r and hist_len.  ACTKV_E_TOOBIG: max_hist from 2^23 on (counts are exact in float32), vocab above
  * 2^30.  One launch; no workspace.
  */
 typedef struct {

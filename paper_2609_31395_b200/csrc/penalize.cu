@@ -222,6 +222,13 @@ __device__ __forceinline__ void sweep(const Row<T>& row, Next&& next, const uint
   for (int i = tid; i < head + v1 - a1; i += NT) one(i < head ? v0 + i : a1 + i - head);
 }
 
+// n tokens of the rows from, from + step, ... below to; out: of row 0.  (A call, so that the kernels carry little of it.)
+template <typename T>
+__device__ __noinline__ void forbid(T* out, int64_t stride, int from, int to, int step, int n) {
+  for (int i = from; i < to; i += step)
+    for (int v = threadIdx.x; v < n; v += NT) store1(out + i * stride + v, -INFINITY);
+}
+
 // MASKED: there are masks.
 template <typename T, bool MASKED, bool IN_PLACE>
 __global__ void __launch_bounds__(NT, 2) penalize_kernel(const __grid_constant__ Args a) {
@@ -240,8 +247,14 @@ __global__ void __launch_bounds__(NT, 2) penalize_kernel(const __grid_constant__
   const int hist = has_history ? a.q.hist_len[r] : 0;
   const int prompt = has_history && a.q.prompt_len != nullptr ? a.q.prompt_len[r] : 0;
   const int b0 = has_bias ? a.q.bias_indptr[r] : 0, b1 = has_bias ? a.q.bias_indptr[r + 1] : 0, n_bias = b1 - b0;
+  const int v0 = sl * a.slice, v1 = min(a.vocab, v0 + a.slice);
+  // Out of place nothing may be drawn from rows that are refused: what the buffer holds is of another step, and without the rules.
+  auto refuse = [&](int from, int to, int step) {
+    if (!IN_PLACE) forbid((T*)a.out + v0, a.out_stride, from, to, step, v1 - v0);
+  };
   if (w0 < 0 || w1 < w0 || w1 > a.sum_win || W > a.max_win) {
     if (first) report(a.status, ACTKV_E_INVALID, r, W);
+    refuse(max(w0, 0) + grp, min(w1, a.sum_win), a.groups);
     return;
   }
   const int i0 = grp * a.rows_per, i1 = min(W, i0 + a.rows_per);
@@ -249,10 +262,10 @@ __global__ void __launch_bounds__(NT, 2) penalize_kernel(const __grid_constant__
   if (!(q.theta >= 0x1p-126f && q.theta <= 0x1p126f) || !(fabsf(q.freq) < INFINITY) || !(fabsf(q.pres) < INFINITY) || hist < 0 || hist > a.max_hist ||
       hist > a.q.token_stride || b0 < 0 || b1 < b0 || b1 > a.q.n_bias) {
     if (first) report(a.status, ACTKV_E_INVALID, r, hist);
+    refuse(w0 + i0, w0 + i1, 1);
     return;
   }
   q.inverse = __frcp_rn(q.theta);                                          // (in its range a normal number: a subnormal one would be taken for 0)
-  const int v0 = sl * a.slice, v1 = min(a.vocab, v0 + a.slice);
   const bool counts = hist > 0 && (q.theta != 1.f || q.freq != 0.f || q.pres != 0.f), words = counts || n_bias > 0;
   const int32_t* tokens = a.q.tokens + (int64_t)r * a.q.token_stride;
   // f of the slice's tokens among the history's [lo, hi), by their place in the slice
@@ -315,6 +328,7 @@ __global__ void __launch_bounds__(NT, 2) penalize_kernel(const __grid_constant__
     }
     if (__syncthreads_or(bad)) {
       if (first) report(a.status, ACTKV_E_BADINDEX, r, b0);
+      refuse(w0 + i0, w0 + i1, 1);
       return;
     }
   }
@@ -326,7 +340,13 @@ __global__ void __launch_bounds__(NT, 2) penalize_kernel(const __grid_constant__
       if (MASKED) load_masks<T>(allow_of(mask), a.alike ? row.walk : walk_of(i + 1), tid, v0, last_word, masks);
     };
     if (!skip && (words || row.allow != nullptr || !IN_PLACE)) sweep<MASKED, IN_PLACE>(row, next, s_word, words, last_word, v0, v1, q, masks);
-    else next();
+    else {
+      next();
+      if (!IN_PLACE) {                                                     // (skipped)
+#pragma unroll 1
+        for (int v = v0 + tid; v < v1; v += NT) store1(row.out + v, -INFINITY);
+      }
+    }
     if (n_bias > 0 && !skip) {
       __syncthreads();                                                     // (what the sweep carried over is there)
       for (int k = tid; k < n_bias; k += NT) {

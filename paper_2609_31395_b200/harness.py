@@ -434,7 +434,8 @@ class Sampler:
 
     def penalize(self, logits, win_indptr, rules: LogitRules, max_win=1, max_hist=0, out=None, stream=None):
         """The rules' biases, penalties and masks on logits [rows, vocab], in place or into out; rows of request r are
-        win_indptr[r] .. win_indptr[r + 1]."""
+        win_indptr[r] .. win_indptr[r + 1].  Rules that are refused (status) leave rows of -inf in out, from which `sample` draws the token -1; in
+        place they leave the rows without the rules, and a token drawn from them is not to be used."""
         B.actkv_penalize(logits, win_indptr, win_indptr.shape[0] - 1, rules.desc, max_win, max_hist, logits if out is None else out, self.status, stream)
 
     def sample(self, logits, u, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
