@@ -420,6 +420,7 @@ class LogitRules:
             by = next((t for t in (tokens, hist_len, prompt_len, repetition, frequency, presence) if t is not None), None)
             n_req = by.shape[0] if by is not None else bias_indptr.shape[0] - 1 if bias_indptr is not None else 0
         self.desc = B.logit_rules_desc(n_req, *self.tensors)
+        self.max_hist = 0 if tokens is None else min(tokens.shape[1], (1 << 23) - 1)   # (the longest that actkv_penalize takes)
 
 
 class Sampler:
@@ -432,10 +433,13 @@ class Sampler:
         self.kept = torch.empty(rows, dtype=torch.int32, device=device)
         self.status = torch.zeros(4, dtype=torch.int32, device=device)
 
-    def penalize(self, logits, win_indptr, rules: LogitRules, max_win=1, max_hist=0, out=None, stream=None):
+    def penalize(self, logits, win_indptr, rules: LogitRules, max_win=1, max_hist: Optional[int] = None, out=None, stream=None):
         """The rules' biases, penalties and masks on logits [rows, vocab], in place or into out; rows of request r are
         win_indptr[r] .. win_indptr[r + 1].  Rules that are refused (status) leave rows of -inf in out, from which `sample` draws the token -1; in
-        place they leave the rows without the rules, and a token drawn from them is not to be used."""
+        place they leave the rows without the rules, and a token drawn from them is not to be used.  max_win: upper bound on a request's
+        rows; max_hist: on a history's length (None: what rules.tokens has room for)."""
+        if max_hist is None:
+            max_hist = rules.max_hist
         B.actkv_penalize(logits, win_indptr, win_indptr.shape[0] - 1, rules.desc, max_win, max_hist, logits if out is None else out, self.status, stream)
 
     def sample(self, logits, u, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
