@@ -753,8 +753,8 @@ int actkv_logprob(const void* logits, int32_t dtype, int32_t n_rows, int32_t voc
  * Behind actkv_compact_inplace, whose survivors do not lie in ascending order, from = { new_order, 0, sel_stride }, and to holds the rank of
  * every entry of new_order among those of its unit.
  * to_inv_freq float32 [rotary_dim/2], NULL: the frequencies stay.  Then keys whose positions stay are left as they are (their bits too).
- * The angle is exact modulo a turn but for the rounding of inv_freq / 2 pi in float64; sine and cosine in float32; the result is rounded once to
- * bf16, so that a key that is moved many times gathers a rounding each time.
+ * The angle is exact modulo a turn but for the rounding of inv_freq / 2 pi in float64; then rounded to 2^-23 turns; sine and cosine in float32, off by
+ * 2^-19.9 at most (with that rounding); the result is rounded once to bf16, so that a key that is moved many times gathers a rounding each time.
  * V, other dims, tokens from n_r on and free pages are not touched.  sum_tok, max_tok: host upper bounds on tok_indptr[n_req]
  * (what the positions hold) and n_r.
  * All or nothing: a request with n_r outside [0, min(seq_len, max_tok)], beyond sum_tok or its table row (ACTKV_E_INVALID), or a page id out of

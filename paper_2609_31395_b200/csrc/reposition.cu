@@ -4,7 +4,7 @@
 // A key cached at position p is R(p f) k, with the rotation R acting on pairs of dims.  Rotations add, so what the key is at position p' under
 // frequencies f' is R(p' f' - p f) of what lies in the page: one turn per pair, k itself is not needed.  The angle is formed in turns, as
 // 64-bit fixed point: F = f / 2 pi modulo 1 in steps of 2^-64 (float64 product, error 2^-56), phase = p' F' - p F modulo 2^64, which is
-// exact however far the positions are apart; its upper 32 bits go to sine and cosine in float32.
+// exact however far the positions are apart; its upper 32 bits, rounded to 23, go to sine and cosine in float32.
 //
 // What bounds it: reading and writing the turned dims of every key that moves once, 4 rotary_dim bytes per (key, head, layer), and 4
 // bytes per position.  A thread has the same dims of every key that it turns (its frequencies stay in registers), and the keys of its next heads or token in
@@ -74,10 +74,11 @@ __device__ __forceinline__ uint64_t turns64(float f) {                      // f
 // The upper half of p F modulo 2^64: a position times the frequency, in steps of 2^-32 turns.
 __device__ __forceinline__ uint32_t phase_of(uint32_t p, uint64_t F) { return p * (uint32_t)(F >> 32) + __umulhi(p, (uint32_t)F); }
 __device__ __forceinline__ uint32_t phase_of(int32_t p, uint64_t F) { return phase_of((uint32_t)p, F) - (p < 0 ? (uint32_t)F : 0u); }
-// (The upper 23 bits as a float32 in [1, 2), without a conversion: those share the special function units with sine and cosine, 24 operations of a lane's 8
-// pairs, and 16 so.)
+// (The phase rounded to its upper 23 bits, as a float32 in [1, 2) without a conversion: those share the special function units with sine and cosine, 24 operations
+// of a lane's 8 pairs, and 16 so.  Half a step is 2^-21.4 rad; with the rounding of the product and of 2 pi the angle is off by 2^-20.7 at most, to both sides alike, and
+// sine and cosine by 2^-21.1 of their own: 2^-19.9 in all.)
 __device__ __forceinline__ void sincos_of(uint32_t phase, float& sn, float& cs) {
-  const float t = (__uint_as_float((phase >> 9 ^ 0x400000u) | 0x3f800000u) - 1.5f) * 6.283185307179586f;       // in [-pi, pi), steps of 2^-23 turns
+  const float t = (__uint_as_float(((phase + 0x100u) >> 9 ^ 0x400000u) | 0x3f800000u) - 1.5f) * 6.283185307179586f;      // in [-pi, pi)
   sn = __sinf(t);
   cs = __cosf(t);
 }
