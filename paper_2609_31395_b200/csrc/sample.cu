@@ -243,6 +243,7 @@ struct Border {
   __device__ __forceinline__ explicit Border(uint64_t k) : key(k), at(k != 0 ? logit_of(k) : -FLT_MAX) {}
   __device__ __forceinline__ bool keeps(float x, uint32_t token) const { return x > at || (x >= at && key_of(x, token) >= key); }
 };
+// (Lists are as long as a histogram has counted, if a token's step comes out the same each time it is formed; their places are bounded all the same.)
 // The step of a histogram in which a token falls, -1: none.  First equal steps of z, of the tokens that a border keeps; then equal steps of the
 // keys from hi down to lo.
 struct Where {
@@ -774,7 +775,9 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
         for (int i = tid; i < n_own; i += NT) {
           if (z(i) < near.x) continue;
           const int b = where(z(i), first + i, border);
-          if (b >= 0 && b <= step) to->all[atomicAdd(&to->n_all, 1u)] = key_of(z(i), first + i);
+          if (b < 0 || b > step) continue;
+          const uint32_t at = atomicAdd(&to->n_all, 1u);
+          if (at < CAP) to->all[at] = key_of(z(i), first + i);
         }
         cluster_barrier();
         if (rank != 0) return;
@@ -825,17 +828,20 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
     // the step's tokens, in every CTA, and sorted
     const float2 near = where.around(step, step);
 #pragma unroll 4
-    for (int i = tid; i < n_own; i += NT)
-      if (z(i) >= near.x && z(i) <= near.y && where(z(i), first + i, border) == step) sh.list[atomicAdd(&sh.n_list, 1u)] = key_of(z(i), first + i);
+    for (int i = tid; i < n_own; i += NT) {
+      if (!(z(i) >= near.x && z(i) <= near.y && where(z(i), first + i, border) == step)) continue;
+      const uint32_t at = atomicAdd(&sh.n_list, 1u);
+      if (at < CAP) sh.list[at] = key_of(z(i), first + i);
+    }
     __syncthreads();
     {
-      const int own = (int)sh.n_list;
+      const int own = min((int)sh.n_list, CAP);
       for (int c = warp; c < C; c += NW) {
         Shared* to = cl.map_shared_rank(&sh, c);
         uint32_t at = 0;
         if (lane == 0) at = atomicAdd(&to->n_all, (uint32_t)own);
         at = __shfl_sync(0xffffffffu, at, 0);
-        for (int i = lane; i < own; i += 32) to->all[at + i] = sh.list[i];
+        for (int i = lane; i < own && at + i < CAP; i += 32) to->all[at + i] = sh.list[i];
       }
     }
     cluster_barrier();
