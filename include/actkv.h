@@ -762,6 +762,7 @@ int actkv_logprob(const void* logits, int32_t dtype, int32_t n_rows, int32_t voc
  * out must not be followed by turns: hand over the status words of the compaction itself).  With status NULL tokens on bad pages, and the
  * requests above, are left out.
  * A page belongs to one request (as everywhere): the keys of a page that the tables hold twice would be turned twice.
+ * A call that can move nothing (no layers, requests or pairs, max_tok 0, neither positions nor other frequencies) looks at nothing on the device.
  * head_dim a multiple of 8, at most 256.  ACTKV_E_TOOBIG: more than 65535 requests or units, max_tok above 2^30.  Two launches; no workspace.
  */
 typedef struct {

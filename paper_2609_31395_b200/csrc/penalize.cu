@@ -7,9 +7,9 @@
 //
 // What bounds it: in place without masks the history (4 bytes a token, from L2 for all but the first CTA of a request; every CTA looks at all of it), else
 // writing, or reading and writing, the logits; in small calls the chain of loads and instructions that are not in the cache yet.
-// Measured: 16 requests of 2000-34000 tokens, in place, 152K: 11.6 us (the longest history: 17 rounds of a CTA); 64 requests, three quarters with masks: 32.1;
-// 4-8 bf16 rows for each of 16 requests, out of place: 31.3; 6 x 200-300 rows out of place, a third with masks: 383, 70 % of the rate of a copy; 15 x 25-37 rows
-// without masks: 108, 81 %.
+// Measured: 16 requests of 2000-34000 tokens, in place, 152K: 11.4 us (the longest history: 17 vectors a thread, in five rounds of four); 64 requests, three quarters
+// with masks: 38; 4-8 bf16 rows for each of 16 requests, out of place: 32.7; 6 x 200-300 rows out of place, a third with masks: 382, 70 % of the rate of a copy; 15 x 25-37
+// rows out of place, histories up to 9000 tokens, without masks and biases: 109, 80 %; up to 34000 tokens and biases: 125, 70 %.
 // Tried: tokens dealt to the CTAs of a cluster, counted through distributed shared memory (25 us instead of 14 for the first case); three CTAs on an SM (registers spill: 19
 // and 666 instead of 14 and 437); 1024 threads and one CTA (11.7 and 458 instead of 13.3 and 442); slices chosen so that the last wave of CTAs is full
 // (single large rows 4 to 7 % faster, drafts and small ones 2 to 4 % slower).

@@ -10,8 +10,8 @@
 // bytes per position.  A thread has the same dims of every key that it turns (its frequencies stay in registers), and the keys of its next heads or token in
 // flight while it turns these.  Positions that all heads share are turned to sine and cosine once per token.
 // Measured: 8 x 9100 keys of 4 heads of 128 dims, positions per head, 6 layers: 148 us, 91 % of the rate of a copy; 8 x 20000-35000 keys to other frequencies,
-// 2 layers: 149 us, 93 %; 16 x 500-6000 keys of 8 heads, 32 of 64 dims, three axes, 2 layers: 50 us, 30 %: bound by instructions (320 a key and lane: six
-// positions, an axis to choose for each pair); 1000 keys: 5.6 us, two launches.
+// 2 layers: 149 us, 93 %; 16 x 500-6000 keys of 8 heads, 32 of 64 dims, three axes, 2 layers: 50 us, 30 %: bound by instructions (320 a key and lane: three
+// positions read, three that are the index, an axis to choose for each pair on both sides; with both given on every axis 53); 1000 keys: 5.5 us, two launches.
 // Without the copies ahead 183, 158 and 72 us.
 //
 // A key in place cannot be turned twice, so the call is all or nothing: a first kernel looks over the lengths and pages, the second does nothing

@@ -2,7 +2,8 @@
 //
 // Weights w = 2^(-y / 16), y = 16 log2(e) (max - z) / T, in float64: 2^(-i/16) from a table, the rest by a polynomial of degree 5 (through the values
 // at the Chebyshev nodes of [-1/2, 1/2], its constant term set to 1: below 2^-46), as whole multiples of 2^-45.  Sums of integers are the same in
-// every order and on every split, so that equal arguments draw equal tokens, and a sum of 150000 weights is off by less than 2^-36 of the largest one.
+// every order and on every split, so that equal arguments draw equal tokens.  A weight is off by less than 2^-45 (the rounding by 2^-46, the polynomial by 2^-46.6), a sum of
+// 150000 weights by less than 2^-27.8 of the largest one; as roundings go, by about 2^-36.
 // (In float32 one draw in some hundred would fall on the neighbour of its token, and top-p would keep a token more or less.)
 //
 // A cluster holds the row in shared memory, in its own type; it is read once.  Tokens are ordered by (logit descending, token ascending), as 64-bit keys
@@ -45,10 +46,10 @@ constexpr int MAX_SLICE = 43008;           // tokens of a CTA
 constexpr double MAGIC = 6755399441055744.0;          // 1.5 * 2^52: adding it rounds to a whole number in the low bits
 constexpr float OCTAVES = 47.f;                       // weights below 2^-47 are 0
 constexpr int NT = 512, NW = NT / 32, BPT = NB / NT;
-// The bound of a small top-k, from maxima of 128 groups: at k = 20 about 22 tokens reach it, at k = 120 some 350 (16 rows of 152K: 13.7 and 18.4 us, by the
-// histogram 20.5 and 23); with fewer groups left over than eight it may lie anywhere.
+// The bound of a small top-k, from maxima of 128 groups: at k = 20 about 22 tokens reach it, at k = 120 some 350 (16 rows of 152K: 13.3 and 18.1 us, by the
+// histogram 20.5 and 22.9); with fewer groups left over than eight it may lie anywhere.
 constexpr int GROUPS = 128, SMALL_K = 120;
-constexpr int FEW = NT / 4;                // tokens of a short list, by counting: k = 20, 16 rows of 152K 13.7 us, by sorting 15.4
+constexpr int FEW = NT / 4;                // tokens of a short list, by counting: k = 20, 16 rows of 152K 13.3 us, by sorting 15.1
 
 // 2^(-i / 16)
 __constant__ double ROOTS[16] = {
