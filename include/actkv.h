@@ -830,11 +830,12 @@ int actkv_penalize(const void* logits, int32_t dtype, int32_t vocab, int64_t row
  * w(t) = exp((z_t - z_max) / T):
  *   the first top_k[i] of them (<= 0: all);
  *   of these the shortest prefix with at least top_p[i] of their sum of w (>= 1: all; at least one token);
- *   of these the ones with w >= min_p[i] (above 1 counts as 1).
+ *   of these the ones with w >= min_p[i] (1 and above: the largest logit and its equals).
  * The token drawn is the first one, in the order of the vocabulary, up to which the sum of w over the kept tokens exceeds u[i] times their sum
  * S; logprob = log(w / S) (NULL to skip), kept = how many tokens were kept (NULL to skip).  T = 0: the first token in order, logprob 0, kept 1.
- * u in [0, 1] is the row's random number (1: the last kept token).  Weights are formed in float64 and summed as whole multiples of 2^-45
- * (weights below 2^-46 are 0 in the sums), so that equal arguments give equal results.
+ * u in [0, 1] is the row's random number (1: the last kept token whose weight is not 0 in the sums).  Weights are formed in float64, right to 2^-45 (as near
+ * to a border of p, m or u a token may fall on either side), and summed as whole multiples of 2^-45 (weights below 2^-46 are 0 in the sums), so that equal arguments
+ * give equal results.  In weights, not in the order, a logit below 2^-126 counts as 0 (which shows at temperatures below 2^-80).
  * temperature, top_p, min_p float32, top_k int32 [n_rows], NULL: 1, 1, 0, 0 for every row.
  * A row with nothing but -inf, a NaN or +inf: token -1, logprob -inf, kept 0.  The same, reported as ACTKV_E_INVALID, for a temperature that is
  * negative, infinite or NaN, top_p or min_p NaN, u outside [0, 1].

@@ -465,10 +465,10 @@ __global__ void __launch_bounds__(NT, 2) sample_kernel(const __grid_constant__ A
     const uint32_t mine = near + lane < 16u ? 0u : near + lane - 16u;
     const float x = okey_inv(mine);
     const double w = power(gap_of(x <= top ? x : top, scale.top, __double2hiint(temp * 690.0)), scale.c, 0.0, sh.tab);
-    const uint32_t hit = __ballot_sync(0xffffffffu, x == x && x >= -FLT_MAX && w >= (m < 1.f ? exact_double(m) : 1.0));
+    const uint32_t hit = __ballot_sync(0xffffffffu, x == x && x >= -FLT_MAX && w >= exact_double(m));
     // (near a logit of 0 floats lie closer than weights are told apart: any of these is right to 2^-46)
     by_m = (uint64_t)(hit == 0 ? near : near + (uint32_t)__ffs((int)hit) - 17u) << 32;
-    by_m = min(by_m, (uint64_t)okey(top) << 32);
+    by_m = min(m < 1.f ? by_m : ~(uint64_t)0, (uint64_t)okey(top) << 32);   // (1: the largest and its equals, however close others come)
   }
 
   // All that can be kept is a list of nn tokens in the first CTA, which sorts it, cuts it and draws from it.  cut: the list is to be cut to k; then
