@@ -23,7 +23,7 @@
  *     replaced by page 0 for the read and reported; a copy whose source or destination page id is
  *     out of range is dropped and reported (nothing is read from or written to a page the request
  *     does not own).  Once status[0] is set, actkv_select and the compaction calls of the same
- *     step do nothing and actkv_resize is refused; behind a refused resize (status[3] is then
+ *     step do nothing, actkv_resize is refused and actkv_reposition turns no key; behind a refused resize (status[3] is then
  *     ACTKV_STATUS_REFUSED) actkv_append and actkv_copy leave the cache as it is, until a resize is carried
  *     out or the status cleared.  The caller clears all four words together.  When the plan step of actkv_compact reports ACTKV_E_NOFREE the copy and
  *     table-update steps of that call do nothing, so pool and tables stay unmodified.
